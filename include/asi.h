@@ -264,6 +264,113 @@ asi_status_t asi_step_host_status(const asi_plan_t* plan, const void* arena, voi
 asi_status_t asi_poll_status(const asi_plan_t* plan, const void* ws, void* stream,
                              asi_status_t* device_status);
 
+/* The rest of a language model's training step.  The compressed layers sit between an embedding and a loss over the
+ * vocabulary, and the gradients of a step (dW of asi_wgrad_batched among them) go to an optimiser.  These entry
+ * points take descriptors instead of plans (nothing about them is worth keeping), follow the conventions at the top,
+ * and write nothing but the outputs they name; two calls with outputs and workspaces of their own may overlap.
+ * Results are bit-identical from call to call.  Token ids and targets are int64. */
+
+/* Log probabilities of given tokens.  With x_j = scale * logits[t][j] over the row's `vocab` entries:
+ *   lse = log sum_j exp(x_j);   logp = x_y - lse for the given token y = targets[t];
+ *   entropy = -sum_j p_j log p_j,  p_j = exp(x_j - lse);
+ *   the top_k largest entries, ties to the lower index: top_logp = x_j - lse, top_ids = j.
+ * Rows the definition leaves open:
+ *   targets[t] == ignore_index       logp 0 and gradient 0; the other outputs as for any row
+ *   targets[t] outside [0, vocab)    logp and gradient NaN
+ *   a logit of -inf                  probability 0, and 0 in every sum
+ *   a row of nothing but -inf        lse and logp -inf, entropy 0, gradient 0; top_logp -inf
+ *   a logit of NaN or +inf           lse, logp, entropy, top_logp and gradient NaN (logp and gradient of an ignored
+ *                                    row stay 0), top_ids 0, 1, 2, ...
+ * Sums are fp32 (in a fixed order). */
+#define ASI_TOP_MAX 32
+#define ASI_LOGPROB_MAX_ROWS (1 << 27)
+#define ASI_LOGPROB_MAX_VOCAB (1 << 30)
+typedef struct {
+  int32_t in_dtype;              /* asi_dtype_t of logits and dlogits */
+  int32_t top_k;                 /* 0 .. min(ASI_TOP_MAX, vocab); asi_token_logprobs alone looks at it */
+  int64_t rows, vocab;           /* rows may be 0 */
+  int64_t ld, ld_grad;           /* elements from one row to the next of logits and dlogits, >= vocab */
+  int64_t ignore_index;
+  float scale;                   /* 1 / temperature: finite, > 0 */
+} asi_logprob_desc_t;
+
+/*   logits [in] device in_dtype [rows][ld], at any element;  targets [in] device [rows]
+ *   logp, entropy, lse [out] device fp32 [rows];  entropy may be null
+ *   top_logp [out] device fp32 [rows][top_k], top_ids [out] device int64 [rows][top_k]; null where top_k is 0 */
+asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logits, const int64_t* targets, float* logp,
+                                float* entropy, float* lse, float* top_logp, int64_t* top_ids, void* stream);
+
+/* Gradient of sum_t (dlogp[t] logp[t] + dentropy[t] entropy[t]) with respect to the logits:
+ *   dlogits[t][j] = scale (dlogp[t] ([j = y] - p_j) - dentropy[t] p_j (log p_j + entropy[t])).
+ *   lse, entropy [in] as asi_token_logprobs wrote them (entropy may be null where dentropy is)
+ *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
+ *   dlogits [out] device in_dtype [rows][ld_grad]; what lies between vocab and ld_grad stays as it was.  It may be
+ *           logits itself (the same address, ld_grad == ld), and overlaps it in no other way. */
+asi_status_t asi_token_logprobs_grad(const asi_logprob_desc_t* desc, const void* logits, const int64_t* targets,
+                                     const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                                     void* dlogits, void* stream);
+
+/* Both in one pass over the logits, for weights that do not depend on the result (cross entropy over n tokens:
+ * dlogp = -1/n, dentropy null).  Arguments as above; entropy may be null. */
+asi_status_t asi_token_loss(const asi_logprob_desc_t* desc, const void* logits, const int64_t* targets,
+                            const float* dlogp, const float* dentropy, float* logp, float* entropy, float* lse,
+                            void* dlogits, void* stream);
+
+/* Embedding: out[t][:] = scale * table[ids[t]][:], an id outside [0, vocab) gives a row of NaN.
+ * Its weight gradient beside those of conv2d and linear layers:
+ *   dW[v][:] = scale * sum over t with ids[t] = v of dOut[t][:]      (fp32, terms in the order of t in fixed groups)
+ * added to what dW holds (accumulate != 0: a table tied to the output layer), or written over all of dW.  Tokens of
+ * padding_idx and ids outside [0, vocab) contribute nothing. */
+typedef struct {
+  int32_t table_dtype;           /* asi_dtype_t of table (asi_embedding_forward) */
+  int32_t in_dtype;              /* asi_dtype_t of out and dOut */
+  int64_t vocab, dim, tokens;    /* at most 2^30, 2^22 and 2^24;  tokens may be 0 */
+  int64_t padding_idx;           /* -1: none */
+  float scale;                   /* finite */
+} asi_embedding_desc_t;
+
+/*   table [in] device [vocab][dim], ids [in] device [tokens], out [out] device in_dtype [tokens][dim] */
+asi_status_t asi_embedding_forward(const asi_embedding_desc_t* desc, const void* table, const int64_t* ids, void* out,
+                                   void* stream);
+/*   dOut [in] device in_dtype [tokens][dim], dW [in/out] device fp32 [vocab][dim]
+ *   ws   device scratch of at least asi_embedding_wgrad_ws_bytes(desc) (0 for a descriptor that is refused); it serves
+ *        fewer tokens of the same descriptor too */
+size_t asi_embedding_wgrad_ws_bytes(const asi_embedding_desc_t* desc);
+asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t* ids, const void* dOut, float* dW,
+                                 int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* One AdamW step over many tensors.  For every element, with g = grad_scale * grad:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
+ *   w = (1 - lr weight_decay) w - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, w rounded to weight_dtype at the end (and once more, to bf16, into `copy`).
+ * States in 8 bits: every ASI_ADAMW_BLOCK consecutive elements of a tensor share a scale 2^k, held as the byte
+ * k + 127; exp_avg holds m / 2^k and exp_avg_sq holds sqrt(v) / 2^k as e4m3 (round to nearest even).  k is the smallest,
+ * from -126 up, with max |.| <= 448 2^k over the block's finite values (0 where all are 0).  A sqrt(v) above 0 is held
+ * as 2^-9 at least: rounded to 0 it would leave eps alone under an m that is not.  A value that is not finite is held as
+ * NaN.  The step itself uses m and v before they are rounded.  All codes 0 is the state before the first step. */
+#define ASI_ADAMW_BLOCK 256
+typedef struct {
+  int32_t weight_dtype, grad_dtype;   /* asi_dtype_t */
+  int32_t state_bits;                 /* 32 or 8 */
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0;  betas in [0, 1);  eps >= 1e-30 */
+  int64_t step;                       /* t >= 1 */
+  /* for steps that are captured into a graph; device pointers or null: */
+  const float* lr_dev;                /* instead of lr */
+  const int64_t* step_dev;            /* instead of step */
+  const float* grad_scale;            /* a factor of every gradient (clipping, loss scaling); null: 1 */
+} asi_adamw_desc_t;
+typedef struct {
+  void* weight;                       /* [in/out] weight_dtype */
+  const void* grad;                   /* [in] grad_dtype */
+  void *exp_avg, *exp_avg_sq;         /* [in/out] fp32, or one byte an element */
+  uint8_t *exp_avg_scale, *exp_avg_sq_scale;   /* [in/out] ceil(n / ASI_ADAMW_BLOCK) bytes each; 8 bits only, else null */
+  void* copy;                         /* [out] bf16, or null */
+  int64_t n;                          /* elements, may be 0 */
+} asi_adamw_tensor_t;
+/* `tensors` is a host array, read before the call returns.  Each buffer starts at any element of its type (16-byte
+ * aligned ones are faster), and no written buffer may overlap another buffer of the call. */
+asi_status_t asi_adamw_step(const asi_adamw_desc_t* desc, const asi_adamw_tensor_t* tensors, int32_t count, void* stream);
+
 /* Number of kernel launches the last call of each kind enqueues for this plan. */
 int32_t asi_launch_count(const asi_plan_t* plan, int32_t which /* 0 compress, 1 wgrad */);
 

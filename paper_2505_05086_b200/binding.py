@@ -36,7 +36,11 @@ EXPORTS = (
     "asi_conv_wgrad", "asi_linear_wgrad", "asi_step_host_arena_bytes", "asi_step_host", "asi_step_host_status",
     "asi_poll_status", "asi_launch_count", "asi_status_string", "asi_profile_begin",
     "asi_profile_end", "asi_last_cuda_error",
+    "asi_token_logprobs", "asi_token_logprobs_grad", "asi_token_loss",
+    "asi_embedding_forward", "asi_embedding_wgrad_ws_bytes", "asi_embedding_wgrad", "asi_adamw_step",
 )
+ASI_TOP_MAX = 32
+ASI_ADAMW_BLOCK = 256
 
 
 class LayerDesc(C.Structure):
@@ -56,6 +60,28 @@ class PlanInfo(C.Structure):
                 ("compressed_elems", C.c_int64), ("ratio_RC", C.c_double),
                 ("macs_O_ASI", C.c_double), ("macs_C_ASI", C.c_double),
                 ("macs_C_vanilla", C.c_double)]
+
+
+class LogprobDesc(C.Structure):
+    _fields_ = [("in_dtype", C.c_int32), ("top_k", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64),
+                ("ld", C.c_int64), ("ld_grad", C.c_int64), ("ignore_index", C.c_int64), ("scale", C.c_float)]
+
+
+class EmbeddingDesc(C.Structure):
+    _fields_ = [("table_dtype", C.c_int32), ("in_dtype", C.c_int32), ("vocab", C.c_int64), ("dim", C.c_int64),
+                ("tokens", C.c_int64), ("padding_idx", C.c_int64), ("scale", C.c_float)]
+
+
+class AdamwDesc(C.Structure):
+    _fields_ = [("weight_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32),
+                ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p),
+                ("grad_scale", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64)]
 
 
 class AsiError(RuntimeError):
@@ -112,13 +138,23 @@ def lib():
     L.asi_profile_end.restype = i32
     L.asi_last_cuda_error.argtypes = []
     L.asi_last_cuda_error.restype = C.c_char_p
+    pl, pe = C.POINTER(LogprobDesc), C.POINTER(EmbeddingDesc)
+    L.asi_token_logprobs.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.asi_token_logprobs_grad.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.asi_token_loss.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.asi_embedding_forward.argtypes = [pe, vp, vp, vp, vp]
+    L.asi_embedding_wgrad_ws_bytes.argtypes = [pe]
+    L.asi_embedding_wgrad_ws_bytes.restype = sz
+    L.asi_embedding_wgrad.argtypes = [pe, vp, vp, vp, i32, vp, sz, vp]
+    L.asi_adamw_step.argtypes = [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), i32, vp]
     L.asi_status_string.argtypes = [i32]
     L.asi_status_string.restype = C.c_char_p
     for name in ("asi_plan_create", "asi_plan_destroy", "asi_plan_query", "asi_compress", "asi_compress_static_ws",
                  "asi_init_factors", "asi_init_factors_seeded", "asi_gaussian_stream", "asi_philox_words",
                  "asi_conv_wgrad", "asi_linear_wgrad", "asi_step_host",
                  "asi_poll_status", "asi_step_host_status", "asi_compress_batched", "asi_wgrad_batched",
-                 "asi_mode_spectrum", "asi_pick_ranks", "asi_perplexity"):
+                 "asi_mode_spectrum", "asi_pick_ranks", "asi_perplexity", "asi_token_logprobs", "asi_token_logprobs_grad",
+                 "asi_token_loss", "asi_embedding_forward", "asi_embedding_wgrad", "asi_adamw_step"):
         getattr(L, name).restype = i32
     _lib = L
     return L
@@ -287,6 +323,41 @@ def philox_words(seed, stream_id, n_groups, out, stream=0):
 
 def perplexity_ws_bytes():
     return lib().asi_perplexity_ws_bytes()
+
+
+def token_logprobs(desc, logits, targets, logp, entropy, lse, top_logp=0, top_ids=0, stream=0):
+    """asi_token_logprobs: log probabilities of the given tokens, entropy, log-sum-exp and the top_k entries of each row."""
+    _check(lib().asi_token_logprobs(desc, logits, targets, logp, entropy, lse, top_logp, top_ids, stream), "asi_token_logprobs")
+
+
+def token_logprobs_grad(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream=0):
+    """asi_token_logprobs_grad: the gradient with respect to the logits from what asi_token_logprobs left."""
+    _check(lib().asi_token_logprobs_grad(desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits, stream),
+           "asi_token_logprobs_grad")
+
+
+def token_loss(desc, logits, targets, dlogp, dentropy, logp, entropy, lse, dlogits, stream=0):
+    """asi_token_loss: log probabilities and their gradient in one pass over the logits."""
+    _check(lib().asi_token_loss(desc, logits, targets, dlogp, dentropy, logp, entropy, lse, dlogits, stream), "asi_token_loss")
+
+
+def embedding_forward(desc, table, ids, out, stream=0):
+    """asi_embedding_forward: out[t] = scale * table[ids[t]]."""
+    _check(lib().asi_embedding_forward(desc, table, ids, out, stream), "asi_embedding_forward")
+
+
+def embedding_wgrad_ws_bytes(desc):
+    return lib().asi_embedding_wgrad_ws_bytes(desc)
+
+
+def embedding_wgrad(desc, ids, dOut, dW, accumulate, ws, ws_bytes, stream=0):
+    """asi_embedding_wgrad: dW[v] = (or +=) scale * sum of dOut[t] over the tokens t of id v."""
+    _check(lib().asi_embedding_wgrad(desc, ids, dOut, dW, int(accumulate), ws, ws_bytes, stream), "asi_embedding_wgrad")
+
+
+def adamw_step(desc, tensors, count, stream=0):
+    """asi_adamw_step over `count` entries of the AdamwTensor array `tensors`."""
+    _check(lib().asi_adamw_step(desc, tensors, count, stream), "asi_adamw_step")
 
 
 KERNEL_IDS = {"modeprod": 1, "expand": 2, "qr": 3, "conv_tail": 4, "sm_pass1": 5, "sm_core": 6,

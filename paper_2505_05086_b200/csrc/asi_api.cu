@@ -804,12 +804,6 @@ void return_lanes(LaneSet* l) {
   g_lane_idle.push_back(l);
 }
 
-// the batched entry points keep lists on the host: a failed allocation is an error code like any other
-asi_status_t no_host_memory() {
-  snprintf(g_cuda_err, sizeof(g_cuda_err), "out of host memory");
-  return ASI_ERR_CUDA;
-}
-
 // What the layers of a batched call write, as address ranges.  Layers that write to the same memory (a workspace that
 // two of them share) run one after another, each with launches of its own.
 struct Written {
@@ -960,6 +954,22 @@ asi_status_t expand_modes(const asi_plan* pl, const void* act, const float* cons
 }
 
 }  // namespace
+
+namespace asi {
+
+// entry points that keep lists on the host: a failed allocation is an error code like any other
+asi_status_t no_host_memory() {
+  snprintf(g_cuda_err, sizeof(g_cuda_err), "out of host memory");
+  return ASI_ERR_CUDA;
+}
+
+asi_status_t cuda_status(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return ASI_OK;
+  snprintf(g_cuda_err, sizeof(g_cuda_err), "%s: %s", what, cudaGetErrorString(e));
+  return ASI_ERR_CUDA;
+}
+
+}  // namespace asi
 
 extern "C" {
 

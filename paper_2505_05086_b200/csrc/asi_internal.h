@@ -328,6 +328,10 @@ static inline cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 
 // so the sizes already granted are remembered per device.
 cudaError_t opt_in_smem(const void* kernel, size_t need);
 
+// Status codes of the entry points that live beside their kernels (asi_api.cu holds the text of asi_last_cuda_error)
+asi_status_t cuda_status(cudaError_t e, const char* what);
+asi_status_t no_host_memory();
+
 // One product of a grouped launch (asi_gemm_kernels.cu): C[m][j] = sum_k A(m, k) B[k][j] per outer index o
 struct GemmProb {
   const void* X;

@@ -2,10 +2,13 @@
 does all the arithmetic."""
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 import torch
 
-from .binding import ASI_OK, Batch, Plan
+from . import binding
+from .binding import ASI_ADAMW_BLOCK, ASI_BF16, ASI_F32, ASI_OK, AdamwDesc, AdamwTensor, Batch, EmbeddingDesc, LogprobDesc, Plan
 
 
 def _stream_handle(stream=None):
@@ -114,3 +117,211 @@ class StepRunner:
         self.batch.wgrad([r.core.data_ptr() for r in rs], [r.U[r.cur].data_ptr() for r in rs],
                          [d.data_ptr() for d in dys], [r.dW.data_ptr() for r in rs],
                          [r.ws_w.data_ptr() for r in rs], [r.ws_w.numel() for r in rs], _stream_handle(stream))
+
+
+# ---- the rest of a language model's training step ---------------------------------------------------
+
+_DTYPES = {torch.float32: ASI_F32, torch.bfloat16: ASI_BF16}
+
+
+def _on(device):
+    """Makes `device` current for a launch; nothing to do where it is."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream_of(device, stream):
+    """The handle of `stream`, or of the current stream of `device` (which _on() has made current)."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"a stream of {device} is needed, got one of {stream.device}")
+    return _stream_handle(stream)
+
+
+def _cuda_device(device):
+    d = torch.device(device)
+    if d.type != "cuda":
+        raise ValueError("the ASI path needs a CUDA device; there is no CPU fallback")
+    if not torch.cuda.is_available():
+        raise RuntimeError("the ASI path needs a CUDA device; there is no CPU fallback")
+    return torch.device("cuda", torch.cuda.current_device() if d.index is None else d.index)
+
+
+def _take(name, x, shape, dtype, device):
+    """The address of a contiguous tensor of that shape and type on that device."""
+    if x.dtype != dtype or tuple(x.shape) != tuple(shape) or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is needed, got {x.dtype} "
+                         f"{tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+class LogprobRunner:
+    """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
+    lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
+    the others as they were."""
+
+    def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.rows, self.vocab, self.top_k = int(rows), int(vocab), int(top_k)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self.desc = LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index), float(scale))
+        f32 = dict(dtype=torch.float32, device=self.device)
+        self.logp, self.entropy, self.lse = (torch.zeros(self.rows, **f32) for _ in range(3))
+        self.top_logp = torch.zeros(self.rows, self.top_k, **f32) if self.top_k else None
+        self.top_ids = torch.zeros(self.rows, self.top_k, dtype=torch.int64, device=self.device) if self.top_k else None
+
+    def _rows_of(self, name, x):
+        if (x.dtype != self.in_dtype or x.dim() != 2 or x.shape[0] > self.rows or x.shape[1] != self.vocab
+                or x.device != self.device or (self.vocab > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < self.vocab)):
+            raise ValueError(f"{name}: {self.in_dtype} rows [<= {self.rows}, {self.vocab}] on {self.device} are needed, each "
+                             f"contiguous, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
+        return max(x.stride(0), self.vocab)
+
+    def _inputs(self, logits, targets, dlogits=None):
+        self.desc.ld = self.desc.ld_grad = self._rows_of("logits", logits)
+        self.desc.rows = n = logits.shape[0]
+        if dlogits is not None:
+            self.desc.ld_grad = self._rows_of("dlogits", dlogits)
+            if dlogits.shape[0] != n:
+                raise ValueError(f"dlogits: {n} rows are needed, got {dlogits.shape[0]}")
+        return n, _take("targets", targets, (n,), torch.int64, self.device)
+
+    def _weights(self, n, dlogp, dentropy):
+        return (_take("dlogp", dlogp, (n,), torch.float32, self.device),
+                _take("dentropy", dentropy, (n,), torch.float32, self.device) if dentropy is not None else 0)
+
+    def forward(self, logits, targets, stream=None):
+        _, y = self._inputs(logits, targets)
+        with _on(self.device):
+            binding.token_logprobs(self.desc, logits.data_ptr(), y, self.logp.data_ptr(), self.entropy.data_ptr(),
+                                   self.lse.data_ptr(), self.top_logp.data_ptr() if self.top_k else 0,
+                                   self.top_ids.data_ptr() if self.top_k else 0, _stream_of(self.device, stream))
+
+    def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
+        """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward()
+        left; dentropy may be None, and dlogits may be logits itself."""
+        n, y = self._inputs(logits, targets, dlogits)
+        a, b = self._weights(n, dlogp, dentropy)
+        with _on(self.device):
+            binding.token_logprobs_grad(self.desc, logits.data_ptr(), y, self.lse.data_ptr(), self.entropy.data_ptr(), a, b,
+                                        dlogits.data_ptr(), _stream_of(self.device, stream))
+
+    def loss(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
+        """forward() without the top entries, and backward(), in one pass over the logits."""
+        n, y = self._inputs(logits, targets, dlogits)
+        a, b = self._weights(n, dlogp, dentropy)
+        with _on(self.device):
+            binding.token_loss(self.desc, logits.data_ptr(), y, a, b, self.logp.data_ptr(), self.entropy.data_ptr(),
+                               self.lse.data_ptr(), dlogits.data_ptr(), _stream_of(self.device, stream))
+
+
+class EmbeddingRunner:
+    """Embedding lookup of up to `tokens` tokens and its weight gradient, with the workspace of the latter."""
+
+    def __init__(self, vocab, dim, tokens, bf16=False, bf16_table=False, scale=1.0, padding_idx=None, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.vocab, self.dim, self.tokens = int(vocab), int(dim), int(tokens)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self.table_dtype = torch.bfloat16 if bf16_table else torch.float32
+        self.desc = EmbeddingDesc(_DTYPES[self.table_dtype], _DTYPES[self.in_dtype], self.vocab, self.dim, self.tokens,
+                                  -1 if padding_idx is None else int(padding_idx), float(scale))
+        self.ws = None                     # allocated with the first wgrad()
+
+    def _ids(self, ids):
+        if ids.dtype != torch.int64 or ids.device != self.device or not ids.is_contiguous() or ids.numel() > self.tokens:
+            raise ValueError(f"ids: a contiguous int64 tensor of up to {self.tokens} tokens on {self.device} is needed, got "
+                             f"{ids.dtype} {tuple(ids.shape)} on {ids.device}")
+        self.desc.tokens = ids.numel()
+        return tuple(ids.shape) + (self.dim,)
+
+    def forward(self, table, ids, out, stream=None):
+        shape = self._ids(ids)
+        w = _take("table", table, (self.vocab, self.dim), self.table_dtype, self.device)
+        o = _take("out", out, shape, self.in_dtype, self.device)
+        with _on(self.device):
+            binding.embedding_forward(self.desc, w, ids.data_ptr(), o, _stream_of(self.device, stream))
+
+    def wgrad(self, ids, dOut, dW, accumulate=False, stream=None):
+        """dW (fp32 [vocab, dim]) overwritten with, or increased by, the gradient."""
+        shape = self._ids(ids)
+        d = _take("dOut", dOut, shape, self.in_dtype, self.device)
+        w = _take("dW", dW, (self.vocab, self.dim), torch.float32, self.device)
+        if self.ws is None:                # as large as the longest batch needs
+            n, self.desc.tokens = self.desc.tokens, self.tokens
+            self.ws = torch.empty(binding.embedding_wgrad_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
+            self.desc.tokens = n
+        with _on(self.device):
+            binding.embedding_wgrad(self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(), self.ws.numel(),
+                                    _stream_of(self.device, stream))
+
+
+class AdamWRunner:
+    """AdamW over a list of weights and their gradient buffers (the dW of layer runners, for example): holds the states and
+    steps all tensors in one call.  States may be given (to resume); the 8-bit ones are float8_e4m3fn with one
+    float8_e8m0fnu (or uint8) scale for each ASI_ADAMW_BLOCK elements of a tensor.  `copies` (bf16) receive the new weights."""
+
+    def __init__(self, weights, grads, bits8=False, copies=None, exp_avg=None, exp_avg_sq=None, exp_avg_scale=None,
+                 exp_avg_sq_scale=None):
+        self.weights, self.grads = list(weights), list(grads)
+        if not self.weights or len(self.grads) != len(self.weights):
+            raise ValueError("one gradient for each of one or more weights is needed")
+        self.device = _cuda_device(self.weights[0].device)
+        self.bits8, self.t = bool(bits8), 0
+        wd, gd = self.weights[0].dtype, self.grads[0].dtype
+        if wd not in _DTYPES or gd not in _DTYPES:
+            raise ValueError("weights and gradients are fp32 or bf16")
+        sd = torch.float8_e4m3fn if self.bits8 else torch.float32
+
+        def states(given, dtype, per, fill):
+            if given is not None:
+                return list(given)
+            new = [torch.empty(-(-w.numel() // per), dtype=dtype, device=self.device) for w in self.weights]
+            for x in new:
+                x.view(torch.uint8).fill_(fill)
+            return new
+
+        self.exp_avg, self.exp_avg_sq = states(exp_avg, sd, 1, 0), states(exp_avg_sq, sd, 1, 0)
+        scales = (states(s, torch.float8_e8m0fnu, ASI_ADAMW_BLOCK, 127) if self.bits8 else [None] * len(self.weights)
+                  for s in (exp_avg_scale, exp_avg_sq_scale))
+        self.exp_avg_scale, self.exp_avg_sq_scale = scales
+        self.copies = list(copies) if copies is not None else [None] * len(self.weights)
+        self.desc = AdamwDesc(weight_dtype=_DTYPES[wd], grad_dtype=_DTYPES[gd], state_bits=8 if self.bits8 else 32)
+        self._tensors = (AdamwTensor * len(self.weights))()
+
+        def at(name, x, n, *dtypes):
+            if x.dtype not in dtypes or x.numel() != n or x.device != self.device or not x.is_contiguous():
+                raise ValueError(f"{name}: {n} contiguous values of {dtypes[0]} on {self.device} are needed, got {x.dtype} "
+                                 f"{tuple(x.shape)} on {x.device}")
+            return x.data_ptr()
+
+        lists = (self.grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, self.copies)
+        if any(len(x) != len(self.weights) for x in lists):
+            raise ValueError("one state (scale, copy) for each weight is needed")
+        for e, w, g, m, v, ms, vs, c in zip(self._tensors, self.weights, *lists):
+            n = w.numel()
+            e.weight, e.grad = at("weight", w, n, wd), at("grad", g, n, gd)
+            e.exp_avg, e.exp_avg_sq = at("exp_avg", m, n, sd), at("exp_avg_sq", v, n, sd)
+            if self.bits8:
+                scale = -(-n // ASI_ADAMW_BLOCK), torch.float8_e8m0fnu, torch.uint8
+                e.exp_avg_scale, e.exp_avg_sq_scale = at("exp_avg_scale", ms, *scale), at("exp_avg_sq_scale", vs, *scale)
+            e.copy = at("copy", c, n, torch.bfloat16) if c is not None else None
+            e.n = n
+
+    def step(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=None, grad_scale=None, stream=None):
+        """One step.  `step` counts from 1 (default: one more than at the call before).  lr (fp32) and step (int64) may be
+        one-element device tensors, so that a captured graph reads new values; grad_scale (fp32) is one if given."""
+        d = self.desc
+        d.beta1, d.beta2, d.eps, d.weight_decay = beta1, beta2, eps, weight_decay
+        d.lr_dev = d.step_dev = d.grad_scale = None
+        if isinstance(lr, torch.Tensor):
+            d.lr, d.lr_dev = 0.0, _take("lr", lr.reshape(1), (1,), torch.float32, self.device)
+        else:
+            d.lr = lr
+        if isinstance(step, torch.Tensor):
+            d.step, d.step_dev = 1, _take("step", step.reshape(1), (1,), torch.int64, self.device)
+        else:
+            d.step = self.t + 1 if step is None else int(step)
+        if grad_scale is not None:
+            d.grad_scale = _take("grad_scale", grad_scale.reshape(1), (1,), torch.float32, self.device)
+        with _on(self.device):
+            binding.adamw_step(d, self._tensors, len(self.weights), _stream_of(self.device, stream))
+        if not isinstance(step, torch.Tensor):
+            self.t = d.step
