@@ -6,13 +6,15 @@
 //   dlogits_j = scale (alpha ([j = y] - p_j) - beta p_j (log p_j + entropy)) = e_j (A + B a_j) + [j = y] scale alpha
 // with A = -scale (alpha + beta (entropy - ln S)) / S and B = -scale beta ln2 / S.
 //
-// What bounds it: the logits, read once (and the gradient, written once).  A row stays in shared memory between the maximum,
-// the sums and the gradient, split over a cluster of up to eight CTAs where it is long or where there are few rows; the
-// cluster's shares (M, S, W and the leading entries) meet through distributed shared memory, in rank order.
+// What bounds it: the logits, read once (and the gradient, written once).  Each thread keeps a running maximum with its sums
+// in packed fp32 (two values an instruction), so that one pass in registers is all that the forward direction needs; for
+// the gradient the row waits in shared memory meanwhile.  Rows are split over a cluster of up to eight CTAs where they are
+// long or few; the cluster's shares (M, S, W and the leading entries) meet through distributed shared memory, in rank order.
 #include <cuda_bf16.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "asi_internal.h"
 
@@ -20,9 +22,11 @@ namespace asi {
 
 namespace {
 
+constexpr int kFwd = 128;                   // threads of a CTA: forward, loss, gradient alone
+constexpr int kLoss = 256, kLossCtas = 3;
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kShare = 72 << 10;            // bytes of a row that a CTA of the loss keeps, where a cluster allows it
 constexpr int kCand = 512;                 // candidates of a CTA's top entries
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
@@ -63,6 +67,45 @@ __device__ __forceinline__ float exp2_approx(float a) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a));
   return r;
 }
+// two fp32 values as one operand of the packed instructions
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 v) {
+  float a, b;
+  unpair(v, a, b);
+  return a + b;
+}
+__device__ __forceinline__ f2 exp2_both(f2 v) {
+  float a, b;
+  unpair(v, a, b);
+  return pair(exp2_approx(a), exp2_approx(b));
+}
+// -inf (of a masked entry, times whose 0 it would be NaN) as a finite exponent whose power is 0 just as well
+__device__ __forceinline__ f2 finite2(f2 v) {
+  float a, b;
+  unpair(v, a, b);
+  return pair(fmaxf(a, -1e4f), fmaxf(b, -1e4f));
+}
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ float remote_f(const float* p, int rank) {       // the same address in another CTA of the cluster
   uint32_t at;
@@ -87,6 +130,7 @@ struct Granule;
 template <>
 struct Granule<__nv_bfloat16> {
   static constexpr int n = 8;
+  static constexpr uint32_t kNone = 0xff80ff80u;                    // -inf
   static __device__ __forceinline__ void floats(const uint4& v, float* f) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -97,6 +141,18 @@ struct Granule<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float largest(const uint4& v) {
     const uint32_t m = nan_max2(nan_max2(v.x, v.y), nan_max2(v.z, v.w));
+    return nan_max(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  static __device__ __forceinline__ void pairs(const uint4& v, f2* p) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  template <int N>
+  static __device__ __forceinline__ float largest_of(const uint4* v) {
+    uint32_t m = nan_max2(nan_max2(v[0].x, v[0].y), nan_max2(v[0].z, v[0].w));
+#pragma unroll
+    for (int q = 1; q < N; ++q) m = nan_max2(m, nan_max2(nan_max2(v[q].x, v[q].y), nan_max2(v[q].z, v[q].w)));
     return nan_max(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
   }
   static __device__ __forceinline__ uint4 pack(const float* f) {
@@ -114,6 +170,7 @@ struct Granule<__nv_bfloat16> {
 template <>
 struct Granule<float> {
   static constexpr int n = 4;
+  static constexpr uint32_t kNone = 0xff800000u;
   static __device__ __forceinline__ void floats(const uint4& v, float* f) {
     f[0] = __uint_as_float(v.x);
     f[1] = __uint_as_float(v.y);
@@ -123,12 +180,32 @@ struct Granule<float> {
   static __device__ __forceinline__ float largest(const uint4& v) {
     return nan_max(nan_max(__uint_as_float(v.x), __uint_as_float(v.y)), nan_max(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
+  static __device__ __forceinline__ void pairs(const uint4& v, f2* p) {
+    p[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+    p[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+  }
+  template <int N>
+  static __device__ __forceinline__ float largest_of(const uint4* v) {
+    float m = largest(v[0]);
+#pragma unroll
+    for (int q = 1; q < N; ++q) m = nan_max(m, largest(v[q]));
+    return m;
+  }
   static __device__ __forceinline__ uint4 pack(const float* f) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
   static __device__ __forceinline__ float one(float f) { return f; }
   static __device__ __forceinline__ float read(const float* p) { return *p; }
 };
+
+// Elements j .. j + n - 1 of a row one by one, -inf outside it.
+template <typename T>
+__device__ __forceinline__ uint4 edge_granule(const T* x, int V, int j) {
+  float f[Granule<T>::n];
+#pragma unroll
+  for (int i = 0; i < Granule<T>::n; ++i) f[i] = j + i >= 0 && j + i < V ? Granule<T>::read(x + j + i) : -INFINITY;
+  return Granule<T>::pack(f);
+}
 
 // A row as granules that start on 16 bytes: granule g holds the elements [g n - mis, g n - mis + n), those outside
 // [0, V) are not the row's (the first and the last granule).
@@ -143,14 +220,11 @@ struct RowView {
     const int j = first(g);
     return j >= 0 && (int64_t)j + Granule<T>::n <= V;
   }
-  __device__ __forceinline__ uint4 edge(int g) const {            // element by element, -inf outside the row
-    float f[Granule<T>::n];
-    const int j = first(g);
-#pragma unroll
-    for (int i = 0; i < Granule<T>::n; ++i)
-      f[i] = j + i >= 0 && j + i < V ? Granule<T>::read(x + j + i) : -INFINITY;
-    return Granule<T>::pack(f);
-  }
+  // granules [first_whole(), end_whole()) are whole: all but perhaps the first and the last
+  __device__ __forceinline__ int first_whole() const { return mis != 0; }
+  __device__ __forceinline__ int end_whole() const { return (int)(((int64_t)mis + V) / Granule<T>::n); }
+  __device__ __forceinline__ const uint4* granule(int g) const { return reinterpret_cast<const uint4*>(x - mis) + g; }
+  __device__ __forceinline__ uint4 edge(int g) const { return edge_granule<T>(x, V, first(g)); }
   __device__ __forceinline__ uint4 load(int g) const {
     if (whole(g)) return *reinterpret_cast<const uint4*>(x + first(g));
     return edge(g);
@@ -171,40 +245,194 @@ __device__ __forceinline__ void store_granule(T* dx, const RowView<T>& row, int 
 }
 
 // Orders entries by value, then by lower index; never 0.
-__device__ __forceinline__ unsigned long long order_key(float v, int j) {
+__device__ __forceinline__ uint32_t order_bits(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);                     // -0 counts as 0
-  const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return ((unsigned long long)o << 32) | (0xffffffffu - (uint32_t)j);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(unsigned long long key) {
-  const uint32_t o = (uint32_t)(key >> 32);
-  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+__device__ __forceinline__ float order_value(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ unsigned long long order_key(float v, int j) {
+  return ((unsigned long long)order_bits(v) << 32) | (0xffffffffu - (uint32_t)j);
 }
+__device__ __forceinline__ float key_value(unsigned long long key) { return order_value((uint32_t)(key >> 32)); }
 __device__ __forceinline__ int key_index(unsigned long long key) { return (int)(0xffffffffu - (uint32_t)key); }
+
+// S and W relative to the maximum M, from shares relative to their own; M >= each, a share of nothing has -inf
+__device__ __forceinline__ void rebase(float& S, float& W, float from, float M, float c2) {
+  if (from == -INFINITY) {
+    S = W = 0.f;
+  } else {
+    const float a = (from - M) * c2, f = exp2_approx(a);
+    W = f * fmaf(fmaxf(a, -1e4f), S, W);
+    S *= f;
+  }
+}
+
+template <int kWarps>
+struct RowShared {
+  float red[3][kWarps];
+  float mine[3];                           // M, S, W of this CTA's share
+  float parts[3][kMaxCluster];
+};
+
+// M over the CTA
+template <int kWarps>
+__device__ __forceinline__ float block_max(float M, float* red) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) M = nan_max(M, __shfl_xor_sync(~0u, M, o));
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = M;
+  __syncthreads();
+  M = red[0];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) M = nan_max(M, red[i]);
+  return M;
+}
+template <int kWarps>
+__device__ __forceinline__ void block_sums(float& S, float& W, float (*red)[kWarps]) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    S += __shfl_xor_sync(~0u, S, o);
+    W += __shfl_xor_sync(~0u, W, o);
+  }
+  if ((threadIdx.x & 31) == 0) red[1][threadIdx.x >> 5] = S, red[2][threadIdx.x >> 5] = W;
+  __syncthreads();
+  S = red[1][0], W = red[2][0];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) S += red[1][i], W += red[2][i];
+}
+// The cluster's shares, in rank order.  Ends with every remote read done and a cluster_arrive(): the caller waits at its end.
+template <int kWarps>
+__device__ __forceinline__ void cluster_sums(float& M, float& S, float& W, float c2, int cl, RowShared<kWarps>& sh) {
+  float Mt = sh.parts[0][0];
+  for (int q = 1; q < cl; ++q) Mt = nan_max(Mt, sh.parts[0][q]);
+  S = W = 0.f;
+  for (int q = 0; q < cl; ++q) {
+    float s = sh.parts[1][q], w = sh.parts[2][q];
+    rebase(s, w, sh.parts[0][q], Mt, c2);
+    S += s;
+    W += w;
+  }
+  M = Mt;
+}
+
+__device__ __forceinline__ void write_row(const LogprobArgs& p, int t, float M, float S, float W, float xy, bool given, bool skip) {
+  const bool dead = M == -INFINITY;
+  const float lnS = logf(S);
+  p.lse[t] = dead ? -INFINITY : fmaf(M, p.scale, lnS);
+  if (p.entropy) p.entropy[t] = dead ? 0.f : lnS - kLn2 * W / S;
+  p.logp[t] = skip ? 0.f : !given ? NAN : dead ? -INFINITY : (xy - M) * p.scale - lnS;
+}
+
+// ---- forward: one pass over the row in registers, each thread with a running maximum
+constexpr int kBatch = 4;                  // granules a thread has in hand
+constexpr int kSlots = 16;                 // maxima a thread remembers of what it has read
+constexpr int kHits = 512;
 
 struct TopShared {
   unsigned long long cand[kCand];
   unsigned long long list[ASI_TOP_MAX];    // this CTA's leading entries, largest first; 0: none
-  float group[32];
+  float slot[kSlots][kFwd];
+  uint16_t hit[kHits];                     // slot * kFwd + thread: granules that may hold candidates
+  float most[kFwd];                        // each thread's maximum
   float tau;
-  int count;
+  int count, hits;
 };
 
-// GRAD: the gradient in the same pass.  TOP: leading entries.  RES: the CTA's share of the row stays in shared memory
-// (else it is read again for each sweep: rows of more than 1.6 MB).
-template <typename T, bool GRAD, bool TOP, bool RES>
-__global__ void __launch_bounds__(kThreads) k_logprob(const __grid_constant__ LogprobArgs p) {
+// S and W of some granules relative to M
+template <typename T>
+__device__ __forceinline__ void add_terms(const uint4& v, f2 minus, f2 k2, f2& S2, f2& W2) {
   constexpr int n = Granule<T>::n;
-  extern __shared__ uint4 buf[];
-  __shared__ float red[3][kWarps];
-  __shared__ float mine[3];                // M, S, W of this CTA's share
-  __shared__ float parts[3][kMaxCluster];
+  f2 x[n / 2];
+  Granule<T>::pairs(v, x);
+#pragma unroll
+  for (int e = 0; e < n / 2; ++e) {
+    const f2 a = mul2(add2(x[e], minus), k2), ex = exp2_both(a);
+    S2 = add2(S2, ex);
+    W2 = fma2(ex, finite2(a), W2);
+  }
+}
+
+// A CTA's share of a row: granules [g0, g0 + cnt), those in [lo, hi) of it whole.
+template <typename T>
+struct Share {
+  RowView<T> row;
+  int g0, cnt, lo, hi;
+  __device__ __forceinline__ Share(const LogprobArgs& p, int t, int rank) : row(static_cast<const T*>(p.x) + (int64_t)t * p.ld, p.V) {
+    const int G = row.granules(), per = (G + p.cl - 1) / p.cl;
+    g0 = min(G, rank * per);
+    cnt = min(G - g0, per);
+    lo = max(row.first_whole() - g0, 0);
+    hi = min(row.end_whole() - g0, cnt);
+  }
+};
+
+// Batch b of a share: granules b kBatch kN + q kN + tid, -inf where it runs past the share (an entry counted twice would
+// spoil tau).
+template <typename T, int kN>
+__device__ __forceinline__ void bring(const Share<T>& s, int b, uint4* v) {
+  const int i0 = b * kBatch * kN;
+  const uint4* src = s.row.granule(s.g0 + i0) + threadIdx.x;
+  if (i0 >= s.lo && i0 + kBatch * kN <= s.hi) {
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) v[q] = src[q * kN];
+  } else {
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = i0 + q * kN + threadIdx.x;
+      v[q] = make_uint4(Granule<T>::kNone, Granule<T>::kNone, Granule<T>::kNone, Granule<T>::kNone);
+      if (i >= s.lo && i < s.hi) v[q] = src[q * kN];
+      else if (i < s.cnt) v[q] = s.row.edge(s.g0 + i);
+    }
+  }
+}
+
+// One pass over the share: M, S and W of this thread's granules, four of them in hand and the next four on their way.
+// seen(b, v, most) gets each batch with its maximum.
+template <typename T, int kN, typename F>
+__device__ __forceinline__ void stream_share(const Share<T>& s, float c2, float& M, float& S, float& W, F seen) {
+  const int batches = (s.cnt + kBatch * kN - 1) / (kBatch * kN);
+  const f2 k2 = pair(c2, c2);
+  M = -INFINITY, S = 0.f, W = 0.f;
+  uint4 v[2][kBatch];
+  if (batches) bring<T, kN>(s, 0, v[0]);
+#pragma unroll 1
+  for (int b0 = 0; b0 < batches; b0 += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int b = b0 + h;
+      if (b >= batches) break;
+      if (b + 1 < batches) bring<T, kN>(s, b + 1, v[h ^ 1]);
+      const float most = Granule<T>::template largest_of<kBatch>(v[h]);
+      seen(b, v[h], most);
+      if (!(most <= M)) {
+        const float to = nan_max(M, most);
+        rebase(S, W, M, to, c2);
+        M = to;
+      }
+      if (M != -INFINITY) {
+        const f2 minus = pair(-M, -M);
+        f2 S2 = 0, W2 = 0;
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) add_terms<T>(v[h][q], minus, k2, S2, W2);
+        S += sum2(S2);
+        W += sum2(W2);
+      }
+    }
+  }
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_constant__ LogprobArgs p) {
+  constexpr int n = Granule<T>::n, kWarps = kFwd / 32;
+  __shared__ RowShared<kWarps> sh;
   __shared__ TopShared top;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cl = p.cl, t = blockIdx.x / cl, rank = blockIdx.x - t * cl;
-  const RowView<T> row(static_cast<const T*>(p.x) + (int64_t)t * p.ld, p.V);
-  const int G = row.granules(), per = (G + cl - 1) / cl;
-  const int g0 = min(G, rank * per), cnt = min(G - g0, per);
+  const Share<T> s(p, t, rank);
+  const RowView<T>& row = s.row;
+  const int g0 = s.g0, cnt = s.cnt;
+  const int batches = (cnt + kBatch * kFwd - 1) / (kBatch * kFwd);
+  const int span = (batches + kSlots - 1) / kSlots;                 // batches that share a slot
+  const float c2 = p.scale * kLog2e;
 
   pdl_wait();
   pdl_launch_dependents();
@@ -213,87 +441,94 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const __grid_constant__ Lo
   float xy = 0.f;
   if (given && tid == 0 && rank == 0) xy = Granule<T>::read(row.x + y);
 
-  if (RES) {
-    for (int i = tid; i < cnt; i += kThreads) {
-      if (row.whole(g0 + i))
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(buf + i)), "l"(row.x + row.first(g0 + i)) : "memory");
-      else
-        buf[i] = row.edge(g0 + i);
-    }
-    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-  }
-  // every thread reads back what it brought itself: no barrier
-  auto at = [&](int i) -> uint4 { return RES ? buf[i] : row.load(g0 + i); };
-
-  float M = -INFINITY;
-  for (int i = tid; i < cnt; i += kThreads) M = nan_max(M, Granule<T>::largest(at(i)));
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    if (TOP && o == 8 && (lane & 7) == 0) top.group[tid >> 3] = M;
-    M = nan_max(M, __shfl_xor_sync(~0u, M, o));
-  }
-  if (lane == 0) red[0][warp] = M;
-  if (TOP && tid == 0) top.count = 0;
-  __syncthreads();
-  M = red[0][0];
-#pragma unroll
-  for (int i = 1; i < kWarps; ++i) M = nan_max(M, red[0][i]);
-  // The k-th largest of the maxima of 32 groups of threads: at least k entries reach it, and few more.
-  float tau = 0.f;
-  if (TOP) {
-    if (warp == 0) {
-      const float v = top.group[lane];
-      int above = 0;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const float o = __shfl_sync(~0u, v, i);
-        above += o > v || (o == v && i < lane);
+  float M, S, W, slot = -INFINITY;
+  int in_slot = 0, slots = 0;
+  stream_share<T, kFwd>(s, c2, M, S, W, [&](int b, const uint4*, float most) {
+    if (TOP) {
+      slot = nan_max(slot, most);
+      if (++in_slot == span || b == batches - 1) {
+        top.slot[slots++][tid] = slot;
+        slot = -INFINITY;
+        in_slot = 0;
       }
-      if (above == p.k - 1) top.tau = v;                         // one lane, unless there are NaNs (then no matter)
     }
-    __syncthreads();
-    tau = top.tau;
-  }
+  });
 
-  const float c2 = p.scale * kLog2e, Mz = M == -INFINITY ? 0.f : M;
-  float S = 0.f, W = 0.f;
-  for (int i = tid; i < cnt; i += kThreads) {
-    const uint4 v = at(i);
-    float f[n];
-    Granule<T>::floats(v, f);
-    if (TOP && Granule<T>::largest(v) >= tau) {
-      const int j = row.first(g0 + i);
+  const float own = M;
+  if (TOP) {
+    top.most[tid] = M;
+    if (tid == 0) top.count = top.hits = 0;
+  }
+  M = block_max<kWarps>(M, sh.red[0]);
+  rebase(S, W, own, M, c2);
+  if (TOP) {
+    // tau, about the k-th largest of the threads' maxima: at least k entries reach it, and few more.  Found bit by bit
+    // below the bits that all of them share: the largest prefix that k of them reach.
+    if (warp == 0) {
+      uint32_t key[kFwd / 32], high = 0, low = ~0u;
 #pragma unroll
-      for (int e = 0; e < n; ++e)
-        if (f[e] >= tau && j + e >= 0 && j + e < p.V) {
-          const int slot = atomicAdd(&top.count, 1);
-          if (slot < kCand) top.cand[slot] = order_key(f[e], j + e);
+      for (int i = 0; i < kFwd / 32; ++i) {
+        key[i] = order_bits(top.most[i * 32 + lane]);
+        high = max(high, key[i]);
+        low = min(low, key[i]);
+      }
+      high = __reduce_max_sync(~0u, high);
+      low = __reduce_min_sync(~0u, low);
+      uint32_t bit = high == low ? 0u : 1u << (31 - __clz(high ^ low)), t = bit ? high & ~(2 * bit - 1) : low;
+      for (; bit; bit >>= 1) {
+        uint32_t reach = 0;
+#pragma unroll
+        for (int i = 0; i < kFwd / 32; ++i) reach += key[i] >= (t | bit);
+        reach = __reduce_add_sync(~0u, reach);
+        if ((int)reach >= p.k) t |= bit;
+        if ((int)reach == p.k) break;
+      }
+      if (lane == 0) top.tau = order_value(max(t, low));
+    }
+  }
+  block_sums<kWarps>(S, W, sh.red);
+
+  if (TOP) {
+    const float tau = top.tau;
+    // The slots that reach it are listed, and each gets a warp that reads its entries once more, one a lane.
+    if (own >= tau)
+      for (int k = 0; k < slots; ++k)
+        if (top.slot[k][tid] >= tau) {
+          const int place = atomicAdd(&top.hits, 1);
+          if (place < kHits) top.hit[place] = (uint16_t)(k * kFwd + tid);
+        }
+    __syncthreads();
+    const int hits = top.hits;
+    if (hits > kHits && tid == 0) top.count = kCand + 1;             // too many: the sweeps below
+    constexpr int kEntries = kBatch * n, kAtOnce = 4;
+    const int pieces = min(hits, kHits) * span;                      // (hit, batch of its slot), four of them in flight
+    for (int h0 = warp; h0 < pieces; h0 += kWarps * kAtOnce) {
+      float f[kAtOnce];
+      int j[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int h = h0 + u * kWarps;
+        j[u] = -1;
+        if (h < pieces && lane < kEntries) {
+          const int at = span == 1 ? h : h / span, which = top.hit[at];
+          const int b = which / kFwd * span + (h - at * span), i = (b * kBatch + lane / n) * kFwd + which % kFwd;
+          if (i < cnt) j[u] = row.first(g0 + i) + lane % n;
+          if (j[u] >= p.V) j[u] = -1;
+        }
+        f[u] = j[u] >= 0 ? Granule<T>::read(row.x + j[u]) : -INFINITY;
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (j[u] >= 0 && f[u] >= tau) {
+          const int place = atomicAdd(&top.count, 1);
+          if (place < kCand) top.cand[place] = order_key(f[u], j[u]);
         }
     }
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      const float a = (f[e] - Mz) * c2, ex = exp2_approx(a);
-      S += ex;
-      W = fmaf(ex, fmaxf(a, -1e4f), W);                             // 0 * -inf would be NaN
-    }
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    S += __shfl_xor_sync(~0u, S, o);
-    W += __shfl_xor_sync(~0u, W, o);
-  }
-  if (lane == 0) red[1][warp] = S, red[2][warp] = W;
-  __syncthreads();
-  S = red[1][0], W = red[2][0];
-#pragma unroll
-  for (int i = 1; i < kWarps; ++i) S += red[1][i], W += red[2][i];
-
-  if (TOP) {                                // this CTA's leading entries, in order
-    const int found = top.count;
     if (tid < ASI_TOP_MAX) top.list[tid] = 0;
     __syncthreads();
+    const int found = top.count;
     if (found <= kCand) {
-      for (int i = tid; i < found; i += kThreads) {
+      for (int i = tid; i < found; i += kFwd) {
         const unsigned long long key = top.cand[i];
         int above = 0;
         for (int q = 0; q < found; ++q) above += top.cand[q] > key;
@@ -303,9 +538,9 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const __grid_constant__ Lo
       unsigned long long prev = ~0ull;
       for (int r = 0; r < p.k; ++r) {
         unsigned long long best = 0;
-        for (int i = tid; i < cnt; i += kThreads) {
+        for (int i = tid; i < cnt; i += kFwd) {
           float f[n];
-          Granule<T>::floats(at(i), f);
+          Granule<T>::floats(row.load(g0 + i), f);
           const int j = row.first(g0 + i);
 #pragma unroll
           for (int e = 0; e < n; ++e)
@@ -330,76 +565,131 @@ __global__ void __launch_bounds__(kThreads) k_logprob(const __grid_constant__ Lo
         prev = best;
       }
     }
+    __syncthreads();
   }
 
   if (cl > 1) {
-    if (tid == 0) mine[0] = M, mine[1] = S, mine[2] = W;
+    if (tid == 0) sh.mine[0] = M, sh.mine[1] = S, sh.mine[2] = W;
     cluster_arrive();                       // (every thread's writes above, the lists among them)
     cluster_wait();
-    if (tid < 3 * cl) parts[tid % 3][tid / 3] = remote_f(&mine[tid % 3], tid / 3);
-    if (TOP && rank == 0)
-      for (int i = tid; i < cl * p.k; i += kThreads) top.cand[i] = remote_u64(&top.list[i % p.k], i / p.k);
-    __syncthreads();
-    cluster_arrive();                       // the others' shared memory is read no more; waited for at the end
-    float Mt = parts[0][0];
-    for (int q = 1; q < cl; ++q) Mt = nan_max(Mt, parts[0][q]);
-    S = W = 0.f;
-    for (int q = 0; q < cl; ++q) {
-      if (parts[0][q] == -INFINITY) continue;                       // nothing there
-      const float a = (parts[0][q] - Mt) * c2, f = exp2_approx(a);
-      S = fmaf(f, parts[1][q], S);
-      W = fmaf(f, fmaf(fmaxf(a, -1e4f), parts[1][q], parts[2][q]), W);
+    if (rank == 0) {
+      if (tid < 3 * cl) sh.parts[tid % 3][tid / 3] = remote_f(&sh.mine[tid % 3], tid / 3);
+      if (TOP)
+        for (int i = tid; i < cl * p.k; i += kFwd) top.cand[i] = remote_u64(&top.list[i % p.k], i / p.k);
+      __syncthreads();
     }
-    M = Mt;
-    if (TOP && rank == 0) {
-      for (int i = tid; i < cl * p.k; i += kThreads) {
+    cluster_arrive();                       // the others' shared memory is read no more
+    cluster_wait();
+    if (rank) return;
+    cluster_sums<kWarps>(M, S, W, c2, cl, sh);
+    if (TOP) {
+      for (int i = tid; i < cl * p.k; i += kFwd) {
         const unsigned long long key = top.cand[i];
         int above = 0;
         for (int q = 0; q < cl * p.k; ++q) above += top.cand[q] > key;
-        if (key && above < p.k) top.list[above] = key;           // (no CTA reads this list any more)
+        if (key && above < p.k) top.list[above] = key;
       }
+      __syncthreads();
     }
   }
-  if (TOP) __syncthreads();
-
-  const bool dead = M == -INFINITY;
-  const float lnS = logf(S);
-  const float H = dead ? 0.f : lnS - kLn2 * W / S;
-  if (rank == 0) {
-    if (tid == 0) {
-      p.lse[t] = dead ? -INFINITY : fmaf(M, p.scale, lnS);
-      if (p.entropy) p.entropy[t] = H;
-      p.logp[t] = skip ? 0.f : !given ? NAN : dead ? -INFINITY : (xy - M) * p.scale - lnS;
-    }
-    if (TOP && tid < p.k) {
-      const bool fine = !isnan(lnS);
-      const unsigned long long key = fine ? top.list[tid] : 0;
-      p.top_ids[(int64_t)t * p.k + tid] = fine ? key_index(key) : tid;
-      p.top_logp[(int64_t)t * p.k + tid] = !fine ? NAN : dead ? -INFINITY : (key_value(key) - M) * p.scale - lnS;
-    }
+  if (tid == 0) write_row(p, t, M, S, W, xy, given, skip);
+  if (TOP && tid < p.k) {
+    const float lnS = logf(S);
+    const bool fine = !isnan(lnS), dead = M == -INFINITY;
+    const unsigned long long key = fine ? top.list[tid] : 0;
+    p.top_ids[(int64_t)t * p.k + tid] = fine ? key_index(key) : tid;
+    p.top_logp[(int64_t)t * p.k + tid] = !fine ? NAN : dead ? -INFINITY : (key_value(key) - M) * p.scale - lnS;
   }
+}
 
-  if (GRAD) {
-    T* dx = static_cast<T*>(p.dx) + (int64_t)t * p.ldg;
-    const bool wide = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0;
-    const float alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f, inv = 1.f / S;
-    const bool zero = skip || dead;
+// ---- forward and gradient.  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
+// is read again: rows of more than 1.6 MB).  Every thread reads back what it left there itself: no barrier.
+template <typename T, bool RES>
+__global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant__ LogprobArgs p) {
+  constexpr int n = Granule<T>::n, kWarps = kLoss / 32;
+  extern __shared__ uint4 buf[];
+  __shared__ RowShared<kWarps> sh;
+  const int tid = threadIdx.x, cl = p.cl, t = blockIdx.x / cl, rank = blockIdx.x - t * cl;
+  const float c2 = p.scale * kLog2e;
+  const Share<T> s(p, t, rank);
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t y = p.y[t];
+  const bool given = y >= 0 && y < p.V, skip = y == p.ignore;
+  // the given entry: read by the thread that reports logp and by the one that writes its gradient (dx may be x)
+  const int yg = given ? (int)((s.row.mis + y) / n) - s.g0 : -1;
+  const bool mine = yg >= 0 && yg < s.cnt && yg % kLoss == tid;
+  float xy = 0.f;
+  if (mine || (given && tid == 0 && rank == 0)) xy = Granule<T>::read(s.row.x + y);
+  const float alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f;
+
+  float M, S, W;
+  stream_share<T, kLoss>(s, c2, M, S, W, [&](int b, const uint4* v, float) {
+    if (RES) {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q)
+        if ((b * kBatch + q) * kLoss + tid < s.cnt) buf[(b * kBatch + q) * kLoss + tid] = v[q];
+    }
+  });
+  const float own = M;
+  M = block_max<kWarps>(M, sh.red[0]);
+  rebase(S, W, own, M, c2);
+  block_sums<kWarps>(S, W, sh.red);
+  if (cl > 1) {
+    if (tid == 0) sh.mine[0] = M, sh.mine[1] = S, sh.mine[2] = W;
+    cluster_arrive();
+    cluster_wait();
+    if (tid < 3 * cl) sh.parts[tid % 3][tid / 3] = remote_f(&sh.mine[tid % 3], tid / 3);
+    __syncthreads();
+    cluster_arrive();                       // the others' shared memory is read no more; waited for at the end
+    cluster_sums<kWarps>(M, S, W, c2, cl, sh);
+  }
+  if (rank == 0 && tid == 0) write_row(p, t, M, S, W, xy, given, skip);
+
+  T* dx = static_cast<T*>(p.dx) + (int64_t)t * p.ldg;
+  // granules stored whole: where dx starts on the same offset within 16 bytes as x
+  const bool wide = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(s.row.x)) & 15) == 0;
+  const int wlo = wide ? s.lo : s.cnt, whi = wide ? s.hi : 0;
+  uint4* to = reinterpret_cast<uint4*>(dx - s.row.mis) + s.g0;
+  auto put = [&](int i, const float (&f)[n]) {
+    if (i >= wlo && i < whi) {
+      to[i] = Granule<T>::pack(f);
+    } else {
+      const int j = s.row.first(s.g0 + i);
+#pragma unroll
+      for (int e = 0; e < n; ++e)
+        if (j + e >= 0 && j + e < s.row.V) dx[j + e] = Granule<T>::one(f[e]);
+    }
+  };
+  if (skip || M == -INFINITY) {
+    float f[n];
+#pragma unroll
+    for (int e = 0; e < n; ++e) f[e] = 0.f;
+    for (int i = tid; i < s.cnt; i += kLoss) put(i, f);
+  } else {
+    const float inv = 1.f / S, lnS = logf(S), H = lnS - kLn2 * W * inv;
     const float A = given ? -p.scale * (alpha + beta * (H - lnS)) * inv : NAN, B = -p.scale * beta * kLn2 * inv;
-    for (int i = tid; i < cnt; i += kThreads) {
-      float f[n];
-      Granule<T>::floats(at(i), f);
-      const int j = row.first(g0 + i);
+    const f2 minus = pair(-M, -M), k2 = pair(c2, c2), A2 = pair(A, A), B2 = pair(B, B);
+    const uint4* src = s.row.granule(s.g0);
+    auto gradient = [&](auto with_entropy) {
+#pragma unroll 2
+      for (int i = tid; i < s.cnt; i += kLoss) {
+        f2 x[n / 2];
+        Granule<T>::pairs(RES ? buf[i] : i >= s.lo && i < s.hi ? src[i] : s.row.edge(s.g0 + i), x);
+        float f[n];
 #pragma unroll
-      for (int e = 0; e < n; ++e) {
-        const float a = (f[e] - M) * c2;
-        f[e] = zero ? 0.f : exp2_approx(a) * fmaf(B, fmaxf(a, -1e4f), A);
+        for (int e = 0; e < n / 2; ++e) {
+          const f2 a = mul2(add2(x[e], minus), k2);
+          unpair(mul2(exp2_both(a), decltype(with_entropy)::value ? fma2(B2, finite2(a), A2) : A2), f[2 * e], f[2 * e + 1]);
+        }
+        put(i, f);
       }
-      if (given && !zero && y >= j && y < j + n) {
-#pragma unroll
-        for (int e = 0; e < n; ++e)
-          if (j + e == y) f[e] += p.scale * alpha;
-      }
-      store_granule(dx, row, g0 + i, f, wide);
+    };
+    if (beta != 0.f) gradient(std::true_type());
+    else gradient(std::false_type());
+    if (mine) {
+      const float a = (xy - M) * c2;
+      dx[y] = Granule<T>::one(fmaf(p.scale, alpha, exp2_approx(a) * fmaf(B, fmaxf(a, -1e4f), A)));
     }
   }
   if (cl > 1) cluster_wait();
@@ -451,25 +741,15 @@ __global__ void __launch_bounds__(kThreads) k_logprob_grad(const __grid_constant
   }
 }
 
-// CTAs of a row: few enough that a share of 72 KB at most lets three CTAs run on an SM, more where the rows alone do not
-// fill the machine and a share keeps two granules a thread.
-int cluster_of(int64_t rows, int64_t granules) {
-  int cl = 1;
-  while (cl < kMaxCluster && granules * 16 > (int64_t)cl * (72 << 10)) cl *= 2;
-  while (cl < kMaxCluster && rows * cl < 148 && granules >= 4 * cl * kThreads) cl *= 2;
-  return cl;
-}
-
-template <typename T, bool GRAD, bool TOP, bool RES>
-cudaError_t launch_one(const LogprobArgs& a, int64_t rows, size_t smem, cudaStream_t st) {
-  auto kernel = k_logprob<T, GRAD, TOP, RES>;
+template <typename K>
+cudaError_t launch_rows(K kernel, int threads, const LogprobArgs& a, int64_t rows, size_t smem, cudaStream_t st) {
   if (smem > 32 << 10) {
     const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * a.cl));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -483,22 +763,31 @@ cudaError_t launch_one(const LogprobArgs& a, int64_t rows, size_t smem, cudaStre
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+// CTAs of a row: more where the rows alone do not give every SM `each` CTAs, while a share keeps `least` granules
+int spread_rows(int64_t rows, int64_t granules, int cl, int each, int least) {
+  while (cl < kMaxCluster && rows * cl < 148 * each && granules >= (int64_t)2 * cl * least) cl *= 2;
+  return cl;
+}
+
 template <typename T>
 cudaError_t launch_logprob(LogprobArgs a, int64_t rows, bool grad, cudaStream_t st) {
   const int64_t granules = ((int64_t)a.V + 2 * Granule<T>::n - 2) / Granule<T>::n;   // of a row at the worst offset
-  a.cl = cluster_of(rows, granules);
+  if (!grad) {
+    a.cl = spread_rows(rows, granules, 1, 5, 2 * kFwd);
+    return a.k ? launch_rows(k_logprob<T, true>, kFwd, a, rows, 0, st) : launch_rows(k_logprob<T, false>, kFwd, a, rows, 0, st);
+  }
+  // shares of 72 KB at most let three CTAs run on an SM
+  a.cl = 1;
+  while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) a.cl *= 2;
+  a.cl = spread_rows(rows, granules, a.cl, 1, kLoss);
   const size_t share = (size_t)((granules + a.cl - 1) / a.cl) * 16;
-  const bool res = share <= 200 << 10;
-  const size_t smem = res ? share : 0;
-  if (grad) return res ? launch_one<T, true, false, true>(a, rows, smem, st) : launch_one<T, true, false, false>(a, rows, smem, st);
-  if (a.k) return res ? launch_one<T, false, true, true>(a, rows, smem, st) : launch_one<T, false, true, false>(a, rows, smem, st);
-  return res ? launch_one<T, false, false, true>(a, rows, smem, st) : launch_one<T, false, false, false>(a, rows, smem, st);
+  return share <= 200 << 10 ? launch_rows(k_loss<T, true>, kLoss, a, rows, share, st) : launch_rows(k_loss<T, false>, kLoss, a, rows, 0, st);
 }
 
 asi_status_t check_desc(const asi_logprob_desc_t* d) {
   if (!d || (d->in_dtype != ASI_F32 && d->in_dtype != ASI_BF16)) return ASI_ERR_INVALID_ARG;
   if (d->rows < 0 || d->vocab < 1 || d->ld < d->vocab) return ASI_ERR_INVALID_ARG;
-  if (!(d->scale > 0.f) || !std::isfinite(d->scale)) return ASI_ERR_INVALID_ARG;
+  if (!(d->scale >= 1e-30f && d->scale <= 1e30f)) return ASI_ERR_INVALID_ARG;
   if (d->rows > ASI_LOGPROB_MAX_ROWS || d->vocab > ASI_LOGPROB_MAX_VOCAB) return ASI_ERR_UNSUPPORTED;
   if (d->ld > INT64_MAX / 8 / std::max<int64_t>(d->rows, 1)) return ASI_ERR_INVALID_ARG;
   return ASI_OK;
