@@ -342,7 +342,8 @@ asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t
 /* One AdamW step over many tensors.  For every element, with g = grad_scale * grad:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
  *   w = (1 - lr weight_decay) w - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, w rounded to weight_dtype at the end (and once more, to bf16, into `copy`).
+ * in fp32, w rounded to weight_dtype at the end (and to bf16 into `copy`).  sqrt and the quotient are off by at most 2^-22,
+ * sqrt(v) of a v below 2^-126 is 0.
  * States in 8 bits: every ASI_ADAMW_BLOCK consecutive elements of a tensor share a scale 2^k, held as the byte
  * k + 127; exp_avg holds m / 2^k and exp_avg_sq holds sqrt(v) / 2^k as e4m3 (round to nearest even).  k is the smallest,
  * from -126 up, with max |.| <= 448 2^k over the block's finite values (0 where all are 0).  A sqrt(v) above 0 is held
@@ -352,7 +353,7 @@ asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t
 typedef struct {
   int32_t weight_dtype, grad_dtype;   /* asi_dtype_t */
   int32_t state_bits;                 /* 32 or 8 */
-  double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0;  betas in [0, 1);  eps >= 1e-30 */
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0;  betas in [0, 1);  eps >= 1e-16 */
   int64_t step;                       /* t >= 1 */
   /* for steps that are captured into a graph; device pointers or null: */
   const float* lr_dev;                /* instead of lr */

@@ -2,8 +2,9 @@
 //
 //   m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;  w = (1 - lr wd) w - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// m, v and sqrt(v) are computed in separately rounded fp32 operations in the order written, so that the 8-bit codes are a
-// function of the inputs alone (no contraction that another build or a plain restatement would do otherwise).
+// m and v are computed in separately rounded fp32 operations in the order written (no contraction that another build or a plain
+// restatement would do otherwise); the square root and the reciprocal are the hardware's, off by a unit or two in the last place,
+// and the root of a subnormal v is 0.
 //
 // What bounds it: weights and states read and written once, gradients read once.  A warp takes blocks of 256 elements,
 // eight a lane: with 8-bit states the block's largest magnitude is one warp reduction away and codes are quantised where
@@ -14,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -41,6 +43,7 @@ struct AwHyper {
   float b1, b2, c1, c2;                       // betas and 1 - beta
   float decay, step, root, eps;               // 1 - lr wd, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   float lr, wd, log_b1, log_b2;               // for lr and t in device memory
+  float one;                                  // a sum x 1 + y: the assembler contracts packed products and sums, but not this
   const float *lr_dev, *scale;
   const int64_t* step_dev;
 };
@@ -54,114 +57,266 @@ struct AwArgs {
   int count;
 };
 
-template <typename T>
-__device__ __forceinline__ void read8(const T* p, int64_t left, bool wide, float* f);
-template <>
-__device__ __forceinline__ void read8<float>(const float* p, int64_t left, bool wide, float* f) {
-  if (wide && left >= 8) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < left ? p[i] : 0.f;
-  }
+// two fp32 values as one operand of the packed instructions (each rounded as the scalar ones round)
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
+__device__ __forceinline__ float2 both(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 twice(float a) { return pair(a, a); }
+__device__ __forceinline__ float root_approx(float v) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float inverse_approx(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// Eight consecutive values of a lane as they lie in memory.  `whole`: all eight are there, 16-byte aligned (8 for codes);
+// else `left` of them, one by one, the others 0.
+template <typename T>
+struct Raw;
 template <>
-__device__ __forceinline__ void read8<__nv_bfloat16>(const __nv_bfloat16* p, int64_t left, bool wide, float* f) {
-  if (wide && left >= 8) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
+struct Raw<float> {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const void* from, int64_t at, int64_t left, bool whole) {
+    const float* p = static_cast<const float*>(from) + at;
+    if (whole) {
+      a = *reinterpret_cast<const uint4*>(p);
+      b = *reinterpret_cast<const uint4*>(p + 4);
+    } else {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+      a = make_uint4(w[0], w[1], w[2], w[3]);
+      b = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+  __device__ __forceinline__ void values(f2* f) const {
+    f[0] = pair(__uint_as_float(a.x), __uint_as_float(a.y)), f[1] = pair(__uint_as_float(a.z), __uint_as_float(a.w));
+    f[2] = pair(__uint_as_float(b.x), __uint_as_float(b.y)), f[3] = pair(__uint_as_float(b.z), __uint_as_float(b.w));
+  }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const void* from, int64_t at, int64_t left, bool whole) {
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(from) + at;
+    if (whole) {
+      a = *reinterpret_cast<const uint4*>(p);
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) w[i >> 1] |= (uint32_t)__bfloat16_as_ushort(p[i]) << (16 * (i & 1));
+      a = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void values(f2* f) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < left ? __bfloat162float(p[i]) : 0.f;
+    for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-}
-__device__ __forceinline__ void write8(float* p, int64_t left, bool wide, const float* f) {
-  if (wide && left >= 8) {
-    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+};
+struct Codes {
+  uint2 a;
+  __device__ __forceinline__ void load(const void* from, int64_t at, int64_t left, bool whole) {
+    const uint8_t* p = static_cast<const uint8_t*>(from) + at;
+    if (whole) {
+      a = *reinterpret_cast<const uint2*>(p);
+    } else {
+      uint32_t w[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+      a = make_uint2(w[0], w[1]);
+    }
+  }
+  __device__ __forceinline__ void store(void* to, int64_t at, int64_t left, bool whole) const {
+    uint8_t* p = static_cast<uint8_t*>(to) + at;
+    if (whole) {
+      *reinterpret_cast<uint2*>(p) = a;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) p[i] = (uint8_t)((i < 4 ? a.x : a.y) >> (8 * (i & 3)));
+    }
+  }
+  __device__ __forceinline__ void values(float scale, f2* f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint16_t two = (uint16_t)((i < 2 ? a.x : a.y) >> (16 * (i & 1)));
+      const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3)));
+      f[i] = mul2(pair(v.x, v.y), twice(scale));
+    }
+  }
+};
+
+__device__ __forceinline__ void store_values(float* base, int64_t at, int64_t left, bool whole, const f2* f) {
+  float* p = base + at;
+  const float2 v[4] = {both(f[0]), both(f[1]), both(f[2]), both(f[3])};
+  if (whole) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = f[i];
+      if (i < left) p[i] = i & 1 ? v[i >> 1].y : v[i >> 1].x;
   }
 }
-__device__ __forceinline__ void write8(__nv_bfloat16* p, int64_t left, bool wide, const float* f) {
-  if (wide && left >= 8) {
-    uint32_t w[4];
+__device__ __forceinline__ void store_values(__nv_bfloat16* base, int64_t at, int64_t left, bool whole, const f2* f) {
+  __nv_bfloat16* p = base + at;
+  uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = both(f[i]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  if (whole) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = __float2bfloat16_rn(f[i]);
+      if (i < left) p[i] = __ushort_as_bfloat16((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
   }
 }
 
 // 2^(byte - 127)
-__device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float(byte ? (uint32_t)byte << 23 : 0x00400000u); }
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 
-__device__ __forceinline__ void decode8(const uint8_t* p, int64_t left, bool wide, float scale, float* f) {
-  uint32_t w[2] = {0, 0};
-  if (wide && left >= 8) {
-    const uint2 a = *reinterpret_cast<const uint2*>(p);
-    w[0] = a.x, w[1] = a.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-  }
+// The block's scale byte from the lanes' eight values each: the smallest 2^k with max <= 448 2^k = 1.75 2^(k + 8), over
+// the finite values.  `finite` tells whether there are others than those (or NaN, which a maximum passes over).
+__device__ __forceinline__ uint32_t block_scale(const f2* f, bool& finite) {
+  float most = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint16_t two = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3);
-    const float2 v = __half22float2(__half2(h));
-    f[2 * i] = v.x * scale, f[2 * i + 1] = v.y * scale;
+    const float2 v = both(f[i]);
+    most = fmaxf(fmaxf(most, fabsf(v.x)), fabsf(v.y));
   }
-}
-
-// The block's scale byte from the lanes' eight values each: the smallest 2^k with max <= 448 2^k = 1.75 2^(k + 8)
-__device__ __forceinline__ uint32_t block_scale(const float* f) {
-  uint32_t top = 0;
+  uint32_t top = __reduce_max_sync(~0u, __float_as_uint(most));   // magnitudes order as their bits do
+  finite = top < 0x7f800000u;
+  if (!finite) {
+    top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
-    if (b < 0x7f800000u) top = max(top, b);                 // finite: magnitudes order as their bits do
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = both(f[i]);
+      const uint32_t x = __float_as_uint(fabsf(v.x)), y = __float_as_uint(fabsf(v.y));
+      top = max(top, max(x < 0x7f800000u ? x : 0u, y < 0x7f800000u ? y : 0u));
+    }
+    top = __reduce_max_sync(~0u, top);
   }
-  top = __reduce_max_sync(~0u, top);
   if (top == 0) return 127;
   const int k = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
   return (uint32_t)(max(k, -126) + 127);
 }
 
-__device__ __forceinline__ void encode8(uint8_t* p, int64_t left, bool wide, uint32_t byte, bool above_zero, const float* f) {
-  const float inv = __uint_as_float((254u - byte) << 23);   // 2^-k; byte is 1 .. 247
+// kRoot: values above 0 whose code is 0 get the smallest code, 1
+template <bool kRoot>
+__device__ __forceinline__ Codes encode(const f2* f, uint32_t byte, bool finite) {
+  const f2 inv = twice(__uint_as_float((254u - byte) << 23));      // 2^-k; byte is 1 .. 247
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = f[2 * i] * inv, b = f[2 * i + 1] * inv;
-    if (above_zero) {
-      if (a > 0.f) a = fmaxf(a, 0.001953125f);              // 2^-9, the smallest code
-      if (b > 0.f) b = fmaxf(b, 0.001953125f);
+    const float2 v = both(mul2(f[i], inv));
+    uint32_t two = __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
+    if (!finite) {                                                 // infinities (saturated above) are held as NaN
+      if (isinf(v.x)) two |= 0x7fu;
+      if (isinf(v.y)) two |= 0x7f00u;
     }
-    uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-    // infinities (saturated above) are held as NaN
-    if (isinf(a)) two |= 0x7fu;
-    if (isinf(b)) two |= 0x7f00u;
     w[i >> 1] |= two << (16 * (i & 1));
   }
-  if (wide && left >= 8) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-  } else {
+  if (kRoot) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    for (int h = 0; h < 2; ++h)
+      if ((w[h] - 0x01010101u) & 0x80808080u & ~w[h]) {            // a code of 0 among the four
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 v = both(f[2 * h + (i >> 1)]);
+          if (!((w[h] >> (8 * i)) & 0xffu) && (i & 1 ? v.y : v.x) > 0.f) w[h] |= 1u << (8 * i);
+        }
+      }
+  }
+  Codes c;
+  c.a = make_uint2(w[0], w[1]);
+  return c;
+}
+
+template <typename TW, typename TG, bool BITS8>
+struct Block {                              // eight values a lane of everything
+  Raw<TW> w;
+  Raw<TG> g;
+  std::conditional_t<BITS8, Codes, Raw<float>> m, v;
+  uint32_t ms, vs;
+  __device__ __forceinline__ void load(const AwTensor& t, int64_t b, int64_t at, int64_t left, bool whole) {
+    w.load(t.w, at, left, whole);
+    g.load(t.g, at, left, whole);
+    m.load(t.m, at, left, whole);
+    v.load(t.v, at, left, whole);
+    if (BITS8) ms = t.ms[b], vs = t.vs[b];
+  }
+};
+struct Rates {
+  float decay, step, root, gs;
+  bool scaled;
+};
+
+template <typename TW, typename TG, bool BITS8>
+__device__ __forceinline__ void step_block(const Block<TW, TG, BITS8>& in, const AwTensor& t, const AwHyper& h, const Rates& r,
+                                           int64_t b, int64_t at, int64_t left, bool whole) {
+  f2 w[4], g[4], m[4], v[4], root[4];
+  in.w.values(w);
+  in.g.values(g);
+  if constexpr (BITS8) {
+    in.m.values(scale_of(in.ms), m);
+    in.v.values(scale_of(in.vs), v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
+  } else {
+    in.m.values(m);
+    in.v.values(v);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (r.scaled) g[i] = mul2(g[i], twice(r.gs));
+    m[i] = fma2(mul2(m[i], twice(h.b1)), twice(h.one), mul2(g[i], twice(h.c1)));
+    v[i] = fma2(mul2(v[i], twice(h.b2)), twice(h.one), mul2(mul2(g[i], g[i]), twice(h.c2)));
+    const float2 x = both(v[i]);
+    root[i] = pair(root_approx(x.x), root_approx(x.y));
+    const float2 d = both(fma2(root[i], twice(r.root), twice(h.eps)));
+    const f2 u = mul2(m[i], pair(inverse_approx(d.x), inverse_approx(d.y)));
+    w[i] = fma2(u, twice(-r.step), mul2(w[i], twice(r.decay)));
+  }
+  store_values(static_cast<TW*>(t.w), at, left, whole, w);
+  if (t.copy) store_values(t.copy, at, left, whole, w);
+  if constexpr (BITS8) {
+    bool fm, fv;
+    const uint32_t sm = block_scale(m, fm), sv = block_scale(root, fv);
+    encode<false>(m, sm, fm).store(t.m, at, left, whole);
+    encode<true>(root, sv, fv).store(t.v, at, left, whole);
+    if ((threadIdx.x & 31) == 0) t.ms[b] = (uint8_t)sm, t.vs[b] = (uint8_t)sv;
+  } else {
+    store_values(static_cast<float*>(t.m), at, left, whole, m);
+    store_values(static_cast<float*>(t.v), at, left, whole, v);
   }
 }
 
@@ -175,57 +330,38 @@ __global__ void __launch_bounds__(kAwThreads) k_adamw(const __grid_constant__ Aw
     else n = half;
   }
   const AwTensor& t = p.t[lo];
-  const bool wide = p.wide[lo];
-  const int64_t b0 = (int64_t)(blockIdx.x - p.first[lo]) * kSpan, blocks = (t.n + kBlock - 1) / kBlock;
+  const int64_t blocks = (t.n + kBlock - 1) / kBlock, b0 = (int64_t)(blockIdx.x - p.first[lo]) * kSpan + warp;
   pdl_wait();
   pdl_launch_dependents();
   const AwHyper& h = p.h;
-  float decay = h.decay, step = h.step, root = h.root;
+  Rates r = {h.decay, h.step, h.root, 1.f, h.scale != nullptr};
   if (h.lr_dev || h.step_dev) {
     const float lr = h.lr_dev ? *h.lr_dev : h.lr;
-    decay = 1.f - lr * h.wd;
+    r.decay = 1.f - lr * h.wd;
     float c = h.step;                                       // 1 / (1 - b1^t) where lr is apart
     if (h.step_dev) {
       const float s = (float)*h.step_dev;
       c = -1.f / expm1f(s * h.log_b1);
-      root = rsqrtf(-expm1f(s * h.log_b2));
+      r.root = rsqrtf(-expm1f(s * h.log_b2));
     }
-    step = lr * c;
+    r.step = lr * c;
   }
-  const float gs = h.scale ? *h.scale : 1.f;
-  for (int64_t b = b0 + warp; b < min(b0 + kSpan, blocks); b += kAwWarps) {
-    const int64_t at = b * kBlock + lane * kLane, left = t.n - at;
-    float w[8], g[8], m[8], v[8];
-    read8<TW>(static_cast<const TW*>(t.w) + at, left, wide, w);
-    read8<TG>(static_cast<const TG*>(t.g) + at, left, wide, g);
-    if (BITS8) {
-      decode8(static_cast<const uint8_t*>(t.m) + at, left, wide, scale_of(t.ms[b]), m);
-      decode8(static_cast<const uint8_t*>(t.v) + at, left, wide, scale_of(t.vs[b]), v);
+  if (r.scaled) r.gs = *h.scale;
+  constexpr int kEach = kSpan / kAwWarps;                   // blocks of a warp, all on their way before the first is worked on
+  if (p.wide[lo] && (b0 - warp + kSpan) * kBlock <= t.n) {
+    Block<TW, TG, BITS8> in[kEach];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
-    } else {
-      read8<float>(static_cast<const float*>(t.m) + at, left, wide, m);
-      read8<float>(static_cast<const float*>(t.v) + at, left, wide, v);
-    }
-    float r[8];
+    for (int i = 0; i < kEach; ++i) in[i].load(t, b0 + i * kAwWarps, (b0 + i * kAwWarps) * kBlock + lane * kLane, 8, true);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float gi = h.scale ? __fmul_rn(g[i], gs) : g[i];
-      m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(gi, h.c1));
-      v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
-      r[i] = __fsqrt_rn(v[i]);
-      w[i] = fmaf(w[i], decay, -step * __fdividef(m[i], fmaf(r[i], root, h.eps)));
-    }
-    write8(static_cast<TW*>(t.w) + at, left, wide, w);
-    if (t.copy) write8(t.copy + at, left, wide, w);
-    if (BITS8) {
-      const uint32_t sm = block_scale(m), sv = block_scale(r);
-      encode8(static_cast<uint8_t*>(t.m) + at, left, wide, sm, false, m);
-      encode8(static_cast<uint8_t*>(t.v) + at, left, wide, sv, true, r);
-      if (lane == 0) t.ms[b] = (uint8_t)sm, t.vs[b] = (uint8_t)sv;
-    } else {
-      write8(static_cast<float*>(t.m) + at, left, wide, m);
-      write8(static_cast<float*>(t.v) + at, left, wide, v);
+    for (int i = 0; i < kEach; ++i)
+      step_block(in[i], t, h, r, b0 + i * kAwWarps, (b0 + i * kAwWarps) * kBlock + lane * kLane, 8, true);
+  } else {
+    for (int64_t b = b0; b < min(b0 - warp + kSpan, blocks); b += kAwWarps) {
+      const int64_t at = b * kBlock + lane * kLane, left = t.n - at;
+      const bool whole = p.wide[lo] && left >= 8;
+      Block<TW, TG, BITS8> in;
+      in.load(t, b, at, left, whole);
+      step_block(in, t, h, r, b, at, left, whole);
     }
   }
 }
@@ -300,7 +436,7 @@ extern "C" asi_status_t asi_adamw_step(const asi_adamw_desc_t* d, const asi_adam
       (d->state_bits != 32 && d->state_bits != 8))
     return ASI_ERR_INVALID_ARG;
   const bool betas = d->beta1 >= 0 && d->beta1 < 1 && d->beta2 >= 0 && d->beta2 < 1;
-  const bool rates = d->weight_decay >= 0 && std::isfinite(d->weight_decay) && d->eps >= 1e-30 && std::isfinite((float)d->eps) &&
+  const bool rates = d->weight_decay >= 0 && std::isfinite(d->weight_decay) && d->eps >= 1e-16 && std::isfinite((float)d->eps) &&
                      (d->lr_dev || (d->lr >= 0 && std::isfinite(d->lr)));
   if (!betas || !rates || (!d->step_dev && d->step < 1)) return ASI_ERR_INVALID_ARG;
   const size_t ew = d->weight_dtype == ASI_BF16 ? 2 : 4, eg = d->grad_dtype == ASI_BF16 ? 2 : 4, es = d->state_bits / 8;
@@ -334,6 +470,7 @@ extern "C" asi_status_t asi_adamw_step(const asi_adamw_desc_t* d, const asi_adam
     if (!fine || !written_apart(ranges)) return ASI_ERR_INVALID_ARG;
     AwHyper h = {};
     h.b1 = (float)d->beta1, h.b2 = (float)d->beta2, h.c1 = (float)(1 - d->beta1), h.c2 = (float)(1 - d->beta2);
+    h.one = 1.f;
     h.eps = (float)d->eps, h.lr = (float)d->lr, h.wd = (float)d->weight_decay;
     h.log_b1 = (float)std::log(d->beta1), h.log_b2 = (float)std::log(d->beta2);
     h.lr_dev = d->lr_dev, h.step_dev = d->step_dev, h.scale = d->grad_scale;
@@ -344,7 +481,10 @@ extern "C" asi_status_t asi_adamw_step(const asi_adamw_desc_t* d, const asi_adam
     }
     h.decay = (float)(1 - d->lr * d->weight_decay);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return cuda_status(count <= 32 ? step_tensors<32>(h, d, tensors, count, st) : step_tensors<400>(h, d, tensors, count, st), "AdamW step");
+    return cuda_status(count <= 16   ? step_tensors<16>(h, d, tensors, count, st)
+                       : count <= 64 ? step_tensors<64>(h, d, tensors, count, st)
+                                     : step_tensors<400>(h, d, tensors, count, st),
+                       "AdamW step");
   } catch (...) {
     return no_host_memory();
   }

@@ -1,7 +1,8 @@
-"""AdamW over many tensors.  m, v and sqrt(v) are separately rounded fp32 operations, so states (and their 8-bit codes and
-scales) have to equal a restatement in numpy's fp32 bit for bit.  The weight: u = 2^-24 a rounding; the product with the
-decay, the denominator (2), its reciprocal and product (4), the step's own rounding and product (2) and the last sum make at
-most 2 u |w| + 10 u |update|, where the update's m and v are taken as the rounded ones; then half a step of the weight's type."""
+"""AdamW over many tensors.  m and v are separately rounded fp32 operations, so states (and the 8-bit codes and scales of m)
+have to equal a restatement in numpy's fp32 bit for bit; sqrt(v) is the hardware's, off by at most 2^-23 of its value, so its
+codes and scales have to be those of a value within that.  The weight, u = 2^-24 a rounding: the root 2 u, its constant, the
+constant eps, the denominator, the step's constant and two products u each, the reciprocal 2 u, so 10 u |update| at most,
+where m and v are taken as rounded; 2 u |w| for the decay and its product; then half a step of the weight's type."""
 import math
 
 import numpy as np
@@ -95,10 +96,19 @@ def check_step(r, t, h=HYPER, gs=None, lr=None, slack=0.0, call=None, **kw):
             tol = U * (2 * np.abs(w) + (10 + slack) * np.abs(up)) + torch.finfo(BF).eps / 2 * np.abs(new) * (1 + 2.0 ** -7) + 2.0 ** -140
             assert (np.abs(r.copies[i].double().cpu().numpy() - new) <= tol).all()
         if r.bits8:
-            for x, codes, scales, sq in ((m, r.exp_avg[i], r.exp_avg_scale[i], False), (rt, r.exp_avg_sq[i], r.exp_avg_sq_scale[i], True)):
-                c, e = encode(x, sq)
-                assert np.array_equal(scales.view(torch.uint8).cpu().numpy(), e), (i, sq)
-                assert torch.equal(codes.view(torch.uint8).cpu(), c.view(torch.uint8)), (i, sq)
+            c, e = encode(m, False)
+            assert np.array_equal(r.exp_avg_scale[i].view(torch.uint8).cpu().numpy(), e), i
+            assert torch.equal(r.exp_avg[i].view(torch.uint8).cpu(), c.view(torch.uint8)), i
+            got_e = r.exp_avg_sq_scale[i].view(torch.uint8).cpu().numpy()
+            (_, e0), (_, e1) = (encode((rt.astype(np.float64) * (1 + s * 2.0 ** -23)).astype(np.float32), True) for s in (-1, 1))
+            assert ((got_e >= e0) & (got_e <= e1)).all(), i
+            # codes of values at either end of the root's error, under the scales that are there
+            got = r.exp_avg_sq[i].float().cpu().numpy()
+            lo, hi = ((rt.astype(np.float64) * (1 + s * 2.0 ** -23) / np.exp2(got_e.astype(np.float64) - 127)[np.arange(len(rt)) // 256])
+                      for s in (-1, 1))
+            lo, hi = (torch.from_numpy(np.minimum(x, 448).astype(np.float32)).to(torch.float8_e4m3fn).float().numpy() for x in (lo, hi))
+            lo, hi = (np.where((rt > 0) & (x == 0), np.float32(2.0 ** -9), x) for x in (lo, hi))
+            assert ((got >= lo) & (got <= hi)).all(), i
         else:
             assert np.array_equal(r.exp_avg[i].cpu().numpy(), m) and np.array_equal(r.exp_avg_sq[i].cpu().numpy(), v), i
 

@@ -164,7 +164,7 @@ def tensors(B, entries):
 
 @pytest.mark.parametrize("bad", [
     dict(weight_dtype=2), dict(grad_dtype=-1), dict(state_bits=16), dict(lr=-1e-9), dict(lr=math.nan), dict(lr=math.inf),
-    dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=math.inf), dict(eps=1e300),
+    dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=9e-17), dict(eps=math.inf), dict(eps=1e300),
     dict(weight_decay=-1.0), dict(weight_decay=math.inf), dict(step=0), dict(lr_dev=at(99) + 2), dict(step_dev=at(99) + 4),
     dict(grad_scale=at(99) + 1),
 ])
