@@ -319,12 +319,13 @@ asi_status_t asi_token_loss(const asi_logprob_desc_t* desc, const void* logits, 
 /* Embedding: out[t][:] = scale * table[ids[t]][:], an id outside [0, vocab) gives a row of NaN.
  * Its weight gradient beside those of conv2d and linear layers:
  *   dW[v][:] = scale * sum over t with ids[t] = v of dOut[t][:]      (fp32, terms in the order of t in fixed groups)
- * added to what dW holds (accumulate != 0: a table tied to the output layer), or written over all of dW.  Tokens of
+ * added to what dW holds (accumulate != 0: a table tied to the output layer; subnormal sums count as 0 there), or written
+ * over all of dW.  Tokens of
  * padding_idx and ids outside [0, vocab) contribute nothing. */
 typedef struct {
   int32_t table_dtype;           /* asi_dtype_t of table (asi_embedding_forward) */
   int32_t in_dtype;              /* asi_dtype_t of out and dOut */
-  int64_t vocab, dim, tokens;    /* at most 2^30, 2^22 and 2^24;  tokens may be 0 */
+  int64_t vocab, dim, tokens;    /* at most 2^30, 2^22, 2^24, dim tokens at most 2^38;  tokens may be 0 */
   int64_t padding_idx;           /* -1: none */
   float scale;                   /* finite */
 } asi_embedding_desc_t;

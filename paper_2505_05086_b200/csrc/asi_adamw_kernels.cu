@@ -25,11 +25,11 @@ namespace asi {
 
 namespace {
 
-constexpr int kAwThreads = 256;
+constexpr int kAwThreads = 128;
 constexpr int kAwWarps = kAwThreads / 32;
 constexpr int kBlock = ASI_ADAMW_BLOCK;
 constexpr int kLane = kBlock / 32;            // elements of a lane
-constexpr int kSpan = 16;                     // blocks of a CTA
+constexpr int kSpan = 8;                     // blocks of a CTA
 
 struct AwTensor {
   void* w;

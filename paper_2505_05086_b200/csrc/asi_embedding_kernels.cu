@@ -6,9 +6,11 @@
 // by id first (a stable radix sort of (id, t), so that equal ids keep the order of t), and runs of equal ids are summed
 // front to back: the same bits from call to call.  The sorted tokens are cut into chunks of equal length, whatever the ids,
 // so that one frequent id does not keep a single CTA busy: a run inside a chunk goes to dW at once, the pieces of a run
-// that crosses chunks meet in a last launch, in order.
+// that crosses chunks are added in order by the CTA that leaves the last of them.
 //
-// What bounds it: dOut read once and dW written once (overwriting: all of it, rows without tokens as zeros).
+// What bounds it: dOut read once and dW written once (overwriting: all of it, rows without tokens as zeros, by a kernel that
+// runs beside sort and sums).
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -18,33 +20,61 @@
 
 namespace asi {
 
+namespace cg = cooperative_groups;
+
 namespace {
 
 constexpr int kEmbThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ float as_float(T v);
+// N consecutive values as one word of N sizeof(T) bytes (at most 16), unpacked to and packed from floats
+template <int kBytes>
+struct WordOf;
 template <>
-__device__ __forceinline__ float as_float<float>(float v) { return v; }
+struct WordOf<16> { using type = uint4; };
 template <>
-__device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_float(float& o, float v) { o = v; }
-__device__ __forceinline__ void from_float(__nv_bfloat16& o, float v) { o = __float2bfloat16_rn(v); }
+struct WordOf<8> { using type = uint2; };
+template <>
+struct WordOf<4> { using type = uint32_t; };
+template <>
+struct WordOf<2> { using type = uint16_t; };
 
 template <typename T, int N>
-struct __align__(sizeof(T) * N) Pack {
-  T v[N];
+struct Word {
+  typename WordOf<sizeof(T) * N>::type w;
+  __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const decltype(w)*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<decltype(w)*>(p) = w; }
+  __device__ __forceinline__ uint32_t part(int i) const {
+    if constexpr (sizeof(w) == 16) return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    else if constexpr (sizeof(w) == 8) return i == 0 ? w.x : w.y;
+    else return w;
+  }
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(part(i));
+    else return __uint_as_float(i & 1 ? part(i >> 1) & 0xffff0000u : part(i >> 1) << 16);
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    uint32_t u[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(f[i]);
+      else u[i >> 1] |= (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f[i])) << (16 * (i & 1));
+    }
+    if constexpr (sizeof(w) == 16) w = make_uint4(u[0], u[1], u[2], u[3]);
+    else if constexpr (sizeof(w) == 8) w = make_uint2(u[0], u[1]);
+    else w = u[0];
+  }
 };
 
-// n consecutive values as floats; loads of up to 16 bytes
+// N consecutive values as floats, in words of up to 16 bytes
 template <typename T, int N>
 __device__ __forceinline__ void load_values(const T* p, float* f) {
   constexpr int kEach = sizeof(T) * N > 16 ? 16 / (int)sizeof(T) : N;
 #pragma unroll
   for (int i = 0; i < N; i += kEach) {
-    const Pack<T, kEach> a = *reinterpret_cast<const Pack<T, kEach>*>(p + i);
+    Word<T, kEach> a;
+    a.load(p + i);
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) f[i + e] = as_float<T>(a.v[e]);
+    for (int e = 0; e < kEach; ++e) f[i + e] = a.value(e);
   }
 }
 template <typename T, int N>
@@ -52,83 +82,101 @@ __device__ __forceinline__ void store_values(T* p, const float* f) {
   constexpr int kEach = sizeof(T) * N > 16 ? 16 / (int)sizeof(T) : N;
 #pragma unroll
   for (int i = 0; i < N; i += kEach) {
-    Pack<T, kEach> a;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) from_float(a.v[e], f[i + e]);
-    *reinterpret_cast<Pack<T, kEach>*>(p + i) = a;
+    Word<T, kEach> a;
+    a.set(f + i);
+    a.store(p + i);
   }
 }
 
-// ---- lookup: one thread for VEC values of a row
+// the same from another CTA's results: past L1, which knows nothing of them
+template <int N>
+__device__ __forceinline__ void load_shared_values(const float* p, float* f) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p + i));
+      f[i] = v.x, f[i + 1] = v.y, f[i + 2] = v.z, f[i + 3] = v.w;
+    }
+  } else if constexpr (N == 2) {
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+    f[0] = v.x, f[1] = v.y;
+  } else {
+    f[0] = __ldcg(p);
+  }
+}
+// ---- lookup: blocks of tx x ty threads, ty rows side by side, VEC values a thread; kRows rows of a thread on their way at once
 struct LookupArgs {
   const void* table;
   const int64_t* ids;
   void* out;
-  int64_t V, D, items;      // items = tokens * ceil(D / VEC)
-  int per_row;
+  int64_t V, D, T;
+  int per_row;              // D / VEC
   float scale;
 };
+constexpr int kRows = 4;
 
 template <typename TT, typename TO, int VEC>
 __global__ void __launch_bounds__(kEmbThreads) k_embed(const __grid_constant__ LookupArgs p) {
   pdl_wait();
   pdl_launch_dependents();
-  for (int64_t i = (int64_t)blockIdx.x * kEmbThreads + threadIdx.x; i < p.items; i += (int64_t)gridDim.x * kEmbThreads) {
-    const int64_t t = i / p.per_row;
-    const int64_t col = (i - t * p.per_row) * VEC;
-    const int64_t id = p.ids[t];
-    float f[VEC];
-    if (id >= 0 && id < p.V) {
-      load_values<TT, VEC>(static_cast<const TT*>(p.table) + id * p.D + col, f);
+  const int64_t t0 = (int64_t)blockIdx.x * blockDim.y * kRows + threadIdx.y;
+  int64_t id[kRows];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) f[e] *= p.scale;
-    } else {
+  for (int r = 0; r < kRows; ++r) {
+    const int64_t t = t0 + r * blockDim.y;
+    id[r] = t < p.T ? p.ids[t] : 0;
+  }
+  for (int c = threadIdx.x; c < p.per_row; c += blockDim.x) {
+    float f[kRows][VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) f[e] = NAN;
+    for (int r = 0; r < kRows; ++r) {
+      if (id[r] >= 0 && id[r] < p.V) {
+        load_values<TT, VEC>(static_cast<const TT*>(p.table) + id[r] * p.D + (int64_t)c * VEC, f[r]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[r][e] = NAN;
+      }
     }
-    store_values<TO, VEC>(static_cast<TO*>(p.out) + t * p.D + col, f);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int64_t t = t0 + r * blockDim.y;
+      if (t >= p.T) break;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[r][e] *= p.scale;
+      store_values<TO, VEC>(static_cast<TO*>(p.out) + t * p.D + (int64_t)c * VEC, f[r]);
+    }
   }
 }
 
-// ---- stable radix sort of (id, t): tiles of kTile tokens, digits of up to ten bits
-constexpr int kSortItems = 8;
-constexpr int kTile = kEmbThreads * kSortItems;
-constexpr int kSortWarps = kEmbThreads / 32;
-constexpr int kMaxBins = 1024;
+// ---- stable radix sort of (id, t), digits of eight bits
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kBins = 256, kDigit = 8;
+constexpr int kItems = 8;                   // a thread's tokens
+constexpr int kTile = kSortThreads * kItems;
+constexpr int kSortCluster = 8;             // CTAs that sort in one launch
+constexpr int kOneTokens = kSortCluster * kTile;
 
 struct SortArgs {
-  const int64_t* ids;       // first pass; else null
+  const int64_t* ids;       // null behind the first pass
   const uint32_t *key_in, *pos_in;
   uint32_t *key_out, *pos_out;
   uint32_t* hist;           // [tiles][bins]
-  int64_t V, padding;
-  int T, tiles, shift, bits;
+  int* count;               // the sums' counters, cleared here
+  float* dW;                // k_clear_rows
+  int64_t V, D, padding;
+  int T, tiles, shift, passes, counters;
+  int seg;                  // k_sort_one: tokens of a CTA (its logarithm)
+  int rows;                 // k_clear_rows: rows of a CTA
 };
 
 // The token's key: its id, or V (sorted behind all ids) where it contributes nothing.
-__device__ __forceinline__ uint32_t token_key(const SortArgs& p, int i) {
-  if (!p.ids) return p.key_in[i];
-  const int64_t id = p.ids[i];
+__device__ __forceinline__ uint32_t id_key(const SortArgs& p, int64_t id) {
   return id >= 0 && id < p.V && id != p.padding ? (uint32_t)id : (uint32_t)p.V;
 }
 
-__global__ void __launch_bounds__(kEmbThreads) k_sort_hist(const __grid_constant__ SortArgs p) {
-  __shared__ uint32_t h[kMaxBins];
-  const int bins = 1 << p.bits;
-  for (int b = threadIdx.x; b < bins; b += kEmbThreads) h[b] = 0;
-  pdl_wait();
-  pdl_launch_dependents();
-  __syncthreads();
-  for (int i = threadIdx.x; i < kTile; i += kEmbThreads) {
-    const int at = blockIdx.x * kTile + i;
-    if (at < p.T) atomicAdd(&h[(token_key(p, at) >> p.shift) & (bins - 1)], 1u);
-  }
-  __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kEmbThreads) p.hist[(int64_t)blockIdx.x * bins + b] = h[b];
-}
-
-// exclusive sum over the CTA's threads
-__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_sum, int warps) {
+// exclusive sum over the CTA's 1024 threads
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_sum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t x = v;
 #pragma unroll
@@ -138,59 +186,34 @@ __device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_s
   }
   if (lane == 31) warp_sum[warp] = x;
   __syncthreads();
-  uint32_t before = 0;
-  for (int w = 0; w < warp; ++w) before += warp_sum[w];
+  const uint32_t before = __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0u);
   __syncthreads();
   return before + x - v;
 }
 
-__global__ void __launch_bounds__(kEmbThreads) k_sort_scatter(const __grid_constant__ SortArgs p) {
-  __shared__ uint16_t wh[kSortWarps][kMaxBins];      // per warp: tokens of each digit so far, then those of earlier warps
-  __shared__ uint32_t start[kMaxBins];
-  __shared__ uint32_t warp_sum[kSortWarps];
-  const int bins = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  for (int b = tid; b < kSortWarps * kMaxBins; b += kEmbThreads) (&wh[0][0])[b] = 0;
-  pdl_wait();
-  pdl_launch_dependents();
-  // where each digit's tokens of this tile start
-  const int each = (bins + kEmbThreads - 1) / kEmbThreads;
-  uint32_t sum = 0, mine[kMaxBins / kEmbThreads], total[kMaxBins / kEmbThreads];
+// Ranks of a tile's tokens among those of the same digit, in order: a thread's item i is token warp 32 items + 32 i + lane, the
+// first `here` of its items are there.  Leaves in wh[w][b] how many tokens of digit b earlier warps have, and returns how
+// many the tile has of digit threadIdx.x.
+__device__ __forceinline__ uint32_t digit_ranks(const uint32_t (&key)[kItems], int here, int items, int shift, uint16_t (*wh)[kBins],
+                                                uint16_t (&rank)[kItems]) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint32_t* clear = reinterpret_cast<uint32_t*>(wh[warp]);
 #pragma unroll
-  for (int e = 0; e < kMaxBins / kEmbThreads; ++e) {
-    mine[e] = total[e] = 0;
-    const int b = tid * each + e;
-    if (e >= each || b >= bins) continue;
-    for (int t = 0; t < p.tiles; ++t) {
-      const uint32_t c = p.hist[(int64_t)t * bins + b];
-      if (t < (int)blockIdx.x) mine[e] += c;
-      total[e] += c;
-    }
-    sum += total[e];
-  }
-  uint32_t run = block_exclusive(sum, warp_sum, kSortWarps);
+  for (int b = 0; b < kBins / 2; b += 32) clear[b + lane] = 0;
+  __syncwarp();
 #pragma unroll
-  for (int e = 0; e < kMaxBins / kEmbThreads; ++e) {
-    const int b = tid * each + e;
-    if (e >= each || b >= bins) continue;
-    start[b] = run + mine[e];
-    run += total[e];
-  }
-  __syncthreads();
-  uint32_t key[kSortItems], pos[kSortItems];
-  uint16_t rank[kSortItems];
-  const int base = blockIdx.x * kTile + warp * 32 * kSortItems + lane;
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const int at = base + i * 32;
-    if (at < p.T) key[i] = token_key(p, at), pos[i] = p.ids ? at : p.pos_in[at];
-  }
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const bool on = base + i * 32 < p.T;
+  for (int i = 0; i < kItems; ++i) {
+    if (i >= items) break;
+    const bool on = i < here;
     const uint32_t active = __ballot_sync(~0u, on);
     if (on) {
-      const uint32_t d = (key[i] >> p.shift) & (bins - 1);
-      const uint32_t peers = __match_any_sync(active, d);
+      const uint32_t d = (key[i] >> shift) & (kBins - 1);
+      uint32_t peers = active;               // the lanes with this digit (a ballot a bit: the match instruction is slower)
+#pragma unroll
+      for (int bit = 1; bit < kBins; bit <<= 1) {
+        const uint32_t have = __ballot_sync(active, d & bit);
+        peers &= d & bit ? have : ~have;
+      }
       const uint16_t before = wh[warp][d];
       __syncwarp(active);
       if (lane == __ffs(peers) - 1) wh[warp][d] = before + __popc(peers);
@@ -199,48 +222,219 @@ __global__ void __launch_bounds__(kEmbThreads) k_sort_scatter(const __grid_const
     __syncwarp();
   }
   __syncthreads();
-  for (int b = tid; b < bins; b += kEmbThreads) {
-    uint16_t so_far = 0;
+  uint32_t total = 0;
+  if (tid < kBins) {
+#pragma unroll 8
     for (int w = 0; w < kSortWarps; ++w) {
-      const uint16_t c = wh[w][b];
-      wh[w][b] = so_far;
-      so_far += c;
+      const uint16_t c = wh[w][tid];
+      wh[w][tid] = (uint16_t)total;
+      total += c;
     }
   }
+  return total;
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_hist(const __grid_constant__ SortArgs p) {
+  __shared__ uint32_t h[kBins];
+  if (threadIdx.x < kBins) h[threadIdx.x] = 0;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (p.ids)
+    for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < p.counters; i += gridDim.x * kSortThreads) p.count[i] = 0;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i)
-    if (base + i * 32 < p.T) {
-      const uint32_t d = (key[i] >> p.shift) & (bins - 1);
+  for (int i = 0; i < kItems; ++i) {
+    const int at = blockIdx.x * kTile + i * kSortThreads + threadIdx.x;
+    if (at < p.T) atomicAdd(&h[((p.ids ? id_key(p, p.ids[at]) : p.key_in[at]) >> p.shift) & (kBins - 1)], 1u);
+  }
+  __syncthreads();
+  if (threadIdx.x < kBins) p.hist[(int64_t)blockIdx.x * kBins + threadIdx.x] = h[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const __grid_constant__ SortArgs p) {
+  __shared__ __align__(4) uint16_t wh[kSortWarps][kBins];
+  __shared__ uint32_t start[kBins], warp_sum[kSortWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  // where each digit's tokens of this tile start
+  uint32_t earlier = 0, total = 0;
+  if (tid < kBins) {
+#pragma unroll 8
+    for (int t = 0; t < p.tiles; ++t) {
+      const uint32_t c = p.hist[(int64_t)t * kBins + tid];
+      if (t < (int)blockIdx.x) earlier += c;
+      total += c;
+    }
+  }
+  const uint32_t before = block_exclusive(total, warp_sum);
+  if (tid < kBins) start[tid] = before + earlier;
+  uint32_t key[kItems], pos[kItems];
+  uint16_t rank[kItems];
+  const int base = blockIdx.x * kTile + warp * 32 * kItems + lane;
+  int here = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int at = base + i * 32;
+    if (at < p.T) {
+      key[i] = p.ids ? id_key(p, p.ids[at]) : p.key_in[at];
+      pos[i] = p.ids ? at : p.pos_in[at];
+      here = i + 1;
+    }
+  }
+  digit_ranks(key, here, kItems, p.shift, wh, rank);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i)
+    if (i < here) {
+      const uint32_t d = (key[i] >> p.shift) & (kBins - 1);
       const uint32_t to = start[d] + wh[warp][d] + rank[i];
       p.key_out[to] = key[i];
       p.pos_out[to] = pos[i];
     }
 }
 
+// Up to 65536 tokens: a cluster of eight CTAs sorts them in one launch, each a segment of 2^seg of them in its shared memory;
+// counts and tokens travel through distributed shared memory.  (32000 ids: 10000 tokens take one CTA 29 us and the cluster 10.)
+__global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant__ SortArgs p) {
+  extern __shared__ uint32_t sort_mem[];
+  const int tid = threadIdx.x;
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ __align__(4) uint16_t wh[kSortWarps][kBins];
+  __shared__ uint32_t start[kBins], count[kBins], warp_sum[kSortWarps];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int warp = tid >> 5, lane = tid & 31, rank0 = blockIdx.x, seg = 1 << p.seg;
+  const int items = (seg + kSortThreads - 1) / kSortThreads;         // of a thread
+  uint32_t* skey = sort_mem;
+  uint16_t* spos = reinterpret_cast<uint16_t*>(skey + seg);
+  for (int i = rank0 * kSortThreads + tid; i < p.counters; i += kSortCluster * kSortThreads) p.count[i] = 0;
+  uint32_t key[kItems];
+  uint16_t pos[kItems], rank[kItems];
+  const int base = warp * 32 * items + lane;                         // of the segment
+  const int mine = min(max(p.T - rank0 * seg, 0), seg);              // tokens of it
+  int here = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int at = base + i * 32;
+    if (i < items && at < mine) {
+      key[i] = id_key(p, p.ids[rank0 * seg + at]);
+      pos[i] = (uint16_t)(rank0 * seg + at);
+      here = i + 1;
+    }
+  }
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * kDigit;
+    const uint32_t own = digit_ranks(key, here, items, shift, wh, rank);
+    if (tid < kBins) count[tid] = own;
+    cluster.sync();                                                  // (every segment is in registers, every count is there)
+    uint32_t earlier = 0, total = 0;
+    if (tid < kBins) {
+      uint32_t c[kSortCluster];
+#pragma unroll
+      for (int q = 0; q < kSortCluster; ++q) c[q] = *cluster.map_shared_rank(&count[tid], q);
+#pragma unroll
+      for (int q = 0; q < kSortCluster; ++q) {
+        if (q < rank0) earlier += c[q];
+        total += c[q];
+      }
+    }
+    const uint32_t before = block_exclusive(total, warp_sum);
+    if (tid < kBins) start[tid] = before + earlier;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (i < here) {
+        const uint32_t d = (key[i] >> shift) & (kBins - 1);
+        const uint32_t to = start[d] + wh[warp][d] + rank[i];
+        *cluster.map_shared_rank(&skey[to & (seg - 1)], to >> p.seg) = key[i];
+        *cluster.map_shared_rank(&spos[to & (seg - 1)], to >> p.seg) = pos[i];
+      }
+    cluster.sync();
+    if (pass + 1 < p.passes) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        if (i < here) key[i] = skey[base + i * 32], pos[i] = spos[base + i * 32];
+    }
+  }
+  for (int i = tid; i < mine; i += kSortThreads) {
+    p.key_out[rank0 * seg + i] = skey[i];
+    p.pos_out[rank0 * seg + i] = spos[i];
+  }
+}
+
+// The rows of dW that no token has, as zeros: most of the work of a large table.  Needs nothing of the sort and the sums before
+// it on the stream and runs beside them (each CTA marks the ids of its own rows first); it ends when they have ended.
+constexpr int kClearThreads = 512;
+__global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_constant__ SortArgs p) {
+  extern __shared__ uint32_t seen[];                                 // a bit for each row
+  const int tid = threadIdx.x;
+  const int64_t v0 = (int64_t)blockIdx.x * p.rows, rows = min((int64_t)p.rows, p.V - v0);
+  for (int i = tid; i < (p.rows + 31) / 32; i += kClearThreads) seen[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid; i < p.T; i += kClearThreads) {
+    const int64_t r = (int64_t)id_key(p, p.ids[i]) - v0;
+    if (r >= 0 && r < rows) atomicOr(&seen[r >> 5], 1u << (r & 31));
+  }
+  __syncthreads();
+  // units of 16 bytes where rows are whole multiples of them, else of 4
+  const bool wide = p.D % 4 == 0 && (reinterpret_cast<uintptr_t>(p.dW) & 15) == 0;
+  const int units = (int)(wide ? p.D / 4 : p.D), down = kClearThreads / units, along = kClearThreads % units;
+  int64_t r = tid / units;
+  int c = tid % units;
+  float* row0 = p.dW + v0 * p.D;
+  while (r < rows) {
+    if (!((seen[r >> 5] >> (r & 31)) & 1u)) {
+      if (wide) reinterpret_cast<float4*>(row0 + r * p.D)[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      else row0[r * p.D + c] = 0.f;
+    }
+    r += down;
+    c += along;
+    if (c >= units) c -= units, ++r;
+  }
+  pdl_wait();
+}
+
 // ---- sums of runs
 constexpr int kMaxChunk = 64;
-constexpr int kZeroRows = 16;
+constexpr int kZeroRows = 64;
+// CTAs of an SM by the values a thread moves, as their registers allow
+constexpr int sum_ctas(int vec) { return vec == 4 ? 3 : 4; }
+constexpr int kInFlight = 16;              // registers of a thread for rows in hand
 
 struct SumArgs {
   const void* dout;
   const uint32_t *key, *pos;
   float* dW;
   float *head, *tail;       // [chunks][D]: the chunk's piece of a run that starts earlier / here and goes on
+  int* count;               // [chunks][slabs]: pieces of the run that starts in a chunk and goes on
   int64_t D;
   uint32_t V;
   int T, C, chunks, accumulate;
   float scale;
 };
 
+// The sum of a run to its row: the one thread that has it writes it, or lets L2 add it (one addition an element: no order
+// to depend on, and nobody waits for the old value).
 template <int VEC>
 __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t v, int64_t col, const float* acc) {
   float* o = p.dW + (int64_t)v * p.D + col;
   float f[VEC];
-  if (p.accumulate) load_values<float, VEC>(o, f);
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) f[e] = p.accumulate ? fmaf(p.scale, acc[e], f[e]) : p.scale * acc[e];
-  store_values<float, VEC>(o, f);
+  for (int e = 0; e < VEC; ++e) f[e] = p.scale * acc[e];
+  if (!p.accumulate) {
+    store_values<float, VEC>(o, f);
+  } else if constexpr (VEC >= 4) {
+#pragma unroll
+    for (int e = 0; e < VEC; e += 4)
+      asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(o + e), "f"(f[e]), "f"(f[e + 1]), "f"(f[e + 2]), "f"(f[e + 3])
+                   : "memory");
+  } else if constexpr (VEC == 2) {
+    asm volatile("red.global.add.v2.f32 [%0], {%1, %2};" ::"l"(o), "f"(f[0]), "f"(f[1]) : "memory");
+  } else {
+    asm volatile("red.global.add.f32 [%0], %1;" ::"l"(o), "f"(f[0]) : "memory");
+  }
 }
 
 // first place whose key is not below v
@@ -254,19 +448,21 @@ __device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t 
   return lo;
 }
 
-// CTAs [0, chunks): sums.  CTAs behind them (overwriting): rows of dW without tokens.
+// CTAs [0, chunks): sums, with one warp more that looks for the ends of the runs that cross chunks.  CTAs behind them (many
+// tokens, overwriting): rows of dW without tokens.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const __grid_constant__ SumArgs p) {
+__global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(const __grid_constant__ SumArgs p) {
+  pdl_launch_dependents();                                           // (what comes next waits for this kernel, or needs nothing of it)
   pdl_wait();
-  pdl_launch_dependents();
-  const int64_t col = ((int64_t)blockIdx.y * kEmbThreads + threadIdx.x) * VEC;
+  const int tid = threadIdx.x, lane = tid & 31, workers = blockDim.x - 32;
+  const int64_t col = tid < workers ? ((int64_t)blockIdx.y * workers + tid) * VEC : p.D;
   if ((int)blockIdx.x >= p.chunks) {
     __shared__ int empty[kZeroRows];
     const int64_t v0 = (int64_t)(blockIdx.x - p.chunks) * kZeroRows;
-    if (threadIdx.x < kZeroRows) {
-      const uint32_t v = (uint32_t)(v0 + threadIdx.x);
+    for (int r = tid; r < kZeroRows; r += blockDim.x) {
+      const uint32_t v = (uint32_t)(v0 + r);
       const int at = lower_bound(p.key, p.T, v);
-      empty[threadIdx.x] = v < p.V && (at == p.T || p.key[at] != v);
+      empty[r] = v < p.V && (at == p.T || p.key[at] != v);
     }
     __syncthreads();
     if (col >= p.D) return;
@@ -278,88 +474,134 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sum(const __grid_constant
     return;
   }
   __shared__ uint32_t sk[kMaxChunk + 2], sp[kMaxChunk];
+  __shared__ int from[2], to[2], done[2];                            // chunks of the run that comes in, and that goes out
   const int c = blockIdx.x, c0 = c * p.C, m = min(p.C, p.T - c0);
   // sk[0] is the key before the chunk, sk[m + 1] the one behind it; V where there is none
-  for (int i = threadIdx.x; i < m + 2; i += kEmbThreads) {
+  for (int i = tid; i < m + 2; i += blockDim.x) {
     const int at = c0 + i - 1;
     sk[i] = at < 0 || at >= p.T ? p.V : p.key[at];
     if (i >= 1 && i <= m) sp[i - 1] = p.pos[at];
   }
-  __syncthreads();
-  if (col >= p.D) return;
-  constexpr int U = 4;
-  float acc[VEC];
+  const int live = __syncthreads_count(tid < m && p.key[c0 + tid] != p.V);   // tokens behind them contribute nothing
+  if (live == 0) return;
+  const bool comes = sk[0] == sk[1], through = comes && sk[m + 1] == sk[m] && sk[1] == sk[m];
+  const bool goes = !through && sk[m] != p.V && sk[m + 1] == sk[m];
+  if (tid >= workers) {
+    int first = c;
+    if (comes) {                                                     // chunks before this one that begin with its key, and one more
+      for (;;) {
+        const int q = first - 1 - lane;
+        const uint32_t other = __ballot_sync(~0u, q < 0 || p.key[q * p.C] != sk[1]);
+        first -= other ? __ffs(other) - 1 : 32;
+        if (other) break;
+      }
+      if (first > 0 && p.key[first * p.C - 1] == sk[1]) --first;
+    }
+    int last = c;
+    if (through || goes) {
+      for (;;) {
+        const int q = last + 1 + lane;
+        const uint32_t other = __ballot_sync(~0u, q >= p.chunks || p.key[q * p.C] != sk[m]);
+        last += other ? __ffs(other) - 1 : 32;
+        if (other) break;
+      }
+    }
+    if (lane == 0) from[0] = first, to[0] = through ? last : c, from[1] = c, to[1] = last;
+  } else if (col < p.D) {
+    // U rows in hand and the next U on their way
+    constexpr int U = kInFlight / (VEC * (int)sizeof(T) > 4 ? VEC * (int)sizeof(T) / 4 : 1);
+    float acc[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-  bool from_before = sk[0] == sk[1];
-  const T* src = static_cast<const T*>(p.dout) + col;
-  for (int i0 = 0; i0 < m && sk[i0 + 1] != p.V; i0 += U) {
-    float f[U][VEC];
+    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+    bool first_run = true;
+    const T* src = static_cast<const T*>(p.dout) + col;
+    Word<T, VEC> f[2][U];
+    auto bring = [&](int i0, Word<T, VEC>* w) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u < m && sk[i0 + u + 1] != p.V) load_values<T, VEC>(src + (int64_t)sp[i0 + u] * p.D, f[u]);
+      for (int u = 0; u < U; ++u)
+        if (i0 + u < live) w[u].load(src + (int64_t)sp[i0 + u] * p.D);
+    };
+    bring(0, f[0]);
+#pragma unroll 1
+    for (int j0 = 0; j0 < live; j0 += 2 * U) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u;
-      if (i >= m || sk[i + 1] == p.V) break;
+      for (int h = 0; h < 2; ++h) {
+        const int i0 = j0 + h * U;
+        if (i0 >= live) break;
+        bring(i0 + U, f[h ^ 1]);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += f[u][e];
-      const bool ends = sk[i + 2] != sk[i + 1];
-      if (!ends && i + 1 < m) continue;
-      if (from_before) store_values<float, VEC>(p.head + (int64_t)c * p.D + col, acc);
-      else if (!ends) store_values<float, VEC>(p.tail + (int64_t)c * p.D + col, acc);
-      else put_row<VEC>(p, sk[i + 1], col, acc);
-      from_before = false;
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u;
+          if (i >= live) break;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+          for (int e = 0; e < VEC; ++e) acc[e] += f[h][u].value(e);
+          const bool ends = sk[i + 2] != sk[i + 1];
+          if (!ends && i + 1 < m) continue;
+          if (first_run && comes) store_values<float, VEC>(p.head + (int64_t)c * p.D + col, acc);
+          else if (!ends) store_values<float, VEC>(p.tail + (int64_t)c * p.D + col, acc);
+          else put_row<VEC>(p, sk[i + 1], col, acc);
+          first_run = false;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+        }
+      }
     }
   }
-}
-
-// The runs that cross chunks: chunk c's CTA joins the pieces of the run that starts in c and goes on behind it.
-template <int VEC>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_join(const __grid_constant__ SumArgs p) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const int c = blockIdx.x, c0 = c * p.C, c1 = c0 + p.C;
-  if (c1 >= p.T) return;
-  const uint32_t v = p.key[c1];
-  if (v == p.V || p.key[c1 - 1] != v) return;                        // nothing goes on
-  if (p.key[c0] == v && c0 > 0 && p.key[c0 - 1] == v) return;        // it started earlier
-  const int64_t col = ((int64_t)blockIdx.y * kEmbThreads + threadIdx.x) * VEC;
-  if (col >= p.D) return;
-  const int last = (lower_bound(p.key + c1, p.T - c1, v + 1) + c1 - 1) / p.C;   // the chunk that holds its last token
-  float acc[VEC], f[VEC];
-  load_values<float, VEC>(p.tail + (int64_t)c * p.D + col, acc);
-  for (int q = c + 1; q <= last; ++q) {
-    load_values<float, VEC>(p.head + (int64_t)q * p.D + col, f);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+  if (!comes && !goes) return;
+  // Runs that cross chunks: the CTA that leaves the last piece of a run joins them, in order.
+  __syncthreads();
+  if (tid < 2) {
+    __threadfence();                                                 // the CTA's pieces before the count, the others' behind it
+    done[tid] = (tid ? goes : comes) && atomicAdd(&p.count[(int64_t)from[tid] * gridDim.y + blockIdx.y], 1) == to[tid] - from[tid];
+    __threadfence();
   }
-  put_row<VEC>(p, v, col, acc);
+  __syncthreads();
+  if (col >= p.D) return;
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {
+    if (!done[side]) continue;
+    float acc[VEC];
+    load_shared_values<VEC>(p.tail + (int64_t)from[side] * p.D + col, acc);
+    constexpr int P = 32 / VEC;                                      // pieces on their way at once
+    const int end = to[side];
+    for (int q = from[side] + 1; q <= end; q += P) {
+      float f[P][VEC];
+#pragma unroll
+      for (int u = 0; u < P; ++u)
+        if (q + u <= end) load_shared_values<VEC>(p.head + (int64_t)(q + u) * p.D + col, f[u]);
+#pragma unroll
+      for (int u = 0; u < P; ++u)
+        if (q + u <= end) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] += f[u][e];
+        }
+    }
+    put_row<VEC>(p, side ? sk[m] : sk[1], col, acc);
+  }
 }
 
 // ---- host side
 struct Layout {
-  int T, C, chunks, tiles, passes, bits;
-  size_t key[2], pos[2], hist, head, tail, bytes;
+  int T, tiles, passes;
+  bool one;                 // a single launch sorts
+  size_t key[2], pos[2], hist, count, head, tail, bytes;
 };
+
+constexpr int kMinChunk = 8, kMostChunks = 148 * 4;
+// Tokens of a chunk: as many chunks as run at once, of 8 to 64 tokens
+int chunk_of(int64_t T, int slabs, int ctas) {
+  return (int)std::min<int64_t>(std::max<int64_t>((T * slabs + 148 * ctas - 1) / (148 * ctas), kMinChunk), kMaxChunk);
+}
 
 Layout layout_of(const asi_embedding_desc_t* d) {
   Layout l = {};
   l.T = (int)d->tokens;
-  // chunks of 8 to 64 tokens, four CTAs an SM where there are tokens enough
-  constexpr int kMost = 148 * 4;
-  l.C = 8;
-  while (l.C < kMaxChunk && l.T > l.C * kMost) l.C *= 2;
-  l.chunks = (l.T + l.C - 1) / l.C;
-  // the most chunks of any shorter batch: a workspace serves fewer tokens too
-  const size_t most = std::max(std::min((l.T + 7) / 8, kMost), (l.T + kMaxChunk - 1) / kMaxChunk);
+  // the most chunks of this and any shorter batch: a workspace serves fewer tokens too
+  const size_t most = std::max(std::min((l.T + kMinChunk - 1) / kMinChunk, kMostChunks), (l.T + kMaxChunk - 1) / kMaxChunk);
+  l.one = l.T <= kOneTokens;
   l.tiles = (l.T + kTile - 1) / kTile;
-  int bits = 1;
-  while ((d->vocab >> bits) != 0) ++bits;             // keys up to vocab itself
-  l.passes = bits <= 8 ? 1 : bits <= 20 ? 2 : (bits + 9) / 10;
-  l.bits = (bits + l.passes - 1) / l.passes;
+  l.passes = 1;
+  while ((d->vocab >> (l.passes * kDigit)) != 0) ++l.passes;          // keys up to vocab itself
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -370,7 +612,8 @@ Layout layout_of(const asi_embedding_desc_t* d) {
     l.key[i] = take((size_t)l.T * 4);
     l.pos[i] = take((size_t)l.T * 4);
   }
-  l.hist = take(((size_t)l.tiles << l.bits) * 4);
+  l.hist = take((size_t)l.tiles * kBins * 4);
+  l.count = take(most * ((d->dim + kEmbThreads - 1) / kEmbThreads) * 4);
   l.head = take(most * d->dim * 4);
   l.tail = take(most * d->dim * 4);
   l.bytes = std::max<size_t>(at, 256);
@@ -381,7 +624,7 @@ asi_status_t check_desc(const asi_embedding_desc_t* d) {
   if (!d || (d->in_dtype != ASI_F32 && d->in_dtype != ASI_BF16)) return ASI_ERR_INVALID_ARG;
   if (d->vocab < 1 || d->dim < 1 || d->tokens < 0 || !std::isfinite(d->scale)) return ASI_ERR_INVALID_ARG;
   if (d->padding_idx < -1 || d->padding_idx >= d->vocab) return ASI_ERR_INVALID_ARG;
-  if (d->vocab > 1 << 30 || d->dim > 1 << 22 || d->tokens > 1 << 24) return ASI_ERR_UNSUPPORTED;
+  if (d->vocab > 1 << 30 || d->dim > 1 << 22 || d->tokens > 1 << 24 || d->dim * d->tokens > (int64_t)1 << 38) return ASI_ERR_UNSUPPORTED;
   return ASI_OK;
 }
 
@@ -393,10 +636,12 @@ bool apart(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 template <typename TT, typename TO>
-cudaError_t launch_lookup(LookupArgs a, int64_t tokens, int vec, cudaStream_t st) {
+cudaError_t launch_lookup(LookupArgs a, int vec, cudaStream_t st) {
   a.per_row = (int)(a.D / vec);
-  a.items = tokens * a.per_row;
-  const dim3 grid((unsigned)std::min<int64_t>((a.items + kEmbThreads - 1) / kEmbThreads, 148 * 64)), block(kEmbThreads);
+  unsigned tx = 32;
+  while (tx < (unsigned)kEmbThreads && (int)tx < a.per_row) tx *= 2;
+  const unsigned ty = kEmbThreads / tx;
+  const dim3 grid((unsigned)((a.T + (int64_t)ty * kRows - 1) / ((int64_t)ty * kRows))), block(tx, ty);
   switch (vec) {
     case 8: return launch_pdl(k_embed<TT, TO, 8>, grid, block, 0, st, a);
     case 4: return launch_pdl(k_embed<TT, TO, 4>, grid, block, 0, st, a);
@@ -405,14 +650,53 @@ cudaError_t launch_lookup(LookupArgs a, int64_t tokens, int vec, cudaStream_t st
   }
 }
 
+// Sorted keys and positions into the layout's buffers *out; clears the sums' counters.
+cudaError_t sort_tokens(SortArgs a, const Layout& l, int counters, char* w, int* out, cudaStream_t st) {
+  a.hist = reinterpret_cast<uint32_t*>(w + l.hist);
+  a.count = reinterpret_cast<int*>(w + l.count);
+  a.counters = counters;
+  a.tiles = l.tiles;
+  a.passes = l.passes;
+  if (l.one) {
+    a.key_out = reinterpret_cast<uint32_t*>(w + l.key[0]);
+    a.pos_out = reinterpret_cast<uint32_t*>(w + l.pos[0]);
+    while (l.T > kSortCluster << a.seg) ++a.seg;
+    const size_t smem = (size_t)6 << a.seg;
+    cudaError_t e = smem > 24 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one), smem) : cudaSuccess;
+    *out = 0;
+    if (e == cudaSuccess) e = launch_pdl(k_sort_one, dim3(kSortCluster), dim3(kSortThreads), smem, st, a);
+    return e;
+  }
+  cudaError_t e = cudaSuccess;
+  for (int pass = 0; pass < l.passes && e == cudaSuccess; ++pass) {
+    const int to = pass & 1;
+    if (pass) a.ids = nullptr;
+    a.key_in = reinterpret_cast<const uint32_t*>(w + l.key[to ^ 1]);
+    a.pos_in = reinterpret_cast<const uint32_t*>(w + l.pos[to ^ 1]);
+    a.key_out = reinterpret_cast<uint32_t*>(w + l.key[to]);
+    a.pos_out = reinterpret_cast<uint32_t*>(w + l.pos[to]);
+    a.shift = pass * kDigit;
+    e = launch_pdl(k_sort_hist, dim3(l.tiles), dim3(kSortThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_pdl(k_sort_scatter, dim3(l.tiles), dim3(kSortThreads), 0, st, a);
+    *out = to;
+  }
+  return e;
+}
+
+cudaError_t clear_rows(SortArgs a, cudaStream_t st) {
+  constexpr int kClear = 148 * 4;
+  a.rows = (int)std::min<int64_t>((a.V + kClear - 1) / kClear, 65536);
+  return launch_pdl(k_clear_rows, dim3((unsigned)((a.V + a.rows - 1) / a.rows)), dim3(kClearThreads), (size_t)(a.rows + 31) / 32 * 4, st, a);
+}
+
+// CTAs that share a row of dW, and their threads
+unsigned slabs_of(int64_t D, int vec) { return (unsigned)((D / vec + kEmbThreads - 1) / kEmbThreads); }
+
 template <typename T, int VEC>
-cudaError_t launch_sums(const SumArgs& a, cudaStream_t st) {
-  const unsigned slabs = (unsigned)((a.D + (int64_t)kEmbThreads * VEC - 1) / ((int64_t)kEmbThreads * VEC));
-  const unsigned zero = a.accumulate ? 0 : (unsigned)((a.V + kZeroRows - 1) / kZeroRows);
-  if (a.chunks + zero == 0) return cudaSuccess;
-  cudaError_t e = launch_pdl(k_embed_sum<T, VEC>, dim3(a.chunks + zero, slabs), dim3(kEmbThreads), 0, st, a);
-  if (e != cudaSuccess || a.chunks < 2) return e;
-  return launch_pdl(k_embed_join<VEC>, dim3(a.chunks, slabs), dim3(kEmbThreads), 0, st, a);
+cudaError_t launch_sums(const SumArgs& a, bool clear, cudaStream_t st) {
+  const unsigned slabs = slabs_of(a.D, VEC), zero = clear ? (unsigned)((a.V + kZeroRows - 1) / kZeroRows) : 0;
+  const unsigned threads = (unsigned)(((a.D / VEC + slabs - 1) / slabs + 31) / 32 * 32);
+  return a.chunks + zero ? launch_pdl(k_embed_sum<T, VEC>, dim3(a.chunks + zero, slabs), dim3(threads + 32), 0, st, a) : cudaSuccess;
 }
 
 }  // namespace
@@ -437,17 +721,16 @@ asi_status_t asi_embedding_forward(const asi_embedding_desc_t* desc, const void*
   a.out = out;
   a.V = desc->vocab;
   a.D = desc->dim;
+  a.T = desc->tokens;
   a.scale = desc->scale;
   int vec = 8;            // values a thread moves: the most that the row length and both addresses allow (16 bytes at a time)
   while (vec > 1 && (desc->dim % vec || !aligned(table, std::min<size_t>(16, vec * et)) || !aligned(out, std::min<size_t>(16, vec * eo)))) vec /= 2;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (desc->table_dtype == ASI_BF16)
-    e = desc->in_dtype == ASI_BF16 ? launch_lookup<__nv_bfloat16, __nv_bfloat16>(a, desc->tokens, vec, st)
-                                   : launch_lookup<__nv_bfloat16, float>(a, desc->tokens, vec, st);
+    e = desc->in_dtype == ASI_BF16 ? launch_lookup<__nv_bfloat16, __nv_bfloat16>(a, vec, st) : launch_lookup<__nv_bfloat16, float>(a, vec, st);
   else
-    e = desc->in_dtype == ASI_BF16 ? launch_lookup<float, __nv_bfloat16>(a, desc->tokens, vec, st)
-                                   : launch_lookup<float, float>(a, desc->tokens, vec, st);
+    e = desc->in_dtype == ASI_BF16 ? launch_lookup<float, __nv_bfloat16>(a, vec, st) : launch_lookup<float, float>(a, vec, st);
   return cuda_status(e, "embedding");
 }
 
@@ -467,47 +750,48 @@ asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t
     return ASI_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* w = static_cast<char*>(ws);
-  int cur = 0;
-  for (int pass = 0; pass < l.passes && l.T > 0; ++pass, cur ^= 1) {
-    SortArgs a = {};
-    a.ids = pass ? nullptr : ids;
-    a.key_in = reinterpret_cast<const uint32_t*>(w + l.key[cur ^ 1]);
-    a.pos_in = reinterpret_cast<const uint32_t*>(w + l.pos[cur ^ 1]);
-    a.key_out = reinterpret_cast<uint32_t*>(w + l.key[cur]);
-    a.pos_out = reinterpret_cast<uint32_t*>(w + l.pos[cur]);
-    a.hist = reinterpret_cast<uint32_t*>(w + l.hist);
-    a.V = desc->vocab;
-    a.padding = desc->padding_idx;
-    a.T = l.T;
-    a.tiles = l.tiles;
-    a.shift = pass * l.bits;
-    a.bits = l.bits;
-    cudaError_t e = launch_pdl(k_sort_hist, dim3(l.tiles), dim3(kEmbThreads), 0, st, a);
-    if (e == cudaSuccess) e = launch_pdl(k_sort_scatter, dim3(l.tiles), dim3(kEmbThreads), 0, st, a);
+  // columns of a thread: the most that the row length and the addresses allow, 16 bytes of dW at a time
+  int vec = 4;
+  while (vec > 1 && (desc->dim % vec || !aligned(dOut, vec * eo) || !aligned(dW, vec * 4))) vec /= 2;
+  try {
+    // (beside the clearing kernel the sums have two CTAs an SM, so that both fit)
+    const bool clear = !accumulate, beside = clear && l.one;
+    const int slabs = (int)slabs_of(desc->dim, vec), C = chunk_of(l.T, slabs, beside ? 2 : sum_ctas(vec)), chunks = (l.T + C - 1) / C;
+    SortArgs sort = {};
+    sort.ids = ids;
+    sort.dW = dW;
+    sort.V = desc->vocab;
+    sort.D = desc->dim;
+    sort.padding = desc->padding_idx;
+    sort.T = l.T;
+    int at = 0;
+    cudaError_t e = cudaSuccess;
+    if (l.T || clear) e = sort_tokens(sort, l, chunks * slabs, w, &at, st);
     if (e != cudaSuccess) return cuda_status(e, "sort of tokens");
+    SumArgs a = {};
+    a.dout = dOut;
+    a.key = reinterpret_cast<const uint32_t*>(w + l.key[at]);
+    a.pos = reinterpret_cast<const uint32_t*>(w + l.pos[at]);
+    a.dW = dW;
+    a.head = reinterpret_cast<float*>(w + l.head);
+    a.tail = reinterpret_cast<float*>(w + l.tail);
+    a.count = reinterpret_cast<int*>(w + l.count);
+    a.D = desc->dim;
+    a.V = (uint32_t)desc->vocab;
+    a.T = l.T;
+    a.C = C;
+    a.chunks = chunks;
+    a.accumulate = accumulate != 0;
+    a.scale = desc->scale;
+    if (desc->in_dtype == ASI_BF16)
+      e = vec == 4 ? launch_sums<__nv_bfloat16, 4>(a, clear && !beside, st) : vec == 2 ? launch_sums<__nv_bfloat16, 2>(a, clear && !beside, st) : launch_sums<__nv_bfloat16, 1>(a, clear && !beside, st);
+    else
+      e = vec == 4 ? launch_sums<float, 4>(a, clear && !beside, st) : vec == 2 ? launch_sums<float, 2>(a, clear && !beside, st) : launch_sums<float, 1>(a, clear && !beside, st);
+    if (e == cudaSuccess && beside) e = clear_rows(sort, st);
+    return cuda_status(e, "embedding weight gradient");
+  } catch (...) {
+    return no_host_memory();
   }
-  cur ^= 1;               // what the last pass wrote
-  SumArgs a = {};
-  a.dout = dOut;
-  a.key = reinterpret_cast<const uint32_t*>(w + l.key[cur]);
-  a.pos = reinterpret_cast<const uint32_t*>(w + l.pos[cur]);
-  a.dW = dW;
-  a.head = reinterpret_cast<float*>(w + l.head);
-  a.tail = reinterpret_cast<float*>(w + l.tail);
-  a.D = desc->dim;
-  a.V = (uint32_t)desc->vocab;
-  a.T = l.T;
-  a.C = l.C;
-  a.chunks = l.chunks;
-  a.accumulate = accumulate != 0;
-  a.scale = desc->scale;
-  const bool wide = aligned(dW, 16) && desc->dim % 4 == 0;
-  cudaError_t e;
-  if (desc->in_dtype == ASI_BF16)
-    e = wide && desc->dim % 8 == 0 && aligned(dOut, 16) ? launch_sums<__nv_bfloat16, 8>(a, st) : launch_sums<__nv_bfloat16, 1>(a, st);
-  else
-    e = wide && aligned(dOut, 16) ? launch_sums<float, 4>(a, st) : launch_sums<float, 1>(a, st);
-  return cuda_status(e, "embedding weight gradient");
 }
 
 }  // extern "C"
