@@ -2,8 +2,6 @@
 does all the arithmetic."""
 from __future__ import annotations
 
-import contextlib
-
 import numpy as np
 import torch
 
@@ -124,16 +122,19 @@ class StepRunner:
 _DTYPES = {torch.float32: ASI_F32, torch.bfloat16: ASI_BF16}
 
 
-def _on(device):
-    """Makes `device` current for a launch; nothing to do where it is."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+# handle of a device's current stream, without a stream object for each call where torch offers that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _stream_of(device, stream):
-    """The handle of `stream`, or of the current stream of `device` (which _on() has made current)."""
+def _call(device, stream, function, *args):
+    """function(*args, handle) with `device` current, on `stream` or that device's current stream."""
     if stream is not None and stream.device != device:
         raise ValueError(f"a stream of {device} is needed, got one of {stream.device}")
-    return _stream_handle(stream)
+    if torch.cuda.current_device() == device.index:
+        function(*args, _raw_stream(device.index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            function(*args, _raw_stream(device.index) if stream is None else stream.cuda_stream)
 
 
 def _cuda_device(device):
@@ -147,7 +148,7 @@ def _cuda_device(device):
 
 def _take(name, x, shape, dtype, device):
     """The address of a contiguous tensor of that shape and type on that device."""
-    if x.dtype != dtype or tuple(x.shape) != tuple(shape) or x.device != device or not x.is_contiguous():
+    if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is needed, got {x.dtype} "
                          f"{tuple(x.shape)} on {x.device}")
     return x.data_ptr()
@@ -167,21 +168,26 @@ class LogprobRunner:
         self.logp, self.entropy, self.lse = (torch.zeros(self.rows, **f32) for _ in range(3))
         self.top_logp = torch.zeros(self.rows, self.top_k, **f32) if self.top_k else None
         self.top_ids = torch.zeros(self.rows, self.top_k, dtype=torch.int64, device=self.device) if self.top_k else None
+        self._stats = tuple(x.data_ptr() for x in (self.logp, self.entropy, self.lse))
+        self._top = (self.top_logp.data_ptr(), self.top_ids.data_ptr()) if self.top_k else (0, 0)
 
     def _rows_of(self, name, x):
-        if (x.dtype != self.in_dtype or x.dim() != 2 or x.shape[0] > self.rows or x.shape[1] != self.vocab
-                or x.device != self.device or (self.vocab > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < self.vocab)):
-            raise ValueError(f"{name}: {self.in_dtype} rows [<= {self.rows}, {self.vocab}] on {self.device} are needed, each "
-                             f"contiguous, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
-        return max(x.stride(0), self.vocab)
+        """Rows and row stride of logits or their gradient."""
+        if x.dim() == 2 and x.dtype == self.in_dtype and x.device == self.device:
+            (n, v), (ld, one) = x.shape, x.stride()
+            if n <= self.rows and v == self.vocab and (one == 1 or v == 1) and (ld >= v or n <= 1):
+                return n, max(ld, v)
+        raise ValueError(f"{name}: {self.in_dtype} rows [<= {self.rows}, {self.vocab}] on {self.device} are needed, each "
+                         f"contiguous, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
 
     def _inputs(self, logits, targets, dlogits=None):
-        self.desc.ld = self.desc.ld_grad = self._rows_of("logits", logits)
-        self.desc.rows = n = logits.shape[0]
+        d = self.desc
+        n, ld = self._rows_of("logits", logits)
+        d.rows, d.ld, d.ld_grad = n, ld, ld
         if dlogits is not None:
-            self.desc.ld_grad = self._rows_of("dlogits", dlogits)
-            if dlogits.shape[0] != n:
-                raise ValueError(f"dlogits: {n} rows are needed, got {dlogits.shape[0]}")
+            m, d.ld_grad = self._rows_of("dlogits", dlogits)
+            if m != n:
+                raise ValueError(f"dlogits: {n} rows are needed, got {m}")
         return n, _take("targets", targets, (n,), torch.int64, self.device)
 
     def _weights(self, n, dlogp, dentropy):
@@ -190,27 +196,21 @@ class LogprobRunner:
 
     def forward(self, logits, targets, stream=None):
         _, y = self._inputs(logits, targets)
-        with _on(self.device):
-            binding.token_logprobs(self.desc, logits.data_ptr(), y, self.logp.data_ptr(), self.entropy.data_ptr(),
-                                   self.lse.data_ptr(), self.top_logp.data_ptr() if self.top_k else 0,
-                                   self.top_ids.data_ptr() if self.top_k else 0, _stream_of(self.device, stream))
+        _call(self.device, stream, binding.token_logprobs, self.desc, logits.data_ptr(), y, *self._stats, *self._top)
 
     def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward()
         left; dentropy may be None, and dlogits may be logits itself."""
         n, y = self._inputs(logits, targets, dlogits)
-        a, b = self._weights(n, dlogp, dentropy)
-        with _on(self.device):
-            binding.token_logprobs_grad(self.desc, logits.data_ptr(), y, self.lse.data_ptr(), self.entropy.data_ptr(), a, b,
-                                        dlogits.data_ptr(), _stream_of(self.device, stream))
+        _, entropy, lse = self._stats
+        _call(self.device, stream, binding.token_logprobs_grad, self.desc, logits.data_ptr(), y, lse, entropy,
+              *self._weights(n, dlogp, dentropy), dlogits.data_ptr())
 
     def loss(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """forward() without the top entries, and backward(), in one pass over the logits."""
         n, y = self._inputs(logits, targets, dlogits)
-        a, b = self._weights(n, dlogp, dentropy)
-        with _on(self.device):
-            binding.token_loss(self.desc, logits.data_ptr(), y, a, b, self.logp.data_ptr(), self.entropy.data_ptr(),
-                               self.lse.data_ptr(), dlogits.data_ptr(), _stream_of(self.device, stream))
+        _call(self.device, stream, binding.token_loss, self.desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
+              *self._stats, dlogits.data_ptr())
 
 
 class EmbeddingRunner:
@@ -226,18 +226,18 @@ class EmbeddingRunner:
         self.ws = None                     # allocated with the first wgrad()
 
     def _ids(self, ids):
-        if ids.dtype != torch.int64 or ids.device != self.device or not ids.is_contiguous() or ids.numel() > self.tokens:
+        n = ids.numel()
+        if ids.dtype != torch.int64 or ids.device != self.device or not ids.is_contiguous() or n > self.tokens:
             raise ValueError(f"ids: a contiguous int64 tensor of up to {self.tokens} tokens on {self.device} is needed, got "
                              f"{ids.dtype} {tuple(ids.shape)} on {ids.device}")
-        self.desc.tokens = ids.numel()
-        return tuple(ids.shape) + (self.dim,)
+        self.desc.tokens = n
+        return (*ids.shape, self.dim)
 
     def forward(self, table, ids, out, stream=None):
         shape = self._ids(ids)
         w = _take("table", table, (self.vocab, self.dim), self.table_dtype, self.device)
         o = _take("out", out, shape, self.in_dtype, self.device)
-        with _on(self.device):
-            binding.embedding_forward(self.desc, w, ids.data_ptr(), o, _stream_of(self.device, stream))
+        _call(self.device, stream, binding.embedding_forward, self.desc, w, ids.data_ptr(), o)
 
     def wgrad(self, ids, dOut, dW, accumulate=False, stream=None):
         """dW (fp32 [vocab, dim]) overwritten with, or increased by, the gradient."""
@@ -248,9 +248,8 @@ class EmbeddingRunner:
             n, self.desc.tokens = self.desc.tokens, self.tokens
             self.ws = torch.empty(binding.embedding_wgrad_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
             self.desc.tokens = n
-        with _on(self.device):
-            binding.embedding_wgrad(self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(), self.ws.numel(),
-                                    _stream_of(self.device, stream))
+        _call(self.device, stream, binding.embedding_wgrad, self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(),
+              self.ws.numel())
 
 
 class AdamWRunner:
@@ -321,7 +320,6 @@ class AdamWRunner:
             d.step = self.t + 1 if step is None else int(step)
         if grad_scale is not None:
             d.grad_scale = _take("grad_scale", grad_scale.reshape(1), (1,), torch.float32, self.device)
-        with _on(self.device):
-            binding.adamw_step(d, self._tensors, len(self.weights), _stream_of(self.device, stream))
+        _call(self.device, stream, binding.adamw_step, d, self._tensors, len(self.weights))
         if not isinstance(step, torch.Tensor):
             self.t = d.step
