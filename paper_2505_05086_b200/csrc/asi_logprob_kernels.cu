@@ -121,6 +121,7 @@ __device__ __forceinline__ unsigned long long remote_u64(const unsigned long lon
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ int remote_int(const int* p, int rank) { return __float_as_int(remote_f(reinterpret_cast<const float*>(p), rank)); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
@@ -131,6 +132,7 @@ template <>
 struct Granule<__nv_bfloat16> {
   static constexpr int n = 8;
   static constexpr uint32_t kNone = 0xff80ff80u;                    // -inf
+  static constexpr uint32_t kUnit = 1u << 16;                       // the last place, of the same value in fp32
   static __device__ __forceinline__ void floats(const uint4& v, float* f) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -171,6 +173,7 @@ template <>
 struct Granule<float> {
   static constexpr int n = 4;
   static constexpr uint32_t kNone = 0xff800000u;
+  static constexpr uint32_t kUnit = 1u;
   static __device__ __forceinline__ void floats(const uint4& v, float* f) {
     f[0] = __uint_as_float(v.x);
     f[1] = __uint_as_float(v.y);
@@ -329,13 +332,62 @@ constexpr int kHits = 512;
 
 struct TopShared {
   unsigned long long cand[kCand];
-  unsigned long long list[ASI_TOP_MAX];    // this CTA's leading entries, largest first; 0: none
+  unsigned long long pool[kCand];          // and of a cluster's
+  unsigned long long list[ASI_TOP_MAX];    // the leading entries, largest first
+  unsigned long long best[kFwd / 32];
   float slot[kSlots][kFwd];
   uint16_t hit[kHits];                     // slot * kFwd + thread: granules that may hold candidates
   float most[kFwd];                        // each thread's maximum
   float tau;
-  int count, hits;
+  uint32_t least;
+  int count, hits, pooled;
 };
+
+// About the k-th largest of a warp's keys: what at least k and hardly more than k + 4 of them reach.  Found bit by bit below the
+// bits that all of them share.  `unit`: the last place that differs; keys of 0 are none.
+template <int N>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&key)[N], int k, uint32_t unit) {
+  uint32_t high = 0, low = ~0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    high = max(high, key[i]);
+    low = min(low, key[i]);
+  }
+  high = __reduce_max_sync(~0u, high);
+  low = __reduce_min_sync(~0u, low);
+  uint32_t bit = high == low ? 0u : 1u << (31 - __clz(high ^ low)), t = bit ? high & ~(2 * bit - 1) : low;
+  for (; bit >= unit; bit >>= 1) {
+    uint32_t reach = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reach += key[i] >= (t | bit);
+    reach = __reduce_add_sync(~0u, reach);
+    if ((int)reach >= k) t |= bit;
+    if ((int)reach >= k && (int)reach <= k + 4) break;
+  }
+  return max(t, low);
+}
+
+// The largest key below prev among those that `each` offers, over the CTA
+template <typename F>
+__device__ __forceinline__ unsigned long long block_best(unsigned long long prev, unsigned long long* warps, F each) {
+  unsigned long long best = 0;
+  each([&](unsigned long long key) {
+    if (key < prev && key > best) best = key;
+  });
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const unsigned long long other = __shfl_xor_sync(~0u, best, o);
+    if (other > best) best = other;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = best;
+  __syncthreads();
+  best = warps[0];
+#pragma unroll
+  for (int i = 1; i < kFwd / 32; ++i)
+    if (warps[i] > best) best = warps[i];
+  return best;
+}
 
 // S and W of some granules relative to M
 template <typename T>
@@ -462,28 +514,13 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
   M = block_max<kWarps>(M, sh.red[0]);
   rebase(S, W, own, M, c2);
   if (TOP) {
-    // tau, about the k-th largest of the threads' maxima: at least k entries reach it, and few more.  Found bit by bit
-    // below the bits that all of them share: the largest prefix that k of them reach.
+    // tau, about the k-th largest of the threads' maxima: at least k entries reach it, and few more
     if (warp == 0) {
-      uint32_t key[kFwd / 32], high = 0, low = ~0u;
+      uint32_t key[kFwd / 32];
 #pragma unroll
-      for (int i = 0; i < kFwd / 32; ++i) {
-        key[i] = order_bits(top.most[i * 32 + lane]);
-        high = max(high, key[i]);
-        low = min(low, key[i]);
-      }
-      high = __reduce_max_sync(~0u, high);
-      low = __reduce_min_sync(~0u, low);
-      uint32_t bit = high == low ? 0u : 1u << (31 - __clz(high ^ low)), t = bit ? high & ~(2 * bit - 1) : low;
-      for (; bit; bit >>= 1) {
-        uint32_t reach = 0;
-#pragma unroll
-        for (int i = 0; i < kFwd / 32; ++i) reach += key[i] >= (t | bit);
-        reach = __reduce_add_sync(~0u, reach);
-        if ((int)reach >= p.k) t |= bit;
-        if ((int)reach == p.k) break;
-      }
-      if (lane == 0) top.tau = order_value(max(t, low));
+      for (int i = 0; i < kFwd / 32; ++i) key[i] = order_bits(top.most[i * 32 + lane]);
+      const uint32_t t = reached_by(key, p.k, Granule<T>::kUnit);
+      if (lane == 0) top.tau = order_value(t);
     }
   }
   block_sums<kWarps>(S, W, sh.red);
@@ -524,73 +561,103 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
           if (place < kCand) top.cand[place] = order_key(f[u], j[u]);
         }
     }
-    if (tid < ASI_TOP_MAX) top.list[tid] = 0;
     __syncthreads();
-    const int found = top.count;
-    if (found <= kCand) {
-      for (int i = tid; i < found; i += kFwd) {
-        const unsigned long long key = top.cand[i];
-        int above = 0;
-        for (int q = 0; q < found; ++q) above += top.cand[q] > key;
-        if (above < p.k) top.list[above] = key;
-      }
-    } else {                                // many equal values: one sweep for each entry
+    if (top.count > kCand) {                // many equal values: one sweep for each entry
       unsigned long long prev = ~0ull;
       for (int r = 0; r < p.k; ++r) {
-        unsigned long long best = 0;
-        for (int i = tid; i < cnt; i += kFwd) {
-          float f[n];
-          Granule<T>::floats(row.load(g0 + i), f);
-          const int j = row.first(g0 + i);
+        prev = block_best(prev, top.best, [&](auto offer) {
+          for (int i = tid; i < cnt; i += kFwd) {
+            float f[n];
+            Granule<T>::floats(row.load(g0 + i), f);
+            const int j = row.first(g0 + i);
 #pragma unroll
-          for (int e = 0; e < n; ++e)
-            if (j + e >= 0 && j + e < p.V) {
-              const unsigned long long key = order_key(f[e], j + e);
-              if (key < prev && key > best) best = key;
-            }
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-          const unsigned long long other = __shfl_xor_sync(~0u, best, o);
-          if (other > best) best = other;
-        }
-        __syncthreads();                    // cand[] is free: the warps' best
-        if (lane == 0) top.cand[warp] = best;
-        __syncthreads();
-        best = top.cand[0];
-#pragma unroll
-        for (int i = 1; i < kWarps; ++i)
-          if (top.cand[i] > best) best = top.cand[i];
-        if (tid == 0) top.list[r] = best;
-        prev = best;
+            for (int e = 0; e < n; ++e)
+              if (j + e >= 0 && j + e < p.V) offer(order_key(f[e], j + e));
+          }
+        });
+        if (tid == 0) top.cand[r] = prev;
       }
+      if (tid == 0) top.count = p.k;
     }
+    if (tid == 0) top.pooled = 0;
     __syncthreads();
   }
 
   if (cl > 1) {
     if (tid == 0) sh.mine[0] = M, sh.mine[1] = S, sh.mine[2] = W;
-    cluster_arrive();                       // (every thread's writes above, the lists among them)
+    cluster_arrive();                       // (every thread's writes above, the candidates among them)
     cluster_wait();
     if (rank == 0) {
       if (tid < 3 * cl) sh.parts[tid % 3][tid / 3] = remote_f(&sh.mine[tid % 3], tid / 3);
-      if (TOP)
-        for (int i = tid; i < cl * p.k; i += kFwd) top.cand[i] = remote_u64(&top.list[i % p.k], i / p.k);
+      if (TOP) {
+        // every CTA's tau is reached by k entries: the cluster's k largest reach the largest tau
+        const float of_lane = remote_f(&top.tau, lane % cl);
+        const int found = remote_int(&top.count, lane % cl);
+        float tau = of_lane;
+#pragma unroll
+        for (int o = 1; o < kMaxCluster; o <<= 1) tau = fmaxf(tau, __shfl_xor_sync(~0u, tau, o));
+        for (int q = warp; q < cl; q += kWarps) {
+          const int of_q = __shfl_sync(~0u, found, q);
+          for (int i = lane; i < of_q; i += 32) {
+            const unsigned long long key = remote_u64(&top.cand[i], q);
+            if (key_value(key) >= tau) {
+              const int place = atomicAdd(&top.pooled, 1);
+              if (place < kCand) top.pool[place] = key;
+            }
+          }
+        }
+        __syncthreads();
+        constexpr int kFew = kCand;
+        if (top.pooled <= kFew) {           // up to eight times as many as wanted: tau once more, over them
+          const int pooled = top.pooled;
+          if (warp == 0) {
+            uint32_t key[kFew / 32];
+#pragma unroll
+            for (int i = 0; i < kFew / 32; ++i) key[i] = i * 32 + lane < pooled ? (uint32_t)(top.pool[i * 32 + lane] >> 32) : 0u;
+            const uint32_t t = reached_by(key, p.k, Granule<T>::kUnit);
+            if (lane == 0) top.least = t;
+          }
+          __syncthreads();
+          unsigned long long keep[kFew / kFwd];
+#pragma unroll
+          for (int i = 0; i < kFew / kFwd; ++i) keep[i] = i * kFwd + tid < pooled ? top.pool[i * kFwd + tid] : 0;
+          if (tid == 0) top.pooled = 0;
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < kFew / kFwd; ++i)
+            if (keep[i] && (uint32_t)(keep[i] >> 32) >= top.least) top.pool[atomicAdd(&top.pooled, 1)] = keep[i];
+        } else if (top.pooled > kCand) {    // many equal values again
+          unsigned long long prev = ~0ull;
+          for (int r = 0; r < p.k; ++r) {
+            prev = block_best(prev, top.best, [&](auto offer) {
+              for (int q = 0; q < cl; ++q) {
+                const int of_q = __shfl_sync(~0u, found, q);
+                for (int i = tid; i < of_q; i += kFwd) offer(remote_u64(&top.cand[i], q));
+              }
+            });
+            if (tid == 0) top.pool[r] = prev;
+          }
+          if (tid == 0) top.pooled = p.k;
+        }
+      }
       __syncthreads();
     }
     cluster_arrive();                       // the others' shared memory is read no more
     cluster_wait();
     if (rank) return;
     cluster_sums<kWarps>(M, S, W, c2, cl, sh);
-    if (TOP) {
-      for (int i = tid; i < cl * p.k; i += kFwd) {
-        const unsigned long long key = top.cand[i];
-        int above = 0;
-        for (int q = 0; q < cl * p.k; ++q) above += top.cand[q] > key;
-        if (key && above < p.k) top.list[above] = key;
-      }
-      __syncthreads();
+  }
+  if (TOP) {
+    const unsigned long long* from = cl > 1 ? top.pool : top.cand;
+    const int found = min(cl > 1 ? top.pooled : top.count, kCand);
+    for (int i = tid; i < found; i += kFwd) {
+      const unsigned long long key = from[i];
+      int above = 0;
+#pragma unroll 4
+      for (int q = 0; q < found; ++q) above += from[q] > key;
+      if (above < p.k) top.list[above] = key;
     }
+    __syncthreads();
   }
   if (tid == 0) write_row(p, t, M, S, W, xy, given, skip);
   if (TOP && tid < p.k) {
