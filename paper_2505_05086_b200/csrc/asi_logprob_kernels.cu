@@ -762,7 +762,55 @@ __global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant
   if (cl > 1) cluster_wait();
 }
 
-// The gradient alone, from lse and entropy: a stream of 1024 granules a CTA.
+// ---- the gradient alone, from lse and entropy: a stream of 1024 granules a CTA.  p = exp(x - lse) is off by 2^-24 |lse|, which
+// is 2^-12 where |lse| is 4096: rows from there on (logits at a type's lowest value, say) sum up for themselves, in one CTA
+// (dx may be x, so nobody else of the row may have begun to write).
+constexpr float kFarLse = 4096.f;
+
+template <typename T>
+__device__ __forceinline__ void far_row(const LogprobGradArgs& p, const RowView<T>& row, T* dx, int64_t t) {
+  constexpr int n = Granule<T>::n, kWarps = kThreads / 32;
+  __shared__ RowShared<kWarps> sh;
+  const int G = row.granules(), tid = threadIdx.x;
+  const int64_t y = p.y[t];
+  const bool given = y >= 0 && y < p.V;
+  const float c2 = p.scale * kLog2e, alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f;
+  float M = -INFINITY, S = 0.f, W = 0.f;
+#pragma unroll 1
+  for (int g = tid; g < G; g += kThreads) M = nan_max(M, Granule<T>::largest(row.load(g)));
+  M = block_max<kWarps>(M, sh.red[0]);
+  const bool zero = y == p.ignore || M == -INFINITY;
+  if (!zero) {
+#pragma unroll 1
+    for (int g = tid; g < G; g += kThreads) {
+      float f[n];
+      Granule<T>::floats(row.load(g), f);
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const float a = (f[e] - M) * c2, ex = exp2_approx(a);
+        S += ex;
+        W = fmaf(ex, fmaxf(a, -1e4f), W);
+      }
+    }
+  }
+  block_sums<kWarps>(S, W, sh.red);
+  const float inv = 1.f / S, lnS = logf(S), H = lnS - kLn2 * W * inv;
+  const float A = given ? -p.scale * (alpha + beta * (H - lnS)) * inv : NAN, B = -p.scale * beta * kLn2 * inv;
+#pragma unroll 1
+  for (int g = tid; g < G; g += kThreads) {
+    float f[n];
+    Granule<T>::floats(row.load(g), f);
+    const int j = row.first(g);
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      const float a = (f[e] - M) * c2, d = exp2_approx(a) * fmaf(B, fmaxf(a, -1e4f), A);
+      f[e] = zero ? 0.f : j + e == y ? fmaf(p.scale, alpha, d) : d;
+    }
+    store_granule(dx, row, g, f, false);
+  }
+  __syncthreads();                           // sh is free
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_logprob_grad(const __grid_constant__ LogprobGradArgs p) {
   constexpr int n = Granule<T>::n, kEach = 4;
@@ -770,14 +818,18 @@ __global__ void __launch_bounds__(kThreads) k_logprob_grad(const __grid_constant
   pdl_launch_dependents();
   for (int64_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
     const int64_t t = b / p.splits;
-    const int g0 = (int)(b - t * p.splits) * kThreads * kEach + threadIdx.x;
+    const int split = (int)(b - t * p.splits), g0 = split * kThreads * kEach + threadIdx.x;
     const RowView<T> row(static_cast<const T*>(p.x) + t * p.ld, p.V);
     const int G = row.granules();
     T* dx = static_cast<T*>(p.dx) + t * p.ldg;
     const bool wide = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0;
     const int64_t y = p.y[t];
     const float lse = p.lse[t], alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f, H = p.dent ? p.ent[t] : 0.f;
-    const bool given = y >= 0 && y < p.V, zero = y == p.ignore || lse == -INFINITY;
+    if (fabsf(lse) >= kFarLse) {
+      if (split == 0) far_row(p, row, dx, t);
+      continue;
+    }
+    const bool given = y >= 0 && y < p.V, zero = y == p.ignore;
     const float A = given ? -p.scale * (alpha + beta * H) : NAN, B = -p.scale * beta;
     uint4 v[kEach];
 #pragma unroll
@@ -832,7 +884,7 @@ cudaError_t launch_rows(K kernel, int threads, const LogprobArgs& a, int64_t row
 
 // CTAs of a row: more where the rows alone do not give every SM `each` CTAs, while a share keeps `least` granules
 int spread_rows(int64_t rows, int64_t granules, int cl, int each, int least) {
-  while (cl < kMaxCluster && rows * cl < 148 * each && granules >= (int64_t)2 * cl * least) cl *= 2;
+  while (cl < kMaxCluster && rows * cl < 148 * each && granules >= (int64_t)(cl + 1) * least) ++cl;
   return cl;
 }
 
@@ -845,7 +897,7 @@ cudaError_t launch_logprob(LogprobArgs a, int64_t rows, bool grad, cudaStream_t 
   }
   // shares of 72 KB at most let three CTAs run on an SM
   a.cl = 1;
-  while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) a.cl *= 2;
+  while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) ++a.cl;
   a.cl = spread_rows(rows, granules, a.cl, 1, kLoss);
   const size_t share = (size_t)((granules + a.cl - 1) / a.cl) * 16;
   return share <= 200 << 10 ? launch_rows(k_loss<T, true>, kLoss, a, rows, share, st) : launch_rows(k_loss<T, false>, kLoss, a, rows, 0, st);

@@ -76,9 +76,9 @@ def check_grad(got, D, y, V, scale, alpha, beta, dt, from_lse=False, ignore=IGN)
     want = torch.where((y == ignore)[:, None], torch.zeros_like(want), want)
     a = (D["d"] / math.log(2)).clamp(min=-150).nan_to_num(0, 0, 0)
     q = rel_S(V) + (4 + 3 * a.abs()) * U
-    if from_lse:            # p = exp(x - lse) with lse rounded to fp32 and off by its own tolerance
-        big = (D["lse"].abs()[:, None] + (D["d"] + D["M"][:, None]).abs().clamp(max=1e4)).nan_to_num(0, 0, 0)
-        q = q + 6 * U * big + rel_S(V)
+    if from_lse:            # p = exp(x - lse) with lse rounded to fp32 and off by its own tolerance; not from |lse| = 4096 on
+        big = (D["lse"].abs()[:, None] + (D["d"] + D["M"][:, None]).abs()).nan_to_num(0, 0, 0)
+        q = q + torch.where(D["lse"].abs()[:, None] < 4096, 6 * U * big.clamp(max=1e5), torch.zeros_like(big)) + rel_S(V)
     # the bracket's largest terms, and the entropy that the kernel uses being off by its own tolerance
     eH = rel_S(V) * (1 + 2 * math.log(2) * (math.log2(max(V, 2)) + 2)) + 4 * U * (1 + math.log(V))
     size = alpha.abs() + beta.abs() * (H.abs() + lpz.abs() + 2 * torch.log(D["S"]).abs()[:, None].nan_to_num(0, 0, 0))
@@ -175,6 +175,30 @@ def test_masked_entries_and_rows_without_any(V, dt):
         check_grad(out[keep], sub, y[keep], V, 1.0, alpha[keep], beta[keep], dt, from_lse=form == "backward")
         assert torch.isfinite(out).all()
         assert (out[1] == 0).all() and (out[5] == 0).all() and (out[6] == 0).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [70, 50000])
+@pytest.mark.parametrize("level", [1000.0, -5000.0, 1e6, -1e30])
+def test_logits_far_from_zero(level, V, dt):
+    """All logits of some rows at a level where lse in fp32 says little about their differences."""
+    T = 5
+    x, y, _ = make(T, V, torch.float32, seed=11)
+    x[1:4] = (x[1:4] * abs(level) * 2.0 ** -7 + level) if abs(level) < 1e5 else level
+    x = x.to(dt)
+    y[3] = IGN
+    run = runner(T, V, dt)
+    run.forward(x, y)
+    D = definition(x, y, 1.0)
+    check_stats(run, T, D, V)
+    alpha, beta = torch.linspace(0.5, 2, T, device="cuda"), torch.linspace(-1, 1, T, device="cuda")
+    for form in ("backward", "loss"):
+        out = torch.empty(T, V, device="cuda", dtype=dt)
+        getattr(run, form)(x, y, alpha, beta, out)
+        check_grad(out, D, y, V, 1.0, alpha, beta, dt, from_lse=form == "backward")
+        again = x.clone()
+        getattr(run, form)(again, y, alpha, beta, again)
+        assert torch.equal(again, out)
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
