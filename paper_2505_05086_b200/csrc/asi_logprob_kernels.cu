@@ -884,7 +884,7 @@ cudaError_t launch_rows(K kernel, int threads, const LogprobArgs& a, int64_t row
 
 // CTAs of a row: more where the rows alone do not give every SM `each` CTAs, while a share keeps `least` granules
 int spread_rows(int64_t rows, int64_t granules, int cl, int each, int least) {
-  while (cl < kMaxCluster && rows * cl < 148 * each && granules >= (int64_t)(cl + 1) * least) ++cl;
+  while (cl < kMaxCluster && rows * cl < 148 * each && granules >= (int64_t)2 * cl * least) cl *= 2;
   return cl;
 }
 
@@ -897,7 +897,7 @@ cudaError_t launch_logprob(LogprobArgs a, int64_t rows, bool grad, cudaStream_t 
   }
   // shares of 72 KB at most let three CTAs run on an SM
   a.cl = 1;
-  while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) ++a.cl;
+  while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) a.cl *= 2;
   a.cl = spread_rows(rows, granules, a.cl, 1, kLoss);
   const size_t share = (size_t)((granules + a.cl - 1) / a.cl) * 16;
   return share <= 200 << 10 ? launch_rows(k_loss<T, true>, kLoss, a, rows, share, st) : launch_rows(k_loss<T, false>, kLoss, a, rows, 0, st);
