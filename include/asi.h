@@ -268,7 +268,8 @@ asi_status_t asi_poll_status(const asi_plan_t* plan, const void* ws, void* strea
  * vocabulary, and the gradients of a step (dW of asi_wgrad_batched among them) go to an optimiser.  These entry
  * points take descriptors instead of plans (nothing about them is worth keeping), follow the conventions at the top,
  * and write nothing but the outputs they name; two calls with outputs and workspaces of their own may overlap.
- * Results are bit-identical from call to call.  Token ids and targets are int64. */
+ * Results are bit-identical from call to call on the same buffers (the order of a row's sums goes by where it starts
+ * within 16 bytes).  Token ids and targets are int64. */
 
 /* Log probabilities of given tokens.  With x_j = scale * logits[t][j] over the row's `vocab` entries:
  *   lse = log sum_j exp(x_j);   logp = x_y - lse for the given token y = targets[t];

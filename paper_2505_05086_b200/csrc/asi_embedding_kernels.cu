@@ -302,8 +302,9 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
   pdl_wait();
   pdl_launch_dependents();
   __shared__ __align__(4) uint16_t wh[kSortWarps][kBins];
-  __shared__ uint32_t start[kBins], count[kBins], warp_sum[kSortWarps];
+  __shared__ uint32_t start[kBins], count[kSortCluster][kBins], warp_sum[kSortWarps];
   cg::cluster_group cluster = cg::this_cluster();
+  cluster.barrier_arrive();                                          // (shared memory of CTAs that run can be written)
   const int warp = tid >> 5, lane = tid & 31, rank0 = blockIdx.x, seg = 1 << p.seg;
   const int items = (seg + kSortThreads - 1) / kSortThreads;         // of a thread
   uint32_t* skey = sort_mem;
@@ -326,17 +327,19 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * kDigit;
     const uint32_t own = digit_ranks(key, here, items, shift, wh, rank);
-    if (tid < kBins) count[tid] = own;
+    if (pass == 0) cluster.barrier_wait();
+    if (tid < kBins) {                                               // to everybody
+#pragma unroll
+      for (int q = 0; q < kSortCluster; ++q) *cluster.map_shared_rank(&count[rank0][tid], q) = own;
+    }
     cluster.sync();                                                  // (every segment is in registers, every count is there)
     uint32_t earlier = 0, total = 0;
     if (tid < kBins) {
-      uint32_t c[kSortCluster];
-#pragma unroll
-      for (int q = 0; q < kSortCluster; ++q) c[q] = *cluster.map_shared_rank(&count[tid], q);
 #pragma unroll
       for (int q = 0; q < kSortCluster; ++q) {
-        if (q < rank0) earlier += c[q];
-        total += c[q];
+        const uint32_t c = count[q][tid];
+        if (q < rank0) earlier += c;
+        total += c;
       }
     }
     const uint32_t before = block_exclusive(total, warp_sum);
@@ -399,8 +402,7 @@ __global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_const
 // ---- sums of runs
 constexpr int kMaxChunk = 64;
 constexpr int kZeroRows = 64;
-// CTAs of an SM by the values a thread moves, as their registers allow
-constexpr int sum_ctas(int vec) { return vec == 4 ? 3 : 4; }
+constexpr int kSumCtas = 3;                 // CTAs of an SM (tied table of 50257 x 770: 26 us, with four 28, with five 33)
 constexpr int kInFlight = 16;              // registers of a thread for rows in hand
 
 struct SumArgs {
@@ -451,7 +453,7 @@ __device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t 
 // CTAs [0, chunks): sums, with one warp more that looks for the ends of the runs that cross chunks.  CTAs behind them (many
 // tokens, overwriting): rows of dW without tokens.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(const __grid_constant__ SumArgs p) {
+__global__ void __launch_bounds__(kEmbThreads + 32, kSumCtas) k_embed_sum(const __grid_constant__ SumArgs p) {
   pdl_launch_dependents();                                           // (what comes next waits for this kernel, or needs nothing of it)
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, workers = blockDim.x - 32;
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(c
       if (empty[r]) store_values<float, VEC>(p.dW + (v0 + r) * p.D + col, f);
     return;
   }
-  __shared__ uint32_t sk[kMaxChunk + 2], sp[kMaxChunk];
+  __shared__ uint32_t sk[kMaxChunk + 2], sp[kMaxChunk], end_bits[2];
   __shared__ int from[2], to[2], done[2];                            // chunks of the run that comes in, and that goes out
   const int c = blockIdx.x, c0 = c * p.C, m = min(p.C, p.T - c0);
   // sk[0] is the key before the chunk, sk[m + 1] the one behind it; V where there is none
@@ -481,6 +483,13 @@ __global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(c
     const int at = c0 + i - 1;
     sk[i] = at < 0 || at >= p.T ? p.V : p.key[at];
     if (i >= 1 && i <= m) sp[i - 1] = p.pos[at];
+  }
+  // a bit for each token that ends a run, or the chunk
+  if (tid < 64) {
+    const int at = c0 + tid;
+    const bool end = tid < m && (tid + 1 == m || p.key[at + 1] != p.key[at]);
+    const uint32_t bits = __ballot_sync(~0u, end);
+    if (lane == 0) end_bits[tid >> 5] = bits;
   }
   const int live = __syncthreads_count(tid < m && p.key[c0 + tid] != p.V);   // tokens behind them contribute nothing
   if (live == 0) return;
@@ -509,10 +518,11 @@ __global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(c
     if (lane == 0) from[0] = first, to[0] = through ? last : c, from[1] = c, to[1] = last;
   } else if (col < p.D) {
     // U rows in hand and the next U on their way
-    constexpr int U = kInFlight / (VEC * (int)sizeof(T) > 4 ? VEC * (int)sizeof(T) / 4 : 1);
+    constexpr int kWordRegs = VEC * (int)sizeof(T) / 4, U = kWordRegs > kInFlight / 8 ? kInFlight / kWordRegs : 8;
     float acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+    const uint64_t ends = (uint64_t)end_bits[1] << 32 | end_bits[0];
     bool first_run = true;
     const T* src = static_cast<const T*>(p.dout) + col;
     Word<T, VEC> f[2][U];
@@ -529,16 +539,16 @@ __global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(c
         const int i0 = j0 + h * U;
         if (i0 >= live) break;
         bring(i0 + U, f[h ^ 1]);
+        const uint32_t here = (uint32_t)(ends >> i0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int i = i0 + u;
           if (i >= live) break;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) acc[e] += f[h][u].value(e);
-          const bool ends = sk[i + 2] != sk[i + 1];
-          if (!ends && i + 1 < m) continue;
+          if (!(here & (1u << u))) continue;
           if (first_run && comes) store_values<float, VEC>(p.head + (int64_t)c * p.D + col, acc);
-          else if (!ends) store_values<float, VEC>(p.tail + (int64_t)c * p.D + col, acc);
+          else if (goes && i + 1 == m) store_values<float, VEC>(p.tail + (int64_t)c * p.D + col, acc);
           else put_row<VEC>(p, sk[i + 1], col, acc);
           first_run = false;
 #pragma unroll
@@ -562,7 +572,7 @@ __global__ void __launch_bounds__(kEmbThreads + 32, sum_ctas(VEC)) k_embed_sum(c
     if (!done[side]) continue;
     float acc[VEC];
     load_shared_values<VEC>(p.tail + (int64_t)from[side] * p.D + col, acc);
-    constexpr int P = 32 / VEC;                                      // pieces on their way at once
+    constexpr int P = VEC == 1 ? 16 : 32 / VEC;                      // pieces on their way at once
     const int end = to[side];
     for (int q = from[side] + 1; q <= end; q += P) {
       float f[P][VEC];
@@ -662,7 +672,7 @@ cudaError_t sort_tokens(SortArgs a, const Layout& l, int counters, char* w, int*
     a.pos_out = reinterpret_cast<uint32_t*>(w + l.pos[0]);
     while (l.T > kSortCluster << a.seg) ++a.seg;
     const size_t smem = (size_t)6 << a.seg;
-    cudaError_t e = smem > 24 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one), smem) : cudaSuccess;
+    cudaError_t e = smem > 16 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one), smem) : cudaSuccess;
     *out = 0;
     if (e == cudaSuccess) e = launch_pdl(k_sort_one, dim3(kSortCluster), dim3(kSortThreads), smem, st, a);
     return e;
@@ -756,7 +766,7 @@ asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t
   try {
     // (beside the clearing kernel the sums have two CTAs an SM, so that both fit)
     const bool clear = !accumulate, beside = clear && l.one;
-    const int slabs = (int)slabs_of(desc->dim, vec), C = chunk_of(l.T, slabs, beside ? 2 : sum_ctas(vec)), chunks = (l.T + C - 1) / C;
+    const int slabs = (int)slabs_of(desc->dim, vec), C = chunk_of(l.T, slabs, beside ? 2 : kSumCtas), chunks = (l.T + C - 1) / C;
     SortArgs sort = {};
     sort.ids = ids;
     sort.dW = dW;

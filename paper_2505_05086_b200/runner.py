@@ -116,6 +116,10 @@ class StepRunner:
                          [d.data_ptr() for d in dys], [r.dW.data_ptr() for r in rs],
                          [r.ws_w.data_ptr() for r in rs], [r.ws_w.numel() for r in rs], _stream_handle(stream))
 
+    def optimizer(self, weights, **kw):
+        """AdamW over the layers' weights (one for each, fp32 or bf16) and the dW buffers that wgrad() fills."""
+        return AdamWRunner(weights, [r.dW for r in self.runners], **kw)
+
 
 # ---- the rest of a language model's training step ---------------------------------------------------
 
