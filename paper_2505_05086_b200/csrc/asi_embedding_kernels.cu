@@ -381,20 +381,33 @@ __global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_const
     if (r >= 0 && r < rows) atomicOr(&seen[r >> 5], 1u << (r & 31));
   }
   __syncthreads();
-  // units of 16 bytes where rows are whole multiples of them, else of 4
-  const bool wide = p.D % 4 == 0 && (reinterpret_cast<uintptr_t>(p.dW) & 15) == 0;
-  const int units = (int)(wide ? p.D / 4 : p.D), down = kClearThreads / units, along = kClearThreads % units;
-  int64_t r = tid / units;
-  int c = tid % units;
   float* row0 = p.dW + v0 * p.D;
-  while (r < rows) {
-    if (!((seen[r >> 5] >> (r & 31)) & 1u)) {
-      if (wide) reinterpret_cast<float4*>(row0 + r * p.D)[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-      else row0[r * p.D + c] = 0.f;
+  auto each = [&](int units, auto put) {                             // (row, unit) without a division for each
+    const int down = kClearThreads / units, along = kClearThreads % units;
+    int64_t r = tid / units;
+    int u = tid % units;
+    while (r < rows) {
+      if (!((seen[r >> 5] >> (r & 31)) & 1u)) put(row0 + r * p.D, u);
+      r += down;
+      u += along;
+      if (u >= units) u -= units, ++r;
     }
-    r += down;
-    c += along;
-    if (c >= units) c -= units, ++r;
+  };
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (p.D % 4 == 0 && (reinterpret_cast<uintptr_t>(p.dW) & 15) == 0) {
+    each((int)(p.D / 4), [&](float* row, int u) { reinterpret_cast<float4*>(row)[u] = zero; });
+  } else {
+    // aligned words of 16 bytes that a row reaches: whole but for its first and last
+    each((int)((p.D + 6) / 4), [&](float* row, int u) {
+      const int64_t j = 4 * (int64_t)u - ((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
+      if (j >= 0 && j + 4 <= p.D) {
+        *reinterpret_cast<float4*>(row + j) = zero;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e >= 0 && j + e < p.D) row[j + e] = 0.f;
+      }
+    });
   }
   pdl_wait();
 }
