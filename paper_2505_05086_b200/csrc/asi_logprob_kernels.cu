@@ -22,11 +22,15 @@ namespace asi {
 
 namespace {
 
-constexpr int kFwd = 128;                   // threads of a CTA: forward, loss, gradient alone
-constexpr int kLoss = 256, kLossCtas = 3;
+// Threads of a CTA and CTAs of an SM, as registers and shared memory allow: forward (one more with leading entries: their
+// search waits a lot), loss, both for rows of a few granules, gradient alone
+constexpr int kFwd = 128, kFwdCtas = 8, kLoss = 256, kLossCtas = 3, kLossMid = 128, kLossMidCtas = 6, kShort = 32, kMid = 64;
+constexpr int ctas_of(int threads, int large) { return threads == kShort ? 32 : threads == kMid ? 1024 / kMid : large; }
 constexpr int kThreads = 256, kEach = 8;    // granules of a thread in the gradient alone (4: 93 us at 4096 x 32000, 8: 86)
 constexpr int kMaxCluster = 8;
 constexpr int kShare = 72 << 10;            // bytes of a row that a CTA of the loss keeps, where a cluster allows it
+// granules of a row for CTAs of one warp, of two, and (loss) of four
+constexpr int kLittle = 160, kFew = 512, kSome = 2100;
 constexpr int kCand = 512;                 // candidates of a CTA's top entries
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
@@ -330,14 +334,15 @@ constexpr int kBatch = 4;                  // granules a thread has in hand
 constexpr int kSlots = 16;                 // maxima a thread remembers of what it has read
 constexpr int kHits = 512;
 
+template <int kN>
 struct TopShared {
   unsigned long long cand[kCand];
   unsigned long long pool[kCand];          // and of a cluster's
   unsigned long long list[ASI_TOP_MAX];    // the leading entries, largest first
-  unsigned long long best[kFwd / 32];
-  float slot[kSlots][kFwd];
-  uint16_t hit[kHits];                     // slot * kFwd + thread: granules that may hold candidates
-  float most[kFwd];                        // each thread's maximum
+  unsigned long long best[kN / 32];
+  float slot[kSlots][kN];
+  uint16_t hit[kHits];                     // slot * kN + thread: granules that may hold candidates
+  float most[kN];                        // each thread's maximum
   float tau;
   uint32_t least;
   int count, hits, pooled;
@@ -368,7 +373,7 @@ __device__ __forceinline__ uint32_t reached_by(const uint32_t (&key)[N], int k, 
 }
 
 // The largest key below prev among those that `each` offers, over the CTA
-template <typename F>
+template <int kN, typename F>
 __device__ __forceinline__ unsigned long long block_best(unsigned long long prev, unsigned long long* warps, F each) {
   unsigned long long best = 0;
   each([&](unsigned long long key) {
@@ -384,7 +389,7 @@ __device__ __forceinline__ unsigned long long block_best(unsigned long long prev
   __syncthreads();
   best = warps[0];
 #pragma unroll
-  for (int i = 1; i < kFwd / 32; ++i)
+  for (int i = 1; i < kN / 32; ++i)
     if (warps[i] > best) best = warps[i];
   return best;
 }
@@ -472,17 +477,17 @@ __device__ __forceinline__ void stream_share(const Share<T>& s, float c2, float&
   }
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_constant__ LogprobArgs p) {
-  constexpr int n = Granule<T>::n, kWarps = kFwd / 32;
+template <typename T, bool TOP, int kN>
+__global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(const __grid_constant__ LogprobArgs p) {
+  constexpr int n = Granule<T>::n, kWarps = kN / 32;
   __shared__ RowShared<kWarps> sh;
-  __shared__ TopShared top;
+  __shared__ TopShared<kN> top;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cl = p.cl, t = blockIdx.x / cl, rank = blockIdx.x - t * cl;
   const Share<T> s(p, t, rank);
   const RowView<T>& row = s.row;
   const int g0 = s.g0, cnt = s.cnt;
-  const int batches = (cnt + kBatch * kFwd - 1) / (kBatch * kFwd);
+  const int batches = (cnt + kBatch * kN - 1) / (kBatch * kN);
   const int span = (batches + kSlots - 1) / kSlots;                 // batches that share a slot
   const float c2 = p.scale * kLog2e;
 
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
 
   float M, S, W, slot = -INFINITY;
   int in_slot = 0, slots = 0;
-  stream_share<T, kFwd>(s, c2, M, S, W, [&](int b, const uint4*, float most) {
+  stream_share<T, kN>(s, c2, M, S, W, [&](int b, const uint4*, float most) {
     if (TOP) {
       slot = nan_max(slot, most);
       if (++in_slot == span || b == batches - 1) {
@@ -516,9 +521,9 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
   if (TOP) {
     // tau, about the k-th largest of the threads' maxima: at least k entries reach it, and few more
     if (warp == 0) {
-      uint32_t key[kFwd / 32];
+      uint32_t key[kN / 32];
 #pragma unroll
-      for (int i = 0; i < kFwd / 32; ++i) key[i] = order_bits(top.most[i * 32 + lane]);
+      for (int i = 0; i < kN / 32; ++i) key[i] = order_bits(top.most[i * 32 + lane]);
       const uint32_t t = reached_by(key, p.k, Granule<T>::kUnit);
       if (lane == 0) top.tau = order_value(t);
     }
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
       for (int k = 0; k < slots; ++k)
         if (top.slot[k][tid] >= tau) {
           const int place = atomicAdd(&top.hits, 1);
-          if (place < kHits) top.hit[place] = (uint16_t)(k * kFwd + tid);
+          if (place < kHits) top.hit[place] = (uint16_t)(k * kN + tid);
         }
     __syncthreads();
     const int hits = top.hits;
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
         j[u] = -1;
         if (h < pieces && lane < kEntries) {
           const int at = span == 1 ? h : h / span, which = top.hit[at];
-          const int b = which / kFwd * span + (h - at * span), i = (b * kBatch + lane / n) * kFwd + which % kFwd;
+          const int b = which / kN * span + (h - at * span), i = (b * kBatch + lane / n) * kN + which % kN;
           if (i < cnt) j[u] = row.first(g0 + i) + lane % n;
           if (j[u] >= p.V) j[u] = -1;
         }
@@ -565,8 +570,8 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
     if (top.count > kCand) {                // many equal values: one sweep for each entry
       unsigned long long prev = ~0ull;
       for (int r = 0; r < p.k; ++r) {
-        prev = block_best(prev, top.best, [&](auto offer) {
-          for (int i = tid; i < cnt; i += kFwd) {
+        prev = block_best<kN>(prev, top.best, [&](auto offer) {
+          for (int i = tid; i < cnt; i += kN) {
             float f[n];
             Granule<T>::floats(row.load(g0 + i), f);
             const int j = row.first(g0 + i);
@@ -618,21 +623,21 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
             if (lane == 0) top.least = t;
           }
           __syncthreads();
-          unsigned long long keep[kFew / kFwd];
+          unsigned long long keep[kFew / kN];
 #pragma unroll
-          for (int i = 0; i < kFew / kFwd; ++i) keep[i] = i * kFwd + tid < pooled ? top.pool[i * kFwd + tid] : 0;
+          for (int i = 0; i < kFew / kN; ++i) keep[i] = i * kN + tid < pooled ? top.pool[i * kN + tid] : 0;
           if (tid == 0) top.pooled = 0;
           __syncthreads();
 #pragma unroll
-          for (int i = 0; i < kFew / kFwd; ++i)
+          for (int i = 0; i < kFew / kN; ++i)
             if (keep[i] && (uint32_t)(keep[i] >> 32) >= top.least) top.pool[atomicAdd(&top.pooled, 1)] = keep[i];
         } else if (top.pooled > kCand) {    // many equal values again
           unsigned long long prev = ~0ull;
           for (int r = 0; r < p.k; ++r) {
-            prev = block_best(prev, top.best, [&](auto offer) {
+            prev = block_best<kN>(prev, top.best, [&](auto offer) {
               for (int q = 0; q < cl; ++q) {
                 const int of_q = __shfl_sync(~0u, found, q);
-                for (int i = tid; i < of_q; i += kFwd) offer(remote_u64(&top.cand[i], q));
+                for (int i = tid; i < of_q; i += kN) offer(remote_u64(&top.cand[i], q));
               }
             });
             if (tid == 0) top.pool[r] = prev;
@@ -650,7 +655,7 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
   if (TOP) {
     const unsigned long long* from = cl > 1 ? top.pool : top.cand;
     const int found = min(cl > 1 ? top.pooled : top.count, kCand);
-    for (int i = tid; i < found; i += kFwd) {
+    for (int i = tid; i < found; i += kN) {
       const unsigned long long key = from[i];
       int above = 0;
 #pragma unroll 4
@@ -671,9 +676,9 @@ __global__ void __launch_bounds__(kFwd, TOP ? 9 : 8) k_logprob(const __grid_cons
 
 // ---- forward and gradient.  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
 // is read again: rows of more than 1.6 MB).  Every thread reads back what it left there itself: no barrier.
-template <typename T, bool RES>
-__global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant__ LogprobArgs p) {
-  constexpr int n = Granule<T>::n, kWarps = kLoss / 32;
+template <typename T, bool RES, int kN>
+__global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLossMid ? kLossMidCtas : kLossCtas)) k_loss(const __grid_constant__ LogprobArgs p) {
+  constexpr int n = Granule<T>::n, kWarps = kN / 32;
   extern __shared__ uint4 buf[];
   __shared__ RowShared<kWarps> sh;
   const int tid = threadIdx.x, cl = p.cl, t = blockIdx.x / cl, rank = blockIdx.x - t * cl;
@@ -685,17 +690,17 @@ __global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant
   const bool given = y >= 0 && y < p.V, skip = y == p.ignore;
   // the given entry: read by the thread that reports logp and by the one that writes its gradient (dx may be x)
   const int yg = given ? (int)((s.row.mis + y) / n) - s.g0 : -1;
-  const bool mine = yg >= 0 && yg < s.cnt && yg % kLoss == tid;
+  const bool mine = yg >= 0 && yg < s.cnt && yg % kN == tid;
   float xy = 0.f;
   if (mine || (given && tid == 0 && rank == 0)) xy = Granule<T>::read(s.row.x + y);
   const float alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f;
 
   float M, S, W;
-  stream_share<T, kLoss>(s, c2, M, S, W, [&](int b, const uint4* v, float) {
+  stream_share<T, kN>(s, c2, M, S, W, [&](int b, const uint4* v, float) {
     if (RES) {
 #pragma unroll
       for (int q = 0; q < kBatch; ++q)
-        if ((b * kBatch + q) * kLoss + tid < s.cnt) buf[(b * kBatch + q) * kLoss + tid] = v[q];
+        if ((b * kBatch + q) * kN + tid < s.cnt) buf[(b * kBatch + q) * kN + tid] = v[q];
     }
   });
   const float own = M;
@@ -732,7 +737,7 @@ __global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant
     float f[n];
 #pragma unroll
     for (int e = 0; e < n; ++e) f[e] = 0.f;
-    for (int i = tid; i < s.cnt; i += kLoss) put(i, f);
+    for (int i = tid; i < s.cnt; i += kN) put(i, f);
   } else {
     const float inv = 1.f / S, lnS = logf(S), H = lnS - kLn2 * W * inv;
     const float A = given ? -p.scale * (alpha + beta * (H - lnS)) * inv : NAN, B = -p.scale * beta * kLn2 * inv;
@@ -740,7 +745,7 @@ __global__ void __launch_bounds__(kLoss, kLossCtas) k_loss(const __grid_constant
     const uint4* src = s.row.granule(s.g0);
     auto gradient = [&](auto with_entropy) {
 #pragma unroll 2
-      for (int i = tid; i < s.cnt; i += kLoss) {
+      for (int i = tid; i < s.cnt; i += kN) {
         f2 x[n / 2];
         Granule<T>::pairs(RES ? buf[i] : i >= s.lo && i < s.hi ? src[i] : s.row.edge(s.g0 + i), x);
         float f[n];
@@ -891,16 +896,26 @@ int spread_rows(int64_t rows, int64_t granules, int cl, int each, int least) {
 template <typename T>
 cudaError_t launch_logprob(LogprobArgs a, int64_t rows, bool grad, cudaStream_t st) {
   const int64_t granules = ((int64_t)a.V + 2 * Granule<T>::n - 2) / Granule<T>::n;   // of a row at the worst offset
+  // Rows of a few granules leave most threads of a large CTA without work and wait for its barriers: where there are many of
+  // them, smaller CTAs (loss of 8192 x 300 bf16: 13 us with 32 threads, 54 with 256; of 4096 x 16000: 56 with 128, 64 with
+  // 256; of 4096 x 24000: 91 and 86.  Forward, 4096 x 3000 and 5 alternatives: 18 us with 64, 21 with 128).
+  const bool many = rows >= 148 * 4, little = many && granules <= kLittle, few = many && granules <= kFew, some = many && granules <= kSome;
   if (!grad) {
-    a.cl = spread_rows(rows, granules, 1, 5, 2 * kFwd);
-    return a.k ? launch_rows(k_logprob<T, true>, kFwd, a, rows, 0, st) : launch_rows(k_logprob<T, false>, kFwd, a, rows, 0, st);
+    a.cl = few ? 1 : spread_rows(rows, granules, 1, 5, 2 * kFwd);
+    if (little) return a.k ? launch_rows(k_logprob<T, true, kShort>, kShort, a, rows, 0, st) : launch_rows(k_logprob<T, false, kShort>, kShort, a, rows, 0, st);
+    if (few) return a.k ? launch_rows(k_logprob<T, true, kMid>, kMid, a, rows, 0, st) : launch_rows(k_logprob<T, false, kMid>, kMid, a, rows, 0, st);
+    return a.k ? launch_rows(k_logprob<T, true, kFwd>, kFwd, a, rows, 0, st) : launch_rows(k_logprob<T, false, kFwd>, kFwd, a, rows, 0, st);
   }
   // shares of 72 KB at most let three CTAs run on an SM
   a.cl = 1;
   while (a.cl < kMaxCluster && granules * 16 > (int64_t)a.cl * kShare) a.cl *= 2;
-  a.cl = spread_rows(rows, granules, a.cl, 1, kLoss);
+  if (!some) a.cl = spread_rows(rows, granules, a.cl, 1, kLoss);
   const size_t share = (size_t)((granules + a.cl - 1) / a.cl) * 16;
-  return share <= 200 << 10 ? launch_rows(k_loss<T, true>, kLoss, a, rows, share, st) : launch_rows(k_loss<T, false>, kLoss, a, rows, 0, st);
+  if (little) return launch_rows(k_loss<T, true, kShort>, kShort, a, rows, share, st);
+  if (few) return launch_rows(k_loss<T, true, kMid>, kMid, a, rows, share, st);
+  if (some) return launch_rows(k_loss<T, true, kLossMid>, kLossMid, a, rows, share, st);
+  return share <= 200 << 10 ? launch_rows(k_loss<T, true, kLoss>, kLoss, a, rows, share, st)
+                            : launch_rows(k_loss<T, false, kLoss>, kLoss, a, rows, 0, st);
 }
 
 asi_status_t check_desc(const asi_logprob_desc_t* d) {
