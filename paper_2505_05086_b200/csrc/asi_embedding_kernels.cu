@@ -737,7 +737,8 @@ asi_status_t asi_embedding_forward(const asi_embedding_desc_t* desc, const void*
   if (desc->tokens == 0) return ASI_OK;
   const size_t et = size_of(desc->table_dtype), eo = size_of(desc->in_dtype);
   if (!table || !ids || !out || !aligned(table, et) || !aligned(out, eo)) return ASI_ERR_INVALID_ARG;
-  if (!apart(table, et * desc->vocab * desc->dim, out, eo * desc->tokens * desc->dim)) return ASI_ERR_INVALID_ARG;
+  const size_t out_bytes = eo * desc->tokens * desc->dim;
+  if (!apart(table, et * desc->vocab * desc->dim, out, out_bytes) || !apart(ids, 8 * desc->tokens, out, out_bytes)) return ASI_ERR_INVALID_ARG;
   LookupArgs a = {};
   a.table = table;
   a.ids = ids;

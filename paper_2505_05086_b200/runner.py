@@ -161,7 +161,7 @@ def _take(name, x, shape, dtype, device):
 class LogprobRunner:
     """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
     lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
-    the others as they were."""
+    the others as they were.  backward() reads lse and entropy of the last forward() or loss()."""
 
     def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
         self.device = _cuda_device(device)
@@ -218,7 +218,8 @@ class LogprobRunner:
 
 
 class EmbeddingRunner:
-    """Embedding lookup of up to `tokens` tokens and its weight gradient, with the workspace of the latter."""
+    """Embedding lookup of up to `tokens` tokens and its weight gradient, with the workspace of the latter: calls of wgrad() (and
+    graphs captured from them) that may run at the same time need a runner each."""
 
     def __init__(self, vocab, dim, tokens, bf16=False, bf16_table=False, scale=1.0, padding_idx=None, device="cuda:0"):
         self.device = _cuda_device(device)

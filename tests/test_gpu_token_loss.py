@@ -107,7 +107,10 @@ def runner(T, V, dt, **kw):
 
 
 SIZES = [(1, 1, 0, 0), (3, 2, 1, 1), (2, 7, 0, 3), (5, 33, 2, 0), (4, 257, 0, 1), (7, 1000, 24, 0), (150, 513, 0, 5),
-         (2, 32000, 0, 0), (300, 32000, 8, 1), (3, 50257, 0, 0), (2, 131073, 7, 1), (1, 400003, 0, 0), (2, 950001, 1, 0)]
+         (2, 32000, 0, 0), (300, 32000, 8, 1), (3, 50257, 0, 0), (2, 131073, 7, 1), (1, 400003, 0, 0), (2, 950001, 1, 0),
+         # many rows, from where small CTAs take them, on both sides of their lines (granules of 8 or 4 values)
+         (600, 1, 0, 1), (600, 300, 1, 3), (593, 641, 0, 1), (593, 1275, 2, 0), (600, 2041, 0, 1), (592, 4089, 0, 5),
+         (600, 8401, 0, 0), (592, 16795, 0, 2)]
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
@@ -137,8 +140,8 @@ def test_forward_and_gradients_match_the_definition(T, V, pad, off, dt):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("V", [5, 600, 40000, 150000])
-def test_masked_entries_and_rows_without_any(V, dt):
+@pytest.mark.parametrize("V,times", [(5, 1), (600, 1), (40000, 1), (150000, 1), (5, 70), (300, 70), (1600, 70), (6000, 70)])
+def test_masked_entries_and_rows_without_any(V, times, dt):
     T = 9
     x, y, _ = make(T, V, dt, seed=3)
     lowest = torch.finfo(dt).min
@@ -154,6 +157,8 @@ def test_masked_entries_and_rows_without_any(V, dt):
     y[6] = IGN
     x[7, 0], y[7] = -math.inf, 0                                   # the given token is masked
     x[8] = 2.5                                                     # all equal
+    x, y = x.repeat(times, 1), y.repeat(times)
+    T *= times
     k = min(32, V)
     run = runner(T, V, dt, top_k=k)
     run.forward(x, y)
@@ -170,11 +175,12 @@ def test_masked_entries_and_rows_without_any(V, dt):
     for form in ("backward", "loss"):
         out = torch.empty(T, V, device="cuda", dtype=dt)
         getattr(run, form)(x, y, alpha, beta, out)
-        keep = torch.tensor([t != 7 for t in range(T)], device="cuda")   # log p of the masked token: -inf * 0 by the formula
+        keep = torch.tensor([t % 9 != 7 for t in range(T)], device="cuda")   # log p of the masked token: -inf * 0 by the formula
         sub = {n: q[keep] for n, q in D.items()}
         check_grad(out[keep], sub, y[keep], V, 1.0, alpha[keep], beta[keep], dt, from_lse=form == "backward")
         assert torch.isfinite(out).all()
-        assert (out[1] == 0).all() and (out[5] == 0).all() and (out[6] == 0).all()
+        for t in (1, 5, 6):
+            assert (out[t::9] == 0).all()
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
@@ -202,8 +208,8 @@ def test_logits_far_from_zero(level, V, dt):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("V", [6, 40000])
-def test_nan_inf_and_targets_outside_the_vocabulary(V, dt):
+@pytest.mark.parametrize("V,times", [(6, 1), (40000, 1), (6, 100), (1700, 100), (9000, 100)])
+def test_nan_inf_and_targets_outside_the_vocabulary(V, times, dt):
     T = 6
     x, y, _ = make(T, V, dt, seed=4)
     x[0, V - 1] = math.nan
@@ -211,31 +217,36 @@ def test_nan_inf_and_targets_outside_the_vocabulary(V, dt):
     x[2, 1], y[2] = math.nan, IGN
     y[3], y[4] = V, -7
     x[5] = math.nan
+    x, y = x.repeat(times, 1), y.repeat(times)
+    T *= times
     run = runner(T, V, dt, top_k=4)
     run.forward(x, y)
     out = torch.empty(T, V, device="cuda", dtype=dt)
     one = torch.ones(T, device="cuda")
 
+    def rows(*which):
+        return torch.tensor([t % 6 in which for t in range(T)], device="cuda")
+
     def look():
         for o in (run.lse, run.entropy):
-            assert torch.isnan(o[[0, 1, 2, 5]]).all() and torch.isfinite(o[[3, 4]]).all()
-        assert torch.isnan(run.logp[[0, 1, 3, 4, 5]]).all() and run.logp[2] == 0
+            assert torch.isnan(o[rows(0, 1, 2, 5)]).all() and torch.isfinite(o[rows(3, 4)]).all()
+        assert torch.isnan(run.logp[rows(0, 1, 3, 4, 5)]).all() and (run.logp[rows(2)] == 0).all()
 
     look()
-    assert torch.isnan(run.top_logp[[0, 1, 2, 5]]).all()
-    assert (run.top_ids[[0, 1, 2, 5]] == torch.arange(4, device="cuda")).all()
-    assert torch.equal(run.top_ids[3:5], top_of(x[3:5], 4)[1])
+    assert torch.isnan(run.top_logp[rows(0, 1, 2, 5)]).all()
+    assert (run.top_ids[rows(0, 1, 2, 5)] == torch.arange(4, device="cuda")).all()
+    assert torch.equal(run.top_ids[rows(3, 4)], top_of(x[rows(3, 4)], 4)[1])
     for form in ("backward", "loss"):
         out.fill_(3)
         getattr(run, form)(x, y, one, one, out)
-        assert torch.isnan(out[[0, 1, 3, 4, 5]]).all() and (out[2] == 0).all()
+        assert torch.isnan(out[rows(0, 1, 3, 4, 5)]).all() and (out[rows(2)] == 0).all()
     look()
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_ties_go_to_the_lowest_index(dt):
     """Many equal values: more candidates than the kernel's list holds, in one CTA and over a cluster."""
-    for T, V in ((200, 9000), (1, 60000)):
+    for T, V in ((200, 9000), (1, 60000), (600, 1000), (600, 4000)):
         g = torch.Generator(device="cuda").manual_seed(5)
         x = torch.randint(-2, 3, (T, V), generator=g, device="cuda").to(dt)
         x[0, 17] = -0.0
@@ -347,3 +358,25 @@ def test_runner_refuses_what_the_call_could_not_read():
     from paper_2505_05086_b200 import AsiError
     with pytest.raises(AsiError):                                   # over the logits, but not row for row
         run.loss(x, y, a, None, body.view(-1)[1:1 + 4 * 50].view(4, 50))
+
+
+def test_results_that_are_not_asked_for():
+    """Through the binding: no entropy, no alternatives."""
+    from paper_2505_05086_b200 import binding as B
+    T, V = 5, 700
+    x, y, _ = make(T, V, torch.float32, seed=12)
+    ref = runner(T, V, torch.float32)
+    ref.forward(x, y)
+    d = B.LogprobDesc(0, 0, T, V, V, V, IGN, 1.0)
+    s = torch.cuda.current_stream().cuda_stream
+    logp, lse, out, want = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    B.token_logprobs(d, x.data_ptr(), y.data_ptr(), logp.data_ptr(), 0, lse.data_ptr(), stream=s)
+    assert torch.equal(logp, ref.logp) and torch.equal(lse, ref.lse)
+    one = torch.ones(T, device="cuda")
+    logp.fill_(0)
+    B.token_loss(d, x.data_ptr(), y.data_ptr(), one.data_ptr(), 0, logp.data_ptr(), 0, lse.data_ptr(), out.data_ptr(), s)
+    ref.loss(x, y, one, None, want)
+    assert torch.equal(logp, ref.logp) and torch.equal(out, want)
+    B.token_logprobs_grad(d, x.data_ptr(), y.data_ptr(), lse.data_ptr(), 0, one.data_ptr(), 0, out.data_ptr(), s)
+    ref.backward(x, y, one, None, want)
+    assert torch.equal(out, want)

@@ -118,7 +118,7 @@ def test_embedding_pointers_and_workspace(B):
     L, d = B.lib(), embedding(B)
     assert L.asi_embedding_forward(embedding(B, table_dtype=7), at(0), at(1), at(2), None) == INVALID
     for args in ((None, at(1), at(2)), (at(0), None, at(2)), (at(0), at(1), None), (at(0) + 2, at(1), at(2)), (at(0), at(1), at(2) + 1),
-                 (at(0), at(1), at(0) + 64)):
+                 (at(0), at(1), at(0) + 64), (at(0), at(2) + 8, at(2))):
         assert L.asi_embedding_forward(d, *args, None) == INVALID
     need = L.asi_embedding_wgrad_ws_bytes(d)
     assert need >= 256 and need % 256 == 0
