@@ -24,10 +24,11 @@ namespace {
 
 // Threads of a CTA and CTAs of an SM, as registers and shared memory allow: forward (one more with leading entries: their
 // search waits a lot), loss, both for rows of a few granules, gradient alone
-constexpr int kFwd = 128, kFwdCtas = 8, kLoss = 256, kLossCtas = 3, kLossMid = 128, kLossMidCtas = 6, kShort = 32, kMid = 64;
+constexpr int kFwd = 128, kFwdCtas = 8, kLoss = 384, kLoss4 = 256, kLoss8 = 128, kShort = 32, kMid = 64;
 constexpr int ctas_of(int threads, int large) { return threads == kShort ? 32 : threads == kMid ? 1024 / kMid : large; }
 constexpr int kThreads = 256, kEach = 8;    // granules of a thread in the gradient alone (4: 93 us at 4096 x 32000, 8: 86)
 constexpr int kMaxCluster = 8;
+constexpr int kShare4 = 55 << 10;           // ... with which four CTAs share an SM
 constexpr int kShare = 72 << 10;            // bytes of a row that a CTA of the loss keeps, where a cluster allows it
 // granules of a row for CTAs of one warp, of two, and (loss) of four
 constexpr int kLittle = 160, kFew = 512, kSome = 2100;
@@ -442,12 +443,29 @@ __device__ __forceinline__ void bring(const Share<T>& s, int b, uint4* v) {
   }
 }
 
+// M, S and W with a batch of granules, the largest of them `most`
+template <typename T>
+__device__ __forceinline__ void add_batch(const uint4* v, float most, float c2, float& M, float& S, float& W) {
+  if (!(most <= M)) {
+    const float to = nan_max(M, most);
+    rebase(S, W, M, to, c2);
+    M = to;
+  }
+  if (M != -INFINITY) {
+    const f2 minus = pair(-M, -M), k2 = pair(c2, c2);
+    f2 S2 = 0, W2 = 0;
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) add_terms<T>(v[q], minus, k2, S2, W2);
+    S += sum2(S2);
+    W += sum2(W2);
+  }
+}
+
 // One pass over the share: M, S and W of this thread's granules, four of them in hand and the next four on their way.
-// seen(b, v, most) gets each batch with its maximum.
+// seen(b, most) gets each batch's maximum.
 template <typename T, int kN, typename F>
 __device__ __forceinline__ void stream_share(const Share<T>& s, float c2, float& M, float& S, float& W, F seen) {
   const int batches = (s.cnt + kBatch * kN - 1) / (kBatch * kN);
-  const f2 k2 = pair(c2, c2);
   M = -INFINITY, S = 0.f, W = 0.f;
   uint4 v[2][kBatch];
   if (batches) bring<T, kN>(s, 0, v[0]);
@@ -459,21 +477,50 @@ __device__ __forceinline__ void stream_share(const Share<T>& s, float c2, float&
       if (b >= batches) break;
       if (b + 1 < batches) bring<T, kN>(s, b + 1, v[h ^ 1]);
       const float most = Granule<T>::template largest_of<kBatch>(v[h]);
-      seen(b, v[h], most);
-      if (!(most <= M)) {
-        const float to = nan_max(M, most);
-        rebase(S, W, M, to, c2);
-        M = to;
-      }
-      if (M != -INFINITY) {
-        const f2 minus = pair(-M, -M);
-        f2 S2 = 0, W2 = 0;
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) add_terms<T>(v[h][q], minus, k2, S2, W2);
-        S += sum2(S2);
-        W += sum2(W2);
-      }
+      seen(b, most);
+      add_batch<T>(v[h], most, c2, M, S, W);
     }
+  }
+}
+
+// all but the `pending` youngest groups of copies of this thread have arrived
+__device__ __forceinline__ void wait_copies(int pending) {
+  if (pending >= 4) asm volatile("cp.async.wait_group 4;" ::: "memory");
+  else if (pending == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+  else if (pending == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (pending == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// The same with the share left in shared memory: all of it is on its way at once, a group of copies a batch.  Every thread reads
+// what it copied itself, here and later: no barrier.
+template <typename T, int kN>
+__device__ __forceinline__ void keep_share(const Share<T>& s, uint4* buf, float c2, float& M, float& S, float& W) {
+  const int tid = threadIdx.x, batches = (s.cnt + kBatch * kN - 1) / (kBatch * kN);
+  const uint4* src = s.row.granule(s.g0);
+  if (tid < s.lo && s.cnt > 0) buf[0] = s.row.edge(s.g0);
+  if (s.hi >= s.lo && s.hi < s.cnt && tid == s.hi % kN) buf[s.hi] = s.row.edge(s.g0 + s.hi);
+#pragma unroll 1
+  for (int b = 0; b < batches; ++b) {
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = (b * kBatch + q) * kN + tid;
+      if (i >= s.lo && i < s.hi) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(buf + i)), "l"(src + i) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  M = -INFINITY, S = 0.f, W = 0.f;
+#pragma unroll 1
+  for (int b = 0; b < batches; ++b) {
+    wait_copies(batches - 1 - b);
+    uint4 v[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = (b * kBatch + q) * kN + tid;
+      v[q] = make_uint4(Granule<T>::kNone, Granule<T>::kNone, Granule<T>::kNone, Granule<T>::kNone);
+      if (i < s.cnt) v[q] = buf[i];
+    }
+    add_batch<T>(v, Granule<T>::template largest_of<kBatch>(v), c2, M, S, W);
   }
 }
 
@@ -500,7 +547,7 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(con
 
   float M, S, W, slot = -INFINITY;
   int in_slot = 0, slots = 0;
-  stream_share<T, kN>(s, c2, M, S, W, [&](int b, const uint4*, float most) {
+  stream_share<T, kN>(s, c2, M, S, W, [&](int b, float most) {
     if (TOP) {
       slot = nan_max(slot, most);
       if (++in_slot == span || b == batches - 1) {
@@ -677,7 +724,7 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(con
 // ---- forward and gradient.  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
 // is read again: rows of more than 1.6 MB).  Every thread reads back what it left there itself: no barrier.
 template <typename T, bool RES, int kN>
-__global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLossMid ? kLossMidCtas : kLossCtas)) k_loss(const __grid_constant__ LogprobArgs p) {
+__global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLoss8 ? 8 : kN == kLoss4 ? 4 : 3)) k_loss(const __grid_constant__ LogprobArgs p) {
   constexpr int n = Granule<T>::n, kWarps = kN / 32;
   extern __shared__ uint4 buf[];
   __shared__ RowShared<kWarps> sh;
@@ -696,13 +743,8 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLossMid ? kLossMidCtas 
   const float alpha = p.dlogp[t], beta = p.dent ? p.dent[t] : 0.f;
 
   float M, S, W;
-  stream_share<T, kN>(s, c2, M, S, W, [&](int b, const uint4* v, float) {
-    if (RES) {
-#pragma unroll
-      for (int q = 0; q < kBatch; ++q)
-        if ((b * kBatch + q) * kN + tid < s.cnt) buf[(b * kBatch + q) * kN + tid] = v[q];
-    }
-  });
+  if (RES) keep_share<T, kN>(s, buf, c2, M, S, W);
+  else stream_share<T, kN>(s, c2, M, S, W, [](int, float) {});
   const float own = M;
   M = block_max<kWarps>(M, sh.red[0]);
   rebase(S, W, own, M, c2);
@@ -913,7 +955,8 @@ cudaError_t launch_logprob(LogprobArgs a, int64_t rows, bool grad, cudaStream_t 
   const size_t share = (size_t)((granules + a.cl - 1) / a.cl) * 16;
   if (little) return launch_rows(k_loss<T, true, kShort>, kShort, a, rows, share, st);
   if (few) return launch_rows(k_loss<T, true, kMid>, kMid, a, rows, share, st);
-  if (some) return launch_rows(k_loss<T, true, kLossMid>, kLossMid, a, rows, share, st);
+  if (some) return launch_rows(k_loss<T, true, kLoss8>, kLoss8, a, rows, share, st);
+  if (share <= kShare4) return launch_rows(k_loss<T, true, kLoss4>, kLoss4, a, rows, share, st);
   return share <= 200 << 10 ? launch_rows(k_loss<T, true, kLoss>, kLoss, a, rows, share, st)
                             : launch_rows(k_loss<T, false, kLoss>, kLoss, a, rows, 0, st);
 }
