@@ -156,6 +156,7 @@ constexpr int kBins = 256, kDigit = 8;
 constexpr int kItems = 8;                   // a thread's tokens
 constexpr int kTile = kSortThreads * kItems;
 constexpr int kSortCluster = 8;             // CTAs that sort in one launch
+constexpr int kFewTokens = 1024;            // sorted by one
 constexpr int kOneTokens = kSortCluster * kTile;
 
 struct SortArgs {
@@ -295,22 +296,30 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const __grid_cons
     }
 }
 
-// Up to 65536 tokens: a cluster of eight CTAs sorts them in one launch, each a segment of 2^seg of them in its shared memory;
-// counts and tokens travel through distributed shared memory.  (32000 ids: 10000 tokens take one CTA 29 us and the cluster 10.)
-__global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant__ SortArgs p) {
+// Up to 65536 tokens: a cluster of CL CTAs sorts them in one launch, each a segment of 2^seg of them in its shared memory;
+// counts and tokens travel through distributed shared memory.  (32000 ids: 10000 tokens take one CTA 29 us and eight 10.  Below
+// kFewTokens one CTA does it without the cluster's barriers; a whole accumulating call over 50257 x 768 with 8 tokens takes 7.5
+// us where eight CTAs take 9.9, with 1000 11.0 and 12.5, with 2000 as much either way.)
+template <int CL>
+__global__ void __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant__ SortArgs p) {
   extern __shared__ uint32_t sort_mem[];
   const int tid = threadIdx.x;
   pdl_wait();
   pdl_launch_dependents();
   __shared__ __align__(4) uint16_t wh[kSortWarps][kBins];
-  __shared__ uint32_t start[kBins], count[kSortCluster][kBins], warp_sum[kSortWarps];
+  __shared__ uint32_t start[kBins], count[CL][kBins], warp_sum[kSortWarps];
   cg::cluster_group cluster = cg::this_cluster();
-  cluster.barrier_arrive();                                          // (shared memory of CTAs that run can be written)
+  auto together = [&] {
+    if constexpr (CL > 1) cluster.sync();
+    else __syncthreads();
+  };
+  auto of = [&](auto* here, int q) { return CL > 1 ? cluster.map_shared_rank(here, q) : here; };
+  if constexpr (CL > 1) cluster.barrier_arrive();                    // (shared memory of CTAs that run can be written)
   const int warp = tid >> 5, lane = tid & 31, rank0 = blockIdx.x, seg = 1 << p.seg;
   const int items = (seg + kSortThreads - 1) / kSortThreads;         // of a thread
   uint32_t* skey = sort_mem;
   uint16_t* spos = reinterpret_cast<uint16_t*>(skey + seg);
-  for (int i = rank0 * kSortThreads + tid; i < p.counters; i += kSortCluster * kSortThreads) p.count[i] = 0;
+  for (int i = rank0 * kSortThreads + tid; i < p.counters; i += CL * kSortThreads) p.count[i] = 0;
   uint32_t key[kItems];
   uint16_t pos[kItems], rank[kItems];
   const int base = warp * 32 * items + lane;                         // of the segment
@@ -328,16 +337,18 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * kDigit;
     const uint32_t own = digit_ranks(key, here, items, shift, wh, rank);
-    if (pass == 0) cluster.barrier_wait();
+    if constexpr (CL > 1) {
+      if (pass == 0) cluster.barrier_wait();
+    }
     if (tid < kBins) {                                               // to everybody
 #pragma unroll
-      for (int q = 0; q < kSortCluster; ++q) *cluster.map_shared_rank(&count[rank0][tid], q) = own;
+      for (int q = 0; q < CL; ++q) *of(&count[rank0][tid], q) = own;
     }
-    cluster.sync();                                                  // (every segment is in registers, every count is there)
+    together();                                                      // (every segment is in registers, every count is there)
     uint32_t earlier = 0, total = 0;
     if (tid < kBins) {
 #pragma unroll
-      for (int q = 0; q < kSortCluster; ++q) {
+      for (int q = 0; q < CL; ++q) {
         const uint32_t c = count[q][tid];
         if (q < rank0) earlier += c;
         total += c;
@@ -351,10 +362,10 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
       if (i < here) {
         const uint32_t d = (key[i] >> shift) & (kBins - 1);
         const uint32_t to = start[d] + wh[warp][d] + rank[i];
-        *cluster.map_shared_rank(&skey[to & (seg - 1)], to >> p.seg) = key[i];
-        *cluster.map_shared_rank(&spos[to & (seg - 1)], to >> p.seg) = pos[i];
+        *of(&skey[to & (seg - 1)], to >> p.seg) = key[i];
+        *of(&spos[to & (seg - 1)], to >> p.seg) = pos[i];
       }
-    cluster.sync();
+    together();
     if (pass + 1 < p.passes) {
 #pragma unroll
       for (int i = 0; i < kItems; ++i)
@@ -686,11 +697,27 @@ cudaError_t sort_tokens(SortArgs a, const Layout& l, int counters, char* w, int*
   if (l.one) {
     a.key_out = reinterpret_cast<uint32_t*>(w + l.key[0]);
     a.pos_out = reinterpret_cast<uint32_t*>(w + l.pos[0]);
-    while (l.T > kSortCluster << a.seg) ++a.seg;
+    const bool few = l.T <= kFewTokens;
+    while (l.T > (few ? 1 : kSortCluster) << a.seg) ++a.seg;
     const size_t smem = (size_t)6 << a.seg;
-    cudaError_t e = smem > 16 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one), smem) : cudaSuccess;
     *out = 0;
-    if (e == cudaSuccess) e = launch_pdl(k_sort_one, dim3(kSortCluster), dim3(kSortThreads), smem, st, a);
+    if (few) return launch_pdl(k_sort_one<1>, dim3(1), dim3(kSortThreads), smem, st, a);
+    cudaError_t e = smem > 16 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one<kSortCluster>), smem) : cudaSuccess;
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortCluster);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = kSortCluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, k_sort_one<kSortCluster>, a);
     return e;
   }
   cudaError_t e = cudaSuccess;
