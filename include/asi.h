@@ -307,7 +307,8 @@ asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logi
  *           2^-24 |lse|; rows with |lse| >= 4096 are summed again instead.
  *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
  *   dlogits [out] device in_dtype [rows][ld_grad]; what lies between vocab and ld_grad stays as it was.  It may be
- *           logits itself (the same address, ld_grad == ld), and overlaps it in no other way. */
+ *           logits itself (the same address, ld_grad == ld), or lie between its rows (ld_grad == ld); beyond that the two
+ *           do not meet. */
 asi_status_t asi_token_logprobs_grad(const asi_logprob_desc_t* desc, const void* logits, const int64_t* targets,
                                      const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                                      void* dlogits, void* stream);
@@ -322,8 +323,7 @@ asi_status_t asi_token_loss(const asi_logprob_desc_t* desc, const void* logits, 
  * Its weight gradient beside those of conv2d and linear layers:
  *   dW[v][:] = scale * sum over t with ids[t] = v of dOut[t][:]      (fp32, terms in the order of t in fixed groups)
  * added to what dW holds (accumulate != 0: a table tied to the output layer; subnormal sums count as 0 there), or written
- * over all of dW.  Tokens of
- * padding_idx and ids outside [0, vocab) contribute nothing. */
+ * over all of dW.  Tokens of padding_idx and ids outside [0, vocab) contribute nothing. */
 typedef struct {
   int32_t table_dtype;           /* asi_dtype_t of table (asi_embedding_forward) */
   int32_t in_dtype;              /* asi_dtype_t of out and dOut */

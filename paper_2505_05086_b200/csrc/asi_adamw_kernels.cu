@@ -437,8 +437,8 @@ extern "C" asi_status_t asi_adamw_step(const asi_adamw_desc_t* d, const asi_adam
       (d->state_bits != 32 && d->state_bits != 8))
     return ASI_ERR_INVALID_ARG;
   const bool betas = d->beta1 >= 0 && d->beta1 < 1 && d->beta2 >= 0 && d->beta2 < 1;
-  const bool rates = d->weight_decay >= 0 && std::isfinite(d->weight_decay) && d->eps >= 1e-16 && std::isfinite((float)d->eps) &&
-                     (d->lr_dev || (d->lr >= 0 && std::isfinite(d->lr)));
+  const bool rates = d->weight_decay >= 0 && std::isfinite((float)d->weight_decay) && d->eps >= 1e-16 && std::isfinite((float)d->eps) &&
+                     (d->lr_dev || (d->lr >= 0 && std::isfinite((float)d->lr)));
   if (!betas || !rates || (!d->step_dev && d->step < 1)) return ASI_ERR_INVALID_ARG;
   const size_t ew = d->weight_dtype == ASI_BF16 ? 2 : 4, eg = d->grad_dtype == ASI_BF16 ? 2 : 4, es = d->state_bits / 8;
   try {

@@ -991,12 +991,14 @@ size_t logit_bytes(const asi_logprob_desc_t* d) { return d->in_dtype == ASI_BF16
 
 bool off_element(const asi_logprob_desc_t* d, const void* p) { return (reinterpret_cast<uintptr_t>(p) & (logit_bytes(d) - 1)) != 0; }
 
-// dlogits is logits itself, row for row, or lies apart from it
+// dlogits is logits itself, row for row, or lies apart from it (between its rows, perhaps, where both have the same stride)
 asi_status_t check_grad(const asi_logprob_desc_t* d, const void* x, const void* dx) {
   if (!dx || off_element(d, dx) || d->ld_grad < d->vocab) return ASI_ERR_INVALID_ARG;
   if (d->ld_grad > INT64_MAX / 8 / std::max<int64_t>(d->rows, 1)) return ASI_ERR_INVALID_ARG;
   const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(dx);
   if (a == b) return d->ld_grad == d->ld || d->rows == 1 ? ASI_OK : ASI_ERR_INVALID_ARG;
+  const uintptr_t row = d->vocab * logit_bytes(d), stride = d->ld * logit_bytes(d), shift = (a < b ? b - a : a - b) % stride;
+  if (d->ld == d->ld_grad && shift >= row && stride - shift >= row) return ASI_OK;
   const uintptr_t na = ((d->rows - 1) * d->ld + d->vocab) * logit_bytes(d), nb = ((d->rows - 1) * d->ld_grad + d->vocab) * logit_bytes(d);
   return a < b + nb && b < a + na ? ASI_ERR_INVALID_ARG : ASI_OK;
 }

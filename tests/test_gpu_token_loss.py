@@ -272,6 +272,24 @@ def test_gradient_in_place(T, V, off, dt, form):
     assert torch.equal(x, other)
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("form", ["loss", "backward"])
+@pytest.mark.parametrize("T,V,gap", [(3, 50257, 0), (700, 1003, 1), (700, 8, 5)])
+def test_gradient_between_the_rows_of_the_logits(T, V, gap, dt, form):
+    x, y, _ = make(T, V, dt, 0, 0, seed=8)
+    alpha, beta = torch.randn(T, device="cuda"), torch.randn(T, device="cuda")
+    run = runner(T, V, dt)
+    both = torch.full((T, 2 * V + gap), 7.0, device="cuda", dtype=dt)
+    both[:, :V] = x
+    run.forward(both[:, :V], y)
+    other = torch.empty(T, 2 * V + gap, device="cuda", dtype=dt)
+    apart = other[:, V:2 * V]
+    getattr(run, form)(both[:, :V], y, alpha, beta, apart)
+    getattr(run, form)(both[:, :V], y, alpha, beta, both[:, V:2 * V])
+    assert torch.equal(both[:, V:2 * V], apart)
+    assert torch.equal(both[:, :V], x) and (both[:, 2 * V:] == 7).all()
+
+
 def test_gradient_against_differences():
     T, V, h = 4, 40, 0.02
     x, y, _ = make(T, V, torch.float32, seed=7, spread=1.0)

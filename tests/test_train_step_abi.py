@@ -82,6 +82,8 @@ def test_gradients_over_the_logits(B):
     assert grad(logprob(B), p[0] + 4 * 399) == (INVALID, INVALID)
     assert grad(logprob(B), p[8] + 1) == (INVALID, INVALID)
     assert grad(logprob(B, ld=120), p[0] + 4 * 100) == (INVALID, INVALID)
+    for shift in (99, 121, -99, 220 + 99, -220 - 99, 220):           # between its rows, and not quite
+        assert grad(logprob(B, ld=220, ld_grad=220), p[0] + 4 * shift) == (INVALID, INVALID)
 
 
 def test_empty_calls_do_nothing(B):
@@ -166,7 +168,7 @@ def tensors(B, entries):
     dict(weight_dtype=2), dict(grad_dtype=-1), dict(state_bits=16), dict(lr=-1e-9), dict(lr=math.nan), dict(lr=math.inf),
     dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=9e-17), dict(eps=math.inf), dict(eps=1e300),
     dict(weight_decay=-1.0), dict(weight_decay=math.inf), dict(step=0), dict(lr_dev=at(99) + 2), dict(step_dev=at(99) + 4),
-    dict(grad_scale=at(99) + 1),
+    dict(grad_scale=at(99) + 1), dict(lr=1e39), dict(weight_decay=1e39),
 ])
 def test_adamw_descriptors(B, bad):
     assert B.lib().asi_adamw_step(adamw(B, **bad), tensors(B, [{}]), 1, None) == INVALID
