@@ -104,8 +104,11 @@ __device__ __forceinline__ void load_shared_values(const float* p, float* f) {
     f[0] = __ldcg(p);
   }
 }
-// ---- lookup: blocks of tx x ty threads, ty rows side by side, VEC values a thread; kRows rows of a thread on their way at once
-// (16384 x 2048 bf16: 25 us, 5.3 TB/s; rows off 16 bytes 31 to 44).
+// ---- lookup: blocks of tx x ty threads, ty rows side by side; kRows rows of a thread on their way at once, by loads that no
+// condition holds up (beyond the row's end they read its last word again).  Where rows lie off 16 bytes words are narrow, and a
+// thread takes several, a block apart.  (16384 x 2048 bf16: 25 us, 5.3 TB/s.  8192 x 2048, 1878 and 1877 bf16: 11.5, 13.4 and
+// 17.4 us; with a word each and conditions 13.2, 16.1 and 23.5.)
+constexpr int words_of(int vec) { return vec >= 4 ? 1 : 4 / vec; }
 struct LookupArgs {
   const void* table;
   const int64_t* ids;
@@ -116,35 +119,42 @@ struct LookupArgs {
 };
 constexpr int kRows = 4;
 
-template <typename TT, typename TO, int VEC>
+template <typename TT, typename TO, int VEC, int W>
 __global__ void __launch_bounds__(kEmbThreads) k_embed(const __grid_constant__ LookupArgs p) {
   pdl_wait();
   pdl_launch_dependents();
   const int64_t t0 = (int64_t)blockIdx.x * blockDim.y * kRows + threadIdx.y;
-  int64_t id[kRows];
+  const TT* row[kRows];
+  float scale[kRows];                      // NaN for an id outside the vocabulary, whose row is read as row 0
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    const int64_t t = t0 + r * blockDim.y;
-    id[r] = t < p.T ? p.ids[t] : 0;
+    const int64_t t = t0 + r * blockDim.y, id = t < p.T ? p.ids[t] : 0;
+    const bool there = id >= 0 && id < p.V;
+    row[r] = static_cast<const TT*>(p.table) + (there ? id * p.D : 0);
+    scale[r] = there ? p.scale : NAN;
   }
-  for (int c = threadIdx.x; c < p.per_row; c += blockDim.x) {
-    float f[kRows][VEC];
+  constexpr int kTake = sizeof(TT) * VEC > 16 ? 16 / (int)sizeof(TT) : VEC;   // (a word has 16 bytes at most)
+  for (int c0 = threadIdx.x; c0 < p.per_row; c0 += W * blockDim.x) {
+    Word<TT, kTake> f[kRows][W][VEC / kTake];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      if (id[r] >= 0 && id[r] < p.V) {
-        load_values<TT, VEC>(static_cast<const TT*>(p.table) + id[r] * p.D + (int64_t)c * VEC, f[r]);
-      } else {
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[r][e] = NAN;
-      }
-    }
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < VEC / kTake; ++i) f[r][w][i].load(row[r] + (int64_t)min(c0 + w * (int)blockDim.x, p.per_row - 1) * VEC + i * kTake);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const int64_t t = t0 + r * blockDim.y;
       if (t >= p.T) break;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) f[r][e] *= p.scale;
-      store_values<TO, VEC>(static_cast<TO*>(p.out) + t * p.D + (int64_t)c * VEC, f[r]);
+      for (int w = 0; w < W; ++w) {
+        const int c = c0 + w * blockDim.x;
+        if (c >= p.per_row) break;
+        float o[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] = f[r][w][e / kTake].value(e % kTake) * scale[r];
+        store_values<TO, VEC>(static_cast<TO*>(p.out) + t * p.D + (int64_t)c * VEC, o);
+      }
     }
   }
 }
@@ -676,14 +686,14 @@ template <typename TT, typename TO>
 cudaError_t launch_lookup(LookupArgs a, int vec, cudaStream_t st) {
   a.per_row = (int)(a.D / vec);
   unsigned tx = 32;
-  while (tx < (unsigned)kEmbThreads && (int)tx < a.per_row) tx *= 2;
+  while (tx < (unsigned)kEmbThreads && (int)tx * words_of(vec) < a.per_row) tx *= 2;
   const unsigned ty = kEmbThreads / tx;
   const dim3 grid((unsigned)((a.T + (int64_t)ty * kRows - 1) / ((int64_t)ty * kRows))), block(tx, ty);
   switch (vec) {
-    case 8: return launch_pdl(k_embed<TT, TO, 8>, grid, block, 0, st, a);
-    case 4: return launch_pdl(k_embed<TT, TO, 4>, grid, block, 0, st, a);
-    case 2: return launch_pdl(k_embed<TT, TO, 2>, grid, block, 0, st, a);
-    default: return launch_pdl(k_embed<TT, TO, 1>, grid, block, 0, st, a);
+    case 8: return launch_pdl(k_embed<TT, TO, 8, words_of(8)>, grid, block, 0, st, a);
+    case 4: return launch_pdl(k_embed<TT, TO, 4, words_of(4)>, grid, block, 0, st, a);
+    case 2: return launch_pdl(k_embed<TT, TO, 2, words_of(2)>, grid, block, 0, st, a);
+    default: return launch_pdl(k_embed<TT, TO, 1, words_of(1)>, grid, block, 0, st, a);
   }
 }
 
