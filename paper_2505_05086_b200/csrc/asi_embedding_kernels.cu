@@ -554,19 +554,20 @@ __global__ void __launch_bounds__(kEmbThreads + 32, kSumCtas) k_embed_sum(const 
     }
     if (lane == 0) from[0] = first, to[0] = through ? last : c, from[1] = c, to[1] = last;
   } else if (col < p.D) {
-    // U rows in hand and the next U on their way
+    // U rows in hand and the next U on their way, without a condition for each: behind the last row it is read and added again,
+    // to a sum that nobody takes (14376 x 1877 bf16: 70 us with conditions, 58; 9973 x 770 fp32: 27 and 25)
     constexpr int kWordRegs = VEC * (int)sizeof(T) / 4, U = kWordRegs > kInFlight / 8 ? kInFlight / kWordRegs : 8;
     float acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-    const uint64_t ends = (uint64_t)end_bits[1] << 32 | end_bits[0];
+    const uint64_t ends = ((uint64_t)end_bits[1] << 32 | end_bits[0]) & (~0ull >> (64 - live));
     bool first_run = true;
     const T* src = static_cast<const T*>(p.dout) + col;
     Word<T, VEC> f[2][U];
     auto bring = [&](int i0, Word<T, VEC>* w) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (i0 + u < live) w[u].load(src + (int64_t)sp[i0 + u] * p.D);
+        w[u].load(src + (int64_t)sp[min(i0 + u, live - 1)] * p.D);
     };
     bring(0, f[0]);
 #pragma unroll 1
@@ -575,12 +576,11 @@ __global__ void __launch_bounds__(kEmbThreads + 32, kSumCtas) k_embed_sum(const 
       for (int h = 0; h < 2; ++h) {
         const int i0 = j0 + h * U;
         if (i0 >= live) break;
-        bring(i0 + U, f[h ^ 1]);
+        if (i0 + U < live) bring(i0 + U, f[h ^ 1]);
         const uint32_t here = (uint32_t)(ends >> i0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int i = i0 + u;
-          if (i >= live) break;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) acc[e] += f[h][u].value(e);
           if (!(here & (1u << u))) continue;
