@@ -388,8 +388,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant
   }
 }
 
-// The rows of dW that no token has, as zeros: most of the work of a large table (32000 x 2048: 43 us of 53).  Needs nothing of the sort and the sums before
-// it on the stream and runs beside them (each CTA marks the ids of its own rows first); it ends when they have ended.
+// The rows of dW that no token has, as zeros: most of the work of a large table (32000 x 2048: 43 us of 51).  Needs nothing of
+// the sort and the sums before it on the stream and runs beside them (each CTA marks the ids of its own rows first); it ends
+// when they have ended.
 constexpr int kClearThreads = 512;
 __global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_constant__ SortArgs p) {
   extern __shared__ uint32_t seen[];                                 // a bit for each row
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_const
 // ---- sums of runs
 constexpr int kMaxChunk = 64;
 constexpr int kZeroRows = 64;
-constexpr int kSumCtas = 3;                 // CTAs of an SM (tied table of 50257 x 770: 26 us, with four 28, with five 33)
+constexpr int kSumCtas = 3;                 // CTAs of an SM (tied table of 50257 x 770: 25 us, with two 32, with four 25 to 27)
 constexpr int kInFlight = 16;              // registers of a thread for rows in hand
 
 struct SumArgs {

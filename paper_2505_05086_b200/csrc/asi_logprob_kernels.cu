@@ -811,9 +811,9 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLoss8 ? 8 : kN == kLoss
   if (cl > 1) cluster_wait();
 }
 
-// ---- the gradient alone, from lse and entropy: a stream of 1024 granules a CTA (79 us at 4096 x 32000 bf16, floor 81).  p = exp(x - lse) is off by 2^-24 |lse|, which
-// is 2^-12 where |lse| is 4096: rows from there on (logits at a type's lowest value, say) sum up for themselves, in one CTA
-// (dx may be x, so nobody else of the row may have begun to write).
+// ---- the gradient alone, from lse and entropy: a stream of 1024 granules a CTA (79 us at 4096 x 32000 bf16, floor 81).
+// p = exp(x - lse) is off by 2^-24 |lse|, which is 2^-12 where |lse| is 4096: rows from there on (logits at a type's lowest
+// value, say) sum up for themselves, in one CTA (dx may be x, so nobody else of the row may have begun to write).
 constexpr float kFarLse = 4096.f;
 
 template <typename T>
