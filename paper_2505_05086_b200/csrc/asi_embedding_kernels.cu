@@ -310,7 +310,11 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const __grid_cons
 // counts and tokens travel through distributed shared memory.  (32000 ids: 10000 tokens take one CTA 29 us and eight 10.  Below
 // kFewTokens one CTA does it without the cluster's barriers; a whole accumulating call over 50257 x 768 with 8 tokens takes 7.5
 // us where eight CTAs take 9.9, with 1000 11.0 and 12.5, with 2000 as much either way.)
-template <int CL>
+// SMALL, up to three passes: a token travels as one word, sixteen bits of its key and its place.  Of a key with three digits
+// the lowest is dropped once the tokens are sorted by it, and read again at the end.  The scattered words are what the cluster
+// waits for (calls over 50257 x 770 with 9973 tokens 25.2 us with a store for the key and one for the place, 23.0 with the
+// word; 128256 x 770 29.6 and 28.1; 65536 tokens 126 and 115).
+template <int CL, bool SMALL>
 __global__ void __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant__ SortArgs p) {
   extern __shared__ uint32_t sort_mem[];
   const int tid = threadIdx.x;
@@ -344,8 +348,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant
       here = i + 1;
     }
   }
+  const int drop = SMALL && p.passes == 3 ? kDigit : 0;              // of the key, once the tokens are sorted by them
   for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * kDigit;
+    const int shift = pass * kDigit - (pass ? drop : 0);
     const uint32_t own = digit_ranks(key, here, items, shift, wh, rank);
     if constexpr (CL > 1) {
       if (pass == 0) cluster.barrier_wait();
@@ -372,19 +377,24 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_one(const __grid_constant
       if (i < here) {
         const uint32_t d = (key[i] >> shift) & (kBins - 1);
         const uint32_t to = start[d] + wh[warp][d] + rank[i];
-        *of(&skey[to & (seg - 1)], to >> p.seg) = key[i];
-        *of(&spos[to & (seg - 1)], to >> p.seg) = pos[i];
+        *of(&skey[to & (seg - 1)], to >> p.seg) = SMALL ? key[i] >> (pass ? 0 : drop) << 16 | pos[i] : key[i];
+        if (!SMALL) *of(&spos[to & (seg - 1)], to >> p.seg) = pos[i];
       }
     together();
     if (pass + 1 < p.passes) {
 #pragma unroll
       for (int i = 0; i < kItems; ++i)
-        if (i < here) key[i] = skey[base + i * 32], pos[i] = spos[base + i * 32];
+        if (i < here) {
+          const uint32_t w = skey[base + i * 32];
+          key[i] = SMALL ? w >> 16 : w;
+          pos[i] = SMALL ? (uint16_t)w : spos[base + i * 32];
+        }
     }
   }
   for (int i = tid; i < mine; i += kSortThreads) {
-    p.key_out[rank0 * seg + i] = skey[i];
-    p.pos_out[rank0 * seg + i] = spos[i];
+    const uint32_t w = skey[i], from = SMALL ? w & 0xffffu : spos[i];
+    p.key_out[rank0 * seg + i] = !SMALL ? w : drop ? id_key(p, p.ids[from]) : w >> 16;
+    p.pos_out[rank0 * seg + i] = from;
   }
 }
 
@@ -712,8 +722,10 @@ cudaError_t sort_tokens(SortArgs a, const Layout& l, int counters, char* w, int*
     while (l.T > (few ? 1 : kSortCluster) << a.seg) ++a.seg;
     const size_t smem = (size_t)6 << a.seg;
     *out = 0;
-    if (few) return launch_pdl(k_sort_one<1>, dim3(1), dim3(kSortThreads), smem, st, a);
-    cudaError_t e = smem > 16 << 10 ? opt_in_smem(reinterpret_cast<const void*>(k_sort_one<kSortCluster>), smem) : cudaSuccess;
+    const bool small = l.passes <= 3;
+    if (few) return launch_pdl(k_sort_one<1, false>, dim3(1), dim3(kSortThreads), smem, st, a);
+    const auto kernel = small ? k_sort_one<kSortCluster, true> : k_sort_one<kSortCluster, false>;
+    cudaError_t e = smem > 16 << 10 ? opt_in_smem(reinterpret_cast<const void*>(kernel), smem) : cudaSuccess;
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kSortCluster);
@@ -728,8 +740,7 @@ cudaError_t sort_tokens(SortArgs a, const Layout& l, int counters, char* w, int*
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_sort_one<kSortCluster>, a);
-    return e;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
   }
   cudaError_t e = cudaSuccess;
   for (int pass = 0; pass < l.passes && e == cudaSuccess; ++pass) {

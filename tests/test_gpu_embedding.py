@@ -54,7 +54,8 @@ def zipf(T, V, g):
 SIZES = [(1, 1, 1, 0), (5, 3, 7, 1), (300, 8, 64, 0), (300, 64, 129, 4), (1000, 770, 2048, 0), (255, 40, 4096, 0),
          (256, 40, 5000, 0), (32000, 64, 4097, 0), (1025, 2056, 900, 0), (70000, 24, 20000, 0), (3, 48, 30000, 0),
          (1 << 21, 4, 3000, 0), (2000, 6000, 50, 0), (40000, 33, 9973, 3),
-         (600, 20, 1024, 0), (600, 20, 1025, 0), (70000, 5, 1023, 1)]
+         (600, 20, 1024, 0), (600, 20, 1025, 0), (70000, 5, 1023, 1),
+         (1 << 24, 1, 5000, 0), (65535, 12, 6000, 0), (65536, 12, 6000, 0), ((1 << 24) - 1, 2, 50000, 0), (70000, 3, 65536, 0)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF])
