@@ -130,15 +130,42 @@ _DTYPES = {torch.float32: ASI_F32, torch.bfloat16: ASI_BF16}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _call(device, stream, function, *args):
-    """function(*args, handle) with `device` current, on `stream` or that device's current stream."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"a stream of {device} is needed, got one of {stream.device}")
-    if torch.cuda.current_device() == device.index:
-        function(*args, _raw_stream(device.index) if stream is None else stream.cuda_stream)
-    else:
+class _Runner:
+    """Calls on a stream, and buffers of the runner's own (`_own`) that any stream of its device may use: one that was not
+    current when they were made waits for what was queued there (what filled them, and what used their memory before), and
+    the allocator learns of it, so that the memory of a runner that is dropped is not given away beneath it."""
+
+    def _made(self, device):
+        """To be called where the buffers have been made, on the device's current stream."""
         with torch.cuda.device(device):
-            function(*args, _raw_stream(device.index) if stream is None else stream.cuda_stream)
+            self._captured = torch.cuda.is_current_stream_capturing()
+            self._ready = torch.cuda.current_stream().record_event()
+        self._streams = {_raw_stream(device.index)}
+
+    def _own(self):
+        return ()
+
+    def _lend(self, stream):
+        for x in self._own():
+            x.record_stream(stream)
+        with torch.cuda.stream(stream):
+            # (a capture cannot wait for what is not part of it; the graph's user has it behind them)
+            if torch.cuda.is_current_stream_capturing() == self._captured:
+                stream.wait_event(self._ready)
+                self._streams.add(stream.cuda_stream)
+
+    def _call(self, stream, function, *args):
+        """function(*args, handle) with the runner's device current, on `stream` or that device's current stream."""
+        device = self.device
+        if stream is not None and stream.device != device:
+            raise ValueError(f"a stream of {device} is needed, got one of {stream.device}")
+        if torch.cuda.current_device() != device.index:
+            with torch.cuda.device(device):
+                return self._call(stream, function, *args)
+        handle = _raw_stream(device.index) if stream is None else stream.cuda_stream
+        if handle not in self._streams:
+            self._lend(torch.cuda.current_stream(device) if stream is None else stream)
+        function(*args, handle)
 
 
 def _cuda_device(device):
@@ -158,7 +185,7 @@ def _take(name, x, shape, dtype, device):
     return x.data_ptr()
 
 
-class LogprobRunner:
+class LogprobRunner(_Runner):
     """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
     lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
     the others as they were.  backward() reads lse and entropy of the last forward() or loss()."""
@@ -174,6 +201,10 @@ class LogprobRunner:
         self.top_ids = torch.zeros(self.rows, self.top_k, dtype=torch.int64, device=self.device) if self.top_k else None
         self._stats = tuple(x.data_ptr() for x in (self.logp, self.entropy, self.lse))
         self._top = (self.top_logp.data_ptr(), self.top_ids.data_ptr()) if self.top_k else (0, 0)
+        self._made(self.device)
+
+    def _own(self):
+        return [x for x in (self.logp, self.entropy, self.lse, self.top_logp, self.top_ids) if x is not None]
 
     def _rows_of(self, name, x):
         """Rows and row stride of logits or their gradient."""
@@ -200,24 +231,24 @@ class LogprobRunner:
 
     def forward(self, logits, targets, stream=None):
         _, y = self._inputs(logits, targets)
-        _call(self.device, stream, binding.token_logprobs, self.desc, logits.data_ptr(), y, *self._stats, *self._top)
+        self._call(stream, binding.token_logprobs, self.desc, logits.data_ptr(), y, *self._stats, *self._top)
 
     def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward()
         left; dentropy may be None, and dlogits may be logits itself."""
         n, y = self._inputs(logits, targets, dlogits)
         _, entropy, lse = self._stats
-        _call(self.device, stream, binding.token_logprobs_grad, self.desc, logits.data_ptr(), y, lse, entropy,
-              *self._weights(n, dlogp, dentropy), dlogits.data_ptr())
+        self._call(stream, binding.token_logprobs_grad, self.desc, logits.data_ptr(), y, lse, entropy,
+                   *self._weights(n, dlogp, dentropy), dlogits.data_ptr())
 
     def loss(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """forward() without the top entries, and backward(), in one pass over the logits."""
         n, y = self._inputs(logits, targets, dlogits)
-        _call(self.device, stream, binding.token_loss, self.desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
-              *self._stats, dlogits.data_ptr())
+        self._call(stream, binding.token_loss, self.desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
+                   *self._stats, dlogits.data_ptr())
 
 
-class EmbeddingRunner:
+class EmbeddingRunner(_Runner):
     """Embedding lookup of up to `tokens` tokens and its weight gradient, with the workspace of the latter: calls of wgrad() (and
     graphs captured from them) that may run at the same time need a runner each."""
 
@@ -228,7 +259,12 @@ class EmbeddingRunner:
         self.table_dtype = torch.bfloat16 if bf16_table else torch.float32
         self.desc = EmbeddingDesc(_DTYPES[self.table_dtype], _DTYPES[self.in_dtype], self.vocab, self.dim, self.tokens,
                                   -1 if padding_idx is None else int(padding_idx), float(scale))
-        self.ws = None                     # allocated with the first wgrad()
+        # as large as the longest batch needs
+        self.ws = torch.empty(binding.embedding_wgrad_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
+        self._made(self.device)
+
+    def _own(self):
+        return (self.ws,)
 
     def _ids(self, ids):
         n = ids.numel()
@@ -242,22 +278,18 @@ class EmbeddingRunner:
         shape = self._ids(ids)
         w = _take("table", table, (self.vocab, self.dim), self.table_dtype, self.device)
         o = _take("out", out, shape, self.in_dtype, self.device)
-        _call(self.device, stream, binding.embedding_forward, self.desc, w, ids.data_ptr(), o)
+        self._call(stream, binding.embedding_forward, self.desc, w, ids.data_ptr(), o)
 
     def wgrad(self, ids, dOut, dW, accumulate=False, stream=None):
         """dW (fp32 [vocab, dim]) overwritten with, or increased by, the gradient."""
         shape = self._ids(ids)
         d = _take("dOut", dOut, shape, self.in_dtype, self.device)
         w = _take("dW", dW, (self.vocab, self.dim), torch.float32, self.device)
-        if self.ws is None:                # as large as the longest batch needs
-            n, self.desc.tokens = self.desc.tokens, self.tokens
-            self.ws = torch.empty(binding.embedding_wgrad_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
-            self.desc.tokens = n
-        _call(self.device, stream, binding.embedding_wgrad, self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(),
-              self.ws.numel())
+        self._call(stream, binding.embedding_wgrad, self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(),
+                   self.ws.numel())
 
 
-class AdamWRunner:
+class AdamWRunner(_Runner):
     """AdamW over a list of weights and their gradient buffers (the dW of layer runners, for example): holds the states and
     steps all tensors in one call.  States may be given (to resume); the 8-bit ones are float8_e4m3fn with one
     float8_e8m0fnu (or uint8) scale for each ASI_ADAMW_BLOCK elements of a tensor.  `copies` (bf16) receive the new weights."""
@@ -274,13 +306,16 @@ class AdamWRunner:
             raise ValueError("weights and gradients are fp32 or bf16")
         sd = torch.float8_e4m3fn if self.bits8 else torch.float32
 
+        new = []
+
         def states(given, dtype, per, fill):
             if given is not None:
                 return list(given)
-            new = [torch.empty(-(-w.numel() // per), dtype=dtype, device=self.device) for w in self.weights]
-            for x in new:
+            made = [torch.empty(-(-w.numel() // per), dtype=dtype, device=self.device) for w in self.weights]
+            for x in made:
                 x.view(torch.uint8).fill_(fill)
-            return new
+            new.extend(made)
+            return made
 
         self.exp_avg, self.exp_avg_sq = states(exp_avg, sd, 1, 0), states(exp_avg_sq, sd, 1, 0)
         scales = (states(s, torch.float8_e8m0fnu, ASI_ADAMW_BLOCK, 127) if self.bits8 else [None] * len(self.weights)
@@ -308,6 +343,11 @@ class AdamWRunner:
                 e.exp_avg_scale, e.exp_avg_sq_scale = at("exp_avg_scale", ms, *scale), at("exp_avg_sq_scale", vs, *scale)
             e.copy = at("copy", c, n, torch.bfloat16) if c is not None else None
             e.n = n
+        self._states = new
+        self._made(self.device)
+
+    def _own(self):
+        return self._states                # (those that were given are their owner's)
 
     def step(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=None, grad_scale=None, stream=None):
         """One step.  `step` counts from 1 (default: one more than at the call before).  lr (fp32) and step (int64) may be
@@ -325,6 +365,6 @@ class AdamWRunner:
             d.step = self.t + 1 if step is None else int(step)
         if grad_scale is not None:
             d.grad_scale = _take("grad_scale", grad_scale.reshape(1), (1,), torch.float32, self.device)
-        _call(self.device, stream, binding.adamw_step, d, self._tensors, len(self.weights))
+        self._call(stream, binding.adamw_step, d, self._tensors, len(self.weights))
         if not isinstance(step, torch.Tensor):
             self.t = d.step

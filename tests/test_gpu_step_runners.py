@@ -1,0 +1,71 @@
+"""Runners of the token loss, embedding and AdamW on streams other than the one their buffers were made on."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def busy(block, fills=50):
+    """Queues work on the current stream that goes on writing to `block`."""
+    big = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for _ in range(fills):
+        big.fill_(1)
+        block.fill_(255)
+    return big
+
+
+def test_first_gradient_on_another_stream_while_the_memory_is_still_in_use():
+    """The workspace lies where the current stream still writes: the other stream waits for it."""
+    from paper_2505_05086_b200.runner import EmbeddingRunner
+    V, D, T = 900, 64, 3000
+    g = torch.Generator(device="cuda").manual_seed(0)
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda")
+    d = torch.randint(-8, 9, (T, D), generator=g, device="cuda").float()
+    want = torch.zeros(V, D, device="cuda").index_add_(0, ids, d)
+    dw = torch.empty(V, D, device="cuda")
+    size = EmbeddingRunner(V, D, T).ws.numel()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        block = torch.empty(size, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        keep, at = busy(block), block.data_ptr()
+        del block
+        r = EmbeddingRunner(V, D, T)
+        assert r.ws.data_ptr() == at
+        r.wgrad(ids, d, dw, stream=side)
+        side.synchronize()
+        assert torch.equal(dw, want)
+        del r, keep
+
+
+def test_a_dropped_runner_keeps_its_memory_until_the_other_stream_is_done():
+    from paper_2505_05086_b200.runner import EmbeddingRunner
+    V, D, T = 900, 64, 3000
+    ids, d, dw = torch.zeros(T, dtype=torch.int64, device="cuda"), torch.ones(T, D, device="cuda"), torch.empty(V, D, device="cuda")
+    side = torch.cuda.Stream()
+    r = EmbeddingRunner(V, D, T)
+    size, at = r.ws.numel(), r.ws.data_ptr()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        keep = busy(torch.empty(16, dtype=torch.uint8, device="cuda"))
+        r.wgrad(ids, d, dw)
+    del r
+    other = torch.empty(size, dtype=torch.uint8, device="cuda")
+    assert other.data_ptr() != at
+    other.fill_(255)
+    side.synchronize()
+    assert (dw[0] == T).all() and (dw[1:] == 0).all()
+    del keep
+
+
+def test_results_on_another_stream_come_behind_what_cleared_them():
+    from paper_2505_05086_b200.runner import LogprobRunner
+    x, y = torch.zeros(64, 100, device="cuda"), torch.zeros(64, dtype=torch.int64, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    keep = busy(torch.empty(16, dtype=torch.uint8, device="cuda"))
+    r = LogprobRunner(64, 100)
+    r.forward(x, y, stream=side)
+    torch.cuda.synchronize()
+    assert (r.logp < -4).all() and (r.lse > 4).all()
+    del keep

@@ -1,0 +1,134 @@
+"""What the runners of the token loss, embedding and AdamW hand to the library, on the CPU: its calls are replaced by a recorder,
+streams and their events by stand-ins."""
+import pytest
+import torch
+
+
+class Stream:
+    """A stand-in for a stream: what it was made to wait for."""
+
+    def __init__(self, handle):
+        self.cuda_stream, self.device, self.waited = handle, torch.device("cpu"), []
+
+    def wait_event(self, event):
+        self.waited.append(event)
+
+    def record_event(self):
+        return f"event of {self.cuda_stream}"
+
+
+class World:
+    """The current stream, whether it is captured, and the calls that went out."""
+
+    def __init__(self):
+        self.home = self.now = Stream(0)
+        self.captured = set()
+        self.calls = []
+
+    def __getitem__(self, name):
+        return [args for n, args in self.calls if n == name]
+
+
+class On:
+    def __init__(self, world, stream):
+        self.world, self.stream = world, stream
+
+    def __enter__(self):
+        self.before, self.world.now = self.world.now, self.stream or self.world.now
+
+    def __exit__(self, *_):
+        self.world.now = self.before
+
+
+@pytest.fixture()
+def world(monkeypatch):
+    from paper_2505_05086_b200 import binding, build, runner
+    build.build()
+    w = World()
+    monkeypatch.setattr(runner, "_cuda_device", lambda d: torch.device("cpu"))
+    monkeypatch.setattr(runner, "_raw_stream", lambda index: w.now.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: On(w, None))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: On(w, s))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: w.now)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: w.now.cuda_stream in w.captured)
+
+    def recorder(name):
+        return lambda *args: w.calls.append((name, args))
+
+    for name in ("token_logprobs", "token_logprobs_grad", "token_loss", "embedding_forward", "embedding_wgrad", "adamw_step"):
+        monkeypatch.setattr(binding, name, recorder(name))
+    return w
+
+
+class Buffer:
+    """A stand-in for a buffer on the device: which streams the allocator was told of."""
+
+    def __init__(self, like):
+        self.like, self.told = like, []
+
+    def record_stream(self, stream):
+        self.told.append(stream.cuda_stream)
+
+    def data_ptr(self):
+        return self.like.data_ptr()
+
+    def numel(self):
+        return self.like.numel()
+
+
+# ---- buffers and streams
+
+def embedding(**kw):
+    from paper_2505_05086_b200.runner import EmbeddingRunner
+    return EmbeddingRunner(50, 8, 6, **kw)
+
+
+def test_the_embedding_has_its_workspace_from_the_start(world):
+    """Made within a call, it would come from the current stream's memory, or from that of a graph that is being captured."""
+    from paper_2505_05086_b200 import binding
+    r = embedding()
+    assert r.ws is not None and r.ws.numel() == binding.embedding_wgrad_ws_bytes(binding.EmbeddingDesc(0, 0, 50, 8, 6, -1, 1.0)) > 0
+    r.ws = ws = Buffer(r.ws)
+    r.wgrad(torch.zeros(6, dtype=torch.int64), torch.zeros(6, 8), torch.zeros(50, 8), stream=Stream(7))
+    assert r.ws is ws and world["embedding_wgrad"][0][5:7] == (ws.data_ptr(), ws.numel())
+
+
+def test_another_stream_waits_for_the_buffers_and_the_allocator_learns_of_it(world):
+    r = embedding()
+    r.ws = Buffer(r.ws)
+    ids, d, dw = torch.zeros(6, dtype=torch.int64), torch.zeros(6, 8), torch.zeros(50, 8)
+    r.wgrad(ids, d, dw)
+    assert r.ws.told == [] and world.home.waited == []               # the stream they were made on
+    side = Stream(7)
+    for _ in range(3):
+        r.wgrad(ids, d, dw, stream=side)
+    assert r.ws.told == [7] and side.waited == ["event of 0"]
+    world.now = other = Stream(9)                                    # the current one, without an argument
+    r.wgrad(ids, d, dw)
+    assert r.ws.told == [7, 9] and other.waited == ["event of 0"]
+    assert [c[-1] for c in world["embedding_wgrad"]] == [0, 7, 7, 7, 9]
+
+
+def test_a_capture_does_not_wait_for_what_is_outside_it(world):
+    r = embedding()
+    r.ws = Buffer(r.ws)
+    ids, d, dw = torch.zeros(6, dtype=torch.int64), torch.zeros(6, 8), torch.zeros(50, 8)
+    side = Stream(7)
+    world.captured.add(7)
+    r.wgrad(ids, d, dw, stream=side)
+    assert r.ws.told and not side.waited
+    world.captured.clear()
+    r.wgrad(ids, d, dw, stream=side)
+    assert side.waited == ["event of 0"]
+
+
+def test_results_and_states_are_lent_too(world):
+    from paper_2505_05086_b200.runner import AdamWRunner, LogprobRunner
+    r = LogprobRunner(4, 10, top_k=2)
+    assert {id(x) for x in r._own()} == {id(x) for x in (r.logp, r.entropy, r.lse, r.top_logp, r.top_ids)}
+    a = AdamWRunner([torch.zeros(300)], [torch.zeros(300)], bits8=True)
+    assert {x.data_ptr() for x in a._own()} == {x[0].data_ptr() for x in (a.exp_avg, a.exp_avg_sq, a.exp_avg_scale, a.exp_avg_sq_scale)}
+    given = [torch.zeros(300)]
+    a = AdamWRunner([torch.zeros(300)], [torch.zeros(300)], exp_avg=given)
+    assert [x.data_ptr() for x in a._own()] == [a.exp_avg_sq[0].data_ptr()]
