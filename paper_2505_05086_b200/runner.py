@@ -2,6 +2,8 @@
 does all the arithmetic."""
 from __future__ import annotations
 
+import threading
+
 import numpy as np
 import torch
 
@@ -130,6 +132,13 @@ _DTYPES = {torch.float32: ASI_F32, torch.bfloat16: ASI_BF16}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+class _Descriptor(threading.local):
+    """A descriptor for each thread: the library reads it while other threads may prepare calls of theirs."""
+
+    def __init__(self, first):
+        self.desc = type(first).from_buffer_copy(first)
+
+
 class _Runner:
     """Calls on a stream, and buffers of the runner's own (`_own`) that any stream of its device may use: one that was not
     current when they were made waits for what was queued there (what filled them, and what used their memory before), and
@@ -141,6 +150,10 @@ class _Runner:
             self._captured = torch.cuda.is_current_stream_capturing()
             self._ready = torch.cuda.current_stream().record_event()
         self._streams = {_raw_stream(device.index)}
+
+    @property
+    def desc(self):
+        return self._descriptor.desc
 
     def _own(self):
         return ()
@@ -188,13 +201,15 @@ def _take(name, x, shape, dtype, device):
 class LogprobRunner(_Runner):
     """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
     lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
-    the others as they were.  backward() reads lse and entropy of the last forward() or loss()."""
+    the others as they were.  backward() reads lse and entropy of the last forward() or loss().  Calls that may run at the
+    same time share these results: they need a runner each."""
 
     def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
         self.device = _cuda_device(device)
         self.rows, self.vocab, self.top_k = int(rows), int(vocab), int(top_k)
         self.in_dtype = torch.bfloat16 if bf16 else torch.float32
-        self.desc = LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index), float(scale))
+        self._descriptor = _Descriptor(LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index),
+                                                   float(scale)))
         f32 = dict(dtype=torch.float32, device=self.device)
         self.logp, self.entropy, self.lse = (torch.zeros(self.rows, **f32) for _ in range(3))
         self.top_logp = torch.zeros(self.rows, self.top_k, **f32) if self.top_k else None
@@ -216,49 +231,49 @@ class LogprobRunner(_Runner):
                          f"contiguous, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
 
     def _inputs(self, logits, targets, dlogits=None):
-        d = self.desc
+        d = self._descriptor.desc
         n, ld = self._rows_of("logits", logits)
         d.rows, d.ld, d.ld_grad = n, ld, ld
         if dlogits is not None:
             m, d.ld_grad = self._rows_of("dlogits", dlogits)
             if m != n:
                 raise ValueError(f"dlogits: {n} rows are needed, got {m}")
-        return n, _take("targets", targets, (n,), torch.int64, self.device)
+        return d, n, _take("targets", targets, (n,), torch.int64, self.device)
 
     def _weights(self, n, dlogp, dentropy):
         return (_take("dlogp", dlogp, (n,), torch.float32, self.device),
                 _take("dentropy", dentropy, (n,), torch.float32, self.device) if dentropy is not None else 0)
 
     def forward(self, logits, targets, stream=None):
-        _, y = self._inputs(logits, targets)
-        self._call(stream, binding.token_logprobs, self.desc, logits.data_ptr(), y, *self._stats, *self._top)
+        desc, _, y = self._inputs(logits, targets)
+        self._call(stream, binding.token_logprobs, desc, logits.data_ptr(), y, *self._stats, *self._top)
 
     def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward()
         left; dentropy may be None, and dlogits may be logits itself."""
-        n, y = self._inputs(logits, targets, dlogits)
+        desc, n, y = self._inputs(logits, targets, dlogits)
         _, entropy, lse = self._stats
-        self._call(stream, binding.token_logprobs_grad, self.desc, logits.data_ptr(), y, lse, entropy,
+        self._call(stream, binding.token_logprobs_grad, desc, logits.data_ptr(), y, lse, entropy,
                    *self._weights(n, dlogp, dentropy), dlogits.data_ptr())
 
     def loss(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """forward() without the top entries, and backward(), in one pass over the logits."""
-        n, y = self._inputs(logits, targets, dlogits)
-        self._call(stream, binding.token_loss, self.desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
+        desc, n, y = self._inputs(logits, targets, dlogits)
+        self._call(stream, binding.token_loss, desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
                    *self._stats, dlogits.data_ptr())
 
 
 class EmbeddingRunner(_Runner):
     """Embedding lookup of up to `tokens` tokens and its weight gradient, with the workspace of the latter: calls of wgrad() (and
-    graphs captured from them) that may run at the same time need a runner each."""
+    graphs captured from them) that may run at the same time need a runner each; threads may share one for forward()."""
 
     def __init__(self, vocab, dim, tokens, bf16=False, bf16_table=False, scale=1.0, padding_idx=None, device="cuda:0"):
         self.device = _cuda_device(device)
         self.vocab, self.dim, self.tokens = int(vocab), int(dim), int(tokens)
         self.in_dtype = torch.bfloat16 if bf16 else torch.float32
         self.table_dtype = torch.bfloat16 if bf16_table else torch.float32
-        self.desc = EmbeddingDesc(_DTYPES[self.table_dtype], _DTYPES[self.in_dtype], self.vocab, self.dim, self.tokens,
-                                  -1 if padding_idx is None else int(padding_idx), float(scale))
+        self._descriptor = _Descriptor(EmbeddingDesc(_DTYPES[self.table_dtype], _DTYPES[self.in_dtype], self.vocab, self.dim,
+                                                     self.tokens, -1 if padding_idx is None else int(padding_idx), float(scale)))
         # as large as the longest batch needs
         self.ws = torch.empty(binding.embedding_wgrad_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
         self._made(self.device)
@@ -271,21 +286,22 @@ class EmbeddingRunner(_Runner):
         if ids.dtype != torch.int64 or ids.device != self.device or not ids.is_contiguous() or n > self.tokens:
             raise ValueError(f"ids: a contiguous int64 tensor of up to {self.tokens} tokens on {self.device} is needed, got "
                              f"{ids.dtype} {tuple(ids.shape)} on {ids.device}")
-        self.desc.tokens = n
-        return (*ids.shape, self.dim)
+        desc = self._descriptor.desc
+        desc.tokens = n
+        return desc, (*ids.shape, self.dim)
 
     def forward(self, table, ids, out, stream=None):
-        shape = self._ids(ids)
+        desc, shape = self._ids(ids)
         w = _take("table", table, (self.vocab, self.dim), self.table_dtype, self.device)
         o = _take("out", out, shape, self.in_dtype, self.device)
-        self._call(stream, binding.embedding_forward, self.desc, w, ids.data_ptr(), o)
+        self._call(stream, binding.embedding_forward, desc, w, ids.data_ptr(), o)
 
     def wgrad(self, ids, dOut, dW, accumulate=False, stream=None):
         """dW (fp32 [vocab, dim]) overwritten with, or increased by, the gradient."""
-        shape = self._ids(ids)
+        desc, shape = self._ids(ids)
         d = _take("dOut", dOut, shape, self.in_dtype, self.device)
         w = _take("dW", dW, (self.vocab, self.dim), torch.float32, self.device)
-        self._call(stream, binding.embedding_wgrad, self.desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(),
+        self._call(stream, binding.embedding_wgrad, desc, ids.data_ptr(), d, w, accumulate, self.ws.data_ptr(),
                    self.ws.numel())
 
 
@@ -322,7 +338,8 @@ class AdamWRunner(_Runner):
                   for s in (exp_avg_scale, exp_avg_sq_scale))
         self.exp_avg_scale, self.exp_avg_sq_scale = scales
         self.copies = list(copies) if copies is not None else [None] * len(self.weights)
-        self.desc = AdamwDesc(weight_dtype=_DTYPES[wd], grad_dtype=_DTYPES[gd], state_bits=8 if self.bits8 else 32)
+        self._descriptor = _Descriptor(AdamwDesc(weight_dtype=_DTYPES[wd], grad_dtype=_DTYPES[gd],
+                                                 state_bits=8 if self.bits8 else 32))
         self._tensors = (AdamwTensor * len(self.weights))()
 
         def at(name, x, n, *dtypes):
@@ -352,7 +369,7 @@ class AdamWRunner(_Runner):
     def step(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=None, grad_scale=None, stream=None):
         """One step.  `step` counts from 1 (default: one more than at the call before).  lr (fp32) and step (int64) may be
         one-element device tensors, so that a captured graph reads new values; grad_scale (fp32) is one if given."""
-        d = self.desc
+        d = self._descriptor.desc
         d.beta1, d.beta2, d.eps, d.weight_decay = beta1, beta2, eps, weight_decay
         d.lr_dev = d.step_dev = d.grad_scale = None
         if isinstance(lr, torch.Tensor):

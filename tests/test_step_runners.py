@@ -1,5 +1,8 @@
 """What the runners of the token loss, embedding and AdamW hand to the library, on the CPU: its calls are replaced by a recorder,
 streams and their events by stand-ins."""
+import sys
+import threading
+
 import pytest
 import torch
 
@@ -132,3 +135,60 @@ def test_results_and_states_are_lent_too(world):
     given = [torch.zeros(300)]
     a = AdamWRunner([torch.zeros(300)], [torch.zeros(300)], exp_avg=given)
     assert [x.data_ptr() for x in a._own()] == [a.exp_avg_sq[0].data_ptr()]
+
+
+# ---- threads
+
+@pytest.fixture()
+def impatient():
+    before = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    yield
+    sys.setswitchinterval(before)
+
+
+def side_by_side(*jobs, times=10000):
+    def repeat(job):
+        for _ in range(times):
+            job()
+    threads = [threading.Thread(target=repeat, args=(job,)) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+
+
+def test_threads_that_share_an_embedding_send_their_own_number_of_tokens(world, impatient, monkeypatch):
+    from paper_2505_05086_b200 import binding
+    from paper_2505_05086_b200.runner import EmbeddingRunner
+    r = EmbeddingRunner(50, 8, 64)
+    table, wrong = torch.zeros(50, 8), []
+    batches = {n: (torch.zeros(n, dtype=torch.int64), torch.zeros(n, 8)) for n in (3, 64)}
+    tokens = {ids.data_ptr(): n for n, (ids, _) in batches.items()}
+
+    def call(desc, table, ids, out, stream):
+        if desc.tokens != tokens[ids]:
+            wrong.append(desc.tokens)
+
+    monkeypatch.setattr(binding, "embedding_forward", call)
+    side_by_side(*(lambda ids=ids, out=out: r.forward(table, ids, out) for ids, out in batches.values()))
+    assert not wrong
+
+
+def test_threads_that_share_a_token_loss_send_their_own_rows(world, impatient, monkeypatch):
+    from paper_2505_05086_b200 import binding
+    from paper_2505_05086_b200.runner import LogprobRunner
+    r, wrong, rows = LogprobRunner(64, 10), [], {}
+
+    def call(desc, logits, *_):
+        if (desc.rows, desc.ld) != rows[logits]:
+            wrong.append((desc.rows, desc.ld))
+
+    monkeypatch.setattr(binding, "token_logprobs", call)
+    jobs = []
+    for n, ld in ((3, 10), (64, 17)):
+        x, y = torch.zeros(n, ld)[:, :10], torch.zeros(n, dtype=torch.int64)
+        rows[x.data_ptr()] = (n, ld)
+        jobs.append(lambda x=x, y=y: r.forward(x, y))
+    side_by_side(*jobs)
+    assert not wrong
