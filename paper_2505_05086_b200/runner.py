@@ -198,11 +198,25 @@ def _take(name, x, shape, dtype, device):
     return x.data_ptr()
 
 
+_address = torch.Tensor.data_ptr
+
+
+def _result(name):
+    """A result buffer as an attribute; another one may take its place."""
+    def put(self, x):
+        self._bind({**self._results, name: x})
+
+    return property(lambda self: self._results[name], put)
+
+
 class LogprobRunner(_Runner):
     """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
     lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
-    the others as they were.  backward() reads lse and entropy of the last forward() or loss().  Calls that may run at the
-    same time share these results: they need a runner each."""
+    the others as they were.  backward() reads lse and entropy of the last forward() or loss(), or those that it is given.
+    Another contiguous buffer may be assigned to each result.  Calls that may run at the same time share these results: they
+    need a runner each."""
+
+    logp, entropy, lse, top_logp, top_ids = map(_result, ("logp", "entropy", "lse", "top_logp", "top_ids"))
 
     def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
         self.device = _cuda_device(device)
@@ -210,16 +224,45 @@ class LogprobRunner(_Runner):
         self.in_dtype = torch.bfloat16 if bf16 else torch.float32
         self._descriptor = _Descriptor(LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index),
                                                    float(scale)))
-        f32 = dict(dtype=torch.float32, device=self.device)
-        self.logp, self.entropy, self.lse = (torch.zeros(self.rows, **f32) for _ in range(3))
-        self.top_logp = torch.zeros(self.rows, self.top_k, **f32) if self.top_k else None
-        self.top_ids = torch.zeros(self.rows, self.top_k, dtype=torch.int64, device=self.device) if self.top_k else None
-        self._stats = tuple(x.data_ptr() for x in (self.logp, self.entropy, self.lse))
-        self._top = (self.top_logp.data_ptr(), self.top_ids.data_ptr()) if self.top_k else (0, 0)
+        self._bind({name: torch.zeros(self.rows, *more, dtype=dtype, device=self.device) if 0 not in more else None
+                    for name, more, dtype in self._layout()})
         self._made(self.device)
 
+    def _layout(self):
+        """Name, sizes behind the rows and type of each result, in the order of the library's arguments."""
+        return [(name, (), torch.float32) for name in ("logp", "entropy", "lse")] + [
+            ("top_logp", (self.top_k,), torch.float32), ("top_ids", (self.top_k,), torch.int64)]
+
+    def _bind(self, results):
+        """Takes buffers for the results, checked, and notes where they lie and for how many rows."""
+        at, rows = {}, {}
+        for name, more, dtype in self._layout():
+            x = results[name]
+            if 0 in more:
+                if x is not None:
+                    raise ValueError(f"{name}: there are no top entries")
+                at[name] = 0
+                continue
+            if (not isinstance(x, torch.Tensor) or x.dim() != 1 + len(more) or tuple(x.shape[1:]) != more or x.dtype != dtype
+                    or x.device != self.device or not x.is_contiguous() or (x.numel() and not x.data_ptr())):
+                raise ValueError(f"{name}: contiguous {dtype} rows of {more} on {self.device} are needed, got "
+                                 + (f"{x.dtype} {tuple(x.shape)} on {x.device}" if isinstance(x, torch.Tensor) else f"{x!r}"))
+            at[name], rows[name] = x.data_ptr(), x.shape[0]
+        self._results = dict(results)
+        self._buffers = tuple(x for x in self._results.values() if x is not None)
+        self._at = tuple(map(_address, self._buffers))
+        self._most, self._most_stats = min(rows.values()), min(rows["entropy"], rows["lse"])
+        self._stats, self._top = (at["logp"], at["entropy"], at["lse"]), (at["top_logp"], at["top_ids"])
+
+    def _outputs(self, n, stats=False):
+        """The results have room for n rows where they lie now (their memory may have been exchanged since the last call)."""
+        if tuple(map(_address, self._buffers)) != self._at:
+            self._bind(self._results)
+        if n > (self._most_stats if stats else self._most):
+            raise ValueError(f"results of {n} rows or more are needed, there are {[len(x) for x in self._buffers]}")
+
     def _own(self):
-        return [x for x in (self.logp, self.entropy, self.lse, self.top_logp, self.top_ids) if x is not None]
+        return self._buffers
 
     def _rows_of(self, name, x):
         """Rows and row stride of logits or their gradient."""
@@ -245,20 +288,30 @@ class LogprobRunner(_Runner):
                 _take("dentropy", dentropy, (n,), torch.float32, self.device) if dentropy is not None else 0)
 
     def forward(self, logits, targets, stream=None):
-        desc, _, y = self._inputs(logits, targets)
+        desc, n, y = self._inputs(logits, targets)
+        self._outputs(n)
         self._call(stream, binding.token_logprobs, desc, logits.data_ptr(), y, *self._stats, *self._top)
 
-    def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
-        """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward()
-        left; dentropy may be None, and dlogits may be logits itself."""
+    def backward(self, logits, targets, dlogp, dentropy, dlogits, stream=None, lse=None, entropy=None):
+        """The gradient of sum(dlogp * logp + dentropy * entropy) into dlogits, from the lse and entropy that forward() left, or
+        from those given (a value a row of logits: what forward() left for an earlier batch); dentropy may be None, and dlogits
+        may be logits itself."""
         desc, n, y = self._inputs(logits, targets, dlogits)
-        _, entropy, lse = self._stats
-        self._call(stream, binding.token_logprobs_grad, desc, logits.data_ptr(), y, lse, entropy,
+        if lse is None and entropy is None:
+            self._outputs(n, stats=True)
+            _, h, z = self._stats
+        elif lse is None or (entropy is None and dentropy is not None):
+            raise ValueError("lse and entropy (where dentropy is there) come together, from the same forward()")
+        else:
+            z = _take("lse", lse, (n,), torch.float32, self.device)
+            h = _take("entropy", entropy, (n,), torch.float32, self.device) if entropy is not None else 0
+        self._call(stream, binding.token_logprobs_grad, desc, logits.data_ptr(), y, z, h,
                    *self._weights(n, dlogp, dentropy), dlogits.data_ptr())
 
     def loss(self, logits, targets, dlogp, dentropy, dlogits, stream=None):
         """forward() without the top entries, and backward(), in one pass over the logits."""
         desc, n, y = self._inputs(logits, targets, dlogits)
+        self._outputs(n)
         self._call(stream, binding.token_loss, desc, logits.data_ptr(), y, *self._weights(n, dlogp, dentropy),
                    *self._stats, dlogits.data_ptr())
 

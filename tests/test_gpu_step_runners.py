@@ -69,3 +69,34 @@ def test_results_on_another_stream_come_behind_what_cleared_them():
     torch.cuda.synchronize()
     assert (r.logp < -4).all() and (r.lse > 4).all()
     del keep
+
+
+def test_gradients_of_micro_batches_from_their_own_forward_pass():
+    """Weights that come after several forward passes: each gradient goes by the lse and entropy of its own batch."""
+    from paper_2505_05086_b200.runner import LogprobRunner
+    T, V = 37, 500
+    g = torch.Generator(device="cuda").manual_seed(1)
+    batches = [(torch.randn(n, V, generator=g, device="cuda"), torch.randint(0, V, (n,), generator=g, device="cuda")) for n in (T, T - 8)]
+    w = torch.randn(T, generator=g, device="cuda")
+    want = []
+    for x, y in batches:
+        r, out = LogprobRunner(T, V), torch.empty_like(x)
+        r.forward(x, y)
+        r.backward(x, y, w[:len(y)], w[:len(y)], out)
+        want.append(out)
+    r, kept = LogprobRunner(T, V), []
+    for x, y in batches:
+        r.forward(x, y)
+        kept.append((r.lse[:len(y)].clone(), r.entropy[:len(y)].clone()))
+    for (x, y), (lse, entropy), right in zip(batches, kept, want):
+        n, out = len(y), torch.empty_like(x)
+        r.backward(x, y, w[:n], w[:n], out, lse=lse, entropy=entropy)
+        assert torch.equal(out, right)
+        r.lse, r.entropy = lse, entropy                              # or in place of the runner's own
+        out.zero_()
+        r.backward(x, y, w[:n], w[:n], out)
+        assert torch.equal(out, right)
+    fresh = torch.full((T,), 9.0, device="cuda")
+    r.lse, r.entropy = fresh, torch.empty(T, device="cuda")
+    r.forward(*batches[0])
+    assert torch.equal(fresh, kept[0][0])

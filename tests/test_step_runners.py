@@ -192,3 +192,78 @@ def test_threads_that_share_a_token_loss_send_their_own_rows(world, impatient, m
         jobs.append(lambda x=x, y=y: r.forward(x, y))
     side_by_side(*jobs)
     assert not wrong
+
+
+# ---- buffers that are exchanged
+
+def token_loss_calls(r, world, n=3):
+    x, y, w = torch.zeros(n, 10), torch.zeros(n, dtype=torch.int64), torch.ones(n)
+    world.calls.clear()
+    r.forward(x, y)
+    r.loss(x, y, w, None, torch.zeros(n, 10))
+    r.backward(x, y, w, w, torch.zeros(n, 10))
+    f, l, b = (args for _, args in world.calls)
+    return f[3:8], l[5:8], b[3:5]
+
+
+@pytest.mark.parametrize("top_k", [0, 2])
+def test_results_go_where_the_attributes_are(world, top_k):
+    from paper_2505_05086_b200.runner import LogprobRunner
+    r = LogprobRunner(4, 10, top_k=top_k)
+
+    def check():
+        tops = (r.top_logp.data_ptr(), r.top_ids.data_ptr()) if top_k else (0, 0)
+        stats = (r.logp.data_ptr(), r.entropy.data_ptr(), r.lse.data_ptr())
+        f, l, b = token_loss_calls(r, world)
+        assert f == stats + tops and l == stats and b == (stats[2], stats[1])
+
+    check()
+    r.lse, r.entropy = torch.zeros(4), torch.zeros(7)                # another buffer, a longer one
+    check()
+    r.logp.data = torch.zeros(4)                                     # other memory beneath the same tensor
+    check()
+    if top_k:
+        r.top_ids = torch.zeros(4, 2, dtype=torch.int64)
+        r.top_logp.set_(torch.zeros(4, 2))
+        check()
+
+
+def test_results_that_could_not_be_written_are_refused(world):
+    from paper_2505_05086_b200.runner import LogprobRunner
+    r = LogprobRunner(4, 10, top_k=2)
+    lse = r.lse
+    for bad in (None, torch.zeros(4, dtype=torch.float64), torch.zeros(8)[::2], torch.zeros(4, 1), [0.0] * 4):
+        with pytest.raises(ValueError):
+            r.lse = bad
+    with pytest.raises(ValueError):
+        r.top_ids = torch.zeros(4, 2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        r.top_logp = torch.zeros(4, 3)
+    assert r.lse is lse                                              # as it was
+    with pytest.raises(ValueError):
+        LogprobRunner(4, 10).top_ids = torch.zeros(4, 2, dtype=torch.int64)
+    r.lse = torch.zeros(2)                                           # of a batch of two
+    token_loss_calls(r, world, 2)
+    with pytest.raises(ValueError):
+        token_loss_calls(r, world, 3)
+    r.lse = torch.zeros(4)
+    r.lse.data = torch.zeros(4, dtype=torch.float64)
+    with pytest.raises(ValueError):
+        token_loss_calls(r, world, 3)
+    r = LogprobRunner(4, 10)
+    r.logp.untyped_storage().resize_(0)                              # no memory at all
+    with pytest.raises(ValueError):
+        token_loss_calls(r, world, 3)
+
+
+def test_gradient_from_the_results_of_an_earlier_batch(world):
+    from paper_2505_05086_b200.runner import LogprobRunner
+    r = LogprobRunner(4, 10)
+    x, y, w, out = torch.zeros(3, 10), torch.zeros(3, dtype=torch.int64), torch.ones(3), torch.zeros(3, 10)
+    lse, h = torch.zeros(3), torch.zeros(3)
+    r.backward(x, y, w, w, out, lse=lse, entropy=h)
+    r.backward(x, y, w, None, out, lse=lse)
+    assert [c[3:5] for c in world["token_logprobs_grad"]] == [(lse.data_ptr(), h.data_ptr()), (lse.data_ptr(), 0)]
+    for kw in (dict(entropy=h), dict(lse=lse), dict(lse=lse[:2], entropy=h), dict(lse=lse.double(), entropy=h)):
+        with pytest.raises(ValueError):
+            r.backward(x, y, w, w, out, **kw)
