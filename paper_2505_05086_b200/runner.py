@@ -361,50 +361,68 @@ class EmbeddingRunner(_Runner):
 class AdamWRunner(_Runner):
     """AdamW over a list of weights and their gradient buffers (the dW of layer runners, for example): holds the states and
     steps all tensors in one call.  States may be given (to resume); the 8-bit ones are float8_e4m3fn with one
-    float8_e8m0fnu (or uint8) scale for each ASI_ADAMW_BLOCK elements of a tensor.  `copies` (bf16) receive the new weights."""
+    float8_e8m0fnu (or uint8) scale for each ASI_ADAMW_BLOCK elements of a tensor.  `copies` (bf16) receive the new weights.
+
+    A weight, gradient or copy whose memory is exchanged (`w.data = ...`) is found by the next step().  The states stay where
+    they were when the runner was made: values are loaded with copy_(), other memory with rebind().  All of it is kept alive
+    until then."""
 
     def __init__(self, weights, grads, bits8=False, copies=None, exp_avg=None, exp_avg_sq=None, exp_avg_scale=None,
                  exp_avg_sq_scale=None):
-        self.weights, self.grads = list(weights), list(grads)
-        if not self.weights or len(self.grads) != len(self.weights):
+        weights, grads = tuple(weights), tuple(grads)
+        if not weights or len(grads) != len(weights):
             raise ValueError("one gradient for each of one or more weights is needed")
-        self.device = _cuda_device(self.weights[0].device)
+        self.device = _cuda_device(weights[0].device)
         self.bits8, self.t = bool(bits8), 0
-        wd, gd = self.weights[0].dtype, self.grads[0].dtype
+        wd, gd = weights[0].dtype, grads[0].dtype
         if wd not in _DTYPES or gd not in _DTYPES:
             raise ValueError("weights and gradients are fp32 or bf16")
         sd = torch.float8_e4m3fn if self.bits8 else torch.float32
-
         new = []
 
         def states(given, dtype, per, fill):
             if given is not None:
-                return list(given)
-            made = [torch.empty(-(-w.numel() // per), dtype=dtype, device=self.device) for w in self.weights]
+                return tuple(given)
+            made = [torch.empty(-(-w.numel() // per), dtype=dtype, device=self.device) for w in weights]
             for x in made:
                 x.view(torch.uint8).fill_(fill)
             new.extend(made)
-            return made
+            return tuple(made)
 
-        self.exp_avg, self.exp_avg_sq = states(exp_avg, sd, 1, 0), states(exp_avg_sq, sd, 1, 0)
-        scales = (states(s, torch.float8_e8m0fnu, ASI_ADAMW_BLOCK, 127) if self.bits8 else [None] * len(self.weights)
-                  for s in (exp_avg_scale, exp_avg_sq_scale))
-        self.exp_avg_scale, self.exp_avg_sq_scale = scales
-        self.copies = list(copies) if copies is not None else [None] * len(self.weights)
+        none = (None,) * len(weights)
+        self._tensors = dict(weights=weights, grads=grads, exp_avg=states(exp_avg, sd, 1, 0), exp_avg_sq=states(exp_avg_sq, sd, 1, 0))
+        for name, given in (("exp_avg_scale", exp_avg_scale), ("exp_avg_sq_scale", exp_avg_sq_scale)):
+            self._tensors[name] = states(given, torch.float8_e8m0fnu, ASI_ADAMW_BLOCK, 127) if self.bits8 else none
+        self._tensors["copies"] = tuple(copies) if copies is not None else none
+        if any(len(x) != len(weights) for x in self._tensors.values()):
+            raise ValueError("one state (scale, copy) for each weight is needed")
+        self._types = wd, gd, sd
         self._descriptor = _Descriptor(AdamwDesc(weight_dtype=_DTYPES[wd], grad_dtype=_DTYPES[gd],
                                                  state_bits=8 if self.bits8 else 32))
-        self._tensors = (AdamwTensor * len(self.weights))()
+        self._watched = (*weights, *grads, *(c for c in self._tensors["copies"] if c is not None))
+        self._states = new
+        self.rebind()
+        self._made(self.device)
+
+    weights, grads, copies, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale = (
+        property(lambda self, name=name: self._tensors[name])
+        for name in ("weights", "grads", "copies", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"))
+
+    def rebind(self):
+        """Takes all tensors as they lie now, checked like those that the runner was made with."""
+        wd, gd, sd = self._types
+        table, kept = (AdamwTensor * len(self.weights))(), []
 
         def at(name, x, n, *dtypes):
-            if x.dtype not in dtypes or x.numel() != n or x.device != self.device or not x.is_contiguous():
+            if (x.dtype not in dtypes or x.numel() != n or x.device != self.device or not x.is_contiguous()
+                    or (n and not x.data_ptr())):
                 raise ValueError(f"{name}: {n} contiguous values of {dtypes[0]} on {self.device} are needed, got {x.dtype} "
                                  f"{tuple(x.shape)} on {x.device}")
+            kept.append(x.detach())        # (another tensor over the same memory: an exchange beneath x leaves it alone)
             return x.data_ptr()
 
-        lists = (self.grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, self.copies)
-        if any(len(x) != len(self.weights) for x in lists):
-            raise ValueError("one state (scale, copy) for each weight is needed")
-        for e, w, g, m, v, ms, vs, c in zip(self._tensors, self.weights, *lists):
+        for e, w, g, m, v, ms, vs, c in zip(table, self.weights, self.grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
+                                            self.exp_avg_sq_scale, self.copies):
             n = w.numel()
             e.weight, e.grad = at("weight", w, n, wd), at("grad", g, n, gd)
             e.exp_avg, e.exp_avg_sq = at("exp_avg", m, n, sd), at("exp_avg_sq", v, n, sd)
@@ -413,8 +431,8 @@ class AdamWRunner(_Runner):
                 e.exp_avg_scale, e.exp_avg_sq_scale = at("exp_avg_scale", ms, *scale), at("exp_avg_sq_scale", vs, *scale)
             e.copy = at("copy", c, n, torch.bfloat16) if c is not None else None
             e.n = n
-        self._states = new
-        self._made(self.device)
+        self._table, self._kept = table, kept
+        self._at = tuple(map(_address, self._watched))
 
     def _own(self):
         return self._states                # (those that were given are their owner's)
@@ -435,6 +453,8 @@ class AdamWRunner(_Runner):
             d.step = self.t + 1 if step is None else int(step)
         if grad_scale is not None:
             d.grad_scale = _take("grad_scale", grad_scale.reshape(1), (1,), torch.float32, self.device)
-        self._call(stream, binding.adamw_step, d, self._tensors, len(self.weights))
+        if tuple(map(_address, self._watched)) != self._at:
+            self.rebind()
+        self._call(stream, binding.adamw_step, d, self._table, len(self._table))
         if not isinstance(step, torch.Tensor):
             self.t = d.step

@@ -100,3 +100,21 @@ def test_gradients_of_micro_batches_from_their_own_forward_pass():
     r.lse, r.entropy = fresh, torch.empty(T, device="cuda")
     r.forward(*batches[0])
     assert torch.equal(fresh, kept[0][0])
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+def test_steps_behind_an_exchange_of_memory(bits8):
+    """The same bits as a runner that was made with the new memory, and nothing in the old."""
+    from paper_2505_05086_b200.runner import AdamWRunner
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ws, gs = ([torch.randn(n, generator=g, device="cuda") for n in (3000, 5)] for _ in range(2))
+    a = AdamWRunner([w.clone() for w in ws], [x.clone() for x in gs], bits8=bits8)
+    b = AdamWRunner([w.clone() for w in ws], [x.clone() for x in gs], bits8=bits8)
+    a.step(), b.step()
+    old = [w.detach() for w in b.weights]
+    before = [w.clone() for w in old]
+    for w, x in zip(b.weights, b.grads):
+        w.data, x.data = w.data.clone(), x.data.clone()
+    a.step(), b.step()
+    assert all(torch.equal(x, y) for x, y in zip(a.weights, b.weights))
+    assert all(torch.equal(x, y) for x, y in zip(old, before))

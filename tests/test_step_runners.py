@@ -267,3 +267,71 @@ def test_gradient_from_the_results_of_an_earlier_batch(world):
     for kw in (dict(entropy=h), dict(lse=lse), dict(lse=lse[:2], entropy=h), dict(lse=lse.double(), entropy=h)):
         with pytest.raises(ValueError):
             r.backward(x, y, w, w, out, **kw)
+
+
+def table_of(call):
+    return [(e.weight, e.grad, e.exp_avg, e.exp_avg_sq, e.exp_avg_scale, e.exp_avg_sq_scale, e.copy, e.n) for e in call[1]]
+
+
+def addresses(r):
+    def at(x):
+        return None if x is None else x.data_ptr()
+    return [tuple(map(at, each)) + (each[0].numel(),) for each in zip(r.weights, r.grads, r.exp_avg, r.exp_avg_sq, r.exp_avg_scale,
+                                                                      r.exp_avg_sq_scale, r.copies)]
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+def test_steps_go_to_the_weights_and_gradients_where_they_lie(world, bits8):
+    from paper_2505_05086_b200.runner import AdamWRunner
+    ws, gs, cs = ([torch.zeros(300, dtype=t), torch.zeros(7, dtype=t)] for t in (torch.float32, torch.float32, torch.bfloat16))
+    r = AdamWRunner(ws, gs, bits8=bits8, copies=cs)
+
+    def check(step=r.step):
+        step()
+        assert table_of(world["adamw_step"][-1]) == addresses(r)
+
+    check()
+    ws[0].data = torch.ones(300)                                     # other memory beneath the same tensor
+    check()
+    gs[1].set_(torch.ones(7))
+    check()
+    cs[0].data = torch.ones(300, dtype=torch.bfloat16)
+    check()
+    r.exp_avg[1].data = torch.ones(7, dtype=r.exp_avg[1].dtype)      # a state: with rebind()
+    r.rebind()
+    check()
+
+
+def test_memory_that_a_step_writes_stays_alive(world):
+    """States that were exchanged without rebind(): the step goes to the old ones, which nobody else gets."""
+    from paper_2505_05086_b200.runner import AdamWRunner
+    w, g, m = torch.zeros(300), torch.zeros(300), torch.zeros(300)
+    r = AdamWRunner([w], [g], exp_avg=[m])
+    before = addresses(r)[0][2]
+    m.data = torch.ones(300)
+    r.step()
+    assert table_of(world["adamw_step"][-1])[0][2] == before in {x.data_ptr() for x in r._kept}
+    r.rebind()
+    assert before not in {x.data_ptr() for x in r._kept}
+
+
+def test_exchanges_that_could_not_be_stepped_are_refused(world):
+    from paper_2505_05086_b200.runner import AdamWRunner
+    ws, gs = [torch.zeros(300)], [torch.zeros(300)]
+    r = AdamWRunner(ws, gs)
+    for name in ("weights", "grads", "exp_avg", "exp_avg_sq"):       # silently without effect before
+        with pytest.raises(AttributeError):
+            setattr(r, name, [torch.zeros(300)])
+        with pytest.raises(TypeError):
+            getattr(r, name)[0] = torch.zeros(300)
+    r.step()
+    for bad in (torch.zeros(299), torch.zeros(300, dtype=torch.float64), torch.zeros(600)[::2]):
+        gs[0].data = bad
+        with pytest.raises(ValueError):
+            r.step()
+    gs[0].data = torch.zeros(300)
+    r.step()
+    ws[0].untyped_storage().resize_(0)                               # no memory at all
+    with pytest.raises(ValueError):
+        r.step()
+    assert len(world["adamw_step"]) == 2
