@@ -268,6 +268,7 @@ asi_status_t asi_poll_status(const asi_plan_t* plan, const void* ws, void* strea
  * vocabulary, and the gradients of a step (dW of asi_wgrad_batched among them) go to an optimiser.  These entry
  * points take descriptors instead of plans (nothing about them is worth keeping), follow the conventions at the top,
  * and write nothing but the outputs they name; two calls with outputs and workspaces of their own may overlap.
+ * No output meets another buffer of its call, but where that is said; one that does is ASI_ERR_INVALID_ARG.
  * Results are bit-identical from call to call on the same buffers (the order of a row's sums goes by where it starts
  * within 16 bytes).  Token ids and targets are int64. */
 
@@ -308,7 +309,7 @@ asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logi
  *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
  *   dlogits [out] device in_dtype [rows][ld_grad]; what lies between vocab and ld_grad stays as it was.  It may be
  *           logits itself (the same address, ld_grad == ld), or lie between its rows (ld_grad == ld); beyond that the two
- *           do not meet. */
+ *           do not meet.  Other buffers may lie between rows of either. */
 asi_status_t asi_token_logprobs_grad(const asi_logprob_desc_t* desc, const void* logits, const int64_t* targets,
                                      const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
                                      void* dlogits, void* stream);

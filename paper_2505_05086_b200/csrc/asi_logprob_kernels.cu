@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "asi_internal.h"
@@ -1003,6 +1004,40 @@ asi_status_t check_grad(const asi_logprob_desc_t* d, const void* x, const void* 
   return a < b + nb && b < a + na ? ASI_ERR_INVALID_ARG : ASI_OK;
 }
 
+// A contiguous buffer of a call; null where the call has none
+struct Span {
+  const void* p;
+  size_t bytes;
+  bool meets(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && a < b + o.bytes && b < a + bytes;
+  }
+};
+
+// The span meets a row of logits or dlogits, `ld` elements apart (it may lie between two of them).
+bool meets_rows(const asi_logprob_desc_t* d, const Span& s, const void* rows, int64_t ld) {
+  if (!s.p || !rows) return false;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(rows), a = reinterpret_cast<uintptr_t>(s.p);
+  const uintptr_t row = d->vocab * logit_bytes(d), stride = ld * logit_bytes(d), end = at + (d->rows - 1) * stride + row;
+  if (a + s.bytes <= at || a >= end) return false;
+  return a < at || (a - at) % stride < row || (a - at) % stride + s.bytes > stride;
+}
+
+// What a call writes (`out`, and dlogits if any) meets nothing that it reads or writes beside.  dlogits over logits is check_grad's.
+bool written_apart(const asi_logprob_desc_t* d, const void* logits, const void* dlogits, std::initializer_list<Span> out,
+                   std::initializer_list<Span> in) {
+  for (const Span* o = out.begin(); o != out.end(); ++o) {
+    if (meets_rows(d, *o, logits, d->ld) || meets_rows(d, *o, dlogits, d->ld_grad)) return false;
+    for (const Span* q = out.begin(); q != o; ++q)
+      if (o->meets(*q)) return false;
+    for (const Span& i : in)
+      if (o->meets(i)) return false;
+  }
+  for (const Span& i : in)
+    if (meets_rows(d, i, dlogits, d->ld_grad)) return false;
+  return true;
+}
+
 LogprobArgs base_args(const asi_logprob_desc_t* d, const void* logits, const int64_t* targets) {
   LogprobArgs a = {};
   a.x = logits;
@@ -1037,6 +1072,10 @@ asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logi
   if (desc->rows == 0) return ASI_OK;
   if (!logits || !targets || !logp || !lse || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   if ((desc->top_k > 0) != (top_logp != nullptr) || (desc->top_k > 0) != (top_ids != nullptr)) return ASI_ERR_INVALID_ARG;
+  const size_t n = (size_t)desc->rows, top = n * desc->top_k;
+  if (!written_apart(desc, logits, nullptr, {{logp, 4 * n}, {entropy, 4 * n}, {lse, 4 * n}, {top_logp, 4 * top}, {top_ids, 8 * top}},
+                     {{targets, 8 * n}}))
+    return ASI_ERR_INVALID_ARG;
   LogprobArgs a = base_args(desc, logits, targets);
   a.logp = logp;
   a.entropy = entropy;
@@ -1059,6 +1098,10 @@ asi_status_t asi_token_loss(const asi_logprob_desc_t* desc, const void* logits, 
   if (!logits || !targets || !dlogp || !logp || !lse || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   const asi_status_t g = check_grad(desc, logits, dlogits);
   if (g != ASI_OK) return g;
+  const size_t n = (size_t)desc->rows;
+  if (!written_apart(desc, logits, dlogits, {{logp, 4 * n}, {entropy, 4 * n}, {lse, 4 * n}},
+                     {{targets, 8 * n}, {dlogp, 4 * n}, {dentropy, 4 * n}}))
+    return ASI_ERR_INVALID_ARG;
   LogprobArgs a = base_args(desc, logits, targets);
   a.logp = logp;
   a.entropy = entropy;
@@ -1081,6 +1124,10 @@ asi_status_t asi_token_logprobs_grad(const asi_logprob_desc_t* desc, const void*
   if (!logits || !targets || !lse || !dlogp || (dentropy && !entropy) || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   const asi_status_t g = check_grad(desc, logits, dlogits);
   if (g != ASI_OK) return g;
+  const size_t rows = (size_t)desc->rows;
+  if (!written_apart(desc, logits, dlogits, {},
+                     {{targets, 8 * rows}, {lse, 4 * rows}, {dlogp, 4 * rows}, {dentropy, 4 * rows}, {dentropy ? entropy : nullptr, 4 * rows}}))
+    return ASI_ERR_INVALID_ARG;
   LogprobGradArgs a = {};
   a.x = logits;
   a.y = targets;
