@@ -268,7 +268,8 @@ asi_status_t asi_poll_status(const asi_plan_t* plan, const void* ws, void* strea
  * vocabulary, and the gradients of a step (dW of asi_wgrad_batched among them) go to an optimiser.  These entry
  * points take descriptors instead of plans (nothing about them is worth keeping), follow the conventions at the top,
  * and write nothing but the outputs they name; two calls with outputs and workspaces of their own may overlap.
- * No output meets another buffer of its call, but where that is said; one that does is ASI_ERR_INVALID_ARG.
+ * Every buffer starts at an element of its type.  No output meets another buffer of its call, but where that is said.
+ * What breaks either is ASI_ERR_INVALID_ARG.
  * Results are bit-identical from call to call on the same buffers (the order of a row's sums goes by where it starts
  * within 16 bytes).  Token ids and targets are int64. */
 

@@ -788,7 +788,7 @@ asi_status_t asi_embedding_forward(const asi_embedding_desc_t* desc, const void*
   if (desc->table_dtype != ASI_F32 && desc->table_dtype != ASI_BF16) return ASI_ERR_INVALID_ARG;
   if (desc->tokens == 0) return ASI_OK;
   const size_t et = size_of(desc->table_dtype), eo = size_of(desc->in_dtype);
-  if (!table || !ids || !out || !aligned(table, et) || !aligned(out, eo)) return ASI_ERR_INVALID_ARG;
+  if (!table || !ids || !out || !aligned(table, et) || !aligned(out, eo) || !aligned(ids, 8)) return ASI_ERR_INVALID_ARG;
   const size_t out_bytes = eo * desc->tokens * desc->dim;
   if (!apart(table, et * desc->vocab * desc->dim, out, out_bytes) || !apart(ids, 8 * desc->tokens, out, out_bytes)) return ASI_ERR_INVALID_ARG;
   LookupArgs a = {};
@@ -817,7 +817,7 @@ asi_status_t asi_embedding_wgrad(const asi_embedding_desc_t* desc, const int64_t
   const asi_status_t s = check_desc(desc);
   if (s != ASI_OK) return s;
   const size_t eo = size_of(desc->in_dtype), dw_bytes = (size_t)desc->vocab * desc->dim * 4;
-  if (!dW || !aligned(dW, 4) || !ws || (desc->tokens && (!ids || !dOut || !aligned(dOut, eo)))) return ASI_ERR_INVALID_ARG;
+  if (!dW || !aligned(dW, 4) || !ws || (desc->tokens && (!ids || !dOut || !aligned(dOut, eo) || !aligned(ids, 8)))) return ASI_ERR_INVALID_ARG;
   const Layout l = layout_of(desc);
   if (ws_bytes < l.bytes || !aligned(ws, 256)) return ASI_ERR_WORKSPACE;
   if (!apart(dW, dw_bytes, ws, l.bytes)) return ASI_ERR_INVALID_ARG;

@@ -332,6 +332,9 @@ cudaError_t opt_in_smem(const void* kernel, size_t need);
 asi_status_t cuda_status(cudaError_t e, const char* what);
 asi_status_t no_host_memory();
 
+// a buffer of `element`-byte values that does not start at one of them
+inline bool off_element(const void* p, size_t element) { return reinterpret_cast<uintptr_t>(p) % element != 0; }
+
 // One product of a grouped launch (asi_gemm_kernels.cu): C[m][j] = sum_k A(m, k) B[k][j] per outer index o
 struct GemmProb {
   const void* X;

@@ -990,7 +990,13 @@ asi_status_t check_desc(const asi_logprob_desc_t* d) {
 
 size_t logit_bytes(const asi_logprob_desc_t* d) { return d->in_dtype == ASI_BF16 ? 2 : 4; }
 
-bool off_element(const asi_logprob_desc_t* d, const void* p) { return (reinterpret_cast<uintptr_t>(p) & (logit_bytes(d) - 1)) != 0; }
+bool off_element(const asi_logprob_desc_t* d, const void* p) { return asi::off_element(p, logit_bytes(d)); }
+
+bool off_float(std::initializer_list<const float*> buffers) {
+  for (const float* p : buffers)
+    if (asi::off_element(p, 4)) return true;
+  return false;
+}
 
 // dlogits is logits itself, row for row, or lies apart from it (between its rows, perhaps, where both have the same stride)
 asi_status_t check_grad(const asi_logprob_desc_t* d, const void* x, const void* dx) {
@@ -1072,6 +1078,7 @@ asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logi
   if (desc->rows == 0) return ASI_OK;
   if (!logits || !targets || !logp || !lse || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   if ((desc->top_k > 0) != (top_logp != nullptr) || (desc->top_k > 0) != (top_ids != nullptr)) return ASI_ERR_INVALID_ARG;
+  if (off_element(targets, 8) || off_element(top_ids, 8) || off_float({logp, entropy, lse, top_logp})) return ASI_ERR_INVALID_ARG;
   const size_t n = (size_t)desc->rows, top = n * desc->top_k;
   if (!written_apart(desc, logits, nullptr, {{logp, 4 * n}, {entropy, 4 * n}, {lse, 4 * n}, {top_logp, 4 * top}, {top_ids, 8 * top}},
                      {{targets, 8 * n}}))
@@ -1098,6 +1105,7 @@ asi_status_t asi_token_loss(const asi_logprob_desc_t* desc, const void* logits, 
   if (!logits || !targets || !dlogp || !logp || !lse || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   const asi_status_t g = check_grad(desc, logits, dlogits);
   if (g != ASI_OK) return g;
+  if (off_element(targets, 8) || off_float({dlogp, dentropy, logp, entropy, lse})) return ASI_ERR_INVALID_ARG;
   const size_t n = (size_t)desc->rows;
   if (!written_apart(desc, logits, dlogits, {{logp, 4 * n}, {entropy, 4 * n}, {lse, 4 * n}},
                      {{targets, 8 * n}, {dlogp, 4 * n}, {dentropy, 4 * n}}))
@@ -1124,6 +1132,7 @@ asi_status_t asi_token_logprobs_grad(const asi_logprob_desc_t* desc, const void*
   if (!logits || !targets || !lse || !dlogp || (dentropy && !entropy) || off_element(desc, logits)) return ASI_ERR_INVALID_ARG;
   const asi_status_t g = check_grad(desc, logits, dlogits);
   if (g != ASI_OK) return g;
+  if (off_element(targets, 8) || off_float({lse, dlogp, dentropy, dentropy ? entropy : nullptr})) return ASI_ERR_INVALID_ARG;
   const size_t rows = (size_t)desc->rows;
   if (!written_apart(desc, logits, dlogits, {},
                      {{targets, 8 * rows}, {lse, 4 * rows}, {dlogp, 4 * rows}, {dentropy, 4 * rows}, {dentropy ? entropy : nullptr, 4 * rows}}))

@@ -1,5 +1,5 @@
-"""Outputs of the log probability entry points that meet another buffer of the call, on the host: each is refused before anything
-is enqueued."""
+"""Outputs of the log probability entry points that meet another buffer of the call, and buffers off their elements, on the host:
+each is refused before anything is enqueued."""
 import pytest
 
 INVALID = 1
@@ -80,3 +80,22 @@ def test_between_the_rows_and_not_quite(B):
             assert L.asi_token_logprobs(d, *args, None, None, None) == INVALID, (dtype, shift)
             assert L.asi_token_loss(d, at(60), *[at(i) for i in range(1, 6)], x + shift // 4 * 4, x, None) == INVALID
             assert L.asi_token_logprobs_grad(d, at(60), at(1), x + shift // 4 * 4, at(3), at(4), at(5), x, None) == INVALID
+
+
+def test_buffers_off_their_elements(B):
+    """Values of 4 and 8 bytes that no kernel could read or write in one piece."""
+    L, d, k = B.lib(), desc(B), desc(B, top_k=2)
+    p = [at(i) for i in range(9)]
+    for i, shift in ((1, 4), (2, 2), (3, 2), (4, 1), (5, 2), (6, 4)):              # targets, logp, entropy, lse, top_logp, top_ids
+        q = [*p[:i], p[i] + shift, *p[i + 1:]]
+        assert L.asi_token_logprobs(k, *q[:7], None) == INVALID, i
+    for i, shift in ((1, 4), (2, 2), (3, 2), (4, 1), (5, 2)):                       # targets, lse, entropy, dlogp, dentropy
+        q = [*p[:i], p[i] + shift, *p[i + 1:]]
+        assert L.asi_token_logprobs_grad(d, *q[:7], None) == INVALID, i
+    for i, shift in ((1, 4), (2, 2), (3, 2), (4, 1), (5, 2), (6, 3)):              # targets, dlogp, dentropy, logp, entropy, lse
+        q = [*p[:i], p[i] + shift, *p[i + 1:]]
+        assert L.asi_token_loss(d, *q[:8], None) == INVALID, i
+    e = B.EmbeddingDesc(0, 1, 50, 16, 9, -1, 1.0)
+    for shift in (1, 2, 4):
+        assert L.asi_embedding_forward(e, at(0), at(1) + shift, at(2), None) == INVALID
+        assert L.asi_embedding_wgrad(e, at(0) + shift, at(1), at(2), 0, at(3), L.asi_embedding_wgrad_ws_bytes(e), None) == INVALID
