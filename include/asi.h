@@ -306,7 +306,7 @@ asi_status_t asi_token_logprobs(const asi_logprob_desc_t* desc, const void* logi
 /* Gradient of sum_t (dlogp[t] logp[t] + dentropy[t] entropy[t]) with respect to the logits:
  *   dlogits[t][j] = scale (dlogp[t] ([j = y] - p_j) - dentropy[t] p_j (log p_j + entropy[t])).
  *   lse, entropy [in] as asi_token_logprobs wrote them (entropy may be null where dentropy is).  p = exp(x - lse) is off by
- *           2^-24 |lse|; rows with |lse| >= 4096 are summed again instead.
+ *           2^-24 |lse|; rows with |lse| >= 128 (fp32) or 4096 (bf16) are summed again instead.
  *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
  *   dlogits [out] device in_dtype [rows][ld_grad]; what lies between vocab and ld_grad stays as it was.  It may be
  *           logits itself (the same address, ld_grad == ld), or lie between its rows (ld_grad == ld); beyond that the two

@@ -31,3 +31,26 @@ def test_results_between_the_rows_of_logits_and_gradient(dt):
     assert torch.equal(behind, torch.cat([logp, ent]))
     assert torch.equal(dx[2, V + 2:V + 2 + 20 // e].view(torch.uint8).view(torch.float32), lse)
     assert (x[0, V:] == 7).all() and (dx[0, V:] == 7).all() and (dx[3:, V:] == 7).all()
+
+
+@pytest.mark.parametrize("T,V,off", [(5, 300, 1), (3, 50257, 0), (700, 1001, 0), (2, 131073, 3)])
+@pytest.mark.parametrize("level", [150.0, -700.0, 1000.0, 3900.0])
+def test_fp32_gradients_of_rows_off_zero_keep_their_digits(level, T, V, off):
+    """An offset that all logits of a row share changes nothing about its gradient: from lse, which says little about differences
+    there, it is as near to the definition as the loss in one pass (the same tolerance, which knows no |lse|)."""
+    from tests.test_gpu_token_loss import check_grad, definition, make, runner
+    x, y, _ = make(T, V, torch.float32, 5, off, seed=13)
+    x += level
+    y[0] = IGN
+    alpha, beta = torch.linspace(0.5, 2, T, device="cuda"), torch.linspace(-1, 1, T, device="cuda")
+    run = runner(T, V, torch.float32)
+    run.forward(x, y)
+    D = definition(x, y, 1.0)
+    for b in (None, beta):
+        out = torch.full((T, V + 5), 7.0, device="cuda")
+        run.backward(x, y, alpha, b, out[:, :V])
+        check_grad(out[:, :V], D, y, V, 1.0, alpha, b, torch.float32)
+        assert (out[:, V:] == 7).all()
+        again = x.clone()
+        run.backward(again, y, alpha, b, again)                      # in place, in rows of another stride
+        check_grad(again, D, y, V, 1.0, alpha, b, torch.float32)
