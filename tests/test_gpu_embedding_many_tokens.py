@@ -90,3 +90,20 @@ def test_same_bits_again_and_in_a_graph():
     # each addition rounds by half a step, 2^-24, of a partial sum that the sum of magnitudes bounds
     count = torch.bincount(ids, minlength=V)[:, None]
     assert ((dw.double() - want).abs() <= (count + 8) * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("T,D,hot", [(1 << 20, 3, 1.0), (1 << 20, 8, 0.6), (40000, 64, 1.0), (70001, 5, 0.3)])
+def test_runs_over_hundreds_of_chunks(T, D, hot):
+    """Where such a run starts and ends is found by a search, not chunk by chunk: between rarer ids, at either end, alone."""
+    V = 900
+    for v in (0, 450, V - 1):
+        g = torch.Generator(device="cuda").manual_seed(v)
+        ids = torch.randint(0, V, (T,), generator=g, device="cuda")
+        ids[torch.rand(T, generator=g, device="cuda") < hot] = v
+        d = torch.randint(-8, 9, (T, D), generator=g, device="cuda").float()
+        r = runner(V, D, T)
+        dw, want = torch.empty(V, D, device="cuda"), plain(V, D, ids, d, 1.0, None)
+        r.wgrad(ids, d, dw)
+        assert torch.equal(dw, want)
+        r.wgrad(ids, d, dw, accumulate=True)
+        assert torch.equal(dw, 2 * want)
