@@ -55,6 +55,14 @@ class LayerRunner:
             off += d * r
         return out
 
+    @property
+    def dW_shape(self):
+        """[Cout, C / groups, kh, kw] or [Dout, Din], row-major in dW."""
+        d = self.plan.desc
+        if self.plan.kind == "conv":
+            return d.cout, d.dims[1] // d.groups, d.kh, d.kw
+        return d.cout, d.dims[d.ndim - 1]
+
     def core_np(self):
         return self.core.cpu().numpy().reshape(self.ranks).copy()
 
@@ -119,7 +127,17 @@ class StepRunner:
                          [r.ws_w.data_ptr() for r in rs], [r.ws_w.numel() for r in rs], _stream_handle(stream))
 
     def optimizer(self, weights, **kw):
-        """AdamW over the layers' weights (one for each, fp32 or bf16) and the dW buffers that wgrad() fills."""
+        """AdamW over the layers' weights (one for each, fp32 or bf16, of dW's sizes, or with neighbouring ones
+        joined or one of them split) and the dW buffers that wgrad() fills."""
+        weights = list(weights)
+
+        def parts(shape):                  # what lies together, from whole rows down to neighbours
+            return {int(np.prod(shape[i:], dtype=np.int64)) for i in range(len(shape))}
+
+        for r, w in zip(self.runners, weights):
+            have, need = parts(w.shape) | {1}, parts(r.dW_shape) | {1}
+            if not (have <= need or need <= have):
+                raise ValueError(f"weight: {r.dW_shape} is needed, as dW is laid out, got {tuple(w.shape)}")
         return AdamWRunner(weights, [r.dW for r in self.runners], **kw)
 
 

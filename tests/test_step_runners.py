@@ -335,3 +335,30 @@ def test_exchanges_that_could_not_be_stepped_are_refused(world):
     with pytest.raises(ValueError):
         r.step()
     assert len(world["adamw_step"]) == 2
+
+
+def test_weights_of_a_step_runner_lie_as_their_gradients(world):
+    """A transposed weight has as many elements as dW, in another order."""
+    from paper_2505_05086_b200.binding import Plan
+    from paper_2505_05086_b200.runner import LayerRunner, StepRunner
+
+    def layer(*a, **kw):
+        r = LayerRunner.__new__(LayerRunner)
+        r.plan = Plan(*a, **kw)
+        r.dW = torch.zeros(r.plan.info.dw_elems)
+        return r
+
+    step = StepRunner.__new__(StepRunner)
+    step.runners = [layer("linear", (4, 5, 12), (2, 2, 2), 10), layer("conv", (4, 6, 7, 8), (2, 2, 2, 2), 9, k=3, pad=1),
+                    layer("conv", (4, 6, 7, 8), (2, 2, 2, 2), 6, k=3, groups=6), layer("conv", (4, 6, 7, 8), (2, 2, 2, 2), 9, k=1)]
+    shapes = [(10, 12), (9, 6, 3, 3), (6, 1, 3, 3), (9, 6, 1, 1)]
+    assert [tuple(r.dW_shape) for r in step.runners] == shapes
+    good = [torch.zeros(s) for s in shapes]
+    step.optimizer(good).step()
+    step.optimizer([w.view(-1) for w in good]).step()
+    step.optimizer([torch.zeros(2, 5, 12), torch.zeros(9, 54), torch.zeros(6, 9), torch.zeros(9, 6)]).step()
+    for i, bad in ((0, (12, 10)), (0, (2, 60)), (1, (6, 9, 3, 3)), (1, (3, 3, 6, 9)), (3, (6, 9, 1, 1))):
+        with pytest.raises(ValueError):
+            step.optimizer([*good[:i], torch.zeros(bad), *good[i + 1:]])
+    with pytest.raises(ValueError):
+        step.optimizer(good[:3])
