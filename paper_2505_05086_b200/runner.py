@@ -456,8 +456,9 @@ class AdamWRunner(_Runner):
         return self._states                # (those that were given are their owner's)
 
     def step(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=None, grad_scale=None, stream=None):
-        """One step.  `step` counts from 1 (default: one more than at the call before).  lr (fp32) and step (int64) may be
-        one-element device tensors, so that a captured graph reads new values; grad_scale (fp32) is one if given."""
+        """One step.  `step` counts from 1 (default: one more than at the call before, which then was not counted on the device).
+        lr (fp32) and step (int64) may be one-element device tensors, so that a captured graph reads new values; grad_scale
+        (fp32) is one if given."""
         d = self._descriptor.desc
         d.beta1, d.beta2, d.eps, d.weight_decay = beta1, beta2, eps, weight_decay
         d.lr_dev = d.step_dev = d.grad_scale = None
@@ -467,6 +468,8 @@ class AdamWRunner(_Runner):
             d.lr = lr
         if isinstance(step, torch.Tensor):
             d.step, d.step_dev = 1, _take("step", step.reshape(1), (1,), torch.int64, self.device)
+        elif step is None and self.t is None:
+            raise ValueError("the step before was counted on the device: which one this is has to be given")
         else:
             d.step = self.t + 1 if step is None else int(step)
         if grad_scale is not None:
@@ -474,5 +477,4 @@ class AdamWRunner(_Runner):
         if tuple(map(_address, self._watched)) != self._at:
             self.rebind()
         self._call(stream, binding.adamw_step, d, self._table, len(self._table))
-        if not isinstance(step, torch.Tensor):
-            self.t = d.step
+        self.t = None if isinstance(step, torch.Tensor) else d.step

@@ -362,3 +362,16 @@ def test_weights_of_a_step_runner_lie_as_their_gradients(world):
             step.optimizer([*good[:i], torch.zeros(bad), *good[i + 1:]])
     with pytest.raises(ValueError):
         step.optimizer(good[:3])
+
+
+def test_steps_behind_one_that_the_device_counted(world):
+    """Their number is on the device: going on from the last one given on the host would spoil the bias correction."""
+    from paper_2505_05086_b200.runner import AdamWRunner
+    r = AdamWRunner([torch.zeros(300)], [torch.zeros(300)])
+    r.step(), r.step()
+    r.step(step=torch.tensor([7]))
+    with pytest.raises(ValueError):
+        r.step()
+    r.step(step=8)
+    r.step()
+    assert r.t == 9 and len(world["adamw_step"]) == 5
