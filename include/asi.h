@@ -294,7 +294,7 @@ typedef struct {
   int64_t rows, vocab;           /* rows may be 0 */
   int64_t ld, ld_grad;           /* elements from one row to the next of logits and dlogits, >= vocab */
   int64_t ignore_index;
-  float scale;                   /* 1 / temperature, 1e-8 to 1e8; scaled logits beyond fp32's range count as infinite */
+  float scale;                   /* 1 / temperature, 1e-8 to 1e8; lse beyond fp32's range is infinite, the rest goes by differences */
 } asi_logprob_desc_t;
 
 /*   logits [in] device in_dtype [rows][ld], at any element;  targets [in] device [rows]

@@ -54,3 +54,36 @@ def test_fp32_gradients_of_rows_off_zero_keep_their_digits(level, T, V, off):
         again = x.clone()
         run.backward(again, y, alpha, b, again)                      # in place, in rows of another stride
         check_grad(again, D, y, V, 1.0, alpha, b, torch.float32)
+
+
+@pytest.mark.parametrize("T", [3, 700])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scaled_logits_beyond_the_range_of_fp32(sign, T):
+    """lse is infinite; all that goes by differences of logits stays what it is."""
+    from tests.test_gpu_token_loss import runner
+    V, scale = 50, 2.0 ** 26                                          # differences that the scale leaves exact
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k = torch.randint(0, 4, (T, V), generator=g, device="cuda").float()
+    level = sign * 2.0 ** 120
+    x = torch.where(k > 0, level, level - 2.0 ** 100)                 # level, or so far below that nothing is left of it
+    x[:, 0] = level
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    run = runner(T, V, torch.float32, scale=scale, top_k=5)
+    run.forward(x, y)
+    lead = x == level
+    n = lead.sum(1)
+    assert (run.lse == sign * float("inf")).all()
+    hit = lead.gather(1, y[:, None])[:, 0]
+    # log of a whole number up to 50 and its product with 1: a few roundings of 2^-24 of values up to 4
+    assert ((run.entropy.double() - torch.log(n.double())).abs() <= 32 * 2.0 ** -24).all()
+    assert ((run.logp.double() + torch.log(n.double())).abs() <= 32 * 2.0 ** -24)[hit].all()
+    assert (run.logp[~hit] == -(2.0 ** 126)).all()                   # 2^26 times 2^100; log n is far below its last place
+    v, i = torch.sort(x, dim=1, descending=True, stable=True)
+    assert torch.equal(run.top_ids, i[:, :5])
+    alpha = torch.randn(T, generator=g, device="cuda")
+    want = scale * alpha[:, None].double() * (torch.zeros(T, V, device="cuda", dtype=torch.float64).scatter_(1, y[:, None], 1.0)
+                                              - lead / n[:, None].double())
+    for form in ("backward", "loss"):
+        out = torch.empty_like(x)
+        getattr(run, form)(x, y, alpha, None, out)
+        assert ((out.double() - want).abs() <= 32 * 2.0 ** -24 * scale * alpha.abs()[:, None]).all()
