@@ -86,7 +86,8 @@ class LayerRunner:
         """Cold start with the library's counter-based Gaussian test matrices (allocates its scratch once)."""
         need = self.plan.init_seeded_ws_bytes()
         if getattr(self, "ws_seed", None) is None or self.ws_seed.numel() < need:
-            self.ws_seed = torch.empty(need, dtype=torch.uint8, device=self.core.device)
+            with torch.cuda.stream(stream):    # (memory that this stream is done with)
+                self.ws_seed = torch.empty(need, dtype=torch.uint8, device=self.core.device)
         new = self.U[1 - self.cur]
         self.plan.init_factors_seeded(act.data_ptr(), seed, new.data_ptr(), self.core.data_ptr(),
                                       self.ws_seed.data_ptr(), self.ws_seed.numel(), _stream_handle(stream))

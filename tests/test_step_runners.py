@@ -375,3 +375,18 @@ def test_steps_behind_one_that_the_device_counted(world):
     r.step(step=8)
     r.step()
     assert r.t == 9 and len(world["adamw_step"]) == 5
+
+
+def test_scratch_of_a_cold_start_comes_from_the_stream_that_uses_it(world, monkeypatch):
+    from types import SimpleNamespace
+    from paper_2505_05086_b200.runner import LayerRunner
+    seen, empty = [], torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: (seen.append(world.now.cuda_stream), empty(*a, **kw))[1])
+    r = LayerRunner.__new__(LayerRunner)
+    r.plan = SimpleNamespace(init_seeded_ws_bytes=lambda: 64, init_factors_seeded=lambda *a: seen.append(a[-1]))
+    r.U, r.cur, r.core = [torch.zeros(4), torch.zeros(4)], 0, torch.zeros(4)
+    r.init_factors_seeded(torch.zeros(4), 1, Stream(7))
+    assert seen == [7, 7]
+    r.ws_seed = None
+    r.init_factors_seeded(torch.zeros(4), 1)
+    assert seen == [7, 7, 0, 0]
