@@ -433,12 +433,13 @@ class AdamWRunner(_Runner):
         table, kept = (AdamwTensor * len(self.weights))(), []
 
         def at(name, x, n, *dtypes):
+            address = x.data_ptr()
             if (x.dtype not in dtypes or x.numel() != n or x.device != self.device or not x.is_contiguous()
-                    or (n and not x.data_ptr())):
+                    or (n and not address)):
                 raise ValueError(f"{name}: {n} contiguous values of {dtypes[0]} on {self.device} are needed, got {x.dtype} "
                                  f"{tuple(x.shape)} on {x.device}")
-            kept.append(x.detach())        # (another tensor over the same memory: an exchange beneath x leaves it alone)
-            return x.data_ptr()
+            kept.append(x.untyped_storage())       # (not x, which may let go of it)
+            return address
 
         for e, w, g, m, v, ms, vs, c in zip(table, self.weights, self.grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
                                             self.exp_avg_sq_scale, self.copies):
