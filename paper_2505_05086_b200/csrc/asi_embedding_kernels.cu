@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kClearThreads) k_clear_rows(const __grid_const
 constexpr int kMaxChunk = 64;
 constexpr int kZeroRows = 64;
 constexpr int kSumCtas = 3;                 // CTAs of an SM (tied table of 50257 x 770: 25 us, with two 32, with four 25 to 27)
-constexpr int kInFlight = 16;              // registers of a thread for rows in hand
+constexpr int kInFlight = 16;              // registers of a thread for the rows in hand, and as many for those on their way
 
 struct SumArgs {
   const void* dout;

@@ -27,7 +27,7 @@ namespace {
 // search waits a lot), loss, both for rows of a few granules, gradient alone
 constexpr int kFwd = 128, kFwdCtas = 8, kLoss = 384, kLoss4 = 256, kLoss8 = 128, kShort = 32, kMid = 64;
 constexpr int ctas_of(int threads, int large) { return threads == kShort ? 32 : threads == kMid ? 1024 / kMid : large; }
-constexpr int kThreads = 128, kEach = 8;    // granules of a thread in the gradient alone (4096 x 32000 bf16: 79 us, with 4 of them 87)
+constexpr int kThreads = 128, kEach = 8;    // granules of a thread in the gradient alone (4096 x 32000 bf16, in bursts: 79 us, with 4 of them 87)
 constexpr int kMaxCluster = 8;
 constexpr int kShare4 = 55 << 10;           // ... with which four CTAs share an SM
 constexpr int kShare = 72 << 10;            // bytes of a row that a CTA of the loss keeps, where a cluster allows it
@@ -308,7 +308,7 @@ __device__ __forceinline__ void block_sums(float& S, float& W, float (*red)[kWar
 #pragma unroll
   for (int i = 1; i < kWarps; ++i) S += red[1][i], W += red[2][i];
 }
-// The cluster's shares, in rank order.  Ends with every remote read done and a cluster_arrive(): the caller waits at its end.
+// M, S and W of the row from the shares of its cluster, in rank order, which the caller has read into sh.parts.
 template <int kWarps>
 __device__ __forceinline__ void cluster_sums(float& M, float& S, float& W, float c2, int cl, RowShared<kWarps>& sh) {
   float Mt = sh.parts[0][0];
@@ -332,7 +332,8 @@ __device__ __forceinline__ void write_row(const LogprobArgs& p, int t, float M, 
 }
 
 // ---- forward: one pass over the row in registers, each thread with a running maximum (two passes over a copy in shared
-// memory: 86 us at 4096 x 32000 bf16; this one 49, 5.4 TB/s, and 62 with five alternatives).  Bound by issue slots (70 %).
+// memory: 86 us at 4096 x 32000 bf16; this one 49, 5.4 TB/s, and in short bursts 62 with five alternatives, under sustained load
+// 64).  Bound by issue slots (70 %).
 constexpr int kBatch = 4;                  // granules a thread has in hand
 constexpr int kSlots = 16;                 // maxima a thread remembers of what it has read
 constexpr int kHits = 512;
@@ -663,26 +664,25 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(con
           }
         }
         __syncthreads();
-        constexpr int kFew = kCand;
-        if (top.pooled <= kFew) {           // up to eight times as many as wanted: tau once more, over them
+        if (top.pooled <= kCand) {          // up to eight times as many as wanted: tau once more, over them
           const int pooled = top.pooled;
           if (warp == 0) {
-            uint32_t key[kFew / 32];
+            uint32_t key[kCand / 32];
 #pragma unroll
-            for (int i = 0; i < kFew / 32; ++i) key[i] = i * 32 + lane < pooled ? (uint32_t)(top.pool[i * 32 + lane] >> 32) : 0u;
+            for (int i = 0; i < kCand / 32; ++i) key[i] = i * 32 + lane < pooled ? (uint32_t)(top.pool[i * 32 + lane] >> 32) : 0u;
             const uint32_t t = reached_by(key, p.k, Granule<T>::kUnit);
             if (lane == 0) top.least = t;
           }
           __syncthreads();
-          unsigned long long keep[kFew / kN];
+          unsigned long long keep[kCand / kN];
 #pragma unroll
-          for (int i = 0; i < kFew / kN; ++i) keep[i] = i * kN + tid < pooled ? top.pool[i * kN + tid] : 0;
+          for (int i = 0; i < kCand / kN; ++i) keep[i] = i * kN + tid < pooled ? top.pool[i * kN + tid] : 0;
           if (tid == 0) top.pooled = 0;
           __syncthreads();
 #pragma unroll
-          for (int i = 0; i < kFew / kN; ++i)
+          for (int i = 0; i < kCand / kN; ++i)
             if (keep[i] && (uint32_t)(keep[i] >> 32) >= top.least) top.pool[atomicAdd(&top.pooled, 1)] = keep[i];
-        } else if (top.pooled > kCand) {    // many equal values again
+        } else {                            // many equal values again
           unsigned long long prev = ~0ull;
           for (int r = 0; r < p.k; ++r) {
             prev = block_best<kN>(prev, top.best, [&](auto offer) {
@@ -725,9 +725,10 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kFwdCtas + TOP)) k_logprob(con
   }
 }
 
-// ---- forward and gradient.  Bound by the exponentials, two an element (4096 x 32000 bf16: 100 us, 67 % of their unit, 5.2 TB/s;
-// 1001 x 50257 fp32: 82 us).  RES: the CTA's share of the row stays in shared memory between the sums and the gradient (else it
-// is read again: rows of more than 1.6 MB).  Every thread reads back what it left there itself: no barrier.
+// ---- forward and gradient.  Bound by the exponentials, two an element (4096 x 32000 bf16: in short bursts 100 us, 67 % of their
+// unit, 5.2 TB/s, under sustained load 108; 1001 x 50257 fp32: 82 and 87 us).  RES: the CTA's share of the row stays in shared
+// memory between the sums and the gradient (else it is read again: rows of more than 1.6 MB).  Every thread reads back what it left
+// there itself: no barrier.
 template <typename T, bool RES, int kN>
 __global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLoss8 ? 8 : kN == kLoss4 ? 4 : 3)) k_loss(const __grid_constant__ LogprobArgs p) {
   constexpr int n = Granule<T>::n, kWarps = kN / 32;
@@ -814,7 +815,8 @@ __global__ void __launch_bounds__(kN, ctas_of(kN, kN == kLoss8 ? 8 : kN == kLoss
   if (cl > 1) cluster_wait();
 }
 
-// ---- the gradient alone, from lse and entropy: a stream of 1024 granules a CTA (79 us at 4096 x 32000 bf16, floor 81).
+// ---- the gradient alone, from lse and entropy: a stream of 1024 granules a CTA (4096 x 32000 bf16: 78 us in short bursts, 83 under
+// sustained load, floor 81).
 // p = exp(x - lse) is off by 2^-24 |lse|: rows where that would show in the type (2^-17 in fp32, 2^-12 beside the 2^-9 of a
 // rounding to bf16; logits that share an offset, or lie at a type's lowest value) sum up for themselves, in one CTA (dx may be
 // x, so nobody else of the row may have begun to write).  fp32, all logits around 1000: 1001 x 50257 takes 111 us instead of 61, 4 x
