@@ -129,7 +129,7 @@ class StepRunner:
 
     def optimizer(self, weights, **kw):
         """AdamW over the layers' weights (one for each, fp32 or bf16, of dW's sizes, or with neighbouring ones
-        joined or one of them split) and the dW buffers that wgrad() fills."""
+        joined or one of them split) and the dW buffers of the layers."""
         weights = list(weights)
 
         def parts(shape):                  # what lies together, from whole rows down to neighbours
