@@ -377,6 +377,114 @@ typedef struct {
  * aligned ones are faster), and no written buffer may overlap another buffer of the call. */
 asi_status_t asi_adamw_step(const asi_adamw_desc_t* desc, const asi_adamw_tensor_t* tensors, int32_t count, void* stream);
 
+/* A transformer block's other operators: dropout, and what joins its branch to the residual stream.  Conventions as for the
+ * entry points of a language model's step above.  Their masks come from the generator of asi_philox_words and are never stored: element e of a
+ * tensor (counted from its first) goes by sixteen bits of group e div 8 of the stream (seed, stream_id): with j = e mod 8 by the low (j even) or
+ * high (j odd) half of word j div 2.  The counter's last word, 0 in that stream, is the step number's low 32 bits.  An element is dropped where its half
+ * is below k = round(65536 p) (halves up), and multiplied with 65536 / (65536 - k) otherwise.  The same numbers give the backward pass the
+ * same mask. */
+typedef struct {
+  double p;                      /* 0 <= p, k < 65536;  p = 0: no mask */
+  uint64_t seed;
+  uint32_t stream_id;            /* another one for each place of a model */
+  int64_t step;                  /* >= 0; another one for each step */
+  const int64_t* step_dev;       /* device pointer, instead of step (for steps that are captured into a graph), or null */
+} asi_dropout_t;
+
+/* out = drop(x) [+ residual].  The gradient of x is drop(dOut), by the same call.  A dropped element is 0 (+ residual), whatever x
+ * holds there.  x, residual and out: device dtype [n], 0 <= n <= 2^40; residual may be null.  out may be x or residual itself (the same address). */
+asi_status_t asi_dropout(const asi_dropout_t* drop, int32_t dtype, int64_t n, const void* x, const void* residual, void* out,
+                         void* stream);
+
+/* The end of a block: its branch's output y joins the residual stream h, and the next block's norm follows.  For row t with the gate's row
+ * s = t div rows_per_gate:
+ *   z = norm_after ? norm(y) * after_weight + after_bias : y
+ *   h_out = res_scale * h + branch_scale * drop(gate[s] * z)            (rounded to res_dtype)
+ *   x = norm(h_out) * next_weight + next_bias                           (of h_out as it is stored)
+ * norm(v) = v / sqrt(mean(v^2) + eps) (ASI_NORM_RMS), or (v - mean v) / sqrt(var v + eps) (ASI_NORM_LAYER, var over dim).  Element e of
+ * the mask is t * dim + column.  Everything between the loads and the stores is fp32; squares of values beyond 1e18 may overflow
+ * there.  Weights, biases and gate are fp32. */
+typedef enum { ASI_NORM_RMS = 0, ASI_NORM_LAYER = 1 } asi_norm_t;
+#define ASI_BRANCH_MAX_DIM 8192
+#define ASI_BRANCH_MAX_ROWS (1 << 27)
+typedef struct {
+  int32_t in_dtype;              /* asi_dtype_t of y, x and their gradients */
+  int32_t res_dtype;             /* of h, h_out and their gradients: ASI_F32, or in_dtype */
+  int32_t norm;                  /* asi_norm_t of both norms */
+  int32_t norm_after;            /* 0: the branch has no norm behind it */
+  int64_t rows, dim;             /* rows may be 0;  dim <= ASI_BRANCH_MAX_DIM */
+  int64_t rows_per_gate;         /* 0: no gate;  rows (or more): one row for all */
+  float eps, res_scale, branch_scale;   /* eps >= 1e-30; all finite */
+  asi_dropout_t drop;
+} asi_branch_desc_t;
+/* Buffers of a call.  Every one is contiguous, [rows][dim] unless said otherwise; those that a direction does not name are not looked at. */
+typedef struct {
+  const void* y;                 /* [in] in_dtype */
+  const void* h;                 /* [in] res_dtype; null: no residual (0) */
+  const float* gate;             /* [in] [ceil(rows / rows_per_gate)][dim]; null where rows_per_gate is 0 */
+  const float *after_weight, *after_bias;      /* [in] [dim], each may be null (1 and 0); both null without norm_after */
+  const float *next_weight, *next_bias;        /* [in] [dim], each may be null (1 and 0) */
+  void* h_out;                   /* [out] res_dtype; [in] of the gradient.  It may be h itself */
+  void* x;                       /* [out] in_dtype; null: no norm follows */
+  float* stats;                  /* [out] [rows][4]: mean and 1 / sqrt(..) of the norm after, of the next one (mean 0 of ASI_NORM_RMS; all
+                                  *       0 of a norm that is not there); [in] of the gradient */
+  /* the gradient alone: */
+  const void* dx;                /* [in] in_dtype; null: no norm follows */
+  const void* dh_out;            /* [in] res_dtype; the gradient that reaches h_out besides; null: none.  One of dx and dh_out is there */
+  void* dy;                      /* [out] in_dtype.  It may be dx itself */
+  void* dh;                      /* [out] res_dtype, may be null.  It may be dh_out itself */
+  float* dgate;                  /* [in/out] as gate; may be null */
+  float *dafter_weight, *dafter_bias;          /* [in/out] [dim], each may be null */
+  float *dnext_weight, *dnext_bias;
+} asi_branch_t;
+asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_t* buffers, void* stream);
+/* Sums over rows (dgate, dafter_*, dnext_*) are fp32 in a fixed order, written over, or added to (accumulate != 0) what is there.
+ *   ws  device scratch of at least asi_branch_backward_ws_bytes(desc) (0 for a descriptor that is refused); it serves fewer rows too */
+size_t asi_branch_backward_ws_bytes(const asi_branch_desc_t* desc);
+asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch_t* buffers, int32_t accumulate, void* ws,
+                                 size_t ws_bytes, void* stream);
+
+/* Output layer and loss in one: asi_token_logprobs, asi_token_logprobs_grad and asi_token_loss for logits = x w^T that are never kept.  With
+ * X_j = scale * sum_d x[t][d] w[j][d] over the vocabulary:
+ *   lse, logp, entropy as of asi_token_logprobs;  G = dlogits of asi_token_logprobs_grad;  dx = G w;  dw = G^T x.
+ * Products of bf16 values are exact, sums fp32 on the tensor cores.  fp32 operands are taken as three bf16 terms each (24 bits, the six
+ * products that matter), and so is G where its product is stored in fp32; G is rounded to bf16 where that is bf16.  Logits are computed
+ * twice, for the sums and for the gradient: G exists for `vocab_chunk` columns at a time, in the workspace.
+ * Rows as there: ignored ones have logp 0 and G 0, targets outside [0, vocab) and logits of NaN or +inf give NaN (in dw as well, whose
+ * every row has a share of such a row; x of an ignored row has to be finite). */
+#define ASI_HEAD_MAX_ROWS (1 << 22)
+#define ASI_HEAD_MAX_VOCAB (1 << 24)
+#define ASI_HEAD_MAX_DIM (1 << 16)
+typedef struct {
+  int32_t in_dtype;              /* asi_dtype_t of x, w and dx */
+  int32_t dw_dtype;              /* of dw: ASI_F32, or in_dtype */
+  int64_t rows, vocab, dim;      /* rows may be 0 */
+  int64_t vocab_chunk;           /* columns of G in the workspace; 0: the library's choice */
+  int64_t ignore_index;
+  float scale;                   /* 1 / temperature, 1e-8 to 1e8 */
+  int32_t flags;                 /* 0 or ASI_FLAG_TEST_EXPIRE_WAIT */
+} asi_head_desc_t;
+/*   ws  device scratch of at least asi_head_ws_bytes(desc, grad), grad 0 for asi_head_logprobs, 1 for the others (0 for a descriptor that
+ *       is refused); it serves fewer rows of the same descriptor too */
+size_t asi_head_ws_bytes(const asi_head_desc_t* desc, int32_t grad);
+/*   x [in] device in_dtype [rows][dim], w [in] device in_dtype [vocab][dim], targets [in] device [rows]
+ *   logp, entropy, lse [out] device fp32 [rows];  entropy may be null */
+asi_status_t asi_head_logprobs(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, float* logp,
+                               float* entropy, float* lse, void* ws, size_t ws_bytes, void* stream);
+/*   lse, entropy [in] as asi_head_logprobs wrote them (entropy may be null where dentropy is)
+ *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
+ *   dx [out] device in_dtype [rows][dim];  dw [in/out] device dw_dtype [vocab][dim], written over, or added to what is there (accumulate
+ *      != 0).  One of them may be null */
+asi_status_t asi_head_grad(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* lse,
+                           const float* entropy, const float* dlogp, const float* dentropy, void* dx, void* dw, int32_t accumulate,
+                           void* ws, size_t ws_bytes, void* stream);
+/* Both, for weights that do not depend on the result. */
+asi_status_t asi_head_loss(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* dlogp,
+                           const float* dentropy, float* logp, float* entropy, float* lse, void* dx, void* dw, int32_t accumulate,
+                           void* ws, size_t ws_bytes, void* stream);
+/* The device status that the last call on `ws` left (ASI_OK or ASI_ERR_TIMEOUT).  Synchronises `stream`. */
+asi_status_t asi_head_status(const void* ws, void* stream, asi_status_t* device_status);
+
 /* Number of kernel launches the last call of each kind enqueues for this plan. */
 int32_t asi_launch_count(const asi_plan_t* plan, int32_t which /* 0 compress, 1 wgrad */);
 

@@ -38,9 +38,13 @@ EXPORTS = (
     "asi_profile_end", "asi_last_cuda_error",
     "asi_token_logprobs", "asi_token_logprobs_grad", "asi_token_loss",
     "asi_embedding_forward", "asi_embedding_wgrad_ws_bytes", "asi_embedding_wgrad", "asi_adamw_step",
+    "asi_dropout", "asi_branch_forward", "asi_branch_backward_ws_bytes", "asi_branch_backward",
+    "asi_head_ws_bytes", "asi_head_logprobs", "asi_head_grad", "asi_head_loss", "asi_head_status",
 )
 ASI_TOP_MAX = 32
 ASI_ADAMW_BLOCK = 256
+ASI_NORM_RMS, ASI_NORM_LAYER = 0, 1
+ASI_BRANCH_MAX_DIM = 8192
 
 
 class LayerDesc(C.Structure):
@@ -82,6 +86,27 @@ class AdamwDesc(C.Structure):
 class AdamwTensor(C.Structure):
     _fields_ = [("weight", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
                 ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64)]
+
+
+class Dropout(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("stream_id", C.c_uint32), ("step", C.c_int64), ("step_dev", C.c_void_p)]
+
+
+class BranchDesc(C.Structure):
+    _fields_ = [("in_dtype", C.c_int32), ("res_dtype", C.c_int32), ("norm", C.c_int32), ("norm_after", C.c_int32),
+                ("rows", C.c_int64), ("dim", C.c_int64), ("rows_per_gate", C.c_int64), ("eps", C.c_float), ("res_scale", C.c_float),
+                ("branch_scale", C.c_float), ("drop", Dropout)]
+
+
+class Branch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in (
+        "y", "h", "gate", "after_weight", "after_bias", "next_weight", "next_bias", "h_out", "x", "stats", "dx", "dh_out", "dy", "dh",
+        "dgate", "dafter_weight", "dafter_bias", "dnext_weight", "dnext_bias")]
+
+
+class HeadDesc(C.Structure):
+    _fields_ = [("in_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64), ("dim", C.c_int64),
+                ("vocab_chunk", C.c_int64), ("ignore_index", C.c_int64), ("scale", C.c_float), ("flags", C.c_int32)]
 
 
 class AsiError(RuntimeError):
@@ -147,6 +172,18 @@ def lib():
     L.asi_embedding_wgrad_ws_bytes.restype = sz
     L.asi_embedding_wgrad.argtypes = [pe, vp, vp, vp, i32, vp, sz, vp]
     L.asi_adamw_step.argtypes = [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), i32, vp]
+    pd, pb, pt, ph = C.POINTER(Dropout), C.POINTER(BranchDesc), C.POINTER(Branch), C.POINTER(HeadDesc)
+    L.asi_dropout.argtypes = [pd, i32, C.c_int64, vp, vp, vp, vp]
+    L.asi_branch_forward.argtypes = [pb, pt, vp]
+    L.asi_branch_backward_ws_bytes.argtypes = [pb]
+    L.asi_branch_backward_ws_bytes.restype = sz
+    L.asi_branch_backward.argtypes = [pb, pt, i32, vp, sz, vp]
+    L.asi_head_ws_bytes.argtypes = [ph, i32]
+    L.asi_head_ws_bytes.restype = sz
+    L.asi_head_logprobs.argtypes = [ph, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.asi_head_grad.argtypes = [ph, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    L.asi_head_loss.argtypes = [ph, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    L.asi_head_status.argtypes = [vp, vp, C.POINTER(i32)]
     L.asi_status_string.argtypes = [i32]
     L.asi_status_string.restype = C.c_char_p
     for name in ("asi_plan_create", "asi_plan_destroy", "asi_plan_query", "asi_compress", "asi_compress_static_ws",
@@ -154,7 +191,9 @@ def lib():
                  "asi_conv_wgrad", "asi_linear_wgrad", "asi_step_host",
                  "asi_poll_status", "asi_step_host_status", "asi_compress_batched", "asi_wgrad_batched",
                  "asi_mode_spectrum", "asi_pick_ranks", "asi_perplexity", "asi_token_logprobs", "asi_token_logprobs_grad",
-                 "asi_token_loss", "asi_embedding_forward", "asi_embedding_wgrad", "asi_adamw_step"):
+                 "asi_token_loss", "asi_embedding_forward", "asi_embedding_wgrad", "asi_adamw_step", "asi_dropout",
+                 "asi_branch_forward", "asi_branch_backward", "asi_head_logprobs", "asi_head_grad", "asi_head_loss",
+                 "asi_head_status"):
         getattr(L, name).restype = i32
     _lib = L
     return L
@@ -358,6 +397,52 @@ def embedding_wgrad(desc, ids, dOut, dW, accumulate, ws, ws_bytes, stream=0):
 def adamw_step(desc, tensors, count, stream=0):
     """asi_adamw_step over `count` entries of the AdamwTensor array `tensors`."""
     _check(lib().asi_adamw_step(desc, tensors, count, stream), "asi_adamw_step")
+
+
+def dropout(drop, dtype, n, x, residual, out, stream=0):
+    """asi_dropout: out = drop(x) [+ residual]; the gradient by the same call on dOut."""
+    _check(lib().asi_dropout(drop, dtype, n, x, residual, out, stream), "asi_dropout")
+
+
+def branch_forward(desc, buffers, stream=0):
+    """asi_branch_forward: norm after a block, gate, dropout, scales and residual sum, and the next block's norm."""
+    _check(lib().asi_branch_forward(desc, buffers, stream), "asi_branch_forward")
+
+
+def branch_backward_ws_bytes(desc):
+    return lib().asi_branch_backward_ws_bytes(desc)
+
+
+def branch_backward(desc, buffers, accumulate, ws, ws_bytes, stream=0):
+    """asi_branch_backward: the gradients of asi_branch_forward's inputs."""
+    _check(lib().asi_branch_backward(desc, buffers, int(accumulate), ws, ws_bytes, stream), "asi_branch_backward")
+
+
+def head_ws_bytes(desc, grad):
+    return lib().asi_head_ws_bytes(desc, int(grad))
+
+
+def head_logprobs(desc, x, w, targets, logp, entropy, lse, ws, ws_bytes, stream=0):
+    """asi_head_logprobs: log probabilities of the given tokens from hidden states and the output layer's weight."""
+    _check(lib().asi_head_logprobs(desc, x, w, targets, logp, entropy, lse, ws, ws_bytes, stream), "asi_head_logprobs")
+
+
+def head_grad(desc, x, w, targets, lse, entropy, dlogp, dentropy, dx, dw, accumulate, ws, ws_bytes, stream=0):
+    """asi_head_grad: the gradients of hidden states and weight from what asi_head_logprobs left."""
+    _check(lib().asi_head_grad(desc, x, w, targets, lse, entropy, dlogp, dentropy, dx, dw, int(accumulate), ws, ws_bytes, stream),
+           "asi_head_grad")
+
+
+def head_loss(desc, x, w, targets, dlogp, dentropy, logp, entropy, lse, dx, dw, accumulate, ws, ws_bytes, stream=0):
+    """asi_head_loss: both, for weights that are known before."""
+    _check(lib().asi_head_loss(desc, x, w, targets, dlogp, dentropy, logp, entropy, lse, dx, dw, int(accumulate), ws, ws_bytes, stream),
+           "asi_head_loss")
+
+
+def head_status(ws, stream=0):
+    out = C.c_int32(0)
+    _check(lib().asi_head_status(ws, stream, C.byref(out)), "asi_head_status")
+    return out.value
 
 
 KERNEL_IDS = {"modeprod": 1, "expand": 2, "qr": 3, "conv_tail": 4, "sm_pass1": 5, "sm_core": 6,

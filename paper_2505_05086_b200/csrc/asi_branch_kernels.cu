@@ -1,0 +1,731 @@
+// A block's end: dropout by a counter-based generator, and what joins a branch to the residual stream, with its gradient.
+//
+//   out = keep(e) x / (1 - p) [+ residual]
+//   z = norm(y);  h' = r h + b drop(gate z);  x = norm(h')
+//
+// and backwards, with hats for what a norm made of its input before weight and bias, D values a row:
+//   a = dx w_n;  d = dh' + s_n (a - h^ mean(a h^) - mean a);   dh = r d;   u = drop(b d);   v = gate u w_a
+//   dy = s_a (v - y^ mean(v y^) - mean v);   dgate = sum u z,  dw_a = sum gate u y^,  db_a = sum gate u,  dw_n = sum dx h^,  db_n = sum dx
+// (mean a and mean v are layer norm's alone).  With S1 = sum u y^ and S0 = sum u over the rows of a gate's row:
+//   dgate = w_a S1 + b_a S0,  dw_a = sum over the gate's rows of gate S1,  db_a = sum of gate S0.
+//
+// What bounds them: bytes.  A thread keeps eight values of its row in registers, a row's sums meet in shared memory, and what the
+// backward pass sums over rows stays in the threads' registers from row to row: each worker (the threads of a row) takes
+// neighbouring rows and leaves one partial sum a column, which k_branch_sums adds up in order.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "asi_internal.h"
+#include "asi_philox.h"
+
+namespace asi {
+
+namespace {
+
+constexpr int kEach = 8;                   // values of a thread: a group of the generator
+constexpr int kDropThreads = 256;
+
+struct Drop {
+  uint64_t seed;
+  const int64_t* step_dev;
+  uint32_t stream, step, below;            // dropped where sixteen bits are below `below`; 0: nothing is
+  float more;                              // 65536 / (65536 - below)
+};
+
+__device__ __forceinline__ uint32_t step_of(const Drop& d) { return d.step_dev ? (uint32_t)*d.step_dev : d.step; }
+__device__ __forceinline__ Words words_of(const Drop& d, uint32_t step, uint64_t group) {
+  return philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), d.stream, step, (uint32_t)d.seed, (uint32_t)(d.seed >> 32));
+}
+__device__ __forceinline__ bool kept(const Drop& d, const Words& w, int j) {
+  const uint32_t x = w.w[j >> 1];
+  return (j & 1 ? x >> 16 : x & 0xffffu) >= d.below;
+}
+__device__ __forceinline__ bool kept_alone(const Drop& d, uint32_t step, uint64_t e) {
+  const Words w = words_of(d, step, e >> 3);
+  const int j = (int)(e & 7);
+  const uint32_t x = j < 4 ? (j < 2 ? w.w[0] : w.w[1]) : (j < 6 ? w.w[2] : w.w[3]);
+  return (j & 1 ? x >> 16 : x & 0xffffu) >= d.below;
+}
+
+// eight neighbouring values, 16-byte aligned
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[kEach]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(u[i] << 16), f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void load8(const float* p, float (&f)[kEach]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&f)[kEach]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&f)[kEach]) {
+  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+template <typename T>
+__device__ __forceinline__ float stored(float x) {
+  if constexpr (sizeof(T) == 2) return __bfloat162float(__float2bfloat16_rn(x));
+  else return x;
+}
+
+struct DropoutArgs {
+  const void *x, *res;
+  void* out;
+  int64_t n;
+  Drop drop;
+};
+
+// A group of eight a thread.  (The words need nothing that the kernel before has written, but for a step number on the device.)
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kDropThreads) k_dropout(const __grid_constant__ DropoutArgs p) {
+  const int64_t g = (int64_t)blockIdx.x * kDropThreads + threadIdx.x, at = g * kEach;
+  if (p.drop.step_dev) pdl_wait();
+  const Words w = words_of(p.drop, step_of(p.drop), (uint64_t)g);
+  if (!p.drop.step_dev) pdl_wait();
+  pdl_launch_dependents();
+  if (at >= p.n) return;
+  const T *x = static_cast<const T*>(p.x) + at, *res = p.res ? static_cast<const T*>(p.res) + at : nullptr;
+  T* out = static_cast<T*>(p.out) + at;
+  if (kVec && at + kEach <= p.n) {
+    float f[kEach], r[kEach];
+    load8(x, f);
+    if (res) load8(res, r);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      f[i] = kept(p.drop, w, i) ? f[i] * p.drop.more : 0.f;
+      if (res) f[i] += r[i];
+    }
+    store8(out, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (at + i < p.n) {
+        const float f = kept(p.drop, w, i) ? value(x[i]) * p.drop.more : 0.f;
+        put(out + i, res ? f + value(res[i]) : f);
+      }
+  }
+}
+
+struct BranchArgs {
+  const void *y, *h;
+  const float *gate, *aw, *ab, *nw, *nb;
+  void *h_out, *x;
+  float* stats;
+  const void *dx, *dh_out;
+  void *dy, *dh;
+  float *dgate, *daw, *dab, *dnw, *dnb;
+  float* part;             // [kParts][workers][dim]
+  int64_t rows, per;       // rows of a gate's row
+  int64_t run;             // rows of a worker (backward)
+  int workers, dim, norm_after, accumulate;
+  float eps, rs, bs, inv_dim;
+  Drop drop;
+};
+// partial sums of a worker: over the first of its gate's rows, over the last one, over all
+enum Part { kHead1 = 0, kTail1 = 1, kNext1 = 2, kAfter1 = 3, kHead0 = 4, kTail0 = 5, kNext0 = 6, kAfter0 = 7, kParts = 8 };
+
+// sums of two values over the threads of a row, for all of them (tpr a multiple of 32; rows side by side in y)
+struct RowSum {
+  float2 (*sh)[32];        // [2][rows of the CTA]
+  int phase = 0;
+  __device__ __forceinline__ float2 operator()(float a, float b) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o), b += __shfl_xor_sync(~0u, b, o);
+    const int warps = blockDim.x >> 5;
+    if (warps == 1) return make_float2(a, b);
+    float2* s = sh[phase * blockDim.y + threadIdx.y];
+    phase ^= 1;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) s[threadIdx.x >> 5] = make_float2(a, b);
+    __syncthreads();
+    const float2 v = lane < warps ? s[lane] : make_float2(0.f, 0.f);
+    a = v.x, b = v.y;
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+      if (o < warps || (warps & (warps - 1))) a += __shfl_xor_sync(~0u, a, o), b += __shfl_xor_sync(~0u, b, o);
+    a = __shfl_sync(~0u, a, 0), b = __shfl_sync(~0u, b, 0);
+    return make_float2(a, b);
+  }
+};
+
+// A thread's columns: eight neighbours, or (rows off 16 bytes) eight a row's threads apart.
+template <bool kVec>
+struct Columns {
+  int first, step, dim;
+  __device__ __forceinline__ Columns(int d) : first(kVec ? threadIdx.x * kEach : threadIdx.x), step(kVec ? 1 : blockDim.x), dim(d) {}
+  __device__ __forceinline__ int at(int i) const { return first + i * step; }
+  __device__ __forceinline__ bool there(int i) const { return kVec ? first < dim : at(i) < dim; }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, float (&f)[kEach], bool any = true) const {
+    if constexpr (kVec) {
+      if (any && first < dim) {
+        load8(row + first, f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) f[i] = 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) f[i] = any && at(i) < dim ? value(row[at(i)]) : 0.f;
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, const float (&f)[kEach]) const {
+    if constexpr (kVec) {
+      if (first < dim) store8(row + first, f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (at(i) < dim) put(row + at(i), f[i]);
+    }
+  }
+  // fp32 parameters, `none` where there are none; they start at any float
+  __device__ __forceinline__ void param(const float* p, float (&f)[kEach], float none, bool wide) const {
+    if (!p) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) f[i] = none;
+    } else if (kVec && wide) {
+      load(p, f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) f[i] = there(i) ? __ldg(p + at(i)) : 0.f;
+    }
+  }
+  // f to drop(f) in row t
+  __device__ __forceinline__ void mask(const Drop& d, uint32_t step_no, int64_t t, float (&f)[kEach]) const {
+    const uint64_t e = (uint64_t)t * dim + first;
+    if constexpr (kVec) {
+      const Words w = words_of(d, step_no, e >> 3);         // (dim is a multiple of eight)
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) f[i] = kept(d, w, i) ? f[i] * d.more : 0.f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (at(i) < dim) f[i] = kept_alone(d, step_no, e + (uint64_t)i * step) ? f[i] * d.more : 0.f;
+    }
+  }
+};
+
+__device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// mean (layer norm) and reciprocal deviation of a row; f without its mean on return
+template <bool kLayer, bool kVec>
+__device__ __forceinline__ float2 normalise(float (&f)[kEach], const Columns<kVec>& c, const BranchArgs& p, RowSum& sum) {
+  float m = 0.f;
+  if constexpr (kLayer) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) s += f[i];
+    m = sum(s, 0.f).x * p.inv_dim;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] = c.there(i) ? f[i] - m : 0.f;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) q = fmaf(f[i], f[i], q);
+  const float r = 1.f / sqrtf(sum(q, 0.f).x * p.inv_dim + p.eps);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) f[i] *= r;
+  return make_float2(m, r);
+}
+
+template <typename TI, typename TR, bool kVec, bool kLayer>
+__global__ void __launch_bounds__(1024) k_branch_forward(const __grid_constant__ BranchArgs p) {
+  __shared__ float2 sh[2 * 8][32];
+  pdl_wait();
+  pdl_launch_dependents();
+  RowSum sum{sh};
+  const Columns<kVec> c(p.dim);
+  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const bool there = t < p.rows;
+  const int64_t at = there ? t * p.dim : 0;
+  float f[kEach], h[kEach], w[kEach], b[kEach];
+  c.load(static_cast<const TI*>(p.y) + at, f, there);
+  c.load(static_cast<const TR*>(p.h) + at, h, there && p.h);
+  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (p.norm_after) {
+    const float2 s = normalise<kLayer>(f, c, p, sum);
+    st.x = s.x, st.y = s.y;
+    c.param(p.aw, w, 1.f, on16(p.aw));
+    c.param(p.ab, b, 0.f, on16(p.ab));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] = fmaf(f[i], w[i], b[i]);
+  }
+  if (p.gate) {
+    const float* gate = p.gate + (there ? t / p.per : 0) * p.dim;
+    c.param(gate, w, 1.f, on16(gate));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] *= w[i];
+  }
+  if (p.drop.below && there) c.mask(p.drop, step_of(p.drop), t, f);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) f[i] = c.there(i) ? stored<TR>(fmaf(p.bs, f[i], p.rs * h[i])) : 0.f;
+  if (there) c.store(static_cast<TR*>(p.h_out) + at, f);
+  if (p.x) {
+    const float2 s = normalise<kLayer>(f, c, p, sum);
+    st.z = s.x, st.w = s.y;
+    c.param(p.nw, w, 1.f, on16(p.nw));
+    c.param(p.nb, b, 0.f, on16(p.nb));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] = fmaf(f[i], w[i], b[i]);
+    if (there) c.store(static_cast<TI*>(p.x) + at, f);
+  }
+  if (there && threadIdx.x == 0) {
+    float* s = p.stats + 4 * t;
+    if (on16(s)) *reinterpret_cast<float4*>(s) = st;
+    else s[0] = st.x, s[1] = st.y, s[2] = st.z, s[3] = st.w;
+  }
+}
+
+// dgate of a gate's row from its sums
+template <bool kVec>
+__device__ __forceinline__ void put_gate(const BranchArgs& p, const Columns<kVec>& c, int64_t s, const float (&s1)[kEach], const float (&s0)[kEach]) {
+  float w[kEach], b[kEach];
+  c.param(p.aw, w, 1.f, on16(p.aw));
+  c.param(p.ab, b, 0.f, on16(p.ab));
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (c.there(i)) {
+      float* g = p.dgate + s * p.dim + c.at(i);
+      const float v = fmaf(w[i], s1[i], b[i] * s0[i]);
+      *g = p.accumulate ? *g + v : v;
+    }
+}
+
+// kGroups: the gate has several rows
+template <typename TI, typename TR, bool kVec, bool kLayer, bool kGroups>
+__global__ void __launch_bounds__(1024) k_branch_backward(const __grid_constant__ BranchArgs p) {
+  __shared__ float2 sh[2 * 8][32];
+  pdl_wait();
+  pdl_launch_dependents();
+  RowSum sum{sh};
+  const Columns<kVec> c(p.dim);
+  const int worker = blockIdx.x * blockDim.y + threadIdx.y;
+  const int64_t t0 = worker * p.run, t1 = t0 + p.run < p.rows ? t0 + p.run : p.rows;
+  const uint32_t step = p.drop.below ? step_of(p.drop) : 0;
+  float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {}, a1[kEach] = {}, a0[kEach] = {};
+  const int64_t first = kGroups && p.per ? t0 / p.per : 0;
+  int64_t group = first;
+  auto part = [&](int which) { return p.part + ((int64_t)which * p.workers + worker) * p.dim; };
+  // the sums over the worker's rows of one of the gate's
+  auto flush = [&](bool whole) {
+    float gate[kEach];
+    c.param(p.gate + group * p.dim, gate, 1.f, on16(p.gate + group * p.dim));
+    if (p.dgate) {
+      if (whole) {
+        put_gate(p, c, group, s1, s0);
+      } else {
+        float *q1 = part(group == first ? kHead1 : kTail1), *q0 = part(group == first ? kHead0 : kTail0);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+          if (c.there(i)) {
+            q1[c.at(i)] = s1[i];
+            if (kLayer) q0[c.at(i)] = s0[i];
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      a1[i] = fmaf(gate[i], s1[i], a1[i]), s1[i] = 0.f;
+      if (kLayer) a0[i] = fmaf(gate[i], s0[i], a0[i]), s0[i] = 0.f;
+    }
+  };
+#pragma unroll 1
+  for (int64_t k = 0; k < p.run; ++k) {                    // (rows side by side in a CTA go on together: their sums share barriers)
+    const int64_t t = t0 + k;
+    const bool there = t < t1;
+    const int64_t at = there ? t * p.dim : 0;
+    float d[kEach], f[kEach], w[kEach];
+    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (there) {
+      const float* s = p.stats + 4 * t;
+      if (on16(s)) st = *reinterpret_cast<const float4*>(s);
+      else st = make_float4(s[0], s[1], s[2], s[3]);
+    }
+    c.load(static_cast<const TR*>(p.dh_out) + at, d, there && p.dh_out);
+    if (p.dx) {
+      float x[kEach];
+      c.load(static_cast<const TI*>(p.dx) + at, x, there);
+      c.load(static_cast<const TR*>(p.h_out) + at, f, there);
+      c.param(p.nw, w, 1.f, on16(p.nw));
+      float q1 = 0.f, q0 = 0.f;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        f[i] = c.there(i) ? (f[i] - st.z) * st.w : 0.f;
+        n1[i] = fmaf(x[i], f[i], n1[i]);
+        if (kLayer) n0[i] += x[i];
+        w[i] *= x[i];
+        q1 = fmaf(w[i], f[i], q1);
+        if (kLayer) q0 += w[i];
+      }
+      const float2 m = sum(q1, q0);
+      const float m1 = m.x * p.inv_dim, m0 = kLayer ? m.y * p.inv_dim : 0.f;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) d[i] += st.w * (w[i] - m0 - f[i] * m1);
+    }
+    if (p.dh && there) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) w[i] = p.rs * d[i];
+      c.store(static_cast<TR*>(p.dh) + at, w);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) d[i] = c.there(i) ? p.bs * d[i] : 0.f;
+    if (p.drop.below && there) c.mask(p.drop, step, t, d);
+    c.load(static_cast<const TI*>(p.y) + at, f, there);
+    if (kGroups && there && t / p.per != group) {
+      flush(group != first || first * p.per >= t0);
+      group = t / p.per;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (p.norm_after) f[i] = c.there(i) ? (f[i] - st.x) * st.y : 0.f;
+      s1[i] = there ? fmaf(d[i], f[i], s1[i]) : s1[i];
+      if (kLayer) s0[i] = there ? s0[i] + d[i] : s0[i];
+    }
+    if (p.gate) {
+      const float* gate = p.gate + (kGroups ? group * p.dim : 0);
+      c.param(gate, w, 1.f, on16(gate));
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) d[i] *= w[i];
+    }
+    if (p.norm_after) {
+      c.param(p.aw, w, 1.f, on16(p.aw));
+      float q1 = 0.f, q0 = 0.f;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        d[i] *= w[i];
+        q1 = fmaf(d[i], f[i], q1);
+        if (kLayer) q0 += d[i];
+      }
+      const float2 m = sum(q1, q0);
+      const float m1 = m.x * p.inv_dim, m0 = kLayer ? m.y * p.inv_dim : 0.f;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) d[i] = st.y * (d[i] - m0 - f[i] * m1);
+    }
+    if (there) c.store(static_cast<TI*>(p.dy) + at, d);
+  }
+  if (t0 >= p.rows) return;
+  if (kGroups) {
+    const int64_t end = (group + 1) * p.per < p.rows ? (group + 1) * p.per : p.rows;
+    flush((group != first || first * p.per >= t0) && end <= t1);
+  }
+  if (!p.part) return;
+  auto keep = [&](int which, const float (&v)[kEach]) {
+    float* q = part(which);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (c.there(i)) q[c.at(i)] = v[i];
+  };
+  if (!kGroups && (p.dgate || p.daw)) keep(kHead1, s1);
+  if (!kGroups && kLayer && (p.dgate || p.dab)) keep(kHead0, s0);
+  if (kGroups && p.daw) keep(kAfter1, a1);
+  if (kGroups && kLayer && p.dab) keep(kAfter0, a0);
+  if (p.dnw) keep(kNext1, n1);
+  if (kLayer && p.dnb) keep(kNext0, n0);
+}
+
+// The workers' sums joined in order: 32 columns a CTA, 32 shares of the workers side by side.  blockIdx.y 0: of the next norm, 1: of the
+// norm after and of a gate of one row; 2 ..: rows of a gate that workers share
+constexpr int kSlices = 32;
+struct SumsArgs {
+  BranchArgs b;
+  int layer, groups;
+};
+__global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_constant__ SumsArgs a) {
+  __shared__ float sh[2][kSlices][33];
+  const BranchArgs& p = a.b;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  // of partial sums `one` and `two` (or none) over workers w0 .. w1; the first worker's from `one0` and `two0`
+  auto total = [&](int one0, int one, int two0, int two, int64_t w0, int64_t w1) {
+    float x = 0.f, y = 0.f;
+    if (col < p.dim)
+#pragma unroll 4
+      for (int64_t w = w0 + slice; w <= w1; w += kSlices) {
+        x += p.part[((int64_t)(w == w0 ? one0 : one) * p.workers + w) * p.dim + col];
+        if (two >= 0) y += p.part[((int64_t)(w == w0 ? two0 : two) * p.workers + w) * p.dim + col];
+      }
+    __syncthreads();
+    sh[0][slice][lane] = x, sh[1][slice][lane] = y;
+    __syncthreads();
+    float2 r = make_float2(0.f, 0.f);
+    if (slice == 0)
+      for (int i = 0; i < kSlices; ++i) r.x += sh[0][i][lane], r.y += sh[1][i][lane];
+    return r;
+  };
+  auto write = [&](float* out, float v) {
+    if (out && slice == 0 && col < p.dim) out[col] = p.accumulate ? out[col] + v : v;
+  };
+  const int64_t last = (p.rows - 1) / p.run;
+  if (blockIdx.y == 0) {
+    if (!p.dnw && !p.dnb) return;
+    const bool one = p.dnw != nullptr, two = p.dnb && a.layer;
+    const float2 r = total(one ? kNext1 : kNext0, one ? kNext1 : kNext0, kNext0, one && two ? kNext0 : -1, 0, last);
+    if (one) write(p.dnw, r.x);
+    if (two) write(p.dnb, one ? r.y : r.x);
+  } else if (blockIdx.y == 1) {
+    if (a.groups) {
+      if (p.daw) write(p.daw, total(kAfter1, kAfter1, 0, -1, 0, last).x);
+      if (p.dab) write(p.dab, total(kAfter0, kAfter0, 0, -1, 0, last).x);
+      return;
+    }
+    if (!p.dgate && !p.daw && !p.dab) return;
+    float2 r = make_float2(0.f, 0.f);
+    if (p.dgate || p.daw) r.x = total(kHead1, kHead1, 0, -1, 0, last).x;
+    if (a.layer && (p.dgate || p.dab)) r.y = total(kHead0, kHead0, 0, -1, 0, last).x;
+    if (slice || col >= p.dim) return;
+    const float w = p.aw ? p.aw[col] : 1.f, b = p.ab ? p.ab[col] : 0.f, g = p.gate ? p.gate[col] : 1.f;
+    write(p.dgate, fmaf(w, r.x, b * r.y));
+    write(p.daw, g * r.x);
+    write(p.dab, g * r.y);
+  } else {
+    for (int64_t s = blockIdx.y - 2; s * p.per < p.rows; s += gridDim.y - 2) {
+      const int64_t end = (s + 1) * p.per < p.rows ? (s + 1) * p.per : p.rows, w0 = s * p.per / p.run, w1 = (end - 1) / p.run;
+      if (w0 == w1) continue;                             // its worker wrote it
+      const bool head = w0 * p.run / p.per == s;          // the first worker's first row is the gate row's too
+      const float2 r = total(head ? kHead1 : kTail1, kHead1, head ? kHead0 : kTail0, a.layer ? kHead0 : -1, w0, w1);
+      if (slice == 0 && col < p.dim) {
+        const float w = p.aw ? p.aw[col] : 1.f, b = p.ab ? p.ab[col] : 0.f;
+        float* g = p.dgate + s * p.dim + col;
+        const float v = fmaf(w, r.x, b * r.y);
+        *g = p.accumulate ? *g + v : v;
+      }
+    }
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------
+
+size_t size_of(int dtype) { return dtype == ASI_BF16 ? 2 : 4; }
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool make_drop(const asi_dropout_t& d, Drop* out) {
+  if (!(d.p >= 0.0 && d.p < 1.0) || d.step < 0 || off_element(d.step_dev, 8)) return false;
+  const double k = std::floor(d.p * 65536.0 + 0.5);
+  if (k >= 65536.0) return false;
+  out->seed = d.seed;
+  out->step_dev = d.step_dev;
+  out->stream = d.stream_id;
+  out->step = (uint32_t)d.step;
+  out->below = (uint32_t)k;
+  out->more = (float)(65536.0 / (65536.0 - k));
+  return true;
+}
+
+// A contiguous buffer of a call; null where the call has none
+struct Span {
+  const void* p;
+  size_t bytes, element;
+  const void* same = nullptr;   // the buffer that it may be
+  bool meets(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && a < b + o.bytes && b < a + bytes;
+  }
+};
+
+// every buffer on an element, what is written apart from what else there is (but for the buffer that it may be, from its start)
+bool fine(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+  for (const auto* list : {&in, &out})
+    for (const Span& s : *list)
+      if (s.p && off_element(s.p, s.element)) return false;
+  for (const Span* o = out.begin(); o != out.end(); ++o) {
+    for (const Span* q = out.begin(); q != o; ++q)
+      if (o->meets(*q)) return false;
+    for (const Span& i : in)
+      if (o->meets(i) && !(o->p == i.p && o->same == i.p && o->bytes == i.bytes)) return false;
+  }
+  return true;
+}
+
+asi_status_t check_desc(const asi_branch_desc_t* d, Drop* drop) {
+  if (!d || (d->in_dtype != ASI_F32 && d->in_dtype != ASI_BF16) || (d->res_dtype != ASI_F32 && d->res_dtype != d->in_dtype)) return ASI_ERR_INVALID_ARG;
+  if ((d->norm != ASI_NORM_RMS && d->norm != ASI_NORM_LAYER) || d->rows < 0 || d->dim < 1 || d->rows_per_gate < 0) return ASI_ERR_INVALID_ARG;
+  if (!(d->eps >= 1e-30f) || !std::isfinite(d->eps) || !std::isfinite(d->res_scale) || !std::isfinite(d->branch_scale)) return ASI_ERR_INVALID_ARG;
+  if (!make_drop(d->drop, drop)) return ASI_ERR_INVALID_ARG;
+  if (d->rows > ASI_BRANCH_MAX_ROWS || d->dim > ASI_BRANCH_MAX_DIM) return ASI_ERR_UNSUPPORTED;
+  return ASI_OK;
+}
+
+// threads of a row, and rows of a CTA
+struct Shape {
+  int tpr, rows;
+};
+Shape shape_of(int64_t dim) {
+  const int tpr = (int)align_up((size_t)ceil_div(dim, kEach), 32);
+  return {tpr, std::max(1, std::min(8, 256 / tpr))};
+}
+// rows of a worker and workers: two CTAs of 256 threads an SM or what has as many threads
+struct Work {
+  int64_t run;
+  int workers;
+};
+Work work_of(int64_t rows, int64_t dim) {
+  const Shape s = shape_of(dim);
+  const int64_t most = (int64_t)148 * std::max(1, 512 / (s.tpr * s.rows)) * s.rows;
+  const int64_t run = std::max<int64_t>(1, ceil_div(rows, most));
+  return {run, (int)std::max<int64_t>(1, ceil_div(rows, run))};
+}
+size_t part_bytes(int64_t rows, int64_t dim) {
+  const Shape s = shape_of(dim);
+  const int64_t most = (int64_t)148 * std::max(1, 512 / (s.tpr * s.rows)) * s.rows;
+  return align_up((size_t)kParts * std::max<int64_t>(1, std::min(rows, most)) * dim * 4, 256);
+}
+
+BranchArgs args_of(const asi_branch_desc_t* d, const asi_branch_t* t, const Drop& drop) {
+  BranchArgs a = {};
+  a.y = t->y, a.gate = d->rows_per_gate ? t->gate : nullptr;
+  a.aw = t->after_weight, a.ab = t->after_bias, a.nw = t->next_weight, a.nb = t->next_bias;
+  a.stats = t->stats;
+  a.rows = d->rows, a.per = d->rows_per_gate, a.dim = (int)d->dim, a.norm_after = d->norm_after != 0;
+  a.eps = d->eps, a.rs = d->res_scale, a.bs = d->branch_scale, a.inv_dim = 1.f / (float)d->dim;
+  a.drop = drop;
+  return a;
+}
+
+template <typename TI, typename TR, bool kVec>
+cudaError_t launch_forward(const BranchArgs& a, bool layer, cudaStream_t st) {
+  const Shape s = shape_of(a.dim);
+  const dim3 grid((unsigned)ceil_div(a.rows, s.rows)), block(s.tpr, s.rows);
+  return layer ? launch_pdl(k_branch_forward<TI, TR, kVec, true>, grid, block, 0, st, a) : launch_pdl(k_branch_forward<TI, TR, kVec, false>, grid, block, 0, st, a);
+}
+
+template <typename TI, typename TR, bool kVec>
+cudaError_t launch_backward(BranchArgs& a, bool layer, cudaStream_t st) {
+  const Shape s = shape_of(a.dim);
+  const Work k = work_of(a.rows, a.dim);
+  a.run = k.run;
+  a.workers = k.workers;
+  const bool groups = a.gate && a.per < a.rows;
+  const dim3 grid((unsigned)ceil_div(k.workers, s.rows)), block(s.tpr, s.rows);
+  cudaError_t e;
+  if (layer) e = groups ? launch_pdl(k_branch_backward<TI, TR, kVec, true, true>, grid, block, 0, st, a) : launch_pdl(k_branch_backward<TI, TR, kVec, true, false>, grid, block, 0, st, a);
+  else e = groups ? launch_pdl(k_branch_backward<TI, TR, kVec, false, true>, grid, block, 0, st, a) : launch_pdl(k_branch_backward<TI, TR, kVec, false, false>, grid, block, 0, st, a);
+  if (e != cudaSuccess || !a.part) return e;
+  const SumsArgs q = {a, layer, groups};
+  const int64_t shared = groups && a.dgate && a.per > 1 ? std::min<int64_t>(ceil_div(a.rows, a.per), 1024) : 0;
+  return launch_pdl(k_branch_sums, dim3((unsigned)ceil_div(a.dim, 32), (unsigned)(2 + shared)), dim3(32 * kSlices), 0, st, q);
+}
+
+}  // namespace
+}  // namespace asi
+
+using namespace asi;
+
+extern "C" {
+
+asi_status_t asi_dropout(const asi_dropout_t* drop, int32_t dtype, int64_t n, const void* x, const void* residual, void* out, void* stream) {
+  DropoutArgs a = {};
+  if (!drop || (dtype != ASI_F32 && dtype != ASI_BF16) || n < 0 || !make_drop(*drop, &a.drop)) return ASI_ERR_INVALID_ARG;
+  if (n > (int64_t)1 << 40) return ASI_ERR_UNSUPPORTED;
+  if (n == 0) return ASI_OK;
+  const size_t e = size_of(dtype), bytes = (size_t)n * e;
+  if (!x || !out) return ASI_ERR_INVALID_ARG;
+  if (!fine({{x, bytes, e}, {residual == x ? nullptr : residual, bytes, e}, {drop->step_dev, 8, 8}}, {{out, bytes, e, residual && out == residual ? residual : x}}))
+    return ASI_ERR_INVALID_ARG;
+  a.x = x, a.res = residual, a.out = out, a.n = n;
+  const bool vec = aligned(x, 16) && aligned(out, 16) && (!residual || aligned(residual, 16));
+  const dim3 grid((unsigned)ceil_div(ceil_div(n, kEach), kDropThreads)), block(kDropThreads);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t r;
+  if (dtype == ASI_BF16) r = vec ? launch_pdl(k_dropout<__nv_bfloat16, true>, grid, block, 0, st, a) : launch_pdl(k_dropout<__nv_bfloat16, false>, grid, block, 0, st, a);
+  else r = vec ? launch_pdl(k_dropout<float, true>, grid, block, 0, st, a) : launch_pdl(k_dropout<float, false>, grid, block, 0, st, a);
+  return cuda_status(r, "dropout");
+}
+
+asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_t* t, void* stream) {
+  Drop drop = {};
+  const asi_status_t s = check_desc(desc, &drop);
+  if (s != ASI_OK) return s;
+  if (!t) return ASI_ERR_INVALID_ARG;
+  if (desc->rows == 0) return ASI_OK;
+  if (!t->y || !t->h_out || !t->stats || (desc->rows_per_gate && !t->gate) || (!desc->norm_after && (t->after_weight || t->after_bias))) return ASI_ERR_INVALID_ARG;
+  const size_t ei = size_of(desc->in_dtype), er = size_of(desc->res_dtype), n = (size_t)desc->rows * desc->dim, w = (size_t)desc->dim * 4;
+  const size_t gates = desc->rows_per_gate ? (size_t)ceil_div(desc->rows, desc->rows_per_gate) * w : 0;
+  const float* gate = desc->rows_per_gate ? t->gate : nullptr;
+  if (!fine({{t->y, n * ei, ei}, {t->h, n * er, er}, {gate, gates, 4}, {t->after_weight, w, 4}, {t->after_bias, w, 4}, {t->next_weight, w, 4},
+             {t->next_bias, w, 4}, {desc->drop.step_dev, 8, 8}},
+            {{t->h_out, n * er, er, t->h}, {t->x, n * ei, ei}, {t->stats, (size_t)desc->rows * 16, 4}}))
+    return ASI_ERR_INVALID_ARG;
+  BranchArgs a = args_of(desc, t, drop);
+  a.h = t->h, a.h_out = t->h_out, a.x = t->x;
+  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 16) && aligned(a.h, 16) && aligned(a.h_out, 16) && aligned(a.x, 16);
+  const bool layer = desc->norm == ASI_NORM_LAYER;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  using B = __nv_bfloat16;
+  cudaError_t e;
+  if (desc->in_dtype == ASI_F32) e = vec ? launch_forward<float, float, true>(a, layer, st) : launch_forward<float, float, false>(a, layer, st);
+  else if (desc->res_dtype == ASI_F32) e = vec ? launch_forward<B, float, true>(a, layer, st) : launch_forward<B, float, false>(a, layer, st);
+  else e = vec ? launch_forward<B, B, true>(a, layer, st) : launch_forward<B, B, false>(a, layer, st);
+  return cuda_status(e, "branch and residual stream");
+}
+
+size_t asi_branch_backward_ws_bytes(const asi_branch_desc_t* desc) {
+  Drop drop = {};
+  return check_desc(desc, &drop) == ASI_OK ? part_bytes(desc->rows, desc->dim) : 0;
+}
+
+asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch_t* t, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  Drop drop = {};
+  const asi_status_t s = check_desc(desc, &drop);
+  if (s != ASI_OK) return s;
+  if (!t) return ASI_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const size_t ei = size_of(desc->in_dtype), er = size_of(desc->res_dtype), n = (size_t)desc->rows * desc->dim, w = (size_t)desc->dim * 4;
+  const bool layer = desc->norm == ASI_NORM_LAYER;
+  if ((t->dgate && !desc->rows_per_gate) || (!desc->norm_after && (t->dafter_weight || t->dafter_bias || t->after_weight || t->after_bias))) return ASI_ERR_INVALID_ARG;
+  if (desc->rows == 0) {                                   // sums of nothing (a gate has no rows then)
+    if (accumulate) return ASI_OK;
+    for (float* p : {t->dafter_weight, t->dafter_bias, t->dnext_weight, t->dnext_bias}) {
+      if (p && off_element(p, 4)) return ASI_ERR_INVALID_ARG;
+      const cudaError_t e = p ? cudaMemsetAsync(p, 0, w, st) : cudaSuccess;
+      if (e != cudaSuccess) return cuda_status(e, "sums of no rows");
+    }
+    return ASI_OK;
+  }
+  if (!t->y || !t->stats || !t->dy || (!t->dx && !t->dh_out) || (t->dx && !t->h_out) || (desc->rows_per_gate && !t->gate)) return ASI_ERR_INVALID_ARG;
+  if (!t->dx && (t->dnext_weight || t->dnext_bias)) return ASI_ERR_INVALID_ARG;
+  const size_t gates = desc->rows_per_gate ? (size_t)ceil_div(desc->rows, desc->rows_per_gate) * w : 0;
+  const float* gate = desc->rows_per_gate ? t->gate : nullptr;
+  const size_t need = part_bytes(desc->rows, desc->dim);
+  const bool sums = t->dgate || t->dafter_weight || t->dafter_bias || t->dnext_weight || t->dnext_bias;
+  if (!ws) return ASI_ERR_INVALID_ARG;
+  if (ws_bytes < need || !aligned(ws, 256)) return ASI_ERR_WORKSPACE;
+  if (!fine({{t->y, n * ei, ei}, {t->dx ? t->h_out : nullptr, n * er, er}, {t->stats, (size_t)desc->rows * 16, 4}, {gate, gates, 4}, {t->after_weight, w, 4},
+             {t->after_bias, w, 4}, {t->dx ? t->next_weight : nullptr, w, 4}, {t->dx, n * ei, ei}, {t->dh_out, n * er, er}, {desc->drop.step_dev, 8, 8}},
+            {{t->dy, n * ei, ei, t->dx}, {t->dh, n * er, er, t->dh_out}, {t->dgate, gates, 4}, {t->dafter_weight, w, 4}, {t->dafter_bias, w, 4},
+             {t->dnext_weight, w, 4}, {t->dnext_bias, w, 4}, {ws, need, 256}}))
+    return ASI_ERR_INVALID_ARG;
+  BranchArgs a = args_of(desc, t, drop);
+  a.h_out = t->h_out;
+  a.dx = t->dx, a.dh_out = t->dh_out, a.dy = t->dy, a.dh = t->dh;
+  a.dgate = t->dgate, a.daw = t->dafter_weight, a.dab = t->dafter_bias, a.dnw = t->dnext_weight, a.dnb = t->dnext_bias;
+  a.accumulate = accumulate != 0;
+  a.part = sums ? static_cast<float*>(ws) : nullptr;
+  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 16) && aligned(t->dx ? a.h_out : nullptr, 16) && aligned(a.dx, 16) && aligned(a.dh_out, 16) &&
+                   aligned(a.dy, 16) && aligned(a.dh, 16);
+  using B = __nv_bfloat16;
+  cudaError_t e;
+  if (desc->in_dtype == ASI_F32) e = vec ? launch_backward<float, float, true>(a, layer, st) : launch_backward<float, float, false>(a, layer, st);
+  else if (desc->res_dtype == ASI_F32) e = vec ? launch_backward<B, float, true>(a, layer, st) : launch_backward<B, float, false>(a, layer, st);
+  else e = vec ? launch_backward<B, B, true>(a, layer, st) : launch_backward<B, B, false>(a, layer, st);
+  return cuda_status(e, "gradient of branch and residual stream");
+}
+
+}  // extern "C"

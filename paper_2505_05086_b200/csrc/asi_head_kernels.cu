@@ -1,0 +1,936 @@
+// Output layer and loss in one: log probabilities of given tokens from the last hidden states x [T][D] and the output layer's weight
+// w [V][D], and their gradients, without logits that outlive a tile.
+//
+//   X_j = scale x_t . w_j;   lse = log sum_j exp X_j;   logp = X_y - lse;   entropy = lse - sum_j p_j X_j
+//   G[t][j] = scale (dlogp ([j = y] - p_j) - dentropy p_j (log p_j + entropy));   dx = G w;   dw = G^T x
+//
+// Four matrix products, all by k_head_gemm: the logits' tiles leave nothing but a maximum and two sums a row (and the target's logit)
+// behind, k_head_rows joins these, and then for a piece of the vocabulary at a time the logits are computed again, this time
+// leaving G (in the workspace), from which one launch makes the piece's share of dx and its rows of dw.
+//
+// What bounds it: the tensor cores, 2 T V D operations a product (for a few rows the bytes of w, read twice, and of dw).
+//
+// Operands are bf16.  fp32 ones are split into three terms each (hi, mid, lo: 24 bits) by k_head_split, and a product takes the
+// six pairs of terms down to 2^-16 of the first (what is left out is 2^-24).  G is split likewise where its product goes to
+// fp32.  Rows of bf16 off 16 bytes, which tensor copies cannot fetch, go through the same kernel as one term.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "asi_internal.h"
+#include "asi_tc_ptx.h"
+
+namespace asi {
+
+namespace {
+
+constexpr int kWorkers = 8;                               // epilogue warps
+constexpr int kThreads = (kWorkers + 2) * 32;             // + the issuer's and the producer's
+constexpr int kTile = 256;                                // rows and columns of a pair's tile
+constexpr int kK = 64;                                    // k per chunk: 64 bf16 = one 128-byte swizzle row
+constexpr int kMaxStages = 6;
+constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's chunk
+constexpr uint32_t kStage = 2 * kHalf;
+constexpr int kPitch = 33;                                // floats of a staged row of 32 (columns in banks of their own)
+constexpr uint32_t kStageOut = 32 * kPitch * 4;           // a warp's staged 32 x 32 results
+constexpr uint32_t kStageG = 32 * 64 * 2;                 // a warp's staged 32 x 64 values of G, one term
+constexpr int kSeg = 16;                                  // chunks that add up in TMEM where results are held to fp32
+constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
+
+enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
+enum Kind { kNone = 0, kF32 = 1, kB16 = 2 };
+
+// One product C[m][n] = sum over k and pairs of terms of A(m, k) B(n, k).  An operand lies with its k together (mn = 0: boxes of 64 k
+// x 128 rows) or with its rows together (mn = 1: boxes of 64 rows x 64 k, two of them); terms are the map's third axis.
+struct HeadProb {
+  CUtensorMap a, b;
+  int a_mn, b_mn;
+  int a_off, a_k, b_off, b_k;   // where the product's first row and first k lie in the operand
+  int M, N, mt, nt, splits;     // tiles; `splits` shares of k one after another
+  int kc, per;                  // chunks of k, and of a share
+  int pairs;                    // pairs of terms
+  uint32_t a_term, b_term;      // two bits a pair
+  int n_first;                  // tiles of a row follow one another (else tiles of a column)
+  const void* add;              // added to the result, laid out like it; null: nothing
+  void* out;
+  int add_kind, out_kind;
+  int64_t ld, split_stride;     // elements
+};
+struct HeadArgs {
+  HeadProb p[2];
+  int np, tiles0, tiles;        // tiles of the first product, of all
+  int nst;                      // stages
+  int seg;                      // chunks that add up in TMEM (kSegmented), or all
+  int* status;
+  int stall;                    // test hook: no copies, short waits
+  // kStats, kGrad:
+  const int64_t* y;
+  int64_t ignore, V;
+  int64_t v0;                   // first column of the piece
+  int T;
+  float c, scale;               // c = scale log2(e)
+  float *pm, *ps, *pw, *xy;     // [2 nt][T]: maximum (base 2), sum, weighted sum; [T]: the target's logit
+  const float2* row;            // maximum (base 2) and log2 of the sum of each row, or
+  const float* lse;             // (null: row)
+  const float *entropy, *dlogp, *dent;
+  CUtensorMap g;                // G: boxes of 64 columns x 32 rows
+  int terms;                    // of G
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t rank_in_pair() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// maximum, sum and weighted sum (of e_j = 2^a_j: sum e_j, sum e_j a_j) of what a thread has seen of its row
+struct RowStats {
+  float top = -INFINITY, m = 0.f, s = 0.f, w = 0.f;      // top: largest logit; m = c top, what exponents are relative to
+  __device__ __forceinline__ void add(const float (&v)[32], float c) {
+    float t = v[0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) t = fmaxf(t, v[i]);
+    if (t > top) {
+      const float m2 = t * c;
+      if (top != -INFINITY) {                            // (else the sums are 0, or NaN for good)
+        const float d = m - m2, r = ex2(d);
+        w = r * fmaf(d, s, w);
+        s *= r;
+      }
+      top = t, m = m2;
+    }
+    float s2 = 0.f, w2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const float a = fmaf(v[i], c, -m), b = fmaf(v[i + 1], c, -m), ea = ex2(a), eb = ex2(b);
+      s += ea, s2 += eb;
+      w = fmaf(ea, fmaxf(a, -200.f), w), w2 = fmaf(eb, fmaxf(b, -200.f), w2);   // (2^-200 is 0 here; 0 * -inf would not be)
+    }
+    s += s2, w += w2;
+  }
+};
+
+// what G of a row needs
+struct RowGrad {
+  float hi, lo, alpha, beta, h;
+  int y;                       // its target's column in the vocabulary, -1: none
+  bool live;
+};
+
+__device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
+  RowGrad r = {0.f, 0.f, 0.f, 0.f, 0.f, -1, false};
+  if (row >= g.T) return r;
+  const int64_t y = g.y[row];
+  r.live = y != g.ignore;
+  const bool in = y >= 0 && y < g.V;
+  r.y = in ? (int)y : -1;
+  r.alpha = in ? g.dlogp[row] : NAN;
+  if (g.dent) r.beta = g.dent[row], r.h = g.entropy[row];
+  if (g.row) {
+    const float2 q = g.row[row];
+    r.hi = q.x, r.lo = q.y;
+  } else {
+    const float l = g.lse[row];
+    r.hi = l * kLog2e;
+    r.lo = fmaf(l, kLog2e, -r.hi) + l * kLog2eLow;
+  }
+  if (r.hi == -INFINITY) r.hi = INFINITY, r.lo = 0.f;      // a row of nothing but -inf: every p is 0
+  return r;
+}
+
+// 32 logits of a row, the first in column j0 of the vocabulary, become their gradients
+__device__ __forceinline__ void to_gradient(float (&v)[32], const RowGrad& r, const HeadArgs& g, int64_t j0) {
+  const int left = (int)(g.V - j0 < 32 ? g.V - j0 : 32), hot = r.y - (int)j0;   // (V <= 2^24)
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const float a = fmaf(v[i], g.c, -r.hi) - r.lo, p = ex2(a);
+    float d = r.alpha * ((i == hot ? 1.f : 0.f) - p);
+    if (r.beta != 0.f) d -= r.beta * p * fmaf(fmaxf(a, -200.f), kLn2, r.h);
+    v[i] = r.live && i < left ? g.scale * d : 0.f;
+  }
+}
+
+// Waits that end: as mbar_wait, for arrivals of the other CTA too
+__device__ __forceinline__ bool mbar_wait_pair(uint64_t* bar, uint32_t parity, int stall) {
+  const bool ok = mbar_wait(bar, parity, stall);
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return ok;
+}
+
+// A pair of CTAs owns a tile of 256 x 256: each brings half of either operand's chunk (128 rows) to its shared memory, products are
+// issued for both by the first one (tcgen05, cta_group 2: each tensor core reads its own half of A and both halves of B), and each
+// has the 128 x 256 accumulators of its rows in its TMEM, twice, so that the next tile's products run under this one's epilogue.
+// (A CTA by itself would read twice the bytes of B for the same products.)  Roles: a producer thread, an issuer thread,
+// eight epilogue warps (a thread a row and half of the columns).
+// kSegmented: results held to fp32.  The unit's own sums truncate, so they go to registers after every kSeg chunks.
+template <int kEpi, bool kSegmented>
+__global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant__ HeadArgs g) {
+  extern __shared__ __align__(1024) uint8_t head_smem[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(head_smem) + 1023) & ~(uintptr_t)1023);
+  __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done[2], acc_free[2], drained[1];
+  __shared__ uint32_t tmem_slot[1];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)rank_in_pair(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  if (tid == 0) {
+    for (int i = 0; i < kMaxStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(done + i, 1), mbar_init(acc_free + i, 2 * kWorkers);
+    mbar_init(drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  pair_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  struct Tile { int q, m, n, s, chunks, k0; };
+  auto tile_of = [&](int t) {
+    Tile x;
+    x.q = t >= g.tiles0 ? 1 : 0;
+    const HeadProb& p = g.p[x.q];
+    if (x.q) t -= g.tiles0;
+    const int each = p.mt * p.nt;
+    x.s = t / each;
+    t -= x.s * each;
+    x.m = p.n_first ? t / p.nt : t % p.mt;
+    x.n = p.n_first ? t % p.nt : t / p.mt;
+    x.k0 = x.s * p.per;
+    x.chunks = (p.kc - x.k0 < p.per ? p.kc - x.k0 : p.per) * p.pairs;
+    if (x.chunks < 0) x.chunks = 0;
+    return x;
+  };
+  const int nst = g.nst;
+  bool ok = true;
+  int loads = 0;
+  if (warp == kWorkers) {
+    // ---- issuer
+    if (lane == 0 && rank == 0) {
+      const uint32_t at = smem_u32(base);
+      int st = 0, seg = 0;
+      uint32_t ph = 0;
+#pragma unroll 1
+      for (int t = pair; t < g.tiles && ok; t += pairs) {
+        const Tile x = tile_of(t);
+        const HeadProb& p = g.p[x.q];
+        const uint32_t idesc = instr_desc_bf16(kTile, kTile, p.a_mn != 0, p.b_mn != 0);
+        // a k-step is 16 bf16: 32 bytes inside the swizzle row of a K-major tile, 16 rows (2048 bytes) of an MN-major one
+        const uint64_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
+        const uint32_t a_lead = p.a_mn ? kHalf / 2 : 16, b_lead = p.b_mn ? kHalf / 2 : 16;
+#pragma unroll 1
+        for (int c0 = 0; c0 < x.chunks && ok; c0 += g.seg, ++seg) {
+          const int buf = seg & 1, turn = seg >> 1;
+          if (turn > 0) {
+            ok = mbar_wait_pair(acc_free + buf, (uint32_t)(turn + 1) & 1u, g.stall);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
+          const int c1 = x.chunks - c0 < g.seg ? x.chunks : c0 + g.seg;
+#pragma unroll 1
+          for (int c = c0; c < c1; ++c) {
+            ok = mbar_wait(full + st, ph, g.stall);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t da = smem_desc_sw128(at + st * kStage, a_lead), db = smem_desc_sw128(at + st * kStage + kHalf, b_lead);
+#pragma unroll
+            for (int ks = 0; ks < kK / 16; ++ks)
+              umma_pair_bf16(tmem + (uint32_t)(buf * kTile), da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | ks) ? 1u : 0u);
+            umma_pair_commit(empty + st);
+            if (++st == nst) st = 0, ph ^= 1u;
+          }
+          if (ok) umma_pair_commit(done + buf);
+        }
+      }
+    }
+  } else if (warp == kWorkers + 1) {
+    // ---- producer: this CTA's half of each chunk, counted by the first CTA's barrier
+    if (lane == 0) {
+      int st = 0;
+      uint32_t ph = 1;
+#pragma unroll 1
+      for (int t = pair; t < g.tiles && ok; t += pairs) {
+        const Tile x = tile_of(t);
+        const HeadProb& p = g.p[x.q];
+        const int am = p.a_off + x.m * kTile + rank * 128, bn = p.b_off + x.n * kTile + rank * 128;
+        int kc = x.k0, e = 0;
+#pragma unroll 1
+        for (int c = 0; c < x.chunks; ++c, ++loads) {
+          if (loads >= nst) {
+            ok = mbar_wait(empty + st, ph, g.stall);
+            if (!ok) break;
+          }
+          if (rank == 0) mbar_expect_tx(full + st, 2 * kStage);
+          if (!g.stall) {
+            uint8_t* A = base + st * kStage;
+            const uint32_t bar = in_cta(full + st, 0);
+            const int at = (int)(p.a_term >> (2 * e)) & 3, bt = (int)(p.b_term >> (2 * e)) & 3;
+            const int ka = p.a_k + kc * kK, kb = p.b_k + kc * kK;
+            if (p.a_mn) {
+              tma_pair_load_3d(A, &p.a, am, ka, at, bar);
+              tma_pair_load_3d(A + kHalf / 2, &p.a, am + 64, ka, at, bar);
+            } else {
+              tma_pair_load_3d(A, &p.a, ka, am, at, bar);
+            }
+            if (p.b_mn) {
+              tma_pair_load_3d(A + kHalf, &p.b, bn, kb, bt, bar);
+              tma_pair_load_3d(A + kHalf + kHalf / 2, &p.b, bn + 64, kb, bt, bar);
+            } else {
+              tma_pair_load_3d(A + kHalf, &p.b, kb, bn, bt, bar);
+            }
+          }
+          if (++e == p.pairs) e = 0, ++kc;
+          if (++st == nst) st = 0, ph ^= 1u;
+        }
+      }
+    }
+  } else {
+    // ---- epilogue: warp w has the lanes 32 (w mod 4) .. of TMEM, warps 0-3 the columns [0, 128) of the tile, warps 4-7 the others
+    const int quad = warp & 3, col0 = (warp >> 2) * 128;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)col0;
+    const uint32_t free0 = in_cta(acc_free, 0), free1 = in_cta(acc_free + 1, 0);
+    uint8_t* out = base + nst * kStage + warp * (kEpi == kGrad ? g.terms * kStageG : kStageOut);
+    int seg = 0;
+#pragma unroll 1
+    for (int t = pair; t < g.tiles && ok; t += pairs) {
+      const Tile x = tile_of(t);
+      const HeadProb& p = g.p[x.q];
+      const int row0 = x.m * kTile + rank * 128 + quad * 32, row = row0 + lane;
+      const int n0 = x.n * kTile + col0;
+      float acc[kSegmented ? 128 : 1];
+      if constexpr (kSegmented) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < x.chunks; c0 += g.seg, ++seg) {
+          const int buf = seg & 1;
+          ok = mbar_wait(done + buf, (uint32_t)(seg >> 1) & 1u, g.stall);
+          if (__any_sync(0xffffffffu, !ok)) ok = false;
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+          for (int cc = 0; cc < 4; ++cc) {
+            uint32_t u[32];
+            tmem_ld32(lanes + (uint32_t)(buf * kTile + cc * 32), u);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[cc * 32 + i] += __uint_as_float(u[i]);
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive_in(buf ? free1 : free0);
+        }
+        if (!ok) break;
+      } else if (x.chunks > 0) {
+        ok = mbar_wait(done + (seg & 1), (uint32_t)(seg >> 1) & 1u, g.stall);
+        if (__any_sync(0xffffffffu, !ok)) ok = false;
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
+      RowStats stats;
+      RowGrad rg;
+      if constexpr (kEpi == kGrad) rg = row_grad(g, row);
+      const int64_t y = kEpi == kStats && row < g.T ? g.y[row] : -1;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        float v[32];
+        if constexpr (kSegmented) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = acc[cc * 32 + i];
+        } else if (x.chunks > 0) {
+          tmem_ld32(lanes + (uint32_t)((seg & 1) * kTile + cc * 32), reinterpret_cast<uint32_t*>(v));
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (cc == 3) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_in(seg & 1 ? free1 : free0);
+            ++seg;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0.f;
+        }
+        const int n = n0 + cc * 32;
+        if constexpr (kEpi == kStats) {
+          const int64_t left = g.V - n;
+          if (left < 32)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i >= left) v[i] = -INFINITY;
+          stats.add(v, g.c);
+          const int64_t hot = y - n;
+          if (hot >= 0 && hot < 32 && y < g.V) {
+            float h = v[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) h = hot == i ? v[i] : h;
+            g.xy[row] = h;
+          }
+        } else if constexpr (kEpi == kGrad) {
+          // rows of 128 bytes (64 columns), 16-byte units swizzled by the row as the tensor copy expects them
+          if ((cc & 1) == 0) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+          }
+          to_gradient(v, rg, g, g.v0 + n);
+#pragma unroll 1
+          for (int e = 0; e < g.terms; ++e) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              uint4 w;
+              w.x = pack2(v[8 * u], v[8 * u + 1]), w.y = pack2(v[8 * u + 2], v[8 * u + 3]);
+              w.z = pack2(v[8 * u + 4], v[8 * u + 5]), w.w = pack2(v[8 * u + 6], v[8 * u + 7]);
+              *reinterpret_cast<uint4*>(out + e * kStageG + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) = w;
+              if (g.terms > 1) {
+                const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  v[8 * u + 2 * i] -= __uint_as_float(q[i] << 16);
+                  v[8 * u + 2 * i + 1] -= __uint_as_float(q[i] & 0xffff0000u);
+                }
+              }
+            }
+          }
+          if (cc & 1) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              for (int e = 0; e < g.terms; ++e) tma_store_3d(&g.g, out + e * kStageG, n - 32, row0, e);
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          }
+        } else {
+          // through shared memory, so that a warp's lanes are neighbouring columns
+          float* s = reinterpret_cast<float*>(out);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) s[lane * kPitch + i] = v[i];
+          __syncwarp();
+          const int col = n + lane;
+          if (col < p.N) {
+            const int64_t at = x.s * p.split_stride + (int64_t)row0 * p.ld + col;
+            const int rows = p.M - row0 < 32 ? p.M - row0 : 32;
+#pragma unroll 1
+            for (int r0 = 0; r0 < rows; r0 += 8) {
+              float f[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) {
+                f[r] = 0.f;
+                if (r0 + r < rows) {
+                  if (p.add_kind == kF32) f[r] = static_cast<const float*>(p.add)[at + (r0 + r) * p.ld];
+                  else if (p.add_kind == kB16) f[r] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.add)[at + (r0 + r) * p.ld]);
+                }
+              }
+#pragma unroll
+              for (int r = 0; r < 8; ++r)
+                if (r0 + r < rows) {
+                  const float o = f[r] + s[(r0 + r) * kPitch + lane];
+                  if (p.out_kind == kF32) static_cast<float*>(p.out)[at + (r0 + r) * p.ld] = o;
+                  else static_cast<__nv_bfloat16*>(p.out)[at + (r0 + r) * p.ld] = __float2bfloat16_rn(o);
+                }
+            }
+          }
+        }
+      }
+      if constexpr (kEpi == kStats) {
+        if (row < g.T) {
+          const int64_t at = (int64_t)(2 * x.n + (warp >> 2)) * g.T + row;
+          g.pm[at] = stats.top == -INFINITY ? -INFINITY : stats.m;
+          g.ps[at] = stats.s;
+          g.pw[at] = stats.w;
+        }
+      }
+    }
+    if constexpr (kEpi == kGrad) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // G is there before the next kernel reads it
+      __syncwarp();
+    }
+  }
+  const bool fail = __syncthreads_or(ok ? 0 : 1) != 0;
+  if (fail) {                                           // what is in flight gets the limit once more
+    if (tid == 0) atomicMax(g.status, (int)ASI_ERR_TIMEOUT);
+    if (warp == kWorkers && lane == 0 && rank == 0) {
+      umma_pair_commit(drained);
+      mbar_wait(drained, 0, g.stall);
+    } else if (warp == kWorkers + 1 && lane == 0 && rank == 0) {
+      for (int i = 0; i < nst; ++i)
+        if (loads > i) mbar_wait(full + i, (uint32_t)((loads - 1 - i) / nst) & 1u, g.stall);
+    }
+    __syncwarp();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  pair_sync();                                          // the other CTA's products read this one's memory
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// The rows' shares joined: 32 rows a CTA, 32 shares side by side
+struct RowsArgs {
+  const float *pm, *ps, *pw, *xy;
+  const int64_t* y;
+  int64_t ignore, V;
+  float *logp, *entropy, *lse;
+  float2* row;
+  int T, parts;
+  float c;
+};
+__global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ RowsArgs p) {
+  __shared__ float sm[32][33], ss[32][33], sw[32][33];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+  float m = -INFINITY, s = 0.f, w = 0.f;
+  auto join = [&](float m2, float s2, float w2) {
+    const float top = fmaxf(m, m2);
+    if (top == -INFINITY) {                              // the sums are 0 or NaN
+      s += s2;
+      return;
+    }
+    const float d = m - top, d2 = m2 - top, r = ex2(d), r2 = ex2(d2);
+    w = (m == -INFINITY ? 0.f : r * fmaf(d, s, w)) + (m2 == -INFINITY ? 0.f : r2 * fmaf(d2, s2, w2));
+    s = r * s + r2 * s2;                                 // (a NaN stays)
+    m = top;
+  };
+  if (row < p.T) {
+#pragma unroll 4
+    for (int i = slice; i < p.parts; i += 32) {
+      const int64_t at = (int64_t)i * p.T + row;
+      join(p.pm[at], p.ps[at], p.pw[at]);
+    }
+  }
+  sm[slice][lane] = m, ss[slice][lane] = s, sw[slice][lane] = w;
+  __syncthreads();
+  if (slice == 0 && row < p.T) {
+    for (int i = 1; i < 32; ++i) join(sm[i][lane], ss[i][lane], sw[i][lane]);
+    const bool nothing = m == -INFINITY && s == 0.f;
+    const float l2 = log2f(s), y2 = nothing ? -INFINITY : l2;
+    const int64_t y = p.y[row];
+    if (p.lse) p.lse[row] = nothing ? -INFINITY : (m + l2) * kLn2;
+    if (p.entropy) p.entropy[row] = nothing ? 0.f : kLn2 * (l2 - w / s);
+    if (p.logp) {
+      float l = 0.f;
+      if (y < 0 || y >= p.V) l = NAN;
+      else if (nothing) l = -INFINITY;
+      else l = (fmaf(p.xy[row], p.c, -m) - l2) * kLn2;
+      p.logp[row] = y == p.ignore ? 0.f : l;
+    }
+    if (p.row) p.row[row] = make_float2(m, nothing ? 0.f : y2);
+  }
+}
+
+// bf16 terms of a matrix, in rows on 16 bytes
+struct SplitArgs {
+  const void* in;
+  __nv_bfloat16* out;          // [terms][rows][ld]
+  int64_t rows, D, ld;
+  int terms;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_split(const __grid_constant__ SplitArgs p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int64_t n = p.rows * p.D;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / p.D, at = r * p.ld + (i - r * p.D);
+    float v = (float)static_cast<const T*>(p.in)[i];
+    for (int e = 0; e < p.terms; ++e) {
+      const __nv_bfloat16 h = __float2bfloat16_rn(v);
+      p.out[e * p.rows * p.ld + at] = h;
+      v -= __bfloat162float(h);
+    }
+  }
+}
+
+// dx from its shares of k, in order
+struct JoinArgs {
+  const float* in;             // [splits][n]
+  void* out;
+  int64_t n;
+  int splits, out_kind;
+};
+__global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ JoinArgs p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.n; i += (int64_t)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < p.splits; ++e) s += p.in[e * p.n + i];
+    if (p.out_kind == kF32) static_cast<float*>(p.out)[i] = s;
+    else static_cast<__nv_bfloat16*>(p.out)[i] = __float2bfloat16_rn(s);
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+size_t size_of(int dtype) { return dtype == ASI_BF16 ? 2 : 4; }
+
+asi_status_t check_desc(const asi_head_desc_t* d) {
+  if (!d || (d->in_dtype != ASI_F32 && d->in_dtype != ASI_BF16) || (d->dw_dtype != ASI_F32 && d->dw_dtype != d->in_dtype)) return ASI_ERR_INVALID_ARG;
+  if (d->rows < 0 || d->vocab < 1 || d->dim < 1 || d->vocab_chunk < 0) return ASI_ERR_INVALID_ARG;
+  if (!(d->scale >= 1e-8f && d->scale <= 1e8f) || (d->flags & ~ASI_FLAG_TEST_EXPIRE_WAIT)) return ASI_ERR_INVALID_ARG;
+  if (d->rows > ASI_HEAD_MAX_ROWS || d->vocab > ASI_HEAD_MAX_VOCAB || d->dim > ASI_HEAD_MAX_DIM) return ASI_ERR_UNSUPPORTED;
+  return ASI_OK;
+}
+
+constexpr int64_t kPieceBytes = 128 << 20;               // of G in the workspace, where 1024 columns take no more
+constexpr int64_t kJoinRows = 4096;                      // rows of shares of dx beyond dx itself
+
+struct Layout {
+  size_t part, xy, row, xs, ws, g, acc, bytes;
+  int64_t ld;                                            // of split operands
+  int64_t cols;                                          // of a piece
+  int in_terms, g_terms;
+  bool split;                                            // operands go through k_head_split
+  int64_t acc_rows;
+};
+
+Layout layout_of(const asi_head_desc_t* d, bool grad) {
+  Layout l = {};
+  const int64_t T = d->rows, V = d->vocab, nt = ceil_div(V, kTile), all = nt * kTile;
+  l.in_terms = d->in_dtype == ASI_F32 ? 3 : 1;
+  l.g_terms = d->dw_dtype == ASI_F32 ? 3 : 1;            // (dx of fp32 operands comes with dw in fp32)
+  l.split = d->in_dtype == ASI_F32 || d->dim % 8 != 0;
+  l.ld = (d->dim + 7) / 8 * 8;
+  size_t at = 256;                                       // status word
+  auto take = [&](size_t bytes) {
+    const size_t a = at;
+    at = align_up(at + bytes, 256);
+    return a;
+  };
+  l.part = take((size_t)2 * nt * T * 12);
+  l.xy = take((size_t)T * 4);
+  l.row = take((size_t)T * 8);
+  if (l.split) {
+    l.xs = take((size_t)l.in_terms * T * l.ld * 2);
+    l.ws = take((size_t)l.in_terms * V * l.ld * 2);
+  }
+  if (grad && T) {
+    const int64_t col = (int64_t)l.g_terms * 2 * T;      // bytes of a column of G
+    int64_t most = d->vocab_chunk ? ceil_div(std::min(d->vocab_chunk, V), kTile) * kTile * col : std::max(kPieceBytes, 1024 * col);
+    most = std::min(most, all * col);
+    l.cols = most / col / kTile * kTile;
+    l.cols = ceil_div(nt, ceil_div(all, l.cols)) * kTile;   // pieces of about the same size
+    l.g = take((size_t)most);
+    l.acc_rows = std::max(T, std::min(64 * T, kJoinRows));
+    l.acc = take((size_t)l.acc_rows * d->dim * 4);
+  }
+  l.bytes = at;
+  return l;
+}
+
+bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows, int64_t ld, int terms, int64_t term_stride, int box_inner, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)terms};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)term_stride * 2};
+  const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1};
+  return encode_bf16_map(map, base, 3, dims, strides, box);
+}
+
+// the pairs of terms that matter, small ones first
+void set_pairs(HeadProb* p, int a_terms, int b_terms) {
+  p->pairs = 0;
+  p->a_term = p->b_term = 0;
+  for (int sum = 2; sum >= 0; --sum)
+    for (int a = 0; a < a_terms; ++a) {
+      const int b = sum - a;
+      if (b < 0 || b >= b_terms) continue;
+      p->a_term |= (uint32_t)a << (2 * p->pairs);
+      p->b_term |= (uint32_t)b << (2 * p->pairs);
+      ++p->pairs;
+    }
+}
+
+template <int kEpi, bool kSegmented>
+cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
+  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (kEpi == kGrad ? (size_t)g.terms * kStageG : kEpi == kOut ? kStageOut : 0);
+  const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented>), smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * std::min(g.tiles, 74)));    // a pair on each pair of SMs
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, k_head_gemm<kEpi, kSegmented>, g);
+}
+
+template <int kEpi>
+cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
+  g.nst = kEpi == kGrad && g.terms == 3 ? 4 : 6;
+  g.seg = segmented ? kSeg : 1 << 30;
+  g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
+  g.tiles = g.tiles0 + (g.np > 1 ? g.p[1].mt * g.p[1].nt * g.p[1].splits : 0);
+  return segmented ? launch_gemm_as<kEpi, true>(g, st) : launch_gemm_as<kEpi, false>(g, st);
+}
+
+cudaError_t launch_split(const asi_head_desc_t* d, const Layout& l, const void* in, int64_t rows, void* out, cudaStream_t st) {
+  SplitArgs a = {in, static_cast<__nv_bfloat16*>(out), rows, d->dim, l.ld, l.in_terms};
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * d->dim, 256 * 4), 148 * 8));
+  return d->in_dtype == ASI_BF16 ? launch_pdl(k_head_split<__nv_bfloat16>, grid, dim3(256), 0, st, a) : launch_pdl(k_head_split<float>, grid, dim3(256), 0, st, a);
+}
+
+// A call's buffers
+struct Call {
+  const void *x, *w;
+  const int64_t* y;
+  float *logp, *entropy, *lse;               // written by the forward direction
+  const float *lse_in, *entropy_in, *dlogp, *dent;
+  void *dx, *dw;
+  bool accumulate, forward, grad;
+};
+
+void size_product(HeadProb* p, int64_t M, int64_t N, int64_t K) {
+  p->M = (int)M;
+  p->N = (int)N;
+  p->mt = (int)ceil_div(M, kTile);
+  p->nt = (int)ceil_div(N, kTile);
+  p->kc = (int)ceil_div(K, kK);
+  p->per = p->kc;
+  p->splits = 1;
+}
+
+asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t st) {
+  const Layout l = layout_of(d, c.grad);
+  const int64_t T = d->rows, V = d->vocab, D = d->dim;
+  const bool fine = d->in_dtype == ASI_F32;              // logits and dx are held to fp32
+  int* status = reinterpret_cast<int*>(ws);
+  cudaError_t e = cudaMemsetAsync(status, 0, 4, st);
+  if (e != cudaSuccess) return cuda_status(e, "output layer's status");
+  const void *x = c.x, *w = c.w;
+  int64_t ld = D;
+  if (l.split) {
+    e = launch_split(d, l, c.x, T, ws + l.xs, st);
+    if (e == cudaSuccess) e = launch_split(d, l, c.w, V, ws + l.ws, st);
+    if (e != cudaSuccess) return cuda_status(e, "terms of the output layer's operands");
+    x = ws + l.xs, w = ws + l.ws, ld = l.ld;
+  }
+  HeadArgs g = {};
+  g.status = status;
+  g.stall = (d->flags & ASI_FLAG_TEST_EXPIRE_WAIT) != 0;
+  g.y = c.y;
+  g.ignore = d->ignore_index;
+  g.V = V;
+  g.T = (int)T;
+  g.scale = d->scale;
+  g.c = (float)(d->scale * 1.4426950408889634);
+  const int64_t nt = ceil_div(V, kTile);
+  g.pm = reinterpret_cast<float*>(ws + l.part);
+  g.ps = g.pm + 2 * nt * T;
+  g.pw = g.ps + 2 * nt * T;
+  g.xy = reinterpret_cast<float*>(ws + l.xy);
+  float2* row = reinterpret_cast<float2*>(ws + l.row);
+  // the logits' product: whole, then in pieces
+  HeadProb logits = {};
+  size_product(&logits, T, V, D);
+  set_pairs(&logits, l.in_terms, l.in_terms);
+  if (!operand_map(&logits.a, x, D, T, ld, l.in_terms, T * ld, kK, 128) || !operand_map(&logits.b, w, D, V, ld, l.in_terms, V * ld, kK, 128))
+    return cuda_status(cudaErrorNotSupported, "tensor map");
+  if (c.forward) {
+    g.p[0] = logits;
+    g.np = 1;
+    e = launch_gemm<kStats>(g, fine, st);
+    if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
+    RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c};
+    e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
+    if (e != cudaSuccess) return cuda_status(e, "rows of the output layer");
+  }
+  if (!c.grad) return ASI_OK;
+  g.row = c.forward ? row : nullptr;
+  g.lse = c.lse_in;
+  g.entropy = c.entropy_in;
+  g.dlogp = c.dlogp;
+  g.dent = c.dent;
+  const int terms = c.dw && d->dw_dtype == ASI_F32 ? 3 : fine ? 3 : 1;   // (without dw in fp32, G of bf16 operands has one)
+  g.terms = terms;
+  void* G = ws + l.g;
+  HeadProb px = {}, pw = {};
+  // (the product's first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
+  bool maps = operand_map(&g.g, G, l.cols, T, l.cols, terms, T * l.cols, 64, 32);
+  maps = maps && operand_map(&px.a, G, l.cols, T, l.cols, terms, T * l.cols, kK, 128) && operand_map(&px.b, w, D, V, ld, l.in_terms, V * ld, 64, kK);
+  maps = maps && operand_map(&pw.a, G, l.cols, T, l.cols, terms, T * l.cols, 64, kK) && operand_map(&pw.b, x, D, T, ld, l.in_terms, T * ld, 64, kK);
+  if (!maps) return cuda_status(cudaErrorNotSupported, "tensor map");
+  const int64_t pieces = ceil_div(V, l.cols);
+  const int dx_kind = d->in_dtype == ASI_BF16 ? kB16 : kF32, dw_kind = d->dw_dtype == ASI_BF16 ? kB16 : kF32;
+  float* acc = reinterpret_cast<float*>(ws + l.acc);
+  int splits = 1;
+  for (int64_t i = 0; i < pieces; ++i) {
+    const int64_t v0 = i * l.cols, nv = std::min(V - v0, l.cols);
+    g.p[0] = logits;
+    g.p[0].N = (int)nv;
+    g.p[0].nt = (int)ceil_div(nv, kTile);
+    g.p[0].b_off = (int)v0;
+    g.np = 1;
+    g.v0 = v0;
+    e = launch_gemm<kGrad>(g, fine, st);
+    if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
+    size_product(&px, T, D, nv);
+    set_pairs(&px, fine ? 3 : 1, fine ? 3 : 1);
+    px.a_mn = 0, px.b_mn = 1, px.b_k = (int)v0, px.n_first = 1;
+    size_product(&pw, nv, D, T);
+    set_pairs(&pw, dw_kind == kF32 ? 3 : 1, l.in_terms);
+    pw.a_mn = 1, pw.b_mn = 1, pw.n_first = 1;
+    pw.ld = D;
+    pw.out = static_cast<char*>(c.dw) + v0 * D * size_of(d->dw_dtype);
+    pw.out_kind = dw_kind;
+    pw.add = c.accumulate ? pw.out : nullptr;
+    pw.add_kind = c.accumulate ? dw_kind : kNone;
+    if (i == 0) {
+      // few tiles of dx: shares of k, about half of what a pair has to do in all
+      const int64_t tx = (int64_t)px.mt * px.nt, tw = c.dw ? (int64_t)pw.mt * pw.nt : 0;
+      const int64_t load = (tx * px.kc * px.pairs + tw * pw.kc * pw.pairs) / 74, share = std::max<int64_t>(load / 2 / px.pairs, 8);
+      splits = (int)std::max<int64_t>(1, std::min({ceil_div(px.kc, share), l.acc_rows / T, (int64_t)64}));
+    }
+    px.per = (int)ceil_div(px.kc, splits);
+    px.splits = splits;
+    px.split_stride = T * D;
+    px.ld = D;
+    const bool last = i + 1 == pieces && splits == 1;
+    px.add = i ? acc : nullptr;
+    px.add_kind = i ? kF32 : kNone;
+    px.out = last ? c.dx : static_cast<void*>(acc);
+    px.out_kind = last ? dx_kind : kF32;
+    g.np = 0;
+    if (c.dx) g.p[g.np++] = px;
+    if (c.dw) g.p[g.np++] = pw;
+    e = launch_gemm<kOut>(g, fine || dw_kind == kF32, st);
+    if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
+  }
+  if (c.dx && splits > 1) {
+    JoinArgs j = {acc, c.dx, T * D, splits, dx_kind};
+    e = launch_pdl(k_head_join, dim3((unsigned)std::min<int64_t>(ceil_div(T * D, 256), 148 * 8)), dim3(256), 0, st, j);
+    if (e != cudaSuccess) return cuda_status(e, "shares of dx");
+  }
+  return ASI_OK;
+}
+
+// A contiguous buffer of a call; null where the call has none
+struct Span {
+  const void* p;
+  size_t bytes;
+  size_t element;
+  bool meets(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && a < b + o.bytes && b < a + bytes;
+  }
+};
+
+asi_status_t check_buffers(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+  for (const auto* list : {&in, &out})
+    for (const Span& s : *list)
+      if (s.p && off_element(s.p, s.element)) return ASI_ERR_INVALID_ARG;
+  for (const Span* o = out.begin(); o != out.end(); ++o) {
+    for (const Span* q = out.begin(); q != o; ++q)
+      if (o->meets(*q)) return ASI_ERR_INVALID_ARG;
+    for (const Span& i : in)
+      if (o->meets(i)) return ASI_ERR_INVALID_ARG;
+  }
+  return ASI_OK;
+}
+
+asi_status_t check_call(const asi_head_desc_t* d, const Call& c, void* ws, size_t ws_bytes) {
+  if (!c.x || !c.w || !c.y || !ws) return ASI_ERR_INVALID_ARG;
+  if (c.forward && (!c.logp || !c.lse)) return ASI_ERR_INVALID_ARG;
+  if (c.grad && (!c.dlogp || (!c.dx && !c.dw) || (!c.forward && !c.lse_in) || (c.dent && !c.entropy_in))) return ASI_ERR_INVALID_ARG;
+  const Layout l = layout_of(d, c.grad);
+  if (ws_bytes < l.bytes || !aligned(ws, 256)) return ASI_ERR_WORKSPACE;
+  if (!l.split && (!aligned(c.x, 16) || !aligned(c.w, 16))) return ASI_ERR_INVALID_ARG;
+  const size_t T = (size_t)d->rows, e = size_of(d->in_dtype), n = T * 4;
+  const bool in_rows = c.grad && !c.forward;
+  return check_buffers({{c.x, T * d->dim * e, e}, {c.w, (size_t)d->vocab * d->dim * e, e}, {c.y, T * 8, 8}, {c.dlogp, n, 4}, {c.dent, n, 4},
+                        {in_rows ? c.lse_in : nullptr, n, 4}, {in_rows ? c.entropy_in : nullptr, n, 4}},
+                       {{c.logp, n, 4}, {c.entropy, n, 4}, {c.lse, n, 4}, {c.dx, T * d->dim * e, e},
+                        {c.dw, (size_t)d->vocab * d->dim * size_of(d->dw_dtype), size_of(d->dw_dtype)}, {ws, l.bytes, 256}});
+}
+
+asi_status_t call(const asi_head_desc_t* d, const Call& c, void* ws, size_t ws_bytes, void* stream) {
+  asi_status_t s = check_desc(d);
+  if (s != ASI_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (d->rows == 0) {
+    if (!c.grad || !c.dw || c.accumulate) return ASI_OK;   // no rows: their gradient of w is 0
+    if (off_element(c.dw, size_of(d->dw_dtype))) return ASI_ERR_INVALID_ARG;
+    return cuda_status(cudaMemsetAsync(c.dw, 0, (size_t)d->vocab * d->dim * size_of(d->dw_dtype), st), "gradient of no rows");
+  }
+  s = check_call(d, c, ws, ws_bytes);
+  if (s != ASI_OK) return s;
+  try {
+    return run(d, c, static_cast<char*>(ws), st);
+  } catch (...) {
+    return no_host_memory();
+  }
+}
+
+}  // namespace
+}  // namespace asi
+
+using namespace asi;
+
+extern "C" {
+
+size_t asi_head_ws_bytes(const asi_head_desc_t* desc, int32_t grad) { return check_desc(desc) == ASI_OK ? layout_of(desc, grad != 0).bytes : 0; }
+
+asi_status_t asi_head_logprobs(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, float* logp,
+                               float* entropy, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Call c = {};
+  c.x = x, c.w = w, c.y = targets, c.logp = logp, c.entropy = entropy, c.lse = lse, c.forward = true;
+  return call(desc, c, ws, ws_bytes, stream);
+}
+
+asi_status_t asi_head_grad(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* lse,
+                           const float* entropy, const float* dlogp, const float* dentropy, void* dx, void* dw, int32_t accumulate,
+                           void* ws, size_t ws_bytes, void* stream) {
+  Call c = {};
+  c.x = x, c.w = w, c.y = targets, c.lse_in = lse, c.entropy_in = entropy, c.dlogp = dlogp, c.dent = dentropy;
+  c.dx = dx, c.dw = dw, c.accumulate = accumulate != 0, c.grad = true;
+  return call(desc, c, ws, ws_bytes, stream);
+}
+
+asi_status_t asi_head_loss(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* dlogp,
+                           const float* dentropy, float* logp, float* entropy, float* lse, void* dx, void* dw, int32_t accumulate,
+                           void* ws, size_t ws_bytes, void* stream) {
+  Call c = {};
+  c.x = x, c.w = w, c.y = targets, c.logp = logp, c.entropy = entropy, c.lse = lse, c.dlogp = dlogp, c.dent = dentropy;
+  c.entropy_in = entropy, c.dx = dx, c.dw = dw, c.accumulate = accumulate != 0, c.forward = c.grad = true;
+  return call(desc, c, ws, ws_bytes, stream);
+}
+
+asi_status_t asi_head_status(const void* ws, void* stream, asi_status_t* device_status) {
+  if (!ws || !device_status) return ASI_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int v = 0;
+  cudaError_t e = cudaMemcpyAsync(&v, ws, sizeof(int), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return cuda_status(e, "status of the output layer");
+  *device_status = static_cast<asi_status_t>(v);
+  return ASI_OK;
+}
+
+}  // extern "C"

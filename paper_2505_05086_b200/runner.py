@@ -8,7 +8,8 @@ import numpy as np
 import torch
 
 from . import binding
-from .binding import ASI_ADAMW_BLOCK, ASI_BF16, ASI_F32, ASI_OK, AdamwDesc, AdamwTensor, Batch, EmbeddingDesc, LogprobDesc, Plan
+from .binding import (ASI_ADAMW_BLOCK, ASI_BF16, ASI_F32, ASI_NORM_LAYER, ASI_NORM_RMS, ASI_OK, AdamwDesc, AdamwTensor, Batch, Branch,
+                      BranchDesc, Dropout, EmbeddingDesc, HeadDesc, LogprobDesc, Plan)
 
 
 def _stream_handle(stream=None):
@@ -228,24 +229,14 @@ def _result(name):
     return property(lambda self: self._results[name], put)
 
 
-class LogprobRunner(_Runner):
-    """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
-    lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
-    the others as they were.  backward() reads lse and entropy of the last forward() or loss(), or those that it is given.
-    Another contiguous buffer may be assigned to each result.  Calls that may run at the same time share these results: they
-    need a runner each."""
+class _RowResults(_Runner):
+    """Result buffers of a value (or `top_k` values) a row, which another contiguous buffer may replace."""
 
     logp, entropy, lse, top_logp, top_ids = map(_result, ("logp", "entropy", "lse", "top_logp", "top_ids"))
 
-    def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
-        self.device = _cuda_device(device)
-        self.rows, self.vocab, self.top_k = int(rows), int(vocab), int(top_k)
-        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
-        self._descriptor = _Descriptor(LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index),
-                                                   float(scale)))
-        self._bind({name: torch.zeros(self.rows, *more, dtype=dtype, device=self.device) if 0 not in more else None
-                    for name, more, dtype in self._layout()})
-        self._made(self.device)
+    def _new(self):
+        return {name: torch.zeros(self.rows, *more, dtype=dtype, device=self.device) if 0 not in more else None
+                for name, more, dtype in self._layout()}
 
     def _layout(self):
         """Name, sizes behind the rows and type of each result, in the order of the library's arguments."""
@@ -282,6 +273,23 @@ class LogprobRunner(_Runner):
 
     def _own(self):
         return self._buffers
+
+
+class LogprobRunner(_RowResults):
+    """Log probabilities of given tokens over logits of up to `rows` rows: device buffers of the results (logp, entropy,
+    lse; top_logp and top_ids where top_k > 0) and the calls that fill them.  A shorter batch fills the first rows and leaves
+    the others as they were.  backward() reads lse and entropy of the last forward() or loss(), or those that it is given.
+    Another contiguous buffer may be assigned to each result.  Calls that may run at the same time share these results: they
+    need a runner each."""
+
+    def __init__(self, rows, vocab, bf16=False, scale=1.0, ignore_index=-100, top_k=0, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.rows, self.vocab, self.top_k = int(rows), int(vocab), int(top_k)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self._descriptor = _Descriptor(LogprobDesc(_DTYPES[self.in_dtype], self.top_k, 0, self.vocab, 0, 0, int(ignore_index),
+                                                   float(scale)))
+        self._bind(self._new())
+        self._made(self.device)
 
     def _rows_of(self, name, x):
         """Rows and row stride of logits or their gradient."""
@@ -480,3 +488,189 @@ class AdamWRunner(_Runner):
             self.rebind()
         self._call(stream, binding.adamw_step, d, self._table, len(self._table))
         self.t = None if isinstance(step, torch.Tensor) else d.step
+
+
+# ---- a block's other operators, and the output layer with its loss ------------------------------------
+
+def _drop(p, seed, stream_id):
+    return Dropout(float(p), int(seed), int(stream_id), 0, None)
+
+
+class _Steps(_Runner):
+    """A mask for each step: `step` may be a number, or a one-element int64 device tensor that a captured graph reads."""
+
+    def _at_step(self, drop, step):
+        if isinstance(step, torch.Tensor):
+            drop.step, drop.step_dev = 0, _take("step", step.reshape(1), (1,), torch.int64, self.device)
+        else:
+            drop.step, drop.step_dev = int(step), None
+
+
+class DropoutRunner(_Steps):
+    """Dropout whose mask follows from (seed, stream_id, step) and an element's place: nothing is kept between forward() and
+    backward(), which have to be given the same step.  No buffers of its own: calls may run at the same time."""
+
+    def __init__(self, p, seed, stream_id=0, bf16=False, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self._descriptor = _Descriptor(_drop(p, seed, stream_id))
+        self._made(self.device)
+
+    def forward(self, x, out, step=0, residual=None, stream=None):
+        """out = x with elements dropped and the others scaled, plus residual if given.  out may be x or residual."""
+        d = self._descriptor.desc
+        self._at_step(d, step)
+        a = _take("x", x, x.shape, self.in_dtype, self.device)
+        o = _take("out", out, x.shape, self.in_dtype, self.device)
+        r = _take("residual", residual, x.shape, self.in_dtype, self.device) if residual is not None else 0
+        self._call(stream, binding.dropout, d, _DTYPES[self.in_dtype], x.numel(), a, r, o)
+
+    def backward(self, dout, dx, step=0, stream=None):
+        """dx = the gradient of x (that of residual is dout itself).  dx may be dout."""
+        self.forward(dout, dx, step, stream=stream)
+
+
+class ResidualNormRunner(_Steps):
+    """The end of a block for up to `rows` rows: norm after its branch, gate, dropout, residual sum and the next block's norm, and their
+    gradient.  Holds the rows' statistics (`stats`, that backward() reads as the last forward() left them; another
+    contiguous fp32 [>= rows, 4] buffer may be assigned) and the backward workspace: calls (and graphs captured from them) that may run
+    at the same time need a runner each."""
+
+    def __init__(self, rows, dim, bf16=False, bf16_residual=False, norm="rms", norm_after=False, rows_per_gate=0, eps=1e-5, res_scale=1.0,
+                 branch_scale=1.0, dropout=0.0, seed=0, stream_id=0, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.rows, self.dim, self.rows_per_gate = int(rows), int(dim), int(rows_per_gate)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self.res_dtype = torch.bfloat16 if bf16_residual else torch.float32
+        self.norm_after = bool(norm_after)
+        kinds = dict(rms=ASI_NORM_RMS, layer=ASI_NORM_LAYER)
+        if norm not in kinds:
+            raise ValueError(f"norm: one of {sorted(kinds)} is needed, got {norm!r}")
+        self._descriptor = _Descriptor(BranchDesc(_DTYPES[self.in_dtype], _DTYPES[self.res_dtype], kinds[norm], self.norm_after, self.rows,
+                                                  self.dim, self.rows_per_gate, eps, res_scale, branch_scale,
+                                                  _drop(dropout, seed, stream_id)))
+        self.stats = torch.zeros(self.rows, 4, dtype=torch.float32, device=self.device)
+        self.ws = torch.empty(binding.branch_backward_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
+        self._made(self.device)
+
+    def _own(self):
+        return (self.stats, self.ws)
+
+    def _buffers(self, y, step, gate, after, next):
+        """Descriptor and buffers with what both directions share."""
+        d, b = self._descriptor.desc, Branch()
+        if y.dim() < 1 or y.shape[-1] != self.dim or y.numel() // self.dim > self.rows:
+            raise ValueError(f"y: up to {self.rows} rows of {self.dim} are needed, got {tuple(y.shape)}")
+        d.rows = n = y.numel() // self.dim
+        self._at_step(d.drop, step)
+        if self.stats.shape[0] < n:
+            raise ValueError(f"stats: {n} rows are needed, there are {self.stats.shape[0]}")
+        b.y = _take("y", y, y.shape, self.in_dtype, self.device)
+        b.stats = _take("stats", self.stats, (self.stats.shape[0], 4), torch.float32, self.device)
+        if (gate is not None) != bool(self.rows_per_gate):
+            raise ValueError("gate: the runner was made " + ("with" if self.rows_per_gate else "without") + " one")
+        for name, x, shape in self._weights(n, gate, after, next):
+            setattr(b, name, _take(name, x, shape, torch.float32, self.device))
+        return d, b, n
+
+    def _weights(self, n, gate, after, next, grad=""):
+        """Names, tensors and sizes of those of gate, weights and biases that are there."""
+        shape = (-(-n // self.rows_per_gate), self.dim) if self.rows_per_gate else ()
+        all_ = [("gate", gate, shape)] + [(f"{of}_{what}", x, (self.dim,)) for of, pair in (("after", after), ("next", next))
+                                          for what, x in zip(("weight", "bias"), pair)]
+        return [(f"{grad}{name}", x, size) for name, x, size in all_ if x is not None]
+
+    def forward(self, y, h, h_out, x=None, gate=None, after=(None, None), next=(None, None), step=0, stream=None):
+        """h_out = res_scale h + branch_scale drop(gate norm(y)), x = norm(h_out); `after` and `next` are (weight, bias) of the two
+        norms.  h may be None (0), h_out may be h; without x no norm follows."""
+        d, b, n = self._buffers(y, step, gate, after, next)
+        b.h = _take("h", h, y.shape, self.res_dtype, self.device) if h is not None else None
+        b.h_out = _take("h_out", h_out, y.shape, self.res_dtype, self.device)
+        b.x = _take("x", x, y.shape, self.in_dtype, self.device) if x is not None else None
+        self._call(stream, binding.branch_forward, d, b)
+
+    def backward(self, y, h_out, dx, dh_out, dy, dh=None, gate=None, after=(None, None), next=(None, None), dgate=None, dafter=(None, None),
+                 dnext=(None, None), accumulate=False, step=0, stream=None):
+        """Gradients from those of x (dx) and h_out (dh_out; either may be None): dy and dh overwritten, dgate, dafter and dnext (where
+        given) overwritten or, with accumulate, increased.  dy may be dx, dh may be dh_out."""
+        d, b, n = self._buffers(y, step, gate, after, next)
+        for name, t, dtype in (("h_out", h_out, self.res_dtype), ("dx", dx, self.in_dtype), ("dh_out", dh_out, self.res_dtype),
+                               ("dy", dy, self.in_dtype), ("dh", dh, self.res_dtype)):
+            setattr(b, name, _take(name, t, y.shape, dtype, self.device) if t is not None else None)
+        for name, t, shape in self._weights(n, dgate, dafter, dnext, "d"):
+            setattr(b, name, _take(name, t, shape, torch.float32, self.device))
+        self._call(stream, binding.branch_backward, d, b, accumulate, self.ws.data_ptr(), self.ws.numel())
+
+
+class HeadRunner(_RowResults):
+    """Output layer and loss for up to `rows` hidden states, without logits: log probabilities of given tokens (logp, entropy and lse, as of
+    LogprobRunner) and the gradients of hidden states and weight.  Holds these results and the workspace (for `grad` that of the
+    gradients, `vocab_chunk` columns of the logits' gradient at a time, 0: the library's choice): calls (and graphs captured
+    from them) that may run at the same time need a runner each."""
+
+    top_k = 0
+
+    def __init__(self, rows, vocab, dim, bf16=False, bf16_dw=False, scale=1.0, ignore_index=-100, vocab_chunk=0, grad=True, flags=0,
+                 device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.rows, self.vocab, self.dim, self.grad = int(rows), int(vocab), int(dim), bool(grad)
+        self.in_dtype = torch.bfloat16 if bf16 else torch.float32
+        self.dw_dtype = torch.bfloat16 if bf16_dw else torch.float32
+        self._descriptor = _Descriptor(HeadDesc(_DTYPES[self.in_dtype], _DTYPES[self.dw_dtype], self.rows, self.vocab, self.dim,
+                                                int(vocab_chunk), int(ignore_index), float(scale), int(flags)))
+        self.ws = torch.empty(binding.head_ws_bytes(self.desc, self.grad), dtype=torch.uint8, device=self.device)
+        self._bind(self._new())
+        self._made(self.device)
+
+    def _own(self):
+        return (self.ws, *self._buffers)
+
+    def _inputs(self, x, weight, targets):
+        d, n = self._descriptor.desc, targets.numel()
+        if n > self.rows:
+            raise ValueError(f"targets: up to {self.rows} are needed, got {n}")
+        d.rows = n
+        return d, n, (_take("x", x, (*targets.shape, self.dim), self.in_dtype, self.device),
+                      _take("weight", weight, (self.vocab, self.dim), self.in_dtype, self.device),
+                      _take("targets", targets, targets.shape, torch.int64, self.device))
+
+    def _gradients(self, n, x, dlogp, dentropy, dx, dw):
+        if not self.grad:
+            raise ValueError("the runner was made without gradients")
+        return ((_take("dlogp", dlogp.reshape(-1), (n,), torch.float32, self.device),
+                 _take("dentropy", dentropy.reshape(-1), (n,), torch.float32, self.device) if dentropy is not None else 0),
+                (_take("dx", dx, x.shape, self.in_dtype, self.device) if dx is not None else 0,
+                 _take("dw", dw, (self.vocab, self.dim), self.dw_dtype, self.device) if dw is not None else 0))
+
+    def forward(self, x, weight, targets, stream=None):
+        desc, n, inputs = self._inputs(x, weight, targets)
+        self._outputs(n)
+        self._call(stream, binding.head_logprobs, desc, *inputs, *self._stats, self.ws.data_ptr(), self.ws.numel())
+
+    def backward(self, x, weight, targets, dlogp, dentropy, dx, dw, accumulate=False, stream=None, lse=None, entropy=None):
+        """The gradient of sum(dlogp * logp + dentropy * entropy) into dx and dw (either may be None; dw is increased with accumulate),
+        from the lse and entropy that forward() left, or from those given."""
+        desc, n, inputs = self._inputs(x, weight, targets)
+        weights, grads = self._gradients(n, x, dlogp, dentropy, dx, dw)
+        if lse is None and entropy is None:
+            self._outputs(n, stats=True)
+            _, h, z = self._stats
+        elif lse is None or (entropy is None and dentropy is not None):
+            raise ValueError("lse and entropy (where dentropy is there) come together, from the same forward()")
+        else:
+            z = _take("lse", lse, (n,), torch.float32, self.device)
+            h = _take("entropy", entropy, (n,), torch.float32, self.device) if entropy is not None else 0
+        self._call(stream, binding.head_grad, desc, *inputs, z, h, *weights, *grads, accumulate, self.ws.data_ptr(), self.ws.numel())
+
+    def loss(self, x, weight, targets, dlogp, dentropy, dx, dw, accumulate=False, stream=None):
+        """forward() and backward() in one, for weights that do not depend on the result."""
+        desc, n, inputs = self._inputs(x, weight, targets)
+        weights, grads = self._gradients(n, x, dlogp, dentropy, dx, dw)
+        self._outputs(n)
+        self._call(stream, binding.head_loss, desc, *inputs, *weights, *self._stats, *grads, accumulate, self.ws.data_ptr(),
+                   self.ws.numel())
+
+    def device_status(self, stream=None):
+        """ASI_OK, or ASI_ERR_TIMEOUT where a bounded wait of the last call expired.  Synchronises."""
+        handle = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+        return binding.head_status(self.ws.data_ptr(), handle)
