@@ -166,11 +166,12 @@ __device__ __forceinline__ void to_gradient(float (&v)[32], const RowGrad& r, co
   }
 }
 
-// Waits that end: as mbar_wait, for arrivals of the other CTA too
-__device__ __forceinline__ bool mbar_wait_pair(uint64_t* bar, uint32_t parity, int stall) {
-  const bool ok = mbar_wait(bar, parity, stall);
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return ok;
+// Waits of a whole warp that end (mbar_wait's limit); one answer for all lanes, so that what follows stays in uniform registers
+__device__ __noinline__ bool warp_wait_on(uint64_t* bar, uint32_t parity, int stall) {
+  return __all_sync(~0u, mbar_wait(bar, parity, stall));
+}
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int stall) {
+  return __all_sync(~0u, mbar_try_wait(bar, parity)) || warp_wait_on(bar, parity, stall);
 }
 
 // A pair of CTAs owns a tile of 256 x 256: each brings half of either operand's chunk (128 rows) to its shared memory, products are
@@ -221,13 +222,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
     if (x.chunks < 0) x.chunks = 0;
     return x;
   };
-  const int nst = g.nst;
+  const int nst = g.nst, stall = g.stall;
   bool ok = true;
   int loads = 0;
   if (warp == kWorkers) {
-    // ---- issuer
-    if (lane == 0 && rank == 0) {
+    // ---- issuer: the warp as a whole goes through the loop, so that addresses and descriptors stay in uniform registers (by one
+    // lane alone a chunk's issue took 600 cycles, its products 512), and one lane issues
+    if (rank == 0) {
       const uint32_t at = smem_u32(base);
+      const int per_seg = g.seg;
       int st = 0, seg = 0;
       uint32_t ph = 0;
 #pragma unroll 1
@@ -237,35 +240,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const uint32_t idesc = instr_desc_bf16(kTile, kTile, p.a_mn != 0, p.b_mn != 0);
         // a k-step is 16 bf16: 32 bytes inside the swizzle row of a K-major tile, 16 rows (2048 bytes) of an MN-major one
         const uint64_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
-        const uint32_t a_lead = p.a_mn ? kHalf / 2 : 16, b_lead = p.b_mn ? kHalf / 2 : 16;
+        const uint64_t da0 = smem_desc_sw128(at, p.a_mn ? kHalf / 2 : 16), db0 = smem_desc_sw128(at + kHalf, p.b_mn ? kHalf / 2 : 16);
 #pragma unroll 1
-        for (int c0 = 0; c0 < x.chunks && ok; c0 += g.seg, ++seg) {
+        for (int c0 = 0; c0 < x.chunks && ok; c0 += per_seg, ++seg) {
           const int buf = seg & 1, turn = seg >> 1;
           if (turn > 0) {
-            ok = mbar_wait_pair(acc_free + buf, (uint32_t)(turn + 1) & 1u, g.stall);
+            ok = warp_wait(acc_free + buf, (uint32_t)(turn + 1) & 1u, stall);
             if (!ok) break;
+            asm volatile("fence.acq_rel.cluster;" ::: "memory");   // arrivals of the other CTA too
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           }
-          const int c1 = x.chunks - c0 < g.seg ? x.chunks : c0 + g.seg;
+          const int c1 = x.chunks - c0 < per_seg ? x.chunks : c0 + per_seg;
+          const uint32_t acc = tmem + (uint32_t)(buf * kTile);
 #pragma unroll 1
           for (int c = c0; c < c1; ++c) {
-            ok = mbar_wait(full + st, ph, g.stall);
+            ok = warp_wait(full + st, ph, stall);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint64_t da = smem_desc_sw128(at + st * kStage, a_lead), db = smem_desc_sw128(at + st * kStage + kHalf, b_lead);
+            const uint64_t da = da0 + (uint64_t)(st * (kStage >> 4)), db = db0 + (uint64_t)(st * (kStage >> 4));
+            if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < kK / 16; ++ks)
-              umma_pair_bf16(tmem + (uint32_t)(buf * kTile), da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | ks) ? 1u : 0u);
-            umma_pair_commit(empty + st);
+              for (int ks = 0; ks < kK / 16; ++ks)
+                umma_pair_bf16(acc, da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | ks) ? 1u : 0u);
+              umma_pair_commit(empty + st);
+              if (c + 1 == c1) umma_pair_commit(done + buf);
+            }
+            __syncwarp();
             if (++st == nst) st = 0, ph ^= 1u;
           }
-          if (ok) umma_pair_commit(done + buf);
         }
       }
     }
   } else if (warp == kWorkers + 1) {
     // ---- producer: this CTA's half of each chunk, counted by the first CTA's barrier
-    if (lane == 0) {
+    {
+      const uint32_t full0 = in_cta(full, 0);
       int st = 0;
       uint32_t ph = 1;
 #pragma unroll 1
@@ -273,33 +282,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const Tile x = tile_of(t);
         const HeadProb& p = g.p[x.q];
         const int am = p.a_off + x.m * kTile + rank * 128, bn = p.b_off + x.n * kTile + rank * 128;
-        int kc = x.k0, e = 0;
+        const CUtensorMap *ma = &p.a, *mb = &p.b;
+        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
+        const uint32_t a_term = p.a_term, b_term = p.b_term;
+        const int pairs_of = p.pairs;
+        int ka = p.a_k + x.k0 * kK, kb = p.b_k + x.k0 * kK, e = 0;
 #pragma unroll 1
         for (int c = 0; c < x.chunks; ++c, ++loads) {
           if (loads >= nst) {
-            ok = mbar_wait(empty + st, ph, g.stall);
+            ok = warp_wait(empty + st, ph, stall);
             if (!ok) break;
           }
-          if (rank == 0) mbar_expect_tx(full + st, 2 * kStage);
-          if (!g.stall) {
+          const bool one = elect_one();
+          if (rank == 0 && one) mbar_expect_tx(full + st, 2 * kStage);
+          if (!stall && one) {
             uint8_t* A = base + st * kStage;
-            const uint32_t bar = in_cta(full + st, 0);
-            const int at = (int)(p.a_term >> (2 * e)) & 3, bt = (int)(p.b_term >> (2 * e)) & 3;
-            const int ka = p.a_k + kc * kK, kb = p.b_k + kc * kK;
-            if (p.a_mn) {
-              tma_pair_load_3d(A, &p.a, am, ka, at, bar);
-              tma_pair_load_3d(A + kHalf / 2, &p.a, am + 64, ka, at, bar);
+            const uint32_t bar = full0 + st * 8;
+            const int at = (int)(a_term >> (2 * e)) & 3, bt = (int)(b_term >> (2 * e)) & 3;
+            if (a_mn) {
+              tma_pair_load_3d(A, ma, am, ka, at, bar);
+              tma_pair_load_3d(A + kHalf / 2, ma, am + 64, ka, at, bar);
             } else {
-              tma_pair_load_3d(A, &p.a, ka, am, at, bar);
+              tma_pair_load_3d(A, ma, ka, am, at, bar);
             }
-            if (p.b_mn) {
-              tma_pair_load_3d(A + kHalf, &p.b, bn, kb, bt, bar);
-              tma_pair_load_3d(A + kHalf + kHalf / 2, &p.b, bn + 64, kb, bt, bar);
+            if (b_mn) {
+              tma_pair_load_3d(A + kHalf, mb, bn, kb, bt, bar);
+              tma_pair_load_3d(A + kHalf + kHalf / 2, mb, bn + 64, kb, bt, bar);
             } else {
-              tma_pair_load_3d(A + kHalf, &p.b, kb, bn, bt, bar);
+              tma_pair_load_3d(A + kHalf, mb, kb, bn, bt, bar);
             }
           }
-          if (++e == p.pairs) e = 0, ++kc;
+          __syncwarp();
+          if (++e == pairs_of) e = 0, ka += kK, kb += kK;
           if (++st == nst) st = 0, ph ^= 1u;
         }
       }
@@ -324,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
 #pragma unroll 1
         for (int c0 = 0; c0 < x.chunks; c0 += g.seg, ++seg) {
           const int buf = seg & 1;
-          ok = mbar_wait(done + buf, (uint32_t)(seg >> 1) & 1u, g.stall);
+          ok = mbar_wait(done + buf, (uint32_t)(seg >> 1) & 1u, stall);
           if (__any_sync(0xffffffffu, !ok)) ok = false;
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -342,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         }
         if (!ok) break;
       } else if (x.chunks > 0) {
-        ok = mbar_wait(done + (seg & 1), (uint32_t)(seg >> 1) & 1u, g.stall);
+        ok = mbar_wait(done + (seg & 1), (uint32_t)(seg >> 1) & 1u, stall);
         if (__any_sync(0xffffffffu, !ok)) ok = false;
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");

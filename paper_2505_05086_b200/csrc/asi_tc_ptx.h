@@ -104,6 +104,13 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// one lane of a warp that is here as a whole
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one)::"memory");
+  return one != 0;
+}
+
 // Two CTAs (a pair: ranks 0 and 1 of a cluster) that share products.  Barriers of the pair's CTAs lie at the same offsets.
 __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank) {   // where CTA `rank` has what lies at p here
   uint32_t ra;
