@@ -83,6 +83,66 @@ __device__ __forceinline__ float stored(float x) {
   else return x;
 }
 
+// Eight values at a time, two an instruction
+__device__ __forceinline__ void fma2(float* d, const float* a, const float* b, const float* c) {
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]), "f"(c[0]), "f"(c[1]));
+}
+__device__ __forceinline__ void mul2(float* d, const float* a, const float* b) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+}
+__device__ __forceinline__ void add2(float* d, const float* a, const float* b) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+}
+using Eight = float[kEach];
+__device__ __forceinline__ void fma8(Eight& d, const Eight& a, const Eight& b, const Eight& c) {
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) fma2(d + i, a + i, b + i, c + i);
+}
+__device__ __forceinline__ void fma8(Eight& d, const Eight& a, float b, const Eight& c) {
+  const float q[2] = {b, b};
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) fma2(d + i, a + i, q, c + i);
+}
+__device__ __forceinline__ void fma8(Eight& d, const Eight& a, float b, float c) {
+  const float q[2] = {b, b}, r[2] = {c, c};
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) fma2(d + i, a + i, q, r);
+}
+__device__ __forceinline__ void mul8(Eight& d, const Eight& a, const Eight& b) {
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) mul2(d + i, a + i, b + i);
+}
+__device__ __forceinline__ void mul8(Eight& d, const Eight& a, float b) {
+  const float q[2] = {b, b};
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) mul2(d + i, a + i, q);
+}
+__device__ __forceinline__ void add8(Eight& d, const Eight& a, const Eight& b) {
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) add2(d + i, a + i, b + i);
+}
+__device__ __forceinline__ void add8(Eight& d, const Eight& a, float b) {
+  const float q[2] = {b, b};
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) add2(d + i, a + i, q);
+}
+__device__ __forceinline__ float dot8(const Eight& a, const Eight& b) {
+  float x[2], y[2];
+  mul2(x, a, b), mul2(y, a + 2, b + 2);
+  fma2(x, a + 4, b + 4, x), fma2(y, a + 6, b + 6, y);
+  add2(x, x, y);
+  return x[0] + x[1];
+}
+__device__ __forceinline__ float sum8(const Eight& a) {
+  float x[2], y[2];
+  add2(x, a, a + 2), add2(y, a + 4, a + 6);
+  add2(x, x, y);
+  return x[0] + x[1];
+}
+
 struct DropoutArgs {
   const void *x, *res;
   void* out;
@@ -131,35 +191,53 @@ struct BranchArgs {
   float *dgate, *daw, *dab, *dnw, *dnb;
   float* part;             // [kParts][workers][dim]
   int64_t rows, per;       // rows of a gate's row
-  int64_t run;             // rows of a worker (backward)
+  int64_t run;             // rows of a worker
   int workers, dim, norm_after, accumulate;
+  int stages;              // rows on their way at once
   float eps, rs, bs, inv_dim;
   Drop drop;
 };
 // partial sums of a worker: over the first of its gate's rows, over the last one, over all
 enum Part { kHead1 = 0, kTail1 = 1, kNext1 = 2, kAfter1 = 3, kHead0 = 4, kTail0 = 5, kNext0 = 6, kAfter0 = 7, kParts = 8 };
 
-// sums of two values over the threads of a row, for all of them (tpr a multiple of 32; rows side by side in y)
+// Sums of a value or two over the threads of a row, for all of them (a multiple of 32, kMax at most; rows side by side in y)
+template <int kMax>
 struct RowSum {
-  float2 (*sh)[32];        // [2][rows of the CTA]
-  int phase = 0;
-  __device__ __forceinline__ float2 operator()(float a, float b) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o), b += __shfl_xor_sync(~0u, b, o);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return make_float2(a, b);
-    float2* s = sh[phase * blockDim.y + threadIdx.y];
-    phase ^= 1;
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) s[threadIdx.x >> 5] = make_float2(a, b);
+  static constexpr int kWarps = kMax / 32, kRows = 8;
+  float* sh;               // [2][kRows][2 kWarps], 0 where no warp writes
+  uint32_t phase = 0;
+  __device__ __forceinline__ RowSum(float* s) : sh(s) {
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < 4 * kRows * kWarps; i += blockDim.x * blockDim.y) s[i] = 0.f;
     __syncthreads();
-    const float2 v = lane < warps ? s[lane] : make_float2(0.f, 0.f);
-    a = v.x, b = v.y;
+  }
+  template <bool kTwo>
+  __device__ __forceinline__ float2 get(float a, float b) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-      if (o < warps || (warps & (warps - 1))) a += __shfl_xor_sync(~0u, a, o), b += __shfl_xor_sync(~0u, b, o);
-    a = __shfl_sync(~0u, a, 0), b = __shfl_sync(~0u, b, 0);
-    return make_float2(a, b);
+    for (int o = 16; o; o >>= 1) {
+      a += __shfl_xor_sync(~0u, a, o);
+      if (kTwo) b += __shfl_xor_sync(~0u, b, o);
+    }
+    if (blockDim.x == 32) return make_float2(a, b);
+    float* s = sh + (phase + threadIdx.y) * (2 * kWarps);
+    phase ^= kRows;
+    if ((threadIdx.x & 31) == 0) {
+      s[threadIdx.x >> 5] = a;
+      if (kTwo) s[kWarps + (threadIdx.x >> 5)] = b;
+    }
+    __syncthreads();
+    float x[2] = {0.f, 0.f}, y[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWarps; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(s + i);
+      const float v0[2] = {v.x, v.y}, v1[2] = {v.z, v.w};
+      add2(x, x, v0), add2(x, x, v1);
+      if (kTwo) {
+        const float4 u = *reinterpret_cast<const float4*>(s + kWarps + i);
+        const float u0[2] = {u.x, u.y}, u1[2] = {u.z, u.w};
+        add2(y, y, u0), add2(y, y, u1);
+      }
+    }
+    return make_float2(x[0] + x[1], y[0] + y[1]);
   }
 };
 
@@ -194,11 +272,11 @@ struct Columns {
         if (at(i) < dim) put(row + at(i), f[i]);
     }
   }
-  // fp32 parameters, `none` where there are none; they start at any float
+  // fp32 parameters, `none` where there are none, 0 where there is no column; they start at any float
   __device__ __forceinline__ void param(const float* p, float (&f)[kEach], float none, bool wide) const {
     if (!p) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) f[i] = none;
+      for (int i = 0; i < kEach; ++i) f[i] = there(i) ? none : 0.f;
     } else if (kVec && wide) {
       load(p, f);
     } else {
@@ -221,74 +299,210 @@ struct Columns {
   }
 };
 
+// Rows on their way: a thread copies its eight values of the next rows to shared memory by itself and reads them there itself, so
+// that nobody waits for anybody (rows on 16 bytes alone).  A stage is a row: kTensors slots of kPieces times 16 bytes a thread.
+constexpr int kMaxStages = 4;
+template <int kTensors, int kPieces>
+struct Ring {
+  uint32_t mine, piece, stage_bytes, at;                   // (at: of the row that is next)
+  int stages, left;
+  __device__ __forceinline__ Ring(void* smem, int n) {
+    const uint32_t threads = blockDim.x * blockDim.y, i = threadIdx.y * blockDim.x + threadIdx.x;
+    mine = at = (uint32_t)__cvta_generic_to_shared(smem) + i * 16;
+    piece = threads * 16;
+    stage_bytes = kTensors * kPieces * piece;
+    stages = left = n;
+  }
+  template <int kTensor, typename T>
+  __device__ __forceinline__ void fetch(uint32_t to, const T* p) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (kTensor * kPieces + i) * piece), "l"(p + i * (16 / (int)sizeof(T))) : "memory");
+  }
+  __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  __device__ __forceinline__ void wait() const {            // the oldest row is there
+    if (stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+  }
+  template <int kTensor, typename T>
+  __device__ __forceinline__ void take(const T*, Eight& f) const {
+    uint32_t u[4], v[4];
+    const uint32_t from = at + kTensor * kPieces * piece;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(from) : "memory");
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(u[i] << 16), f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    } else {
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(from + piece) : "memory");
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]), f[4 + i] = __uint_as_float(v[i]);
+    }
+  }
+  __device__ __forceinline__ void advance() {
+    at += stage_bytes;
+    if (--left == 0) left = stages, at = mine;
+  }
+};
+
+__device__ __forceinline__ void clear8(float (&f)[kEach]) {
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) f[i] = 0.f;
+}
+
 __device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// mean (layer norm) and reciprocal deviation of a row; f without its mean on return
-template <bool kLayer, bool kVec>
-__device__ __forceinline__ float2 normalise(float (&f)[kEach], const Columns<kVec>& c, const BranchArgs& p, RowSum& sum) {
+// Mean (layer norm) and reciprocal deviation of a row; f is what the norm makes of it on return (rubbish in columns that are not there).
+template <bool kLayer, bool kVec, int kMax>
+__device__ __forceinline__ float2 normalise(Eight& f, const Columns<kVec>& c, const BranchArgs& p, RowSum<kMax>& sum) {
   float m = 0.f;
   if constexpr (kLayer) {
-    float s = 0.f;
+    m = sum.template get<false>(sum8(f), 0.f).x * p.inv_dim;   // (0 where there is no column)
+    add8(f, f, -m);
+    if (!kVec) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) s += f[i];
-    m = sum(s, 0.f).x * p.inv_dim;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) f[i] = c.there(i) ? f[i] - m : 0.f;
+      for (int i = 0; i < kEach; ++i) f[i] = c.there(i) ? f[i] : 0.f;
+    }
   }
-  float q = 0.f;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) q = fmaf(f[i], f[i], q);
-  const float r = 1.f / sqrtf(sum(q, 0.f).x * p.inv_dim + p.eps);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) f[i] *= r;
+  float q = dot8(f, f);
+  if (kLayer && kVec) q = c.there(0) ? q : 0.f;
+  const float r = rsqrtf(fmaf(sum.template get<false>(q, 0.f).x, p.inv_dim, p.eps));   // (off by 2^-22 at most)
+  mul8(f, f, r);
   return make_float2(m, r);
 }
 
-template <typename TI, typename TR, bool kVec, bool kLayer>
-__global__ void __launch_bounds__(1024) k_branch_forward(const __grid_constant__ BranchArgs p) {
-  __shared__ float2 sh[2 * 8][32];
+constexpr int ctas_of(int most, int small) { return most == 256 ? small : 1; }
+
+// A thread's columns of a parameter: in registers from row to row (kHeld), or read again for each (from L1; rows of 1024 threads,
+// which have 64 registers each)
+template <bool kVec, bool kHeld>
+struct Param {
+  const float* p;
+  float none;
+  float v[kHeld ? kEach : 1];
+  __device__ __forceinline__ Param(const float* q, float n, const Columns<kVec>& c) : p(q), none(n) {
+    if constexpr (kHeld) c.param(q, v, n, on16(q));
+  }
+  __device__ __forceinline__ void get(float (&f)[kEach], const Columns<kVec>& c) const {
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) f[i] = v[i];
+    } else {
+      c.param(p, f, none, on16(p));
+    }
+  }
+};
+
+// The branch's factor and offset: drop(f W + B) with W = b gate w_a, B = b gate b_a in a row of the gate
+template <bool kVec>
+__device__ __forceinline__ void branch_factor(float (&w)[kEach], const float* a, float none, float scale, const float* gate, const Columns<kVec>& c) {
+  c.param(a, w, none, on16(a));
+  float g[kEach];
+  c.param(gate, g, 1.f, on16(gate));
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) w[i] *= scale * g[i];
+}
+
+template <typename TI, typename TR, bool kVec, bool kLayer, int kMax>
+__global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const __grid_constant__ BranchArgs p) {
+  extern __shared__ __align__(16) uint8_t ring_smem[];
+  __shared__ __align__(16) float sh[kMax];
+  constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
-  RowSum sum{sh};
+  RowSum<kMax> sum(sh);
   const Columns<kVec> c(p.dim);
-  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const bool there = t < p.rows;
-  const int64_t at = there ? t * p.dim : 0;
-  float f[kEach], h[kEach], w[kEach], b[kEach];
-  c.load(static_cast<const TI*>(p.y) + at, f, there);
-  c.load(static_cast<const TR*>(p.h) + at, h, there && p.h);
-  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (p.norm_after) {
-    const float2 s = normalise<kLayer>(f, c, p, sum);
-    st.x = s.x, st.y = s.y;
-    c.param(p.aw, w, 1.f, on16(p.aw));
-    c.param(p.ab, b, 0.f, on16(p.ab));
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) f[i] = fmaf(f[i], w[i], b[i]);
+  const int worker = blockIdx.x * blockDim.y + threadIdx.y;
+  const int64_t t0 = worker * p.run, t1 = t0 + p.run < p.rows ? t0 + p.run : p.rows;
+  const uint32_t step = p.drop.below ? step_of(p.drop) : 0;
+  Ring<2, sizeof(TR) / 2> ring(ring_smem, p.stages);
+  const bool mine = c.there(0), res = p.h != nullptr, groups = p.gate && p.per < p.rows;
+  const TI* y = static_cast<const TI*>(p.y);
+  const TR* h_in = static_cast<const TR*>(p.h);
+  const int rows = t1 > t0 ? (int)(t1 - t0) : 0;           // (of this worker)
+  int64_t ahead = t0 * p.dim + c.first;                    // first element of the row to be fetched next
+  int fetched = 0;
+  auto fetch = [&](uint32_t to) {
+    if (fetched++ < rows && mine) {
+      ring.template fetch<0>(to, y + ahead);
+      if (res) ring.template fetch<1>(to, h_in + ahead);
+    }
+    ahead += p.dim;
+    ring.commit();
+  };
+  if (kVec)
+    for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
+  int64_t next_group = groups ? t0 : INT64_MAX;            // row from which on another of the gate's rows holds
+  const float* gate = p.gate;
+  float w[kEach], b[kEach];
+  if (kHeld && !groups) {
+    branch_factor(w, p.aw, 1.f, p.bs, gate, c);
+    if (kLayer) branch_factor(b, p.ab, 0.f, p.bs, gate, c);
   }
-  if (p.gate) {
-    const float* gate = p.gate + (there ? t / p.per : 0) * p.dim;
-    c.param(gate, w, 1.f, on16(gate));
+  const Param<kVec, kHeld> nw(p.nw, 1.f, c), nb(kLayer ? p.nb : nullptr, 0.f, c);
+  const int run = (int)p.run;
+  int64_t at = t0 < p.rows ? t0 * p.dim : 0;
+#pragma unroll 1
+  for (int k = 0; k < run; ++k, at += k < rows ? p.dim : 0) {   // (rows side by side in a CTA go on together: their sums share barriers)
+    const int64_t t = t0 + k;
+    const bool there = k < rows;
+    float f[kEach], h[kEach], x[kEach];
+    if constexpr (kVec) {
+      clear8(f);
+      clear8(h);
+      ring.wait();
+      if (there && mine) {
+        ring.template take<0>(y, f);
+        if (res) ring.template take<1>(h_in, h);
+      }
+      fetch(ring.at);
+      ring.advance();
+    } else {
+      c.load(y + at, f, there);
+      c.load(h_in + at, h, there && res);
+    }
+    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p.norm_after) {
+      const float2 s = normalise<kLayer>(f, c, p, sum);
+      st.x = s.x, st.y = s.y;
+    }
+    if (!kHeld || (there && t >= next_group)) {
+      if (groups && there && t >= next_group) {
+        const int64_t group = t / p.per;
+        gate = p.gate + group * p.dim;
+        next_group = (group + 1) * p.per;
+      }
+      branch_factor(w, p.aw, 1.f, p.bs, gate, c);
+      if (kLayer) branch_factor(b, p.ab, 0.f, p.bs, gate, c);
+    }
+    if (kLayer) fma8(f, f, w, b);
+    else mul8(f, f, w);
+    if (p.drop.below && there) c.mask(p.drop, step, t, f);
+    fma8(f, h, p.rs, f);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) f[i] *= w[i];
-  }
-  if (p.drop.below && there) c.mask(p.drop, step_of(p.drop), t, f);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) f[i] = c.there(i) ? stored<TR>(fmaf(p.bs, f[i], p.rs * h[i])) : 0.f;
-  if (there) c.store(static_cast<TR*>(p.h_out) + at, f);
-  if (p.x) {
-    const float2 s = normalise<kLayer>(f, c, p, sum);
-    st.z = s.x, st.w = s.y;
-    c.param(p.nw, w, 1.f, on16(p.nw));
-    c.param(p.nb, b, 0.f, on16(p.nb));
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) f[i] = fmaf(f[i], w[i], b[i]);
-    if (there) c.store(static_cast<TI*>(p.x) + at, f);
-  }
-  if (there && threadIdx.x == 0) {
-    float* s = p.stats + 4 * t;
-    if (on16(s)) *reinterpret_cast<float4*>(s) = st;
-    else s[0] = st.x, s[1] = st.y, s[2] = st.z, s[3] = st.w;
+    for (int i = 0; i < kEach; ++i) {
+      f[i] = stored<TR>(f[i]);
+      if (!kVec) f[i] = c.there(i) ? f[i] : 0.f;
+    }
+    if (there) c.store(static_cast<TR*>(p.h_out) + at, f);
+    if (p.x) {
+      const float2 s = normalise<kLayer>(f, c, p, sum);
+      st.z = s.x, st.w = s.y;
+      nw.get(x, c);
+      if (kLayer) {
+        nb.get(h, c);
+        fma8(f, f, x, h);
+      } else {
+        mul8(f, f, x);
+      }
+      if (there) c.store(static_cast<TI*>(p.x) + at, f);
+    }
+    if (there && threadIdx.x == 0) {
+      float* s = p.stats + 4 * t;
+      if (on16(s)) *reinterpret_cast<float4*>(s) = st;
+      else s[0] = st.x, s[1] = st.y, s[2] = st.z, s[3] = st.w;
+    }
   }
 }
 
@@ -308,24 +522,51 @@ __device__ __forceinline__ void put_gate(const BranchArgs& p, const Columns<kVec
 }
 
 // kGroups: the gate has several rows
-template <typename TI, typename TR, bool kVec, bool kLayer, bool kGroups>
-__global__ void __launch_bounds__(1024) k_branch_backward(const __grid_constant__ BranchArgs p) {
-  __shared__ float2 sh[2 * 8][32];
+template <typename TI, typename TR, bool kVec, bool kLayer, bool kGroups, int kMax>
+__global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(const __grid_constant__ BranchArgs p) {
+  extern __shared__ __align__(16) uint8_t ring_smem[];
+  __shared__ __align__(16) float sh[kMax];
+  constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
-  RowSum sum{sh};
+  RowSum<kMax> sum(sh);
   const Columns<kVec> c(p.dim);
   const int worker = blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t t0 = worker * p.run, t1 = t0 + p.run < p.rows ? t0 + p.run : p.rows;
   const uint32_t step = p.drop.below ? step_of(p.drop) : 0;
+  Ring<4, sizeof(TR) / 2> ring(ring_smem, p.stages);
+  const bool mine = c.there(0), next = p.dx != nullptr, more = p.dh_out != nullptr;
+  const TI *dx = static_cast<const TI*>(p.dx), *y = static_cast<const TI*>(p.y);
+  const TR *h_out = static_cast<const TR*>(p.h_out), *dh_out = static_cast<const TR*>(p.dh_out);
+  const int rows = t1 > t0 ? (int)(t1 - t0) : 0;           // (of this worker)
+  int64_t ahead = t0 * p.dim + c.first;                    // first element of the row to be fetched next
+  int fetched = 0;
+  auto fetch = [&](uint32_t to) {
+    if (fetched++ < rows && mine) {
+      if (next) {
+        ring.template fetch<0>(to, dx + ahead);
+        ring.template fetch<1>(to, h_out + ahead);
+      }
+      if (more) ring.template fetch<2>(to, dh_out + ahead);
+      ring.template fetch<3>(to, y + ahead);
+    }
+    ahead += p.dim;
+    ring.commit();
+  };
+  if (kVec)
+    for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
   float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {}, a1[kEach] = {}, a0[kEach] = {};
-  const int64_t first = kGroups && p.per ? t0 / p.per : 0;
-  int64_t group = first;
+  const int64_t first = kGroups ? t0 / p.per : 0;
+  int64_t group = first, next_group = kGroups ? (first + 1) * p.per : INT64_MAX;
+  const float* gate = p.gate ? p.gate + (kGroups && t0 < p.rows ? group * p.dim : 0) : nullptr;
+  float w[kEach];                                          // gate w_a
+  if (kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
+  const Param<kVec, kHeld> nw(p.nw, 1.f, c);
   auto part = [&](int which) { return p.part + ((int64_t)which * p.workers + worker) * p.dim; };
   // the sums over the worker's rows of one of the gate's
   auto flush = [&](bool whole) {
-    float gate[kEach];
-    c.param(p.gate + group * p.dim, gate, 1.f, on16(p.gate + group * p.dim));
+    float g[kEach];
+    c.param(gate, g, 1.f, on16(gate));
     if (p.dgate) {
       if (whole) {
         put_gate(p, c, group, s1, s0);
@@ -341,81 +582,89 @@ __global__ void __launch_bounds__(1024) k_branch_backward(const __grid_constant_
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      a1[i] = fmaf(gate[i], s1[i], a1[i]), s1[i] = 0.f;
-      if (kLayer) a0[i] = fmaf(gate[i], s0[i], a0[i]), s0[i] = 0.f;
+      a1[i] = fmaf(g[i], s1[i], a1[i]), s1[i] = 0.f;
+      if (kLayer) a0[i] = fmaf(g[i], s0[i], a0[i]), s0[i] = 0.f;
     }
   };
+  const int run = (int)p.run;
+  int64_t at = t0 < p.rows ? t0 * p.dim : 0;
 #pragma unroll 1
-  for (int64_t k = 0; k < p.run; ++k) {                    // (rows side by side in a CTA go on together: their sums share barriers)
+  for (int k = 0; k < run; ++k, at += k < rows ? p.dim : 0) {   // (rows side by side in a CTA go on together: their sums share barriers)
     const int64_t t = t0 + k;
-    const bool there = t < t1;
-    const int64_t at = there ? t * p.dim : 0;
-    float d[kEach], f[kEach], w[kEach];
+    const bool there = k < rows;
+    float d[kEach], f[kEach], x[kEach];
     float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
     if (there) {
       const float* s = p.stats + 4 * t;
       if (on16(s)) st = *reinterpret_cast<const float4*>(s);
       else st = make_float4(s[0], s[1], s[2], s[3]);
     }
-    c.load(static_cast<const TR*>(p.dh_out) + at, d, there && p.dh_out);
-    if (p.dx) {
-      float x[kEach];
-      c.load(static_cast<const TI*>(p.dx) + at, x, there);
-      c.load(static_cast<const TR*>(p.h_out) + at, f, there);
-      c.param(p.nw, w, 1.f, on16(p.nw));
-      float q1 = 0.f, q0 = 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        f[i] = c.there(i) ? (f[i] - st.z) * st.w : 0.f;
-        n1[i] = fmaf(x[i], f[i], n1[i]);
-        if (kLayer) n0[i] += x[i];
-        w[i] *= x[i];
-        q1 = fmaf(w[i], f[i], q1);
-        if (kLayer) q0 += w[i];
+    if constexpr (kVec) {
+      ring.wait();
+      clear8(d);
+      if (mine && there && more) ring.template take<2>(dh_out, d);
+    } else {
+      c.load(dh_out + at, d, there && more);
+    }
+    if (next) {
+      if constexpr (kVec) {
+        clear8(x);
+        clear8(f);
+        if (mine && there) {
+          ring.template take<0>(dx, x);
+          ring.template take<1>(h_out, f);
+        }
+      } else {
+        c.load(dx + at, x, there);
+        c.load(h_out + at, f, there);
       }
-      const float2 m = sum(q1, q0);
-      const float m1 = m.x * p.inv_dim, m0 = kLayer ? m.y * p.inv_dim : 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) d[i] += st.w * (w[i] - m0 - f[i] * m1);
+      float v[kEach];
+      nw.get(v, c);
+      if (kLayer) fma8(f, f, st.w, -st.z * st.w);
+      else mul8(f, f, st.w);
+      fma8(n1, x, f, n1);                                  // (x is 0 where there is no column, and so are its products)
+      if (kLayer) add8(n0, n0, x);
+      mul8(x, x, v);
+      const float2 m = sum.template get<kLayer>(dot8(x, f), kLayer ? sum8(x) : 0.f);
+      // d + s (x - m0 - f m1)
+      fma8(x, f, -m.x * p.inv_dim, x);
+      if (kLayer) add8(x, x, -m.y * p.inv_dim);
+      fma8(d, x, st.w, d);
     }
     if (p.dh && there) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) w[i] = p.rs * d[i];
-      c.store(static_cast<TR*>(p.dh) + at, w);
+      mul8(x, d, p.rs);
+      c.store(static_cast<TR*>(p.dh) + at, x);
     }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) d[i] = c.there(i) ? p.bs * d[i] : 0.f;
+    mul8(d, d, there ? p.bs : 0.f);
     if (p.drop.below && there) c.mask(p.drop, step, t, d);
-    c.load(static_cast<const TI*>(p.y) + at, f, there);
-    if (kGroups && there && t / p.per != group) {
+    if constexpr (kVec) {
+      clear8(f);
+      if (mine && there) ring.template take<3>(y, f);
+      fetch(ring.at);
+      ring.advance();
+    } else {
+      c.load(y + at, f, there);
+    }
+    if (kGroups && there && t >= next_group) {
       flush(group != first || first * p.per >= t0);
       group = t / p.per;
+      next_group = (group + 1) * p.per;
+      gate = p.gate + group * p.dim;
+      if (kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
     }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if (p.norm_after) f[i] = c.there(i) ? (f[i] - st.x) * st.y : 0.f;
-      s1[i] = there ? fmaf(d[i], f[i], s1[i]) : s1[i];
-      if (kLayer) s0[i] = there ? s0[i] + d[i] : s0[i];
-    }
-    if (p.gate) {
-      const float* gate = p.gate + (kGroups ? group * p.dim : 0);
-      c.param(gate, w, 1.f, on16(gate));
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) d[i] *= w[i];
-    }
+    if (!kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
     if (p.norm_after) {
-      c.param(p.aw, w, 1.f, on16(p.aw));
-      float q1 = 0.f, q0 = 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        d[i] *= w[i];
-        q1 = fmaf(d[i], f[i], q1);
-        if (kLayer) q0 += d[i];
-      }
-      const float2 m = sum(q1, q0);
-      const float m1 = m.x * p.inv_dim, m0 = kLayer ? m.y * p.inv_dim : 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) d[i] = st.y * (d[i] - m0 - f[i] * m1);
+      if (kLayer) fma8(f, f, st.y, -st.x * st.y);
+      else mul8(f, f, st.y);
+    }
+    fma8(s1, d, f, s1);
+    if (kLayer) add8(s0, s0, d);
+    mul8(d, d, w);                                         // (w is 0 where there is no column)
+    if (p.norm_after) {
+      const float2 m = sum.template get<kLayer>(dot8(d, f), kLayer ? sum8(d) : 0.f);
+      fma8(d, f, -m.x * p.inv_dim, d);
+      if (kLayer) add8(d, d, -m.y * p.inv_dim);
+      mul8(d, d, st.y);
     }
     if (there) c.store(static_cast<TI*>(p.dy) + at, d);
   }
@@ -425,12 +674,7 @@ __global__ void __launch_bounds__(1024) k_branch_backward(const __grid_constant_
     flush((group != first || first * p.per >= t0) && end <= t1);
   }
   if (!p.part) return;
-  auto keep = [&](int which, const float (&v)[kEach]) {
-    float* q = part(which);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (c.there(i)) q[c.at(i)] = v[i];
-  };
+  auto keep = [&](int which, const float (&v)[kEach]) { c.store(part(which), v); };
   if (!kGroups && (p.dgate || p.daw)) keep(kHead1, s1);
   if (!kGroups && kLayer && (p.dgate || p.dab)) keep(kHead0, s0);
   if (kGroups && p.daw) keep(kAfter1, a1);
@@ -439,9 +683,9 @@ __global__ void __launch_bounds__(1024) k_branch_backward(const __grid_constant_
   if (kLayer && p.dnb) keep(kNext0, n0);
 }
 
-// The workers' sums joined in order: 32 columns a CTA, 32 shares of the workers side by side.  blockIdx.y 0: of the next norm, 1: of the
+// The workers' sums joined in order: 32 columns a CTA, 16 shares of the workers side by side.  blockIdx.y 0: of the next norm, 1: of the
 // norm after and of a gate of one row; 2 ..: rows of a gate that workers share
-constexpr int kSlices = 32;
+constexpr int kSlices = 16;
 struct SumsArgs {
   BranchArgs b;
   int layer, groups;
@@ -456,7 +700,7 @@ __global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_const
   auto total = [&](int one0, int one, int two0, int two, int64_t w0, int64_t w1) {
     float x = 0.f, y = 0.f;
     if (col < p.dim)
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t w = w0 + slice; w <= w1; w += kSlices) {
         x += p.part[((int64_t)(w == w0 ? one0 : one) * p.workers + w) * p.dim + col];
         if (two >= 0) y += p.part[((int64_t)(w == w0 ? two0 : two) * p.workers + w) * p.dim + col];
@@ -486,9 +730,9 @@ __global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_const
       return;
     }
     if (!p.dgate && !p.daw && !p.dab) return;
-    float2 r = make_float2(0.f, 0.f);
-    if (p.dgate || p.daw) r.x = total(kHead1, kHead1, 0, -1, 0, last).x;
-    if (a.layer && (p.dgate || p.dab)) r.y = total(kHead0, kHead0, 0, -1, 0, last).x;
+    const bool one = p.dgate || p.daw, two = a.layer && (p.dgate || p.dab);
+    float2 r = total(one ? kHead1 : kHead0, one ? kHead1 : kHead0, kHead0, one && two ? kHead0 : -1, 0, last);
+    if (!one) r.y = r.x;
     if (slice || col >= p.dim) return;
     const float w = p.aw ? p.aw[col] : 1.f, b = p.ab ? p.ab[col] : 0.f, g = p.gate ? p.gate[col] : 1.f;
     write(p.dgate, fmaf(w, r.x, b * r.y));
@@ -571,21 +815,29 @@ Shape shape_of(int64_t dim) {
   const int tpr = (int)align_up((size_t)ceil_div(dim, kEach), 32);
   return {tpr, std::max(1, std::min(8, 256 / tpr))};
 }
-// rows of a worker and workers: two CTAs of 256 threads an SM or what has as many threads
+// Rows of a worker and workers: `ctas` CTAs of up to 256 threads an SM, or one larger one
 struct Work {
   int64_t run;
   int workers;
 };
-Work work_of(int64_t rows, int64_t dim) {
+constexpr int kForwardCtas = 3, kBackwardCtas = 2;
+int64_t most_workers(int64_t dim, int ctas) {
   const Shape s = shape_of(dim);
-  const int64_t most = (int64_t)148 * std::max(1, 512 / (s.tpr * s.rows)) * s.rows;
-  const int64_t run = std::max<int64_t>(1, ceil_div(rows, most));
+  return (int64_t)148 * (s.tpr * s.rows <= 256 ? ctas : 1) * s.rows;
+}
+Work work_of(int64_t rows, int64_t dim, int ctas) {
+  const int64_t run = std::max<int64_t>(1, ceil_div(rows, most_workers(dim, ctas)));
   return {run, (int)std::max<int64_t>(1, ceil_div(rows, run))};
 }
 size_t part_bytes(int64_t rows, int64_t dim) {
-  const Shape s = shape_of(dim);
-  const int64_t most = (int64_t)148 * std::max(1, 512 / (s.tpr * s.rows)) * s.rows;
-  return align_up((size_t)kParts * std::max<int64_t>(1, std::min(rows, most)) * dim * 4, 256);
+  return align_up((size_t)kParts * std::max<int64_t>(1, std::min(rows, most_workers(dim, kBackwardCtas))) * dim * 4, 256);
+}
+// shared memory of the rows on their way: as many stages as `room` bytes hold
+size_t stages_of(BranchArgs* a, bool vec, int tensors, int pieces, size_t room) {
+  const Shape s = shape_of(a->dim);
+  const size_t each = (size_t)tensors * pieces * 16 * s.tpr * s.rows;
+  a->stages = vec ? (int)std::max<size_t>(1, std::min<size_t>(kMaxStages, room / each)) : 0;
+  return a->stages * each;
 }
 
 BranchArgs args_of(const asi_branch_desc_t* d, const asi_branch_t* t, const Drop& drop) {
@@ -599,28 +851,54 @@ BranchArgs args_of(const asi_branch_desc_t* d, const asi_branch_t* t, const Drop
   return a;
 }
 
-template <typename TI, typename TR, bool kVec>
-cudaError_t launch_forward(const BranchArgs& a, bool layer, cudaStream_t st) {
-  const Shape s = shape_of(a.dim);
-  const dim3 grid((unsigned)ceil_div(a.rows, s.rows)), block(s.tpr, s.rows);
-  return layer ? launch_pdl(k_branch_forward<TI, TR, kVec, true>, grid, block, 0, st, a) : launch_pdl(k_branch_forward<TI, TR, kVec, false>, grid, block, 0, st, a);
+template <typename... P>
+cudaError_t launch_ring(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const BranchArgs& a) {
+  if (smem > 40 << 10) {
+    const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(kernel, grid, block, smem, st, a);
 }
 
-template <typename TI, typename TR, bool kVec>
-cudaError_t launch_backward(BranchArgs& a, bool layer, cudaStream_t st) {
+template <typename TI, typename TR, bool kVec, int kMax>
+cudaError_t launch_forward_as(BranchArgs& a, bool layer, cudaStream_t st) {
   const Shape s = shape_of(a.dim);
-  const Work k = work_of(a.rows, a.dim);
+  const Work k = work_of(a.rows, a.dim, kForwardCtas);
+  a.run = k.run;
+  a.workers = k.workers;
+  const size_t smem = stages_of(&a, kVec, 2, sizeof(TR) == 4 ? 2 : 1, (kMax == 256 ? 200 / kForwardCtas : 200) << 10);
+  const dim3 grid((unsigned)ceil_div(k.workers, s.rows)), block(s.tpr, s.rows);
+  return layer ? launch_ring(k_branch_forward<TI, TR, kVec, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_forward<TI, TR, kVec, false, kMax>, grid, block, smem, st, a);
+}
+template <typename TI, typename TR, bool kVec>
+cudaError_t launch_forward(BranchArgs& a, bool layer, cudaStream_t st) {
+  const int tpr = shape_of(a.dim).tpr;
+  if (tpr <= 256) return launch_forward_as<TI, TR, kVec, 256>(a, layer, st);
+  return tpr <= 512 ? launch_forward_as<TI, TR, kVec, 512>(a, layer, st) : launch_forward_as<TI, TR, kVec, 1024>(a, layer, st);
+}
+
+template <typename TI, typename TR, bool kVec, int kMax>
+cudaError_t launch_backward_as(BranchArgs& a, bool layer, cudaStream_t st) {
+  const Shape s = shape_of(a.dim);
+  const Work k = work_of(a.rows, a.dim, kBackwardCtas);
   a.run = k.run;
   a.workers = k.workers;
   const bool groups = a.gate && a.per < a.rows;
+  const size_t smem = stages_of(&a, kVec, 4, sizeof(TR) == 4 ? 2 : 1, (kMax == 256 ? 200 / kBackwardCtas : 200) << 10);
   const dim3 grid((unsigned)ceil_div(k.workers, s.rows)), block(s.tpr, s.rows);
   cudaError_t e;
-  if (layer) e = groups ? launch_pdl(k_branch_backward<TI, TR, kVec, true, true>, grid, block, 0, st, a) : launch_pdl(k_branch_backward<TI, TR, kVec, true, false>, grid, block, 0, st, a);
-  else e = groups ? launch_pdl(k_branch_backward<TI, TR, kVec, false, true>, grid, block, 0, st, a) : launch_pdl(k_branch_backward<TI, TR, kVec, false, false>, grid, block, 0, st, a);
+  if (layer) e = groups ? launch_ring(k_branch_backward<TI, TR, kVec, true, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_backward<TI, TR, kVec, true, false, kMax>, grid, block, smem, st, a);
+  else e = groups ? launch_ring(k_branch_backward<TI, TR, kVec, false, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_backward<TI, TR, kVec, false, false, kMax>, grid, block, smem, st, a);
   if (e != cudaSuccess || !a.part) return e;
   const SumsArgs q = {a, layer, groups};
   const int64_t shared = groups && a.dgate && a.per > 1 ? std::min<int64_t>(ceil_div(a.rows, a.per), 1024) : 0;
   return launch_pdl(k_branch_sums, dim3((unsigned)ceil_div(a.dim, 32), (unsigned)(2 + shared)), dim3(32 * kSlices), 0, st, q);
+}
+template <typename TI, typename TR, bool kVec>
+cudaError_t launch_backward(BranchArgs& a, bool layer, cudaStream_t st) {
+  const int tpr = shape_of(a.dim).tpr;
+  if (tpr <= 256) return launch_backward_as<TI, TR, kVec, 256>(a, layer, st);
+  return tpr <= 512 ? launch_backward_as<TI, TR, kVec, 512>(a, layer, st) : launch_backward_as<TI, TR, kVec, 1024>(a, layer, st);
 }
 
 }  // namespace
