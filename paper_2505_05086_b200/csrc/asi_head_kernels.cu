@@ -34,9 +34,7 @@ constexpr int kK = 64;                                    // k per chunk: 64 bf1
 constexpr int kMaxStages = 6;
 constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's chunk
 constexpr uint32_t kStage = 2 * kHalf;
-constexpr int kPitch = 33;                                // floats of a staged row of 32 (columns in banks of their own)
-constexpr uint32_t kStageOut = 32 * kPitch * 4;           // a warp's staged 32 x 32 results
-constexpr uint32_t kStageG = 32 * 64 * 2;                 // a warp's staged 32 x 64 values of G, one term
+constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
 constexpr int kSeg = 16;                                  // chunks that add up in TMEM where results are held to fp32
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
@@ -58,10 +56,15 @@ struct HeadProb {
   void* out;
   int add_kind, out_kind;
   int64_t ld, split_stride;     // elements
+  CUtensorMap o;                // the result in boxes of 32 rows of 128 bytes
+  int how;                      // Store: how results leave
 };
+// by coalesced words (any alignment, `add` of any kind), by tensor copies, or added to fp32 by tensor copies (add is out)
+enum Store { kWords = 0, kCopy = 1, kAdd = 2 };
 struct HeadArgs {
   HeadProb p[2];
   int np, tiles0, tiles;        // tiles of the first product, of all
+  int few, each_few, more_few, each_rest, more_rest;   // of the second product: how many a pair takes (see Mine)
   int nst;                      // stages
   int seg;                      // chunks that add up in TMEM (kSegmented), or all
   int* status;
@@ -174,6 +177,20 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int st
   return __all_sync(~0u, mbar_try_wait(bar, parity)) || warp_wait_on(bar, parity, stall);
 }
 
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// Column `lane` of staged results (32 x 32, column i of row r at i ^ r), up to 32 rows, added to another's and stored.  What is added is on its way for all rows at once.
+template <typename TO, typename TA>
+__device__ __forceinline__ void put_words(const float* s, int lane, TO* to, const TA* add, int64_t ld, int rows) {
+  float f[32];
+#pragma unroll
+  for (int r = 0; r < 32; ++r) f[r] = add && r < rows ? as_float(add[r * ld]) : 0.f;
+#pragma unroll
+  for (int r = 0; r < 32; ++r)
+    if (r < rows) to[r * ld] = (TO)(f[r] + s[r * 32 + (lane ^ r)]);
+}
+
 // A pair of CTAs owns a tile of 256 x 256: each brings half of either operand's chunk (128 rows) to its shared memory, products are
 // issued for both by the first one (tcgen05, cta_group 2: each tensor core reads its own half of A and both halves of B), and each
 // has the 128 x 256 accumulators of its rows in its TMEM, twice, so that the next tile's products run under this one's epilogue.
@@ -207,11 +224,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   pdl_launch_dependents();
 
   struct Tile { int q, m, n, s, chunks, k0; };
-  auto tile_of = [&](int t) {
+  // The tiles of a pair: every `pairs`-th of the first product; of the second one a stretch, whose length makes up for what the
+  // first left uneven (pairs below `few` had one tile more)
+  const int mine0 = (g.tiles0 - pair + pairs - 1) / pairs;
+  const bool late = pair >= g.few;
+  const int q1 = late ? pair - g.few : pair, each1 = late ? g.each_rest : g.each_few, more1 = late ? g.more_rest : g.more_few;
+  const int from1 = (late ? g.few * g.each_few + g.more_few : 0) + q1 * each1 + (q1 < more1 ? q1 : more1);
+  const int mine = mine0 + (g.np > 1 ? each1 + (q1 < more1 ? 1 : 0) : 0);
+  auto tile_of = [&](int i) {
     Tile x;
-    x.q = t >= g.tiles0 ? 1 : 0;
+    x.q = i >= mine0 ? 1 : 0;
     const HeadProb& p = g.p[x.q];
-    if (x.q) t -= g.tiles0;
+    int t = x.q ? from1 + i - mine0 : pair + i * pairs;
     const int each = p.mt * p.nt;
     x.s = t / each;
     t -= x.s * each;
@@ -234,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
       int st = 0, seg = 0;
       uint32_t ph = 0;
 #pragma unroll 1
-      for (int t = pair; t < g.tiles && ok; t += pairs) {
+      for (int t = 0; t < mine && ok; ++t) {
         const Tile x = tile_of(t);
         const HeadProb& p = g.p[x.q];
         const uint32_t idesc = instr_desc_bf16(kTile, kTile, p.a_mn != 0, p.b_mn != 0);
@@ -278,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
       int st = 0;
       uint32_t ph = 1;
 #pragma unroll 1
-      for (int t = pair; t < g.tiles && ok; t += pairs) {
+      for (int t = 0; t < mine && ok; ++t) {
         const Tile x = tile_of(t);
         const HeadProb& p = g.p[x.q];
         const int am = p.a_off + x.m * kTile + rank * 128, bn = p.b_off + x.n * kTile + rank * 128;
@@ -323,10 +347,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
     const int quad = warp & 3, col0 = (warp >> 2) * 128;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)col0;
     const uint32_t free0 = in_cta(acc_free, 0), free1 = in_cta(acc_free + 1, 0);
-    uint8_t* out = base + nst * kStage + warp * (kEpi == kGrad ? g.terms * kStageG : kStageOut);
+    uint8_t* out = base + nst * kStage + warp * (kEpi == kGrad ? g.terms * kStaged : kStaged);
     int seg = 0;
 #pragma unroll 1
-    for (int t = pair; t < g.tiles && ok; t += pairs) {
+    for (int t = 0; t < mine && ok; ++t) {
       const Tile x = tile_of(t);
       const HeadProb& p = g.p[x.q];
       const int row0 = x.m * kTile + rank * 128 + quad * 32, row = row0 + lane;
@@ -413,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
               uint4 w;
               w.x = pack2(v[8 * u], v[8 * u + 1]), w.y = pack2(v[8 * u + 2], v[8 * u + 3]);
               w.z = pack2(v[8 * u + 4], v[8 * u + 5]), w.w = pack2(v[8 * u + 6], v[8 * u + 7]);
-              *reinterpret_cast<uint4*>(out + e * kStageG + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) = w;
+              *reinterpret_cast<uint4*>(out + e * kStaged + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) = w;
               if (g.terms > 1) {
                 const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -428,39 +452,60 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-              for (int e = 0; e < g.terms; ++e) tma_store_3d(&g.g, out + e * kStageG, n - 32, row0, e);
+              for (int e = 0; e < g.terms; ++e) tma_store_3d(&g.g, out + e * kStaged, n - 32, row0, e);
               asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
           }
         } else {
-          // through shared memory, so that a warp's lanes are neighbouring columns
-          float* s = reinterpret_cast<float*>(out);
-          __syncwarp();
+          if (p.how != kWords) {
+            // rows of 128 bytes, 32 columns of fp32 or 64 of bf16, their 16-byte units swizzled by the row
+            const bool wide = p.out_kind == kF32;
+            if (wide || (cc & 1) == 0) {
+              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              __syncwarp();
+            }
+            uint8_t* r = out + lane * 128;
+            if (wide) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) s[lane * kPitch + i] = v[i];
-          __syncwarp();
-          const int col = n + lane;
-          if (col < p.N) {
-            const int64_t at = x.s * p.split_stride + (int64_t)row0 * p.ld + col;
-            const int rows = p.M - row0 < 32 ? p.M - row0 : 32;
-#pragma unroll 1
-            for (int r0 = 0; r0 < rows; r0 += 8) {
-              float f[8];
+              for (int u = 0; u < 8; ++u) *reinterpret_cast<float4*>(r + ((u ^ (lane & 7)) * 16)) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+            } else {
 #pragma unroll
-              for (int r = 0; r < 8; ++r) {
-                f[r] = 0.f;
-                if (r0 + r < rows) {
-                  if (p.add_kind == kF32) f[r] = static_cast<const float*>(p.add)[at + (r0 + r) * p.ld];
-                  else if (p.add_kind == kB16) f[r] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.add)[at + (r0 + r) * p.ld]);
+              for (int u = 0; u < 4; ++u)
+                *reinterpret_cast<uint4*>(r + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) =
+                    make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]), pack2(v[8 * u + 6], v[8 * u + 7]));
+            }
+            if (wide || (cc & 1)) {
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                const int col = wide ? n : n - 32;
+                if (col < p.N && row0 < p.M) {
+                  if (p.how == kAdd) tma_add_3d(&p.o, out, col, row0, x.s);
+                  else tma_store_3d(&p.o, out, col, row0, x.s);
                 }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
               }
+            }
+          } else {
+            // through shared memory, so that a warp's lanes are neighbouring columns
+            float* s = reinterpret_cast<float*>(out);
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (of a tile of the other product)
+            __syncwarp();
 #pragma unroll
-              for (int r = 0; r < 8; ++r)
-                if (r0 + r < rows) {
-                  const float o = f[r] + s[(r0 + r) * kPitch + lane];
-                  if (p.out_kind == kF32) static_cast<float*>(p.out)[at + (r0 + r) * p.ld] = o;
-                  else static_cast<__nv_bfloat16*>(p.out)[at + (r0 + r) * p.ld] = __float2bfloat16_rn(o);
-                }
+            for (int i = 0; i < 32; ++i) s[lane * 32 + (i ^ lane)] = v[i];
+            __syncwarp();
+            const int rows = p.M - row0 < 32 ? p.M - row0 : 32;
+            if (n + lane < p.N && rows > 0) {
+              const int64_t at = x.s * p.split_stride + (int64_t)row0 * p.ld + n + lane;
+              if (p.out_kind == kF32) {
+                float* to = static_cast<float*>(p.out) + at;
+                if (p.add_kind == kF32) put_words<float, float>(s, lane, to, static_cast<const float*>(p.add) + at, p.ld, rows);
+                else put_words<float, float>(s, lane, to, nullptr, p.ld, rows);
+              } else {
+                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + at;
+                if (p.add_kind == kF32) put_words<__nv_bfloat16, float>(s, lane, to, static_cast<const float*>(p.add) + at, p.ld, rows);
+                else put_words<__nv_bfloat16, __nv_bfloat16>(s, lane, to, p.add_kind == kB16 ? static_cast<const __nv_bfloat16*>(p.add) + at : nullptr, p.ld, rows);
+              }
             }
           }
         }
@@ -474,8 +519,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         }
       }
     }
-    if constexpr (kEpi == kGrad) {
-      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // G is there before the next kernel reads it
+    if constexpr (kEpi != kStats) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // all is there before the next kernel reads it
       __syncwarp();
     }
   }
@@ -676,7 +721,7 @@ void set_pairs(HeadProb* p, int a_terms, int b_terms) {
 
 template <int kEpi, bool kSegmented>
 cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
-  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (kEpi == kGrad ? (size_t)g.terms * kStageG : kEpi == kOut ? kStageOut : 0);
+  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (kEpi == kGrad ? (size_t)g.terms * kStaged : kEpi == kOut ? kStaged : 0);
   const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented>), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -696,12 +741,35 @@ cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k_head_gemm<kEpi, kSegmented>, g);
 }
 
+// Shares out the tiles of the second product so that all pairs end at about the same time: `few` pairs have had one tile more of the
+// first (each worth `ratio` of the second's).
+void share_tiles(HeadArgs* g, int pairs) {
+  const int tiles1 = g->tiles - g->tiles0, base = g->tiles0 / pairs;
+  g->few = g->tiles0 - base * pairs;
+  const int rest = pairs - g->few;
+  const double ratio = (double)g->p[0].per * g->p[0].pairs / ((double)g->p[1].per * g->p[1].pairs);
+  // each_few x few + (each_few + ratio) x rest = tiles1
+  double share = (tiles1 - ratio * rest) / pairs;
+  int to_few = share > 0 ? (int)std::lround(share * g->few) : 0;
+  if (g->few == 0) to_few = 0;
+  to_few = std::min(to_few, tiles1);
+  if (rest == 0) to_few = tiles1;
+  g->each_few = g->few ? to_few / g->few : 0;
+  g->more_few = g->few ? to_few - g->each_few * g->few : 0;
+  const int to_rest = tiles1 - to_few;
+  g->each_rest = rest ? to_rest / rest : 0;
+  g->more_rest = rest ? to_rest - g->each_rest * rest : 0;
+}
+
 template <int kEpi>
 cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   g.nst = kEpi == kGrad && g.terms == 3 ? 4 : 6;
   g.seg = segmented ? kSeg : 1 << 30;
   g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
   g.tiles = g.tiles0 + (g.np > 1 ? g.p[1].mt * g.p[1].nt * g.p[1].splits : 0);
+  g.few = 0;
+  g.each_few = g.more_few = g.each_rest = g.more_rest = 0;
+  if (g.np > 1) share_tiles(&g, std::min(g.tiles, 74));
   return segmented ? launch_gemm_as<kEpi, true>(g, st) : launch_gemm_as<kEpi, false>(g, st);
 }
 
@@ -709,6 +777,18 @@ cudaError_t launch_split(const asi_head_desc_t* d, const Layout& l, const void* 
   SplitArgs a = {in, static_cast<__nv_bfloat16*>(out), rows, d->dim, l.ld, l.in_terms};
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * d->dim, 256 * 4), 148 * 8));
   return d->in_dtype == ASI_BF16 ? launch_pdl(k_head_split<__nv_bfloat16>, grid, dim3(256), 0, st, a) : launch_pdl(k_head_split<float>, grid, dim3(256), 0, st, a);
+}
+
+// How a product's results leave: by copies where their rows lie on 16 bytes and what is added is what is there, in fp32
+void set_store(HeadProb* p, int64_t rows, int64_t N) {
+  const size_t e = p->out_kind == kF32 ? 4 : 2;
+  p->how = kWords;
+  if ((p->ld * e) % 16 != 0 || !aligned(p->out, 16) || (p->add && (p->out_kind != kF32 || p->add != p->out))) return;
+  const cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)rows, (cuuint64_t)p->splits};
+  const cuuint64_t strides[2] = {(cuuint64_t)p->ld * e, (cuuint64_t)std::max(p->split_stride, p->ld) * e};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / e), 32, 1};
+  if (!encode_map(&p->o, e == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p->out, 3, dims, strides, box)) return;
+  p->how = p->add ? kAdd : kCopy;
 }
 
 // A call's buffers
@@ -834,7 +914,10 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
     g.np = 0;
     if (c.dx) g.p[g.np++] = px;
     if (c.dw) g.p[g.np++] = pw;
-    e = launch_gemm<kOut>(g, fine || dw_kind == kF32, st);
+    for (int q = 0; q < g.np; ++q) set_store(&g.p[q], g.p[q].M, D);
+    // sums that leave TMEM on the way, where results are held to fp32 and long enough for it to show
+    const bool long_dw = c.dw && dw_kind == kF32 && pw.kc * pw.pairs > kSeg, long_dx = c.dx && fine && px.per * px.pairs > kSeg;
+    e = launch_gemm<kOut>(g, long_dw || long_dx, st);
     if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
   }
   if (c.dx && splits > 1) {

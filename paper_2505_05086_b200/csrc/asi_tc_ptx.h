@@ -133,6 +133,11 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void*
                "r"(z), "r"(smem_u32(src))
                : "memory");
 }
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, const void* src, int x, int y, int z) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+               "r"(z), "r"(smem_u32(src))
+               : "memory");
+}
 __device__ __forceinline__ void umma_pair_bf16(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -160,7 +165,9 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {   // 32
       : "memory");
 }
 
-// A tensor map of bf16 values in boxes with rows of 128 bytes at most, 128-byte swizzle, zeros outside (asi_tc_kernels.cu)
+// A tensor map of boxes with rows of 128 bytes at most, 128-byte swizzle, zeros outside (asi_tc_kernels.cu)
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                const cuuint32_t* box);
 bool encode_bf16_map(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
                      const cuuint32_t* box);
 
