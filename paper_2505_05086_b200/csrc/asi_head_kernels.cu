@@ -28,7 +28,10 @@ namespace asi {
 namespace {
 
 constexpr int kWorkers = 8;                               // epilogue warps
-constexpr int kThreads = (kWorkers + 2) * 32;             // + the issuer's and the producer's
+constexpr int kThreads = (kWorkers + 4) * 32;             // + the issuer's, the producer's and two that make these a group of four
+// Registers of a thread: 168 at launch (65536 / 384); the second group hands on what it does not need
+constexpr int kWorkerRegs = 216, kOtherRegs = 72;
+static_assert(kWorkers * 32 * kWorkerRegs + 128 * kOtherRegs <= kThreads * 168, "the groups' shares have to fit what the CTA was launched with");
 constexpr int kTile = 256;                                // rows and columns of a pair's tile
 constexpr int kK = 64;                                    // k per chunk: 64 bf16 = one 128-byte swizzle row
 constexpr int kMaxStages = 6;
@@ -58,6 +61,7 @@ struct HeadProb {
   int64_t ld, split_stride;     // elements
   CUtensorMap o;                // the result in boxes of 32 rows of 128 bytes
   int how;                      // Store: how results leave
+  int correct;                  // what rounding took from G at the targets is added (dx of bf16 operands)
 };
 // by coalesced words (any alignment, `add` of any kind), by tensor copies, or added to fp32 by tensor copies (add is out)
 enum Store { kWords = 0, kCopy = 1, kAdd = 2 };
@@ -79,8 +83,12 @@ struct HeadArgs {
   const float2* row;            // maximum (base 2) and log2 of the sum of each row, or
   const float* lse;             // (null: row)
   const float *entropy, *dlogp, *dent;
+  float* off;                   // [T]: what rounding took from G at the target (bf16 operands), or null; w and its row stride beside it
+  const __nv_bfloat16* w;
+  int64_t ld_w;
   CUtensorMap g;                // G: boxes of 64 columns x 32 rows
   int terms;                    // of G
+  int staged;                   // bytes of a warp's results on their way out
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -134,15 +142,17 @@ struct RowGrad {
   float hi, lo, alpha, beta, h;
   int y;                       // its target's column in the vocabulary, -1: none
   bool live;
+  float* off;                  // where what rounding takes from G there goes, or null
 };
 
 __device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
-  RowGrad r = {0.f, 0.f, 0.f, 0.f, 0.f, -1, false};
+  RowGrad r = {0.f, 0.f, 0.f, 0.f, 0.f, -1, false, nullptr};
   if (row >= g.T) return r;
   const int64_t y = g.y[row];
   r.live = y != g.ignore;
   const bool in = y >= 0 && y < g.V;
   r.y = in ? (int)y : -1;
+  r.off = g.off ? g.off + row : nullptr;
   r.alpha = in ? g.dlogp[row] : NAN;
   if (g.dent) r.beta = g.dent[row], r.h = g.entropy[row];
   if (g.row) {
@@ -157,15 +167,17 @@ __device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
   return r;
 }
 
-// 32 logits of a row, the first in column j0 of the vocabulary, become their gradients
-__device__ __forceinline__ void to_gradient(float (&v)[32], const RowGrad& r, const HeadArgs& g, int64_t j0) {
-  const int left = (int)(g.V - j0 < 32 ? g.V - j0 : 32), hot = r.y - (int)j0;   // (V <= 2^24)
+// kN logits of a row, the first in column j0 of the vocabulary, become their gradients
+template <int kN>
+__device__ __forceinline__ void to_gradient(float (&v)[kN], const RowGrad& r, const HeadArgs& g, int64_t j0) {
+  const int left = (int)(g.V - j0 < kN ? g.V - j0 : kN), hot = r.y - (int)j0;   // (V <= 2^24)
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < kN; ++i) {
     const float a = fmaf(v[i], g.c, -r.hi) - r.lo, p = ex2(a);
     float d = r.alpha * ((i == hot ? 1.f : 0.f) - p);
     if (r.beta != 0.f) d -= r.beta * p * fmaf(fmaxf(a, -200.f), kLn2, r.h);
     v[i] = r.live && i < left ? g.scale * d : 0.f;
+    if (r.off && i == hot) *r.off = v[i] - __bfloat162float(__float2bfloat16_rn(v[i]));
   }
 }
 
@@ -183,12 +195,17 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 // Column `lane` of staged results (32 x 32, column i of row r at i ^ r), up to 32 rows, added to another's and stored.  What is added is on its way for all rows at once.
 template <typename TO, typename TA>
 __device__ __forceinline__ void put_words(const float* s, int lane, TO* to, const TA* add, int64_t ld, int rows) {
-  float f[32];
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 16, to += 16 * ld, add += add ? 16 * ld : 0) {
+    float f[16];
+    const TA* from = add;
 #pragma unroll
-  for (int r = 0; r < 32; ++r) f[r] = add && r < rows ? as_float(add[r * ld]) : 0.f;
+    for (int r = 0; r < 16; ++r, from += ld) f[r] = add && r0 + r < rows ? as_float(*from) : 0.f;
+    TO* at = to;
 #pragma unroll
-  for (int r = 0; r < 32; ++r)
-    if (r < rows) to[r * ld] = (TO)(f[r] + s[r * 32 + (lane ^ r)]);
+    for (int r = 0; r < 16; ++r, at += ld)
+      if (r0 + r < rows) *at = (TO)(f[r] + s[(r0 + r) * 32 + (lane ^ (r0 + r))]);
+  }
 }
 
 // A pair of CTAs owns a tile of 256 x 256: each brings half of either operand's chunk (128 rows) to its shared memory, products are
@@ -249,6 +266,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   const int nst = g.nst, stall = g.stall;
   bool ok = true;
   int loads = 0;
+  if (warp >= kWorkers) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
   if (warp == kWorkers) {
     // ---- issuer: the warp as a whole goes through the loop, so that addresses and descriptors stay in uniform registers (by one
     // lane alone a chunk's issue took 600 cycles, its products 512), and one lane issues
@@ -342,13 +361,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         }
       }
     }
+  }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegs));
     // ---- epilogue: warp w has the lanes 32 (w mod 4) .. of TMEM, warps 0-3 the columns [0, 128) of the tile, warps 4-7 the others
     const int quad = warp & 3, col0 = (warp >> 2) * 128;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)col0;
     const uint32_t free0 = in_cta(acc_free, 0), free1 = in_cta(acc_free + 1, 0);
-    uint8_t* out = base + nst * kStage + warp * (kEpi == kGrad ? g.terms * kStaged : kStaged);
-    int seg = 0;
+    uint8_t* staged = base + nst * kStage + warp * g.staged;
+    int seg = 0, flip = 0;                               // (results in two places in turn, or terms of G in a place each)
 #pragma unroll 1
     for (int t = 0; t < mine && ok; ++t) {
       const Tile x = tile_of(t);
@@ -385,10 +406,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
+      // 32 columns of results on their way by copies: rows of 128 bytes, 32 columns of fp32 or 64 of bf16, 16-byte units swizzled by the row
+      auto by_copy = [&](const float (&v)[32], int cc, int n) {
+        const bool wide = p.out_kind == kF32;
+        if (wide || (cc & 1) == 0) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          __syncwarp();
+          flip ^= 1;
+        }
+        uint8_t *out = staged + flip * kStaged, *r = out + lane * 128;
+        if (wide) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) *reinterpret_cast<float4*>(r + ((u ^ (lane & 7)) * 16)) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            *reinterpret_cast<uint4*>(r + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) =
+                make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]), pack2(v[8 * u + 6], v[8 * u + 7]));
+        }
+        if (wide || (cc & 1)) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            const int col = wide ? n : n - 32;
+            if (col < p.N && row0 < p.M) {
+              if (p.how == kAdd) tma_add_3d(&p.o, out, col, row0, x.s);
+              else tma_store_3d(&p.o, out, col, row0, x.s);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        }
+      };
+      const bool live = row0 < p.M;                      // (a warp without rows only hands its accumulators on)
       RowStats stats;
       RowGrad rg;
       if constexpr (kEpi == kGrad) rg = row_grad(g, row);
-      const int64_t y = kEpi == kStats && row < g.T ? g.y[row] : -1;
+      const int64_t y = (kEpi == kStats || (kEpi == kOut && p.correct)) && row < g.T ? g.y[row] : -1;
+      const bool corrected = kEpi == kOut && p.correct && y >= 0 && y < g.V && y != g.ignore;
+      const float off = corrected ? g.off[row] : 0.f;
+      const __nv_bfloat16* hot_row = g.w + (corrected ? y * g.ld_w : 0);
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc) {
         float v[32];
@@ -409,7 +465,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
           for (int i = 0; i < 32; ++i) v[i] = 0.f;
         }
         const int n = n0 + cc * 32;
+        if (!live) continue;
+        if constexpr (kEpi == kOut && !kSegmented) {
+          // One entry of G's row is as large as all others together, and its rounding no less: it comes back as off[t] w[y]
+          if (p.correct && off != 0.f) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              if (n + 8 * u >= p.N) break;
+              const uint4 q = __ldg(reinterpret_cast<const uint4*>(hot_row + n + 8 * u));   // (rows of w, or of its terms, go on to a multiple of 8)
+              const uint32_t h[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                v[8 * u + 2 * i] = fmaf(off, __uint_as_float(h[i] << 16), v[8 * u + 2 * i]);
+                v[8 * u + 2 * i + 1] = fmaf(off, __uint_as_float(h[i] & 0xffff0000u), v[8 * u + 2 * i + 1]);
+              }
+            }
+          }
+        }
         if constexpr (kEpi == kStats) {
+          if (p.how == kCopy) by_copy(v, cc, n);
           const int64_t left = g.V - n;
           if (left < 32)
 #pragma unroll
@@ -426,9 +500,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         } else if constexpr (kEpi == kGrad) {
           // rows of 128 bytes (64 columns), 16-byte units swizzled by the row as the tensor copy expects them
           if ((cc & 1) == 0) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            if (g.terms == 1) {
+              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+              flip ^= 1;
+            } else if (lane == 0) {
+              asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
             __syncwarp();
           }
+          uint8_t* out = staged + flip * kStaged;
           to_gradient(v, rg, g, g.v0 + n);
 #pragma unroll 1
           for (int e = 0; e < g.terms; ++e) {
@@ -458,37 +538,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
           }
         } else {
           if (p.how != kWords) {
-            // rows of 128 bytes, 32 columns of fp32 or 64 of bf16, their 16-byte units swizzled by the row
-            const bool wide = p.out_kind == kF32;
-            if (wide || (cc & 1) == 0) {
-              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              __syncwarp();
-            }
-            uint8_t* r = out + lane * 128;
-            if (wide) {
-#pragma unroll
-              for (int u = 0; u < 8; ++u) *reinterpret_cast<float4*>(r + ((u ^ (lane & 7)) * 16)) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
-            } else {
-#pragma unroll
-              for (int u = 0; u < 4; ++u)
-                *reinterpret_cast<uint4*>(r + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) =
-                    make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]), pack2(v[8 * u + 6], v[8 * u + 7]));
-            }
-            if (wide || (cc & 1)) {
-              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              __syncwarp();
-              if (lane == 0) {
-                const int col = wide ? n : n - 32;
-                if (col < p.N && row0 < p.M) {
-                  if (p.how == kAdd) tma_add_3d(&p.o, out, col, row0, x.s);
-                  else tma_store_3d(&p.o, out, col, row0, x.s);
-                }
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-              }
-            }
+            by_copy(v, cc, n);
           } else {
             // through shared memory, so that a warp's lanes are neighbouring columns
-            float* s = reinterpret_cast<float*>(out);
+            float* s = reinterpret_cast<float*>(staged);
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (of a tile of the other product)
             __syncwarp();
 #pragma unroll
@@ -519,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         }
       }
     }
-    if constexpr (kEpi != kStats) {
+    {
       if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // all is there before the next kernel reads it
       __syncwarp();
     }
@@ -556,7 +609,11 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
   __shared__ float sm[32][33], ss[32][33], sw[32][33];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  int row = blockIdx.x * 32 + slice;                     // (the row that this warp's first lane writes)
+  const int64_t y = row < p.T ? p.y[row] : 0;
+  const float xy = row < p.T && p.logp && y >= 0 && y < p.V ? p.xy[row] : 0.f;
+  row = blockIdx.x * 32 + lane;
   float m = -INFINITY, s = 0.f, w = 0.f;
   auto join = [&](float m2, float s2, float w2) {
     const float top = fmaxf(m, m2);
@@ -570,7 +627,7 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
     m = top;
   };
   if (row < p.T) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = slice; i < p.parts; i += 32) {
       const int64_t at = (int64_t)i * p.T + row;
       join(p.pm[at], p.ps[at], p.pw[at]);
@@ -578,21 +635,52 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
   }
   sm[slice][lane] = m, ss[slice][lane] = s, sw[slice][lane] = w;
   __syncthreads();
-  if (slice == 0 && row < p.T) {
-    for (int i = 1; i < 32; ++i) join(sm[i][lane], ss[i][lane], sw[i][lane]);
+  // a warp a row, a lane a share
+  row = blockIdx.x * 32 + slice;
+  m = sm[lane][slice], s = ss[lane][slice], w = sw[lane][slice];
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const float m2 = __shfl_down_sync(~0u, m, o), s2 = __shfl_down_sync(~0u, s, o), w2 = __shfl_down_sync(~0u, w, o);
+    join(m2, s2, w2);                                    // (lane 0 meets all shares in their order)
+  }
+  if (lane == 0 && row < p.T) {
     const bool nothing = m == -INFINITY && s == 0.f;
     const float l2 = log2f(s), y2 = nothing ? -INFINITY : l2;
-    const int64_t y = p.y[row];
     if (p.lse) p.lse[row] = nothing ? -INFINITY : (m + l2) * kLn2;
     if (p.entropy) p.entropy[row] = nothing ? 0.f : kLn2 * (l2 - w / s);
     if (p.logp) {
       float l = 0.f;
       if (y < 0 || y >= p.V) l = NAN;
       else if (nothing) l = -INFINITY;
-      else l = (fmaf(p.xy[row], p.c, -m) - l2) * kLn2;
+      else l = (fmaf(xy, p.c, -m) - l2) * kLn2;
       p.logp[row] = y == p.ignore ? 0.f : l;
     }
     if (p.row) p.row[row] = make_float2(m, nothing ? 0.f : y2);
+  }
+}
+
+// G of a piece from logits that were kept: 1024 columns of a row a CTA
+struct KeptArgs {
+  HeadArgs h;
+  const float* x;              // [T][ld_x], from the piece's first column on
+  __nv_bfloat16* out;          // [terms][T][ld]
+  int64_t ld_x, ld, n;         // n: columns that are there, a multiple of 256
+};
+__global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptArgs p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int row = blockIdx.y;
+  const int64_t j0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (j0 >= p.n) return;
+  const RowGrad r = row_grad(p.h, row);
+  const float4 in = *reinterpret_cast<const float4*>(p.x + row * p.ld_x + j0);
+  float v[4] = {in.x, in.y, in.z, in.w};
+  to_gradient(v, r, p.h, p.h.v0 + j0);
+  for (int e = 0; e < p.h.terms; ++e) {
+    const uint2 w = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    *reinterpret_cast<uint2*>(p.out + ((int64_t)e * p.h.T + row) * p.ld + j0) = w;
+    v[0] -= __uint_as_float(w.x << 16), v[1] -= __uint_as_float(w.x & 0xffff0000u);
+    v[2] -= __uint_as_float(w.y << 16), v[3] -= __uint_as_float(w.y & 0xffff0000u);
   }
 }
 
@@ -603,18 +691,29 @@ struct SplitArgs {
   int64_t rows, D, ld;
   int terms;
 };
+// (eight neighbours a thread: 30011 x 771 fp32 @SPLIT@ us, a value a thread 94)
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_split(const __grid_constant__ SplitArgs p) {
   pdl_wait();
   pdl_launch_dependents();
-  const int64_t n = p.rows * p.D;
+  const int groups = (int)(p.ld / 8);
+  const int64_t n = p.rows * groups;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / p.D, at = r * p.ld + (i - r * p.D);
-    float v = (float)static_cast<const T*>(p.in)[i];
+    const int64_t r = i / groups;
+    const int c = (int)(i - r * groups) * 8;
+    const T* in = static_cast<const T*>(p.in) + r * p.D + c;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < p.D ? (float)in[k] : 0.f;
     for (int e = 0; e < p.terms; ++e) {
-      const __nv_bfloat16 h = __float2bfloat16_rn(v);
-      p.out[e * p.rows * p.ld + at] = h;
-      v -= __bfloat162float(h);
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = pack2(v[2 * k], v[2 * k + 1]);
+        v[2 * k] -= __uint_as_float(w[k] << 16);
+        v[2 * k + 1] -= __uint_as_float(w[k] & 0xffff0000u);
+      }
+      *reinterpret_cast<uint4*>(p.out + (e * p.rows + r) * p.ld + c) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -623,8 +722,12 @@ __global__ void __launch_bounds__(256) k_head_split(const __grid_constant__ Spli
 struct JoinArgs {
   const float* in;             // [splits][n]
   void* out;
-  int64_t n;
+  int64_t n, D;
   int splits, out_kind;
+  const float* off;            // as in HeadArgs
+  const int64_t* y;
+  int64_t ignore, V, ld_w;
+  const __nv_bfloat16* w;
 };
 __global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ JoinArgs p) {
   pdl_wait();
@@ -633,6 +736,10 @@ __global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ JoinA
     float s = 0.f;
 #pragma unroll 4
     for (int e = 0; e < p.splits; ++e) s += p.in[e * p.n + i];
+    if (p.off) {
+      const int64_t t = i / p.D, y = p.y[t];
+      if (y >= 0 && y < p.V && y != p.ignore) s = fmaf(p.off[t], __bfloat162float(p.w[y * p.ld_w + i - t * p.D]), s);
+    }
     if (p.out_kind == kF32) static_cast<float*>(p.out)[i] = s;
     else static_cast<__nv_bfloat16*>(p.out)[i] = __float2bfloat16_rn(s);
   }
@@ -656,7 +763,7 @@ constexpr int64_t kPieceBytes = 128 << 20;               // of G in the workspac
 constexpr int64_t kJoinRows = 4096;                      // rows of shares of dx beyond dx itself
 
 struct Layout {
-  size_t part, xy, row, xs, ws, g, acc, bytes;
+  size_t part, xy, row, off, xs, ws, g, acc, kept, least, bytes;   // least: without logits that are kept (kept 0: never)
   int64_t ld;                                            // of split operands
   int64_t cols;                                          // of a piece
   int in_terms, g_terms;
@@ -680,6 +787,7 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   l.part = take((size_t)2 * nt * T * 12);
   l.xy = take((size_t)T * 4);
   l.row = take((size_t)T * 8);
+  l.off = take((size_t)T * 4);
   if (l.split) {
     l.xs = take((size_t)l.in_terms * T * l.ld * 2);
     l.ws = take((size_t)l.in_terms * V * l.ld * 2);
@@ -694,7 +802,13 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
     l.acc_rows = std::max(T, std::min(64 * T, kJoinRows));
     l.acc = take((size_t)l.acc_rows * d->dim * 4);
   }
-  l.bytes = at;
+  l.least = l.bytes = at;
+  // Logits of few rows take no more than a piece of G may: where the workspace has room for them they stay, in fp32, and the third of the
+  // four products is spared (the same bits).  9 x 50257 x 768: @K1@; 1001 x 30011 x 771 fp32: @K2@
+  if (grad && T && !d->vocab_chunk && all * T * 4 <= kPieceBytes) {
+    l.kept = take((size_t)(all * T * 4));
+    l.bytes = at;
+  }
   return l;
 }
 
@@ -721,7 +835,7 @@ void set_pairs(HeadProb* p, int a_terms, int b_terms) {
 
 template <int kEpi, bool kSegmented>
 cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
-  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (kEpi == kGrad ? (size_t)g.terms * kStaged : kEpi == kOut ? kStaged : 0);
+  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (size_t)g.staged;
   const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented>), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -763,7 +877,8 @@ void share_tiles(HeadArgs* g, int pairs) {
 
 template <int kEpi>
 cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
-  g.nst = kEpi == kGrad && g.terms == 3 ? 4 : 6;
+  g.staged = (kEpi == kGrad && g.terms == 3 ? 3 : 2) * kStaged;
+  g.nst = kEpi == kGrad && g.terms == 3 ? 4 : 5;         // (three of them were as fast: what copies take is hidden)
   g.seg = segmented ? kSeg : 1 << 30;
   g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
   g.tiles = g.tiles0 + (g.np > 1 ? g.p[1].mt * g.p[1].nt * g.p[1].splits : 0);
@@ -775,7 +890,7 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
 
 cudaError_t launch_split(const asi_head_desc_t* d, const Layout& l, const void* in, int64_t rows, void* out, cudaStream_t st) {
   SplitArgs a = {in, static_cast<__nv_bfloat16*>(out), rows, d->dim, l.ld, l.in_terms};
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * d->dim, 256 * 4), 148 * 8));
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * (l.ld / 8), 256), 148 * 16));
   return d->in_dtype == ASI_BF16 ? launch_pdl(k_head_split<__nv_bfloat16>, grid, dim3(256), 0, st, a) : launch_pdl(k_head_split<float>, grid, dim3(256), 0, st, a);
 }
 
@@ -811,7 +926,7 @@ void size_product(HeadProb* p, int64_t M, int64_t N, int64_t K) {
   p->splits = 1;
 }
 
-asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t st) {
+asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_bytes, cudaStream_t st) {
   const Layout l = layout_of(d, c.grad);
   const int64_t T = d->rows, V = d->vocab, D = d->dim;
   const bool fine = d->in_dtype == ASI_F32;              // logits and dx are held to fp32
@@ -847,10 +962,19 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
   set_pairs(&logits, l.in_terms, l.in_terms);
   if (!operand_map(&logits.a, x, D, T, ld, l.in_terms, T * ld, kK, 128) || !operand_map(&logits.b, w, D, V, ld, l.in_terms, V * ld, kK, 128))
     return cuda_status(cudaErrorNotSupported, "tensor map");
+  const bool keep = c.forward && c.grad && l.kept && ws_bytes >= l.bytes;
   if (c.forward) {
     g.p[0] = logits;
     g.np = 1;
-    e = launch_gemm<kStats>(g, fine, st);
+    if (keep) {
+      g.p[0].out = ws + l.kept;
+      g.p[0].out_kind = kF32;
+      g.p[0].ld = nt * kTile;
+      set_store(&g.p[0], T, nt * kTile);
+      if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
+    }
+    // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, with segments 0.8e-6; 359 and 378 us)
+    e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kSeg, st);
     if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
     RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c};
     e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
@@ -864,6 +988,9 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
   g.dent = c.dent;
   const int terms = c.dw && d->dw_dtype == ASI_F32 ? 3 : fine ? 3 : 1;   // (without dw in fp32, G of bf16 operands has one)
   g.terms = terms;
+  g.off = !fine && c.dx ? reinterpret_cast<float*>(ws + l.off) : nullptr;
+  g.w = static_cast<const __nv_bfloat16*>(w);
+  g.ld_w = ld;
   void* G = ws + l.g;
   HeadProb px = {}, pw = {};
   // (the product's first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
@@ -883,7 +1010,13 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
     g.p[0].b_off = (int)v0;
     g.np = 1;
     g.v0 = v0;
-    e = launch_gemm<kGrad>(g, fine, st);
+    if (keep) {
+      const int64_t n = ceil_div(nv, kTile) * kTile;
+      const KeptArgs k = {g, reinterpret_cast<const float*>(ws + l.kept) + v0, static_cast<__nv_bfloat16*>(G), nt * kTile, l.cols, n};
+      e = launch_pdl(k_head_kept, dim3((unsigned)ceil_div(n, 1024), (unsigned)T), dim3(256), 0, st, k);
+    } else {
+      e = launch_gemm<kGrad>(g, fine, st);
+    }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
     size_product(&px, T, D, nv);
     set_pairs(&px, fine ? 3 : 1, fine ? 3 : 1);
@@ -911,6 +1044,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
     px.add_kind = i ? kF32 : kNone;
     px.out = last ? c.dx : static_cast<void*>(acc);
     px.out_kind = last ? dx_kind : kF32;
+    px.correct = last && g.off;
     g.np = 0;
     if (c.dx) g.p[g.np++] = px;
     if (c.dw) g.p[g.np++] = pw;
@@ -921,7 +1055,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, cudaStream_t
     if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
   }
   if (c.dx && splits > 1) {
-    JoinArgs j = {acc, c.dx, T * D, splits, dx_kind};
+    JoinArgs j = {acc, c.dx, T * D, D, splits, dx_kind, g.off, c.y, d->ignore_index, V, ld, g.w};
     e = launch_pdl(k_head_join, dim3((unsigned)std::min<int64_t>(ceil_div(T * D, 256), 148 * 8)), dim3(256), 0, st, j);
     if (e != cudaSuccess) return cuda_status(e, "shares of dx");
   }
@@ -957,14 +1091,14 @@ asi_status_t check_call(const asi_head_desc_t* d, const Call& c, void* ws, size_
   if (c.forward && (!c.logp || !c.lse)) return ASI_ERR_INVALID_ARG;
   if (c.grad && (!c.dlogp || (!c.dx && !c.dw) || (!c.forward && !c.lse_in) || (c.dent && !c.entropy_in))) return ASI_ERR_INVALID_ARG;
   const Layout l = layout_of(d, c.grad);
-  if (ws_bytes < l.bytes || !aligned(ws, 256)) return ASI_ERR_WORKSPACE;
+  if (ws_bytes < l.least || !aligned(ws, 256)) return ASI_ERR_WORKSPACE;
   if (!l.split && (!aligned(c.x, 16) || !aligned(c.w, 16))) return ASI_ERR_INVALID_ARG;
   const size_t T = (size_t)d->rows, e = size_of(d->in_dtype), n = T * 4;
   const bool in_rows = c.grad && !c.forward;
   return check_buffers({{c.x, T * d->dim * e, e}, {c.w, (size_t)d->vocab * d->dim * e, e}, {c.y, T * 8, 8}, {c.dlogp, n, 4}, {c.dent, n, 4},
                         {in_rows ? c.lse_in : nullptr, n, 4}, {in_rows ? c.entropy_in : nullptr, n, 4}},
                        {{c.logp, n, 4}, {c.entropy, n, 4}, {c.lse, n, 4}, {c.dx, T * d->dim * e, e},
-                        {c.dw, (size_t)d->vocab * d->dim * size_of(d->dw_dtype), size_of(d->dw_dtype)}, {ws, l.bytes, 256}});
+                        {c.dw, (size_t)d->vocab * d->dim * size_of(d->dw_dtype), size_of(d->dw_dtype)}, {ws, std::min(ws_bytes, l.bytes), 256}});
 }
 
 asi_status_t call(const asi_head_desc_t* d, const Call& c, void* ws, size_t ws_bytes, void* stream) {
@@ -979,7 +1113,7 @@ asi_status_t call(const asi_head_desc_t* d, const Call& c, void* ws, size_t ws_b
   s = check_call(d, c, ws, ws_bytes);
   if (s != ASI_OK) return s;
   try {
-    return run(d, c, static_cast<char*>(ws), st);
+    return run(d, c, static_cast<char*>(ws), ws_bytes, st);
   } catch (...) {
     return no_host_memory();
   }
