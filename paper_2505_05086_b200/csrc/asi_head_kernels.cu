@@ -33,12 +33,11 @@ constexpr int kThreads = (kWorkers + 4) * 32;             // + the issuer's, the
 constexpr int kWorkerRegs = 216, kOtherRegs = 72;
 static_assert(kWorkers * 32 * kWorkerRegs + 128 * kOtherRegs <= kThreads * 168, "the groups' shares have to fit what the CTA was launched with");
 constexpr int kTile = 256;                                // rows and columns of a pair's tile
-constexpr int kK = 64;                                    // k per chunk: 64 bf16 = one 128-byte swizzle row
-constexpr int kMaxStages = 6;
-constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's chunk
-constexpr uint32_t kStage = 2 * kHalf;
+constexpr int kK = 64;                                    // k of a box: 64 bf16 = one 128-byte swizzle row
+constexpr int kMaxStages = 3;
+constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's box
 constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
-constexpr int kSeg = 16;                                  // chunks that add up in TMEM where results are held to fp32
+constexpr int kSeg = 16;                                  // pairs of boxes that add up in TMEM where results are held to fp32
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -52,8 +51,11 @@ struct HeadProb {
   int a_off, a_k, b_off, b_k;   // where the product's first row and first k lie in the operand
   int M, N, mt, nt, splits;     // tiles; `splits` shares of k one after another
   int kc, per;                  // chunks of k, and of a share
-  int pairs;                    // pairs of terms
-  uint32_t a_term, b_term;      // two bits a pair
+  // A chunk of `sub` times 64 k shares a stage: `sub` boxes of each of A's terms, then B's
+  int sub, a_boxes, b_boxes;
+  int pairs;                    // pairs of boxes that are multiplied
+  uint32_t a_box, b_box;        // of each pair, two bits
+  int seg;                      // chunks that add up in TMEM (kSegmented), or all
   int n_first;                  // tiles of a row follow one another (else tiles of a column)
   const void* add;              // added to the result, laid out like it; null: nothing
   void* out;
@@ -69,8 +71,8 @@ struct HeadArgs {
   HeadProb p[2];
   int np, tiles0, tiles;        // tiles of the first product, of all
   int few, each_few, more_few, each_rest, more_rest;   // of the second product: how many a pair takes (see Mine)
-  int nst;                      // stages
-  int seg;                      // chunks that add up in TMEM (kSegmented), or all
+  int nst, stage;               // stages, and bytes of one
+  int place;
   int* status;
   int stall;                    // test hook: no copies, short waits
   // kStats, kGrad:
@@ -86,9 +88,8 @@ struct HeadArgs {
   float* off;                   // [T]: what rounding took from G at the target (bf16 operands), or null; w and its row stride beside it
   const __nv_bfloat16* w;
   int64_t ld_w;
-  CUtensorMap g;                // G: boxes of 64 columns x 32 rows
+  CUtensorMap g;                // G: boxes of 32 rows of 64 columns (one term) or 32
   int terms;                    // of G
-  int staged;                   // bytes of a warp's results on their way out
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -167,26 +168,51 @@ __device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
   return r;
 }
 
-// kN logits of a row, the first in column j0 of the vocabulary, become their gradients
-template <int kN>
+// kN logits of a row, the first in column j0 of the vocabulary, become their gradients (by a whole warp; kFine: G is stored in terms)
+template <int kN, bool kFine>
 __device__ __forceinline__ void to_gradient(float (&v)[kN], const RowGrad& r, const HeadArgs& g, int64_t j0) {
-  const int left = (int)(g.V - j0 < kN ? g.V - j0 : kN), hot = r.y - (int)j0;   // (V <= 2^24)
+  const float a = -g.scale * r.alpha;
+  if (__any_sync(~0u, r.beta != 0.f)) {
+    const float b = g.scale * r.beta;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    const float a = fmaf(v[i], g.c, -r.hi) - r.lo, p = ex2(a);
-    float d = r.alpha * ((i == hot ? 1.f : 0.f) - p);
-    if (r.beta != 0.f) d -= r.beta * p * fmaf(fmaxf(a, -200.f), kLn2, r.h);
-    v[i] = r.live && i < left ? g.scale * d : 0.f;
-    if (r.off && i == hot) *r.off = v[i] - __bfloat162float(__float2bfloat16_rn(v[i]));
+    for (int i = 0; i < kN; ++i) {
+      const float x = fmaf(v[i], g.c, -r.hi) - r.lo, p = ex2(x);
+      v[i] = p * fmaf(-b, fmaf(fmaxf(x, -200.f), kLn2, r.h), a);
+    }
+  } else if (kFine) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = ex2(fmaf(v[i], g.c, -r.hi) - r.lo) * a;
+  } else {
+    const float z = -(r.hi + r.lo);                        // (off by 2^-24 of it: less than bf16 shows)
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = ex2(fmaf(v[i], g.c, z)) * a;
+  }
+  const int hot = r.y - (int)j0;                           // (V <= 2^24)
+  if (hot >= 0 && hot < kN) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (i == hot) {
+        v[i] -= a;
+        if (r.off) *r.off = v[i] - __bfloat162float(__float2bfloat16_rn(v[i]));
+      }
+  }
+  if (!r.live) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = 0.f;
+  }
+  if (g.V - j0 < kN) {
+    const int left = (int)(g.V - j0);
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (i >= left) v[i] = 0.f;
   }
 }
 
 // Waits of a whole warp that end (mbar_wait's limit); one answer for all lanes, so that what follows stays in uniform registers
-__device__ __noinline__ bool warp_wait_on(uint64_t* bar, uint32_t parity, int stall) {
-  return __all_sync(~0u, mbar_wait(bar, parity, stall));
-}
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int stall) {
-  return __all_sync(~0u, mbar_try_wait(bar, parity)) || warp_wait_on(bar, parity, stall);
+  bool ok = __all_sync(~0u, mbar_try_wait(bar, parity));
+  if (!ok) ok = __all_sync(~0u, mbar_wait(bar, parity, stall));
+  return ok;
 }
 
 __device__ __forceinline__ float as_float(float x) { return x; }
@@ -259,11 +285,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
     x.m = p.n_first ? t / p.nt : t % p.mt;
     x.n = p.n_first ? t % p.nt : t / p.mt;
     x.k0 = x.s * p.per;
-    x.chunks = (p.kc - x.k0 < p.per ? p.kc - x.k0 : p.per) * p.pairs;
+    x.chunks = p.kc - x.k0 < p.per ? p.kc - x.k0 : p.per;
     if (x.chunks < 0) x.chunks = 0;
     return x;
   };
-  const int nst = g.nst, stall = g.stall;
+  const int nst = g.nst, stall = g.stall, stage = g.stage;
   bool ok = true;
   int loads = 0;
   if (warp >= kWorkers) {
@@ -273,9 +299,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
     // lane alone a chunk's issue took 600 cycles, its products 512), and one lane issues
     if (rank == 0) {
       const uint32_t at = smem_u32(base);
-      const int per_seg = g.seg;
       int st = 0, seg = 0;
       uint32_t ph = 0;
+      bool ready = false;
+      const uint32_t empty0 = smem_u32(empty), done0 = smem_u32(done);
 #pragma unroll 1
       for (int t = 0; t < mine && ok; ++t) {
         const Tile x = tile_of(t);
@@ -283,33 +310,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const uint32_t idesc = instr_desc_bf16(kTile, kTile, p.a_mn != 0, p.b_mn != 0);
         // a k-step is 16 bf16: 32 bytes inside the swizzle row of a K-major tile, 16 rows (2048 bytes) of an MN-major one
         const uint64_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
-        const uint64_t da0 = smem_desc_sw128(at, p.a_mn ? kHalf / 2 : 16), db0 = smem_desc_sw128(at + kHalf, p.b_mn ? kHalf / 2 : 16);
+        const uint64_t da0 = smem_desc_sw128(at, p.a_mn ? kHalf / 2 : 16), db0 = smem_desc_sw128(at + p.a_boxes * kHalf, p.b_mn ? kHalf / 2 : 16);
+        const int per_seg = p.seg, box_pairs = p.pairs;
+        const uint32_t a_box = p.a_box, b_box = p.b_box;
 #pragma unroll 1
         for (int c0 = 0; c0 < x.chunks && ok; c0 += per_seg, ++seg) {
           const int buf = seg & 1, turn = seg >> 1;
           if (turn > 0) {
             ok = warp_wait(acc_free + buf, (uint32_t)(turn + 1) & 1u, stall);
             if (!ok) break;
-            asm volatile("fence.acq_rel.cluster;" ::: "memory");   // arrivals of the other CTA too
+            // (TMEM is ordered by tcgen05's own fences; one of the cluster's memory took 2400 cycles here)
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           }
           const int c1 = x.chunks - c0 < per_seg ? x.chunks : c0 + per_seg;
           const uint32_t acc = tmem + (uint32_t)(buf * kTile);
 #pragma unroll 1
           for (int c = c0; c < c1; ++c) {
-            ok = warp_wait(full + st, ph, stall);
+            ok = __all_sync(~0u, ready);
+            if (!ok) ok = warp_wait(full + st, ph, stall);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint64_t da = da0 + (uint64_t)(st * (kStage >> 4)), db = db0 + (uint64_t)(st * (kStage >> 4));
-            if (elect_one()) {
+            const uint64_t da1 = da0 + (uint64_t)(st * (stage >> 4)), db1 = db0 + (uint64_t)(st * (stage >> 4));
+            const uint32_t used = empty0 + st * 8;
+            if (++st == nst) st = 0, ph ^= 1u;
+            ready = mbar_test(full + st, ph);              // (the answer comes while products are issued)
+#pragma unroll 1
+            for (int e = 0; e < box_pairs; ++e) {
+              const uint64_t da = da1 + ((a_box >> (2 * e)) & 3) * (kHalf >> 4), db = db1 + ((b_box >> (2 * e)) & 3) * (kHalf >> 4);
 #pragma unroll
               for (int ks = 0; ks < kK / 16; ++ks)
-                umma_pair_bf16(acc, da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | ks) ? 1u : 0u);
-              umma_pair_commit(empty + st);
-              if (c + 1 == c1) umma_pair_commit(done + buf);
+                umma_pair_bf16_one(acc, da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | e | ks) ? 1u : 0u);
             }
-            __syncwarp();
-            if (++st == nst) st = 0, ph ^= 1u;
+            umma_pair_commit_one(used);
+            if (c + 1 == c1) umma_pair_commit_one(done0 + buf * 8);
           }
         }
       }
@@ -327,36 +360,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const int am = p.a_off + x.m * kTile + rank * 128, bn = p.b_off + x.n * kTile + rank * 128;
         const CUtensorMap *ma = &p.a, *mb = &p.b;
         const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
-        const uint32_t a_term = p.a_term, b_term = p.b_term;
-        const int pairs_of = p.pairs;
-        int ka = p.a_k + x.k0 * kK, kb = p.b_k + x.k0 * kK, e = 0;
+        const int a_boxes = p.a_boxes, b_boxes = p.b_boxes, sub = p.sub;
+        int ka = p.a_k + x.k0 * sub * kK, kb = p.b_k + x.k0 * sub * kK;
 #pragma unroll 1
         for (int c = 0; c < x.chunks; ++c, ++loads) {
           if (loads >= nst) {
             ok = warp_wait(empty + st, ph, stall);
             if (!ok) break;
           }
-          const bool one = elect_one();
-          if (rank == 0 && one) mbar_expect_tx(full + st, 2 * kStage);
-          if (!stall && one) {
-            uint8_t* A = base + st * kStage;
+          if (rank == 0) mbar_expect_tx_one(smem_u32(full) + st * 8, 2 * (a_boxes + b_boxes) * kHalf);
+          if (!stall) {
+            uint32_t to = smem_u32(base) + st * stage;
             const uint32_t bar = full0 + st * 8;
-            const int at = (int)(a_term >> (2 * e)) & 3, bt = (int)(b_term >> (2 * e)) & 3;
-            if (a_mn) {
-              tma_pair_load_3d(A, ma, am, ka, at, bar);
-              tma_pair_load_3d(A + kHalf / 2, ma, am + 64, ka, at, bar);
-            } else {
-              tma_pair_load_3d(A, ma, ka, am, at, bar);
-            }
-            if (b_mn) {
-              tma_pair_load_3d(A + kHalf, mb, bn, kb, bt, bar);
-              tma_pair_load_3d(A + kHalf + kHalf / 2, mb, bn + 64, kb, bt, bar);
-            } else {
-              tma_pair_load_3d(A + kHalf, mb, kb, bn, bt, bar);
-            }
+            auto fetch = [&](const CUtensorMap* map, bool mn, int row, int k, int boxes) {
+              int term = 0, half = 0;
+#pragma unroll 1
+              for (int e = 0; e < boxes; ++e, to += kHalf) {
+                const int at = k + half * kK;
+                if (mn) {
+                  tma_pair_load_3d_one(to, map, row, at, term, bar);
+                  tma_pair_load_3d_one(to + kHalf / 2, map, row + 64, at, term, bar);
+                } else {
+                  tma_pair_load_3d_one(to, map, at, row, term, bar);
+                }
+                if (++half == sub) half = 0, ++term;
+              }
+            };
+            fetch(ma, a_mn, am, ka, a_boxes);
+            fetch(mb, b_mn, bn, kb, b_boxes);
           }
-          __syncwarp();
-          if (++e == pairs_of) e = 0, ka += kK, kb += kK;
+          ka += sub * kK, kb += sub * kK;
           if (++st == nst) st = 0, ph ^= 1u;
         }
       }
@@ -368,8 +401,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
     const int quad = warp & 3, col0 = (warp >> 2) * 128;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)col0;
     const uint32_t free0 = in_cta(acc_free, 0), free1 = in_cta(acc_free + 1, 0);
-    uint8_t* staged = base + nst * kStage + warp * g.staged;
-    int seg = 0, flip = 0;                               // (results in two places in turn, or terms of G in a place each)
+    const int place = g.place;                           // results on their way out have two places in turn, `place` bytes apart, or (0) one
+    uint8_t* staged = base + nst * stage + warp * (kStaged + (kEpi == kGrad && g.terms > 1 ? 0 : place));
+    int seg = 0, flip = 0;
+    auto next_place = [&]() {                            // its last contents have left
+      if (lane == 0) {
+        if (place) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      }
+      __syncwarp();
+      flip ^= 1;
+      return staged + flip * place;
+    };
+    uint8_t* out = staged;
 #pragma unroll 1
     for (int t = 0; t < mine && ok; ++t) {
       const Tile x = tile_of(t);
@@ -381,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
 #pragma unroll
         for (int i = 0; i < 128; ++i) acc[i] = 0.f;
 #pragma unroll 1
-        for (int c0 = 0; c0 < x.chunks; c0 += g.seg, ++seg) {
+        for (int c0 = 0; c0 < x.chunks; c0 += p.seg, ++seg) {
           const int buf = seg & 1;
           ok = mbar_wait(done + buf, (uint32_t)(seg >> 1) & 1u, stall);
           if (__any_sync(0xffffffffu, !ok)) ok = false;
@@ -409,12 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
       // 32 columns of results on their way by copies: rows of 128 bytes, 32 columns of fp32 or 64 of bf16, 16-byte units swizzled by the row
       auto by_copy = [&](const float (&v)[32], int cc, int n) {
         const bool wide = p.out_kind == kF32;
-        if (wide || (cc & 1) == 0) {
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          __syncwarp();
-          flip ^= 1;
-        }
-        uint8_t *out = staged + flip * kStaged, *r = out + lane * 128;
+        if (wide || (cc & 1) == 0) out = next_place();
+        uint8_t* r = out + lane * 128;
         if (wide) {
 #pragma unroll
           for (int u = 0; u < 8; ++u) *reinterpret_cast<float4*>(r + ((u ^ (lane & 7)) * 16)) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
@@ -498,42 +538,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             g.xy[row] = h;
           }
         } else if constexpr (kEpi == kGrad) {
-          // rows of 128 bytes (64 columns), 16-byte units swizzled by the row as the tensor copy expects them
-          if ((cc & 1) == 0) {
-            if (g.terms == 1) {
-              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-              flip ^= 1;
-            } else if (lane == 0) {
-              asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            }
-            __syncwarp();
-          }
-          uint8_t* out = staged + flip * kStaged;
-          to_gradient(v, rg, g, g.v0 + n);
-#pragma unroll 1
-          for (int e = 0; e < g.terms; ++e) {
+          if (g.terms == 1) {
+            // rows of 128 bytes (64 columns), 16-byte units swizzled by the row as the tensor copy expects them
+            if ((cc & 1) == 0) out = next_place();
+            to_gradient<32, false>(v, rg, g, g.v0 + n);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              uint4 w;
-              w.x = pack2(v[8 * u], v[8 * u + 1]), w.y = pack2(v[8 * u + 2], v[8 * u + 3]);
-              w.z = pack2(v[8 * u + 4], v[8 * u + 5]), w.w = pack2(v[8 * u + 6], v[8 * u + 7]);
-              *reinterpret_cast<uint4*>(out + e * kStaged + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) = w;
-              if (g.terms > 1) {
-                const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+            for (int u = 0; u < 4; ++u)
+              *reinterpret_cast<uint4*>(out + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) =
+                  make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]), pack2(v[8 * u + 6], v[8 * u + 7]));
+            if (cc & 1) {
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&g.g, out, n - 32, row0, 0);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
+            }
+          } else {
+            // a term after the other, rows of 64 bytes (32 columns)
+            to_gradient<32, true>(v, rg, g, g.v0 + n);
+#pragma unroll 1
+            for (int e = 0; e < 3; ++e) {
+              out = next_place();
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                uint32_t q[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                  q[i] = pack2(v[8 * u + 2 * i], v[8 * u + 2 * i + 1]);
                   v[8 * u + 2 * i] -= __uint_as_float(q[i] << 16);
                   v[8 * u + 2 * i + 1] -= __uint_as_float(q[i] & 0xffff0000u);
                 }
+                *reinterpret_cast<uint4*>(out + lane * 64 + ((u ^ ((lane >> 1) & 3)) * 16)) = make_uint4(q[0], q[1], q[2], q[3]);
               }
-            }
-          }
-          if (cc & 1) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-              for (int e = 0; e < g.terms; ++e) tma_store_3d(&g.g, out + e * kStaged, n - 32, row0, e);
-              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&g.g, out, n, row0, e);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
             }
           }
         } else {
@@ -580,8 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   const bool fail = __syncthreads_or(ok ? 0 : 1) != 0;
   if (fail) {                                           // what is in flight gets the limit once more
     if (tid == 0) atomicMax(g.status, (int)ASI_ERR_TIMEOUT);
-    if (warp == kWorkers && lane == 0 && rank == 0) {
-      umma_pair_commit(drained);
+    if (warp == kWorkers && rank == 0) {
+      umma_pair_commit_one(smem_u32(drained));
       mbar_wait(drained, 0, g.stall);
     } else if (warp == kWorkers + 1 && lane == 0 && rank == 0) {
       for (int i = 0; i < nst; ++i)
@@ -605,6 +648,7 @@ struct RowsArgs {
   int T, parts;
   float c;
 };
+constexpr int kAhead = 8;
 __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ RowsArgs p) {
   __shared__ float sm[32][33], ss[32][33], sw[32][33];
   pdl_wait();
@@ -627,10 +671,17 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
     m = top;
   };
   if (row < p.T) {
-#pragma unroll 8
-    for (int i = slice; i < p.parts; i += 32) {
-      const int64_t at = (int64_t)i * p.T + row;
-      join(p.pm[at], p.ps[at], p.pw[at]);
+    for (int i0 = slice; i0 < p.parts; i0 += 32 * kAhead) {
+      float m2[kAhead], s2[kAhead], w2[kAhead];            // (all on their way at once)
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const bool there = i0 + 32 * k < p.parts;
+        const int64_t at = (int64_t)(there ? i0 + 32 * k : i0) * p.T + row;
+        m2[k] = p.pm[at], s2[k] = p.ps[at], w2[k] = p.pw[at];
+        if (!there) m2[k] = -INFINITY, s2[k] = w2[k] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) join(m2[k], s2[k], w2[k]);
     }
   }
   sm[slice][lane] = m, ss[slice][lane] = s, sw[slice][lane] = w;
@@ -664,7 +715,7 @@ struct KeptArgs {
   HeadArgs h;
   const float* x;              // [T][ld_x], from the piece's first column on
   __nv_bfloat16* out;          // [terms][T][ld]
-  int64_t ld_x, ld, n;         // n: columns that are there, a multiple of 256
+  int64_t ld_x, ld, n;         // n: columns that are there, a multiple of 256 (whole warps)
 };
 __global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptArgs p) {
   pdl_wait();
@@ -675,7 +726,7 @@ __global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptA
   const RowGrad r = row_grad(p.h, row);
   const float4 in = *reinterpret_cast<const float4*>(p.x + row * p.ld_x + j0);
   float v[4] = {in.x, in.y, in.z, in.w};
-  to_gradient(v, r, p.h, p.h.v0 + j0);
+  to_gradient<4, true>(v, r, p.h, p.h.v0 + j0);
   for (int e = 0; e < p.h.terms; ++e) {
     const uint2 w = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
     *reinterpret_cast<uint2*>(p.out + ((int64_t)e * p.h.T + row) * p.ld + j0) = w;
@@ -777,7 +828,7 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   l.in_terms = d->in_dtype == ASI_F32 ? 3 : 1;
   l.g_terms = d->dw_dtype == ASI_F32 ? 3 : 1;            // (dx of fp32 operands comes with dw in fp32)
   l.split = d->in_dtype == ASI_F32 || d->dim % 8 != 0;
-  l.ld = (d->dim + 7) / 8 * 8;
+  l.ld = (d->dim + 63) / 64 * 64;                        // (rows on 128 bytes: on 16 alone a row of a copy meets two lines, and 771 fp32 columns took @LD@)
   size_t at = 256;                                       // status word
   auto take = [&](size_t bytes) {
     const size_t a = at;
@@ -812,30 +863,41 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   return l;
 }
 
-bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows, int64_t ld, int terms, int64_t term_stride, int box_inner, int box_rows) {
+bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows, int64_t ld, int terms, int64_t term_stride, int box_inner, int box_rows,
+                 CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)terms};
   const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)term_stride * 2};
   const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1};
-  return encode_bf16_map(map, base, 3, dims, strides, box);
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, 3, dims, strides, box, swizzle);
 }
 
-// the pairs of terms that matter, small ones first
-void set_pairs(HeadProb* p, int a_terms, int b_terms) {
+// The chunks of a product over K: of one term of either operand 128 k a stage (its two boxes, each with its like), of more 64 with the pairs of
+// terms that matter, small ones first
+void set_chunks(HeadProb* p, int64_t K, int a_terms, int b_terms) {
   p->pairs = 0;
-  p->a_term = p->b_term = 0;
-  for (int sum = 2; sum >= 0; --sum)
-    for (int a = 0; a < a_terms; ++a) {
-      const int b = sum - a;
-      if (b < 0 || b >= b_terms) continue;
-      p->a_term |= (uint32_t)a << (2 * p->pairs);
-      p->b_term |= (uint32_t)b << (2 * p->pairs);
-      ++p->pairs;
-    }
+  p->a_box = p->b_box = 0;
+  auto pair = [&](int a, int b) {
+    p->a_box |= (uint32_t)a << (2 * p->pairs);
+    p->b_box |= (uint32_t)b << (2 * p->pairs);
+    ++p->pairs;
+  };
+  p->sub = a_terms == 1 && b_terms == 1 ? 2 : 1;
+  p->a_boxes = a_terms * p->sub, p->b_boxes = b_terms * p->sub;
+  if (p->sub == 2) {
+    pair(0, 0), pair(1, 1);
+  } else {
+    for (int sum = 2; sum >= 0; --sum)
+      for (int a = 0; a < a_terms; ++a)
+        if (sum - a >= 0 && sum - a < b_terms) pair(a, sum - a);
+  }
+  p->kc = (int)ceil_div(K, kK * p->sub);
+  p->per = p->kc;
+  p->splits = 1;
 }
 
 template <int kEpi, bool kSegmented>
 cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
-  const size_t smem = 1024 + (size_t)g.nst * kStage + kWorkers * (size_t)g.staged;
+  const size_t smem = 1024 + (size_t)g.nst * g.stage + kWorkers * (kStaged + (kEpi == kGrad && g.terms > 1 ? 0 : g.place));
   const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented>), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -877,9 +939,18 @@ void share_tiles(HeadArgs* g, int pairs) {
 
 template <int kEpi>
 cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
-  g.staged = (kEpi == kGrad && g.terms == 3 ? 3 : 2) * kStaged;
-  g.nst = kEpi == kGrad && g.terms == 3 ? 4 : 5;         // (three of them were as fast: what copies take is hidden)
-  g.seg = segmented ? kSeg : 1 << 30;
+  // Stages of what the larger chunk takes (64 KB for one term of either operand, 96 for three), as many as 192 KB hold, beside a place for
+  // each warp's results on their way out.  What bounds the issuer is not the bytes: a stage of 64 k took it 560 cycles for 512 of products
+  // (waiting 120, four products 270, commit 170), and five stages were no faster than three.
+  int boxes = 0;
+  for (int q = 0; q < g.np; ++q) {
+    HeadProb& p = g.p[q];
+    boxes = std::max(boxes, p.a_boxes + p.b_boxes);
+    p.seg = segmented ? std::max(1, kSeg / p.pairs) : 1 << 30;
+  }
+  g.stage = boxes * kHalf;
+  g.nst = (192 << 10) / g.stage;
+  g.place = kEpi == kGrad && g.terms > 1 ? kStaged / 2 : 0;
   g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
   g.tiles = g.tiles0 + (g.np > 1 ? g.p[1].mt * g.p[1].nt * g.p[1].splits : 0);
   g.few = 0;
@@ -916,14 +987,11 @@ struct Call {
   bool accumulate, forward, grad;
 };
 
-void size_product(HeadProb* p, int64_t M, int64_t N, int64_t K) {
+void size_product(HeadProb* p, int64_t M, int64_t N) {
   p->M = (int)M;
   p->N = (int)N;
   p->mt = (int)ceil_div(M, kTile);
   p->nt = (int)ceil_div(N, kTile);
-  p->kc = (int)ceil_div(K, kK);
-  p->per = p->kc;
-  p->splits = 1;
 }
 
 asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_bytes, cudaStream_t st) {
@@ -958,8 +1026,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   float2* row = reinterpret_cast<float2*>(ws + l.row);
   // the logits' product: whole, then in pieces
   HeadProb logits = {};
-  size_product(&logits, T, V, D);
-  set_pairs(&logits, l.in_terms, l.in_terms);
+  size_product(&logits, T, V);
+  set_chunks(&logits, D, l.in_terms, l.in_terms);
   if (!operand_map(&logits.a, x, D, T, ld, l.in_terms, T * ld, kK, 128) || !operand_map(&logits.b, w, D, V, ld, l.in_terms, V * ld, kK, 128))
     return cuda_status(cudaErrorNotSupported, "tensor map");
   const bool keep = c.forward && c.grad && l.kept && ws_bytes >= l.bytes;
@@ -994,7 +1062,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   void* G = ws + l.g;
   HeadProb px = {}, pw = {};
   // (the product's first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
-  bool maps = operand_map(&g.g, G, l.cols, T, l.cols, terms, T * l.cols, 64, 32);
+  bool maps = operand_map(&g.g, G, l.cols, T, l.cols, terms, T * l.cols, terms == 1 ? 64 : 32, 32, terms == 1 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
   maps = maps && operand_map(&px.a, G, l.cols, T, l.cols, terms, T * l.cols, kK, 128) && operand_map(&px.b, w, D, V, ld, l.in_terms, V * ld, 64, kK);
   maps = maps && operand_map(&pw.a, G, l.cols, T, l.cols, terms, T * l.cols, 64, kK) && operand_map(&pw.b, x, D, T, ld, l.in_terms, T * ld, 64, kK);
   if (!maps) return cuda_status(cudaErrorNotSupported, "tensor map");
@@ -1018,11 +1086,11 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       e = launch_gemm<kGrad>(g, fine, st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
-    size_product(&px, T, D, nv);
-    set_pairs(&px, fine ? 3 : 1, fine ? 3 : 1);
+    size_product(&px, T, D);
+    set_chunks(&px, nv, fine ? 3 : 1, fine ? 3 : 1);
     px.a_mn = 0, px.b_mn = 1, px.b_k = (int)v0, px.n_first = 1;
-    size_product(&pw, nv, D, T);
-    set_pairs(&pw, dw_kind == kF32 ? 3 : 1, l.in_terms);
+    size_product(&pw, nv, D);
+    set_chunks(&pw, T, dw_kind == kF32 ? 3 : 1, l.in_terms);
     pw.a_mn = 1, pw.b_mn = 1, pw.n_first = 1;
     pw.ld = D;
     pw.out = static_cast<char*>(c.dw) + v0 * D * size_of(d->dw_dtype);
