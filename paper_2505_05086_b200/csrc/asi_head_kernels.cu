@@ -44,17 +44,17 @@ enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
 enum Kind { kNone = 0, kF32 = 1, kB16 = 2 };
 
 // One product C[m][n] = sum over k and pairs of terms of A(m, k) B(n, k).  An operand lies with its k together (mn = 0: boxes of 64 k
-// x 128 rows) or with its rows together (mn = 1: boxes of 64 rows x 64 k, two of them); terms are the map's third axis.
+// x 128 rows) or with its rows together (mn = 1: boxes of 64 rows x all k of the chunk, two of them); terms are the map's third axis.
 struct HeadProb {
   CUtensorMap a, b;
   int a_mn, b_mn;
   int a_off, a_k, b_off, b_k;   // where the product's first row and first k lie in the operand
   int M, N, mt, nt, splits;     // tiles; `splits` shares of k one after another
   int kc, per;                  // chunks of k, and of a share
-  // A chunk of `sub` times 64 k shares a stage: `sub` boxes of each of A's terms, then B's
-  int sub, a_boxes, b_boxes;
-  int pairs;                    // pairs of boxes that are multiplied
-  uint32_t a_box, b_box;        // of each pair, two bits
+  // A chunk of `sub` times 64 k shares a stage: A's terms, then B's, `sub` times 16 KB each
+  int sub, a_terms, b_terms;
+  int pairs;                    // pairs of parts (64 k of a term) that are multiplied
+  uint32_t a_part, b_part;      // of each pair, two bits
   int seg;                      // chunks that add up in TMEM (kSegmented), or all
   int n_first;                  // tiles of a row follow one another (else tiles of a column)
   const void* add;              // added to the result, laid out like it; null: nothing
@@ -310,9 +310,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const uint32_t idesc = instr_desc_bf16(kTile, kTile, p.a_mn != 0, p.b_mn != 0);
         // a k-step is 16 bf16: 32 bytes inside the swizzle row of a K-major tile, 16 rows (2048 bytes) of an MN-major one
         const uint64_t a_step = p.a_mn ? 128 : 2, b_step = p.b_mn ? 128 : 2;
-        const uint64_t da0 = smem_desc_sw128(at, p.a_mn ? kHalf / 2 : 16), db0 = smem_desc_sw128(at + p.a_boxes * kHalf, p.b_mn ? kHalf / 2 : 16);
-        const int per_seg = p.seg, box_pairs = p.pairs;
-        const uint32_t a_box = p.a_box, b_box = p.b_box;
+        const uint64_t da0 = smem_desc_sw128(at, p.a_mn ? p.sub * kHalf / 2 : 16), db0 = smem_desc_sw128(at + p.a_terms * p.sub * kHalf, p.b_mn ? p.sub * kHalf / 2 : 16);
+        // the second 64 k of a chunk: the next box, or the next rows of the same ones
+        const uint32_t a_next = (p.a_mn && p.sub > 1 ? kHalf / 2 : kHalf) >> 4, b_next = (p.b_mn && p.sub > 1 ? kHalf / 2 : kHalf) >> 4;
+        const int per_seg = p.seg, pairs_of = p.pairs;
+        const uint32_t a_part = p.a_part, b_part = p.b_part;
 #pragma unroll 1
         for (int c0 = 0; c0 < x.chunks && ok; c0 += per_seg, ++seg) {
           const int buf = seg & 1, turn = seg >> 1;
@@ -335,8 +337,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             if (++st == nst) st = 0, ph ^= 1u;
             ready = mbar_test(full + st, ph);              // (the answer comes while products are issued)
 #pragma unroll 1
-            for (int e = 0; e < box_pairs; ++e) {
-              const uint64_t da = da1 + ((a_box >> (2 * e)) & 3) * (kHalf >> 4), db = db1 + ((b_box >> (2 * e)) & 3) * (kHalf >> 4);
+            for (int e = 0; e < pairs_of; ++e) {
+              const uint64_t da = da1 + ((a_part >> (2 * e)) & 3) * a_next, db = db1 + ((b_part >> (2 * e)) & 3) * b_next;
 #pragma unroll
               for (int ks = 0; ks < kK / 16; ++ks)
                 umma_pair_bf16_one(acc, da + ks * a_step, db + ks * b_step, idesc, ((c - c0) | e | ks) ? 1u : 0u);
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const int am = p.a_off + x.m * kTile + rank * 128, bn = p.b_off + x.n * kTile + rank * 128;
         const CUtensorMap *ma = &p.a, *mb = &p.b;
         const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
-        const int a_boxes = p.a_boxes, b_boxes = p.b_boxes, sub = p.sub;
+        const int a_terms = p.a_terms, b_terms = p.b_terms, sub = p.sub;
         int ka = p.a_k + x.k0 * sub * kK, kb = p.b_k + x.k0 * sub * kK;
 #pragma unroll 1
         for (int c = 0; c < x.chunks; ++c, ++loads) {
@@ -368,26 +370,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             ok = warp_wait(empty + st, ph, stall);
             if (!ok) break;
           }
-          if (rank == 0) mbar_expect_tx_one(smem_u32(full) + st * 8, 2 * (a_boxes + b_boxes) * kHalf);
+          if (rank == 0) mbar_expect_tx_one(smem_u32(full) + st * 8, 2 * (a_terms + b_terms) * sub * kHalf);
           if (!stall) {
             uint32_t to = smem_u32(base) + st * stage;
             const uint32_t bar = full0 + st * 8;
-            auto fetch = [&](const CUtensorMap* map, bool mn, int row, int k, int boxes) {
-              int term = 0, half = 0;
+            auto fetch = [&](const CUtensorMap* map, bool mn, int row, int k, int terms) {
 #pragma unroll 1
-              for (int e = 0; e < boxes; ++e, to += kHalf) {
-                const int at = k + half * kK;
-                if (mn) {
-                  tma_pair_load_3d_one(to, map, row, at, term, bar);
-                  tma_pair_load_3d_one(to + kHalf / 2, map, row + 64, at, term, bar);
-                } else {
-                  tma_pair_load_3d_one(to, map, at, row, term, bar);
-                }
-                if (++half == sub) half = 0, ++term;
+              for (int e = 0; e < terms; ++e, to += sub * kHalf) {
+                tma_pair_load_3d_one(to, map, mn ? row : k, mn ? k : row, e, bar);
+                if (mn) tma_pair_load_3d_one(to + sub * kHalf / 2, map, row + 64, k, e, bar);
+                else if (sub > 1) tma_pair_load_3d_one(to + kHalf, map, k + kK, row, e, bar);
               }
             };
-            fetch(ma, a_mn, am, ka, a_boxes);
-            fetch(mb, b_mn, bn, kb, b_boxes);
+            fetch(ma, a_mn, am, ka, a_terms);
+            fetch(mb, b_mn, bn, kb, b_terms);
           }
           ka += sub * kK, kb += sub * kK;
           if (++st == nst) st = 0, ph ^= 1u;
@@ -871,18 +867,18 @@ bool operand_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows
   return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, 3, dims, strides, box, swizzle);
 }
 
-// The chunks of a product over K: of one term of either operand 128 k a stage (its two boxes, each with its like), of more 64 with the pairs of
+// The chunks of a product over K: of one term of either operand 128 k a stage, of more 64 with the pairs of
 // terms that matter, small ones first
 void set_chunks(HeadProb* p, int64_t K, int a_terms, int b_terms) {
   p->pairs = 0;
-  p->a_box = p->b_box = 0;
+  p->a_part = p->b_part = 0;
   auto pair = [&](int a, int b) {
-    p->a_box |= (uint32_t)a << (2 * p->pairs);
-    p->b_box |= (uint32_t)b << (2 * p->pairs);
+    p->a_part |= (uint32_t)a << (2 * p->pairs);
+    p->b_part |= (uint32_t)b << (2 * p->pairs);
     ++p->pairs;
   };
   p->sub = a_terms == 1 && b_terms == 1 ? 2 : 1;
-  p->a_boxes = a_terms * p->sub, p->b_boxes = b_terms * p->sub;
+  p->a_terms = a_terms, p->b_terms = b_terms;
   if (p->sub == 2) {
     pair(0, 0), pair(1, 1);
   } else {
@@ -942,13 +938,13 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   // Stages of what the larger chunk takes (64 KB for one term of either operand, 96 for three), as many as 192 KB hold, beside a place for
   // each warp's results on their way out.  What bounds the issuer is not the bytes: a stage of 64 k took it 560 cycles for 512 of products
   // (waiting 120, four products 270, commit 170), and five stages were no faster than three.
-  int boxes = 0;
+  int parts = 0;
   for (int q = 0; q < g.np; ++q) {
     HeadProb& p = g.p[q];
-    boxes = std::max(boxes, p.a_boxes + p.b_boxes);
+    parts = std::max(parts, (p.a_terms + p.b_terms) * p.sub);
     p.seg = segmented ? std::max(1, kSeg / p.pairs) : 1 << 30;
   }
-  g.stage = boxes * kHalf;
+  g.stage = parts * kHalf;
   g.nst = (192 << 10) / g.stage;
   g.place = kEpi == kGrad && g.terms > 1 ? kStaged / 2 : 0;
   g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
@@ -1061,11 +1057,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   g.ld_w = ld;
   void* G = ws + l.g;
   HeadProb px = {}, pw = {};
-  // (the product's first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
-  bool maps = operand_map(&g.g, G, l.cols, T, l.cols, terms, T * l.cols, terms == 1 ? 64 : 32, 32, terms == 1 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
-  maps = maps && operand_map(&px.a, G, l.cols, T, l.cols, terms, T * l.cols, kK, 128) && operand_map(&px.b, w, D, V, ld, l.in_terms, V * ld, 64, kK);
-  maps = maps && operand_map(&pw.a, G, l.cols, T, l.cols, terms, T * l.cols, 64, kK) && operand_map(&pw.b, x, D, T, ld, l.in_terms, T * ld, 64, kK);
-  if (!maps) return cuda_status(cudaErrorNotSupported, "tensor map");
+  if (!operand_map(&g.g, G, l.cols, T, l.cols, terms, T * l.cols, terms == 1 ? 64 : 32, 32, terms == 1 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+    return cuda_status(cudaErrorNotSupported, "tensor map");
   const int64_t pieces = ceil_div(V, l.cols);
   const int dx_kind = d->in_dtype == ASI_BF16 ? kB16 : kF32, dw_kind = d->dw_dtype == ASI_BF16 ? kB16 : kF32;
   float* acc = reinterpret_cast<float*>(ws + l.acc);
@@ -1086,12 +1079,18 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       e = launch_gemm<kGrad>(g, fine, st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
+    // (the first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
     size_product(&px, T, D);
     set_chunks(&px, nv, fine ? 3 : 1, fine ? 3 : 1);
     px.a_mn = 0, px.b_mn = 1, px.b_k = (int)v0, px.n_first = 1;
     size_product(&pw, nv, D);
     set_chunks(&pw, T, dw_kind == kF32 ? 3 : 1, l.in_terms);
     pw.a_mn = 1, pw.b_mn = 1, pw.n_first = 1;
+    if (i == 0) {
+      bool maps = operand_map(&px.a, G, l.cols, T, l.cols, terms, T * l.cols, kK, 128) && operand_map(&px.b, w, D, V, ld, l.in_terms, V * ld, 64, kK * px.sub);
+      maps = maps && operand_map(&pw.a, G, l.cols, T, l.cols, terms, T * l.cols, 64, kK * pw.sub) && operand_map(&pw.b, x, D, T, ld, l.in_terms, T * ld, 64, kK * pw.sub);
+      if (!maps) return cuda_status(cudaErrorNotSupported, "tensor map");
+    }
     pw.ld = D;
     pw.out = static_cast<char*>(c.dw) + v0 * D * size_of(d->dw_dtype);
     pw.out_kind = dw_kind;
