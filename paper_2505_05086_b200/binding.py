@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libasi_b200.so")
@@ -99,9 +100,18 @@ class BranchDesc(C.Structure):
 
 
 class Branch(C.Structure):
+    """asi_branch_t; pack() makes its bytes at once from all addresses in their order (0: none)."""
     _fields_ = [(n, C.c_void_p) for n in (
         "y", "h", "gate", "after_weight", "after_bias", "next_weight", "next_bias", "h_out", "x", "stats", "dx", "dh_out", "dy", "dh",
         "dgate", "dafter_weight", "dafter_bias", "dnext_weight", "dnext_bias")]
+    pack = struct.Struct("@19P").pack
+
+
+class _BranchArg:
+    """The argument as ctypes takes it: a Branch, or the bytes that pack() made."""
+    @staticmethod
+    def from_param(x):
+        return C.c_char_p.from_param(x) if isinstance(x, bytes) else C.POINTER(Branch).from_param(x)
 
 
 class HeadDesc(C.Structure):
@@ -172,7 +182,7 @@ def lib():
     L.asi_embedding_wgrad_ws_bytes.restype = sz
     L.asi_embedding_wgrad.argtypes = [pe, vp, vp, vp, i32, vp, sz, vp]
     L.asi_adamw_step.argtypes = [C.POINTER(AdamwDesc), C.POINTER(AdamwTensor), i32, vp]
-    pd, pb, pt, ph = C.POINTER(Dropout), C.POINTER(BranchDesc), C.POINTER(Branch), C.POINTER(HeadDesc)
+    pd, pb, pt, ph = C.POINTER(Dropout), C.POINTER(BranchDesc), _BranchArg, C.POINTER(HeadDesc)
     L.asi_dropout.argtypes = [pd, i32, C.c_int64, vp, vp, vp, vp]
     L.asi_branch_forward.argtypes = [pb, pt, vp]
     L.asi_branch_backward_ws_bytes.argtypes = [pb]

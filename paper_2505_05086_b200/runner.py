@@ -496,14 +496,26 @@ def _drop(p, seed, stream_id):
     return Dropout(float(p), int(seed), int(stream_id), 0, None)
 
 
+class _Masked(_Descriptor):
+    """... and the part of it that draws the mask."""
+
+    def __init__(self, first):
+        super().__init__(first)
+        self.drop, self.on_device = getattr(self.desc, "drop", self.desc), False
+
+
 class _Steps(_Runner):
     """A mask for each step: `step` may be a number, or a one-element int64 device tensor that a captured graph reads."""
 
-    def _at_step(self, drop, step):
+    def _at_step(self, local, step):
+        drop = local.drop
         if isinstance(step, torch.Tensor):
             drop.step, drop.step_dev = 0, _take("step", step.reshape(1), (1,), torch.int64, self.device)
+            local.on_device = True
         else:
-            drop.step, drop.step_dev = int(step), None
+            drop.step = int(step)
+            if local.on_device:
+                drop.step_dev, local.on_device = None, False
 
 
 class DropoutRunner(_Steps):
@@ -513,17 +525,16 @@ class DropoutRunner(_Steps):
     def __init__(self, p, seed, stream_id=0, bf16=False, device="cuda:0"):
         self.device = _cuda_device(device)
         self.in_dtype = torch.bfloat16 if bf16 else torch.float32
-        self._descriptor = _Descriptor(_drop(p, seed, stream_id))
+        self._descriptor = _Masked(_drop(p, seed, stream_id))
         self._made(self.device)
 
     def forward(self, x, out, step=0, residual=None, stream=None):
         """out = x with elements dropped and the others scaled, plus residual if given.  out may be x or residual."""
-        d = self._descriptor.desc
-        self._at_step(d, step)
-        a = _take("x", x, x.shape, self.in_dtype, self.device)
-        o = _take("out", out, x.shape, self.in_dtype, self.device)
-        r = _take("residual", residual, x.shape, self.in_dtype, self.device) if residual is not None else 0
-        self._call(stream, binding.dropout, d, _DTYPES[self.in_dtype], x.numel(), a, r, o)
+        local, dtype, device, shape = self._descriptor, self.in_dtype, self.device, x.shape
+        self._at_step(local, step)
+        a, o = _take("x", x, shape, dtype, device), _take("out", out, shape, dtype, device)
+        r = _take("residual", residual, shape, dtype, device) if residual is not None else 0
+        self._call(stream, binding.dropout, local.desc, _DTYPES[dtype], x.numel(), a, r, o)
 
     def backward(self, dout, dx, step=0, stream=None):
         """dx = the gradient of x (that of residual is dout itself).  dx may be dout."""
@@ -546,60 +557,74 @@ class ResidualNormRunner(_Steps):
         kinds = dict(rms=ASI_NORM_RMS, layer=ASI_NORM_LAYER)
         if norm not in kinds:
             raise ValueError(f"norm: one of {sorted(kinds)} is needed, got {norm!r}")
-        self._descriptor = _Descriptor(BranchDesc(_DTYPES[self.in_dtype], _DTYPES[self.res_dtype], kinds[norm], self.norm_after, self.rows,
-                                                  self.dim, self.rows_per_gate, eps, res_scale, branch_scale,
-                                                  _drop(dropout, seed, stream_id)))
+        self._descriptor = _Masked(BranchDesc(_DTYPES[self.in_dtype], _DTYPES[self.res_dtype], kinds[norm], self.norm_after, self.rows,
+                                              self.dim, self.rows_per_gate, eps, res_scale, branch_scale, _drop(dropout, seed, stream_id)))
+        self._row = torch.Size((self.dim,))
         self.stats = torch.zeros(self.rows, 4, dtype=torch.float32, device=self.device)
         self.ws = torch.empty(binding.branch_backward_ws_bytes(self.desc), dtype=torch.uint8, device=self.device)
         self._made(self.device)
 
     def _own(self):
-        return (self.stats, self.ws)
+        return (self._stats, self.ws)
 
-    def _buffers(self, y, step, gate, after, next):
-        """Descriptor and buffers with what both directions share."""
-        d, b = self._descriptor.desc, Branch()
-        if y.dim() < 1 or y.shape[-1] != self.dim or y.numel() // self.dim > self.rows:
-            raise ValueError(f"y: up to {self.rows} rows of {self.dim} are needed, got {tuple(y.shape)}")
-        d.rows = n = y.numel() // self.dim
-        self._at_step(d.drop, step)
-        if self.stats.shape[0] < n:
-            raise ValueError(f"stats: {n} rows are needed, there are {self.stats.shape[0]}")
-        b.y = _take("y", y, y.shape, self.in_dtype, self.device)
-        b.stats = _take("stats", self.stats, (self.stats.shape[0], 4), torch.float32, self.device)
-        if (gate is not None) != bool(self.rows_per_gate):
-            raise ValueError("gate: the runner was made " + ("with" if self.rows_per_gate else "without") + " one")
-        for name, x, shape in self._weights(n, gate, after, next):
-            setattr(b, name, _take(name, x, shape, torch.float32, self.device))
-        return d, b, n
+    @property
+    def stats(self):
+        return self._stats
 
-    def _weights(self, n, gate, after, next, grad=""):
-        """Names, tensors and sizes of those of gate, weights and biases that are there."""
-        shape = (-(-n // self.rows_per_gate), self.dim) if self.rows_per_gate else ()
-        all_ = [("gate", gate, shape)] + [(f"{of}_{what}", x, (self.dim,)) for of, pair in (("after", after), ("next", next))
-                                          for what, x in zip(("weight", "bias"), pair)]
-        return [(f"{grad}{name}", x, size) for name, x, size in all_ if x is not None]
+    @stats.setter
+    def stats(self, x):
+        _take("stats", x, (len(x), 4), torch.float32, self.device)
+        self._stats, self._stats_at, self._most = x, x.data_ptr(), min(self.rows, len(x))
+
+    def _begin(self, y, step):
+        """The thread's descriptor for y's rows, how many these are, their sizes, and the statistics' address."""
+        local, shape = self._descriptor, y.shape
+        if self._stats.data_ptr() != self._stats_at:       # (its memory was exchanged)
+            self.stats = self._stats
+        n = y.numel() // self.dim
+        if not shape or shape[-1] != self.dim or n > self._most:
+            raise ValueError(f"y: up to {self._most} rows of {self.dim} are needed (as many as the runner and its stats have), got {tuple(shape)}")
+        local.desc.rows = n
+        self._at_step(local, step)
+        return local.desc, n, shape, self._stats_at
+
+    def _shared(self, n, gate, after, next):
+        """Addresses of the gate and of the norms' weights and biases."""
+        per, row, f32, device = self.rows_per_gate, self._row, torch.float32, self.device
+        if (gate is None) is bool(per):
+            raise ValueError("gate: the runner was made " + ("with" if per else "without") + " one")
+        (aw, ab), (nw, nb) = after, next
+        return (_take("gate", gate, (-(-n // per), self.dim), f32, device) if per else 0,
+                0 if aw is None else _take("after's weight", aw, row, f32, device), 0 if ab is None else _take("after's bias", ab, row, f32, device),
+                0 if nw is None else _take("next's weight", nw, row, f32, device), 0 if nb is None else _take("next's bias", nb, row, f32, device))
 
     def forward(self, y, h, h_out, x=None, gate=None, after=(None, None), next=(None, None), step=0, stream=None):
         """h_out = res_scale h + branch_scale drop(gate norm(y)), x = norm(h_out); `after` and `next` are (weight, bias) of the two
         norms.  h may be None (0), h_out may be h; without x no norm follows."""
-        d, b, n = self._buffers(y, step, gate, after, next)
-        b.h = _take("h", h, y.shape, self.res_dtype, self.device) if h is not None else None
-        b.h_out = _take("h_out", h_out, y.shape, self.res_dtype, self.device)
-        b.x = _take("x", x, y.shape, self.in_dtype, self.device) if x is not None else None
-        self._call(stream, binding.branch_forward, d, b)
+        d, n, shape, stats = self._begin(y, step)
+        it, rt, device = self.in_dtype, self.res_dtype, self.device
+        buffers = binding.Branch.pack(
+            _take("y", y, shape, it, device), 0 if h is None else _take("h", h, shape, rt, device), *self._shared(n, gate, after, next),
+            _take("h_out", h_out, shape, rt, device), 0 if x is None else _take("x", x, shape, it, device), stats, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+        self._call(stream, binding.branch_forward, d, buffers)
 
     def backward(self, y, h_out, dx, dh_out, dy, dh=None, gate=None, after=(None, None), next=(None, None), dgate=None, dafter=(None, None),
                  dnext=(None, None), accumulate=False, step=0, stream=None):
         """Gradients from those of x (dx) and h_out (dh_out; either may be None): dy and dh overwritten, dgate, dafter and dnext (where
         given) overwritten or, with accumulate, increased.  dy may be dx, dh may be dh_out."""
-        d, b, n = self._buffers(y, step, gate, after, next)
-        for name, t, dtype in (("h_out", h_out, self.res_dtype), ("dx", dx, self.in_dtype), ("dh_out", dh_out, self.res_dtype),
-                               ("dy", dy, self.in_dtype), ("dh", dh, self.res_dtype)):
-            setattr(b, name, _take(name, t, y.shape, dtype, self.device) if t is not None else None)
-        for name, t, shape in self._weights(n, dgate, dafter, dnext, "d"):
-            setattr(b, name, _take(name, t, shape, torch.float32, self.device))
-        self._call(stream, binding.branch_backward, d, b, accumulate, self.ws.data_ptr(), self.ws.numel())
+        d, n, shape, stats = self._begin(y, step)
+        it, rt, f32, device, row = self.in_dtype, self.res_dtype, torch.float32, self.device, self._row
+        per, (daw, dab), (dnw, dnb) = self.rows_per_gate, dafter, dnext
+        if dgate is not None and not per:
+            raise ValueError("dgate: the runner was made without a gate")
+        buffers = binding.Branch.pack(
+            _take("y", y, shape, it, device), 0, *self._shared(n, gate, after, next), 0 if h_out is None else _take("h_out", h_out, shape, rt, device), 0,
+            stats, 0 if dx is None else _take("dx", dx, shape, it, device), 0 if dh_out is None else _take("dh_out", dh_out, shape, rt, device),
+            _take("dy", dy, shape, it, device), 0 if dh is None else _take("dh", dh, shape, rt, device),
+            0 if dgate is None else _take("dgate", dgate, (-(-n // per), self.dim), f32, device),
+            0 if daw is None else _take("dafter's weight", daw, row, f32, device), 0 if dab is None else _take("dafter's bias", dab, row, f32, device),
+            0 if dnw is None else _take("dnext's weight", dnw, row, f32, device), 0 if dnb is None else _take("dnext's bias", dnb, row, f32, device))
+        self._call(stream, binding.branch_backward, d, buffers, accumulate, self.ws.data_ptr(), self.ws.numel())
 
 
 class HeadRunner(_RowResults):

@@ -12,7 +12,9 @@ def world(plain_world, monkeypatch):  # noqa: F811
 
     def recorder(name):
         # (descriptors are read within the call)
-        return lambda *args: plain_world.calls.append((name, tuple(type(a).from_buffer_copy(a) if hasattr(a, "_fields_") else a for a in args)))
+        def read(a):
+            return type(a).from_buffer_copy(a) if hasattr(a, "_fields_") else binding.Branch.from_buffer_copy(a) if isinstance(a, bytes) else a
+        return lambda *args: plain_world.calls.append((name, tuple(map(read, args))))
     for name in ("dropout", "branch_forward", "branch_backward", "head_logprobs", "head_grad", "head_loss"):
         monkeypatch.setattr(binding, name, recorder(name))
     return plain_world
@@ -119,7 +121,7 @@ def test_another_stream_waits_for_their_buffers(world):
         r._call(side, lambda *a: None)
     assert ws.told == [7] and side.waited == ["event of 0"]
     b = branch_runner()
-    b.ws, b.stats = Buffer(b.ws), Buffer(b.stats)
+    b.ws, b._stats = Buffer(b.ws), Buffer(b.stats)
     other = Stream(9)
     b._call(other, lambda *a: None)
-    assert b.ws.told == b.stats.told == [9] and other.waited == ["event of 0"]
+    assert b.ws.told == b._stats.told == [9] and other.waited == ["event of 0"]
