@@ -12,6 +12,7 @@
 // What bounds them: bytes.  A thread keeps eight values of its row in registers, a row's sums meet in shared memory, and what the
 // backward pass sums over rows stays in the threads' registers from row to row: each worker (the threads of a row) takes
 // neighbouring rows and leaves one partial sum a column, which k_branch_sums adds up in order.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -200,14 +201,14 @@ struct BranchArgs {
 // partial sums of a worker: over the first of its gate's rows, over the last one, over all
 enum Part { kHead1 = 0, kTail1 = 1, kNext1 = 2, kAfter1 = 3, kHead0 = 4, kTail0 = 5, kNext0 = 6, kAfter0 = 7, kParts = 8 };
 
-// Sums of a value or two over the threads of a row, for all of them (a multiple of 32, kMax at most; rows side by side in y)
+// Sums of a value or two over the threads of a CTA, for all of them (a multiple of 32, kMax at most)
 template <int kMax>
 struct RowSum {
-  static constexpr int kWarps = kMax / 32, kRows = 8;
-  float* sh;               // [2][kRows][2 kWarps], 0 where no warp writes
+  static constexpr int kWarps = kMax / 32;
+  float* sh;               // [2][2 kWarps], 0 where no warp writes
   uint32_t phase = 0;
   __device__ __forceinline__ RowSum(float* s) : sh(s) {
-    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < 4 * kRows * kWarps; i += blockDim.x * blockDim.y) s[i] = 0.f;
+    for (int i = threadIdx.x; i < 4 * kWarps; i += blockDim.x) s[i] = 0.f;
     __syncthreads();
   }
   template <bool kTwo>
@@ -218,8 +219,8 @@ struct RowSum {
       if (kTwo) b += __shfl_xor_sync(~0u, b, o);
     }
     if (blockDim.x == 32) return make_float2(a, b);
-    float* s = sh + (phase + threadIdx.y) * (2 * kWarps);
-    phase ^= kRows;
+    float* s = sh + phase;
+    phase ^= 2 * kWarps;
     if ((threadIdx.x & 31) == 0) {
       s[threadIdx.x >> 5] = a;
       if (kTwo) s[kWarps + (threadIdx.x >> 5)] = b;
@@ -307,9 +308,8 @@ struct Ring {
   uint32_t mine, piece, stage_bytes, at;                   // (at: of the row that is next)
   int stages, left;
   __device__ __forceinline__ Ring(void* smem, int n) {
-    const uint32_t threads = blockDim.x * blockDim.y, i = threadIdx.y * blockDim.x + threadIdx.x;
-    mine = at = (uint32_t)__cvta_generic_to_shared(smem) + i * 16;
-    piece = threads * 16;
+    mine = at = (uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16;
+    piece = blockDim.x * 16;
     stage_bytes = kTensors * kPieces * piece;
     stages = left = n;
   }
@@ -407,13 +407,13 @@ __device__ __forceinline__ void branch_factor(float (&w)[kEach], const float* a,
 template <typename TI, typename TR, bool kVec, bool kLayer, int kMax>
 __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const __grid_constant__ BranchArgs p) {
   extern __shared__ __align__(16) uint8_t ring_smem[];
-  __shared__ __align__(16) float sh[kMax];
+  __shared__ __align__(16) float sh[kMax / 8];
   constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
   RowSum<kMax> sum(sh);
   const Columns<kVec> c(p.dim);
-  const int worker = blockIdx.x * blockDim.y + threadIdx.y;
+  const int worker = blockIdx.x;
   const int64_t t0 = worker * p.run, t1 = t0 + p.run < p.rows ? t0 + p.run : p.rows;
   const uint32_t step = p.drop.below ? step_of(p.drop) : 0;
   Ring<2, sizeof(TR) / 2> ring(ring_smem, p.stages);
@@ -441,34 +441,32 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
     if (kLayer) branch_factor(b, p.ab, 0.f, p.bs, gate, c);
   }
   const Param<kVec, kHeld> nw(p.nw, 1.f, c), nb(kLayer ? p.nb : nullptr, 0.f, c);
-  const int run = (int)p.run;
-  int64_t at = t0 < p.rows ? t0 * p.dim : 0;
+  int64_t at = t0 * p.dim;
 #pragma unroll 1
-  for (int k = 0; k < run; ++k, at += k < rows ? p.dim : 0) {   // (rows side by side in a CTA go on together: their sums share barriers)
+  for (int k = 0; k < rows; ++k, at += p.dim) {
     const int64_t t = t0 + k;
-    const bool there = k < rows;
     float f[kEach], h[kEach], x[kEach];
     if constexpr (kVec) {
       clear8(f);
       clear8(h);
       ring.wait();
-      if (there && mine) {
+      if (mine) {
         ring.template take<0>(y, f);
         if (res) ring.template take<1>(h_in, h);
       }
       fetch(ring.at);
       ring.advance();
     } else {
-      c.load(y + at, f, there);
-      c.load(h_in + at, h, there && res);
+      c.load(y + at, f);
+      c.load(h_in + at, h, res);
     }
     float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p.norm_after) {
       const float2 s = normalise<kLayer>(f, c, p, sum);
       st.x = s.x, st.y = s.y;
     }
-    if (!kHeld || (there && t >= next_group)) {
-      if (groups && there && t >= next_group) {
+    if (!kHeld || t >= next_group) {
+      if (groups && t >= next_group) {
         const int64_t group = t / p.per;
         gate = p.gate + group * p.dim;
         next_group = (group + 1) * p.per;
@@ -478,14 +476,14 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
     }
     if (kLayer) fma8(f, f, w, b);
     else mul8(f, f, w);
-    if (p.drop.below && there) c.mask(p.drop, step, t, f);
+    if (p.drop.below) c.mask(p.drop, step, t, f);
     fma8(f, h, p.rs, f);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       f[i] = stored<TR>(f[i]);
       if (!kVec) f[i] = c.there(i) ? f[i] : 0.f;
     }
-    if (there) c.store(static_cast<TR*>(p.h_out) + at, f);
+    c.store(static_cast<TR*>(p.h_out) + at, f);
     if (p.x) {
       const float2 s = normalise<kLayer>(f, c, p, sum);
       st.z = s.x, st.w = s.y;
@@ -496,9 +494,9 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
       } else {
         mul8(f, f, x);
       }
-      if (there) c.store(static_cast<TI*>(p.x) + at, f);
+      c.store(static_cast<TI*>(p.x) + at, f);
     }
-    if (there && threadIdx.x == 0) {
+    if (threadIdx.x == 0) {
       float* s = p.stats + 4 * t;
       if (on16(s)) *reinterpret_cast<float4*>(s) = st;
       else s[0] = st.x, s[1] = st.y, s[2] = st.z, s[3] = st.w;
@@ -525,13 +523,13 @@ __device__ __forceinline__ void put_gate(const BranchArgs& p, const Columns<kVec
 template <typename TI, typename TR, bool kVec, bool kLayer, bool kGroups, int kMax>
 __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(const __grid_constant__ BranchArgs p) {
   extern __shared__ __align__(16) uint8_t ring_smem[];
-  __shared__ __align__(16) float sh[kMax];
+  __shared__ __align__(16) float sh[kMax / 8];
   constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
   RowSum<kMax> sum(sh);
   const Columns<kVec> c(p.dim);
-  const int worker = blockIdx.x * blockDim.y + threadIdx.y;
+  const int worker = blockIdx.x;
   const int64_t t0 = worker * p.run, t1 = t0 + p.run < p.rows ? t0 + p.run : p.rows;
   const uint32_t step = p.drop.below ? step_of(p.drop) : 0;
   Ring<4, sizeof(TR) / 2> ring(ring_smem, p.stages);
@@ -555,7 +553,8 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   };
   if (kVec)
     for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
-  float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {}, a1[kEach] = {}, a0[kEach] = {};
+  float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {};
+  bool again = false;                                      // (kGroups) the sums over all of the gate's rows have been begun
   const int64_t first = kGroups ? t0 / p.per : 0;
   int64_t group = first, next_group = kGroups ? (first + 1) * p.per : INT64_MAX;
   const float* gate = p.gate ? p.gate + (kGroups && t0 < p.rows ? group * p.dim : 0) : nullptr;
@@ -580,43 +579,45 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
           }
       }
     }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      a1[i] = fmaf(g[i], s1[i], a1[i]), s1[i] = 0.f;
-      if (kLayer) a0[i] = fmaf(g[i], s0[i], a0[i]), s0[i] = 0.f;
-    }
+    // gate S1 and gate S0 add up in the worker's own partial sums (rarely: registers for them would cost every row)
+    auto add = [&](int which, Eight& v) {
+      Eight sum;
+      clear8(sum);
+      if (again) c.load(part(which), sum);
+      fma8(sum, g, v, sum);
+      c.store(part(which), sum);
+    };
+    if (p.daw) add(kAfter1, s1);
+    if (kLayer && p.dab) add(kAfter0, s0);
+    again = true;
+    clear8(s1);
+    clear8(s0);
   };
-  const int run = (int)p.run;
-  int64_t at = t0 < p.rows ? t0 * p.dim : 0;
+  int64_t at = t0 * p.dim;
 #pragma unroll 1
-  for (int k = 0; k < run; ++k, at += k < rows ? p.dim : 0) {   // (rows side by side in a CTA go on together: their sums share barriers)
+  for (int k = 0; k < rows; ++k, at += p.dim) {
     const int64_t t = t0 + k;
-    const bool there = k < rows;
     float d[kEach], f[kEach], x[kEach];
-    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (there) {
-      const float* s = p.stats + 4 * t;
-      if (on16(s)) st = *reinterpret_cast<const float4*>(s);
-      else st = make_float4(s[0], s[1], s[2], s[3]);
-    }
+    const float* s = p.stats + 4 * t;
+    const float4 st = on16(s) ? *reinterpret_cast<const float4*>(s) : make_float4(s[0], s[1], s[2], s[3]);
     if constexpr (kVec) {
       ring.wait();
       clear8(d);
-      if (mine && there && more) ring.template take<2>(dh_out, d);
+      if (mine && more) ring.template take<2>(dh_out, d);
     } else {
-      c.load(dh_out + at, d, there && more);
+      c.load(dh_out + at, d, more);
     }
     if (next) {
       if constexpr (kVec) {
         clear8(x);
         clear8(f);
-        if (mine && there) {
+        if (mine) {
           ring.template take<0>(dx, x);
           ring.template take<1>(h_out, f);
         }
       } else {
-        c.load(dx + at, x, there);
-        c.load(h_out + at, f, there);
+        c.load(dx + at, x);
+        c.load(h_out + at, f);
       }
       float v[kEach];
       nw.get(v, c);
@@ -631,21 +632,21 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
       if (kLayer) add8(x, x, -m.y * p.inv_dim);
       fma8(d, x, st.w, d);
     }
-    if (p.dh && there) {
+    if (p.dh) {
       mul8(x, d, p.rs);
       c.store(static_cast<TR*>(p.dh) + at, x);
     }
-    mul8(d, d, there ? p.bs : 0.f);
-    if (p.drop.below && there) c.mask(p.drop, step, t, d);
+    mul8(d, d, p.bs);
+    if (p.drop.below) c.mask(p.drop, step, t, d);
     if constexpr (kVec) {
       clear8(f);
-      if (mine && there) ring.template take<3>(y, f);
+      if (mine) ring.template take<3>(y, f);
       fetch(ring.at);
       ring.advance();
     } else {
-      c.load(y + at, f, there);
+      c.load(y + at, f);
     }
-    if (kGroups && there && t >= next_group) {
+    if (kGroups && t >= next_group) {
       flush(group != first || first * p.per >= t0);
       group = t / p.per;
       next_group = (group + 1) * p.per;
@@ -666,7 +667,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
       if (kLayer) add8(d, d, -m.y * p.inv_dim);
       mul8(d, d, st.y);
     }
-    if (there) c.store(static_cast<TI*>(p.dy) + at, d);
+    c.store(static_cast<TI*>(p.dy) + at, d);
   }
   if (t0 >= p.rows) return;
   if (kGroups) {
@@ -677,77 +678,106 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   auto keep = [&](int which, const float (&v)[kEach]) { c.store(part(which), v); };
   if (!kGroups && (p.dgate || p.daw)) keep(kHead1, s1);
   if (!kGroups && kLayer && (p.dgate || p.dab)) keep(kHead0, s0);
-  if (kGroups && p.daw) keep(kAfter1, a1);
-  if (kGroups && kLayer && p.dab) keep(kAfter0, a0);
   if (p.dnw) keep(kNext1, n1);
   if (kLayer && p.dnb) keep(kNext0, n0);
 }
 
-// The workers' sums joined in order: 32 columns a CTA, 16 shares of the workers side by side.  blockIdx.y 0: of the next norm, 1: of the
-// norm after and of a gate of one row; 2 ..: rows of a gate that workers share
-constexpr int kSlices = 16;
+// The workers' sums joined in order: 32 columns a cluster of up to eight CTAs, eight shares of the workers side by side in each, joined in
+// shared memory and then across the cluster (one CTA with 44 of 701 workers a thread took 15 us, loads waiting for one another).
+// blockIdx.y 0: of the next norm, 1: of the norm after and of a gate of one row; 2 ..: rows of a gate that workers share
+constexpr int kSlices = 8, kSumCtas = 8;
 struct SumsArgs {
   BranchArgs b;
   int layer, groups;
+  int each;                // warps that share a row of the gate
 };
 __global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_constant__ SumsArgs a) {
   __shared__ float sh[2][kSlices][33];
+  __shared__ float2 joined[32];
+  namespace cg = cooperative_groups;
   const BranchArgs& p = a.b;
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
-  // of partial sums `one` and `two` (or none) over workers w0 .. w1; the first worker's from `one0` and `two0`
-  auto total = [&](int one0, int one, int two0, int two, int64_t w0, int64_t w1) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, rank = (int)cluster.block_rank(), ctas = (int)gridDim.z;
+  // of partial sums `one` and `two` (or none) over the workers; for the first warp of the first CTA
+  auto total = [&](int one, int two) {
+    const int64_t share = (p.workers + ctas - 1) / ctas, w0 = rank * share, w1 = w0 + share < p.workers ? w0 + share : p.workers;
     float x = 0.f, y = 0.f;
     if (col < p.dim)
 #pragma unroll 8
-      for (int64_t w = w0 + slice; w <= w1; w += kSlices) {
-        x += p.part[((int64_t)(w == w0 ? one0 : one) * p.workers + w) * p.dim + col];
-        if (two >= 0) y += p.part[((int64_t)(w == w0 ? two0 : two) * p.workers + w) * p.dim + col];
+      for (int64_t w = w0 + slice; w < w1; w += kSlices) {
+        x += p.part[((int64_t)one * p.workers + w) * p.dim + col];
+        if (two >= 0) y += p.part[((int64_t)two * p.workers + w) * p.dim + col];
       }
-    __syncthreads();
     sh[0][slice][lane] = x, sh[1][slice][lane] = y;
     __syncthreads();
-    float2 r = make_float2(0.f, 0.f);
-    if (slice == 0)
+    if (slice == 0) {
+      float2 r = make_float2(0.f, 0.f);
       for (int i = 0; i < kSlices; ++i) r.x += sh[0][i][lane], r.y += sh[1][i][lane];
+      joined[lane] = r;
+    }
+    cluster.sync();
+    float2 r = make_float2(0.f, 0.f);
+    if (rank == 0 && slice == 0)
+      for (int i = 0; i < ctas; ++i) {
+        const float2 v = cluster.map_shared_rank(joined, i)[lane];
+        r.x += v.x, r.y += v.y;
+      }
+    cluster.sync();                                       // (all have been read)
     return r;
   };
   auto write = [&](float* out, float v) {
-    if (out && slice == 0 && col < p.dim) out[col] = p.accumulate ? out[col] + v : v;
+    if (out && rank == 0 && slice == 0 && col < p.dim) out[col] = p.accumulate ? out[col] + v : v;
   };
-  const int64_t last = (p.rows - 1) / p.run;
   if (blockIdx.y == 0) {
     if (!p.dnw && !p.dnb) return;
     const bool one = p.dnw != nullptr, two = p.dnb && a.layer;
-    const float2 r = total(one ? kNext1 : kNext0, one ? kNext1 : kNext0, kNext0, one && two ? kNext0 : -1, 0, last);
+    const float2 r = total(one ? kNext1 : kNext0, one && two ? kNext0 : -1);
     if (one) write(p.dnw, r.x);
     if (two) write(p.dnb, one ? r.y : r.x);
   } else if (blockIdx.y == 1) {
     if (a.groups) {
-      if (p.daw) write(p.daw, total(kAfter1, kAfter1, 0, -1, 0, last).x);
-      if (p.dab) write(p.dab, total(kAfter0, kAfter0, 0, -1, 0, last).x);
+      if (p.daw) write(p.daw, total(kAfter1, -1).x);
+      if (p.dab) write(p.dab, total(kAfter0, -1).x);
       return;
     }
     if (!p.dgate && !p.daw && !p.dab) return;
     const bool one = p.dgate || p.daw, two = a.layer && (p.dgate || p.dab);
-    float2 r = total(one ? kHead1 : kHead0, one ? kHead1 : kHead0, kHead0, one && two ? kHead0 : -1, 0, last);
+    float2 r = total(one ? kHead1 : kHead0, one && two ? kHead0 : -1);
     if (!one) r.y = r.x;
-    if (slice || col >= p.dim) return;
+    if (rank || slice || col >= p.dim) return;
     const float w = p.aw ? p.aw[col] : 1.f, b = p.ab ? p.ab[col] : 0.f, g = p.gate ? p.gate[col] : 1.f;
     write(p.dgate, fmaf(w, r.x, b * r.y));
     write(p.daw, g * r.x);
     write(p.dab, g * r.y);
   } else {
-    for (int64_t s = blockIdx.y - 2; s * p.per < p.rows; s += gridDim.y - 2) {
-      const int64_t end = (s + 1) * p.per < p.rows ? (s + 1) * p.per : p.rows, w0 = s * p.per / p.run, w1 = (end - 1) / p.run;
-      if (w0 == w1) continue;                             // its worker wrote it
-      const bool head = w0 * p.run / p.per == s;          // the first worker's first row is the gate row's too
-      const float2 r = total(head ? kHead1 : kTail1, kHead1, head ? kHead0 : kTail0, a.layer ? kHead0 : -1, w0, w1);
-      if (slice == 0 && col < p.dim) {
-        const float w = p.aw ? p.aw[col] : 1.f, b = p.ab ? p.ab[col] : 0.f;
+    // `each` warps a row of the gate
+    const int sub = slice % a.each, rows = kSlices / a.each;
+    for (int64_t s0 = ((int64_t)(blockIdx.y - 2) * ctas + rank) * rows; s0 * p.per < p.rows; s0 += (int64_t)(gridDim.y - 2) * ctas * rows) {
+      const int64_t s = s0 + slice / a.each;
+      float x = 0.f, y = 0.f;
+      bool shared = false;
+      if (s * p.per < p.rows) {
+        const int64_t end = (s + 1) * p.per < p.rows ? (s + 1) * p.per : p.rows, w0 = s * p.per / p.run, w1 = (end - 1) / p.run;
+        shared = w0 != w1;                                // (else its worker wrote it)
+        const bool head = w0 * p.run / p.per == s;        // the first worker's first row is the gate row's too
+        if (shared && col < p.dim)
+#pragma unroll 8
+          for (int64_t w = w0 + sub; w <= w1; w += a.each) {
+            const bool tail = w == w0 && !head;
+            x += p.part[((int64_t)(tail ? kTail1 : kHead1) * p.workers + w) * p.dim + col];
+            if (a.layer) y += p.part[((int64_t)(tail ? kTail0 : kHead0) * p.workers + w) * p.dim + col];
+          }
+      }
+      __syncthreads();
+      sh[0][slice][lane] = x, sh[1][slice][lane] = y;
+      __syncthreads();
+      if (sub == 0 && shared && col < p.dim) {
+        x = y = 0.f;
+        for (int i = 0; i < a.each; ++i) x += sh[0][slice + i][lane], y += sh[1][slice + i][lane];
         float* g = p.dgate + s * p.dim + col;
-        const float v = fmaf(w, r.x, b * r.y);
+        const float v = fmaf(p.aw ? p.aw[col] : 1.f, x, (p.ab ? p.ab[col] : 0.f) * y);
         *g = p.accumulate ? *g + v : v;
       }
     }
@@ -807,35 +837,25 @@ asi_status_t check_desc(const asi_branch_desc_t* d, Drop* drop) {
   return ASI_OK;
 }
 
-// threads of a row, and rows of a CTA
-struct Shape {
-  int tpr, rows;
-};
-Shape shape_of(int64_t dim) {
-  const int tpr = (int)align_up((size_t)ceil_div(dim, kEach), 32);
-  return {tpr, std::max(1, std::min(8, 256 / tpr))};
-}
-// Rows of a worker and workers: `ctas` CTAs of up to 256 threads an SM, or one larger one
+// A CTA a row at a time: its threads
+int threads_of(int64_t dim) { return (int)align_up((size_t)ceil_div(dim, kEach), 32); }
+// Rows of a worker (a CTA) and workers: as many as registers leave room for, `threads` an SM
 struct Work {
   int64_t run;
   int workers;
 };
-constexpr int kForwardCtas = 3, kBackwardCtas = 2;
-int64_t most_workers(int64_t dim, int ctas) {
-  const Shape s = shape_of(dim);
-  return (int64_t)148 * (s.tpr * s.rows <= 256 ? ctas : 1) * s.rows;
-}
-Work work_of(int64_t rows, int64_t dim, int ctas) {
-  const int64_t run = std::max<int64_t>(1, ceil_div(rows, most_workers(dim, ctas)));
+constexpr int kForwardThreads = 768, kBackwardThreads = 512;
+int ctas_of_sm(int64_t dim, int threads) { return std::min(24, std::max(1, threads / threads_of(dim))); }
+Work work_of(int64_t rows, int64_t dim, int threads) {
+  const int64_t run = std::max<int64_t>(1, ceil_div(rows, 148 * ctas_of_sm(dim, threads)));
   return {run, (int)std::max<int64_t>(1, ceil_div(rows, run))};
 }
 size_t part_bytes(int64_t rows, int64_t dim) {
-  return align_up((size_t)kParts * std::max<int64_t>(1, std::min(rows, most_workers(dim, kBackwardCtas))) * dim * 4, 256);
+  return align_up((size_t)kParts * std::max<int64_t>(1, std::min<int64_t>(rows, 148 * ctas_of_sm(dim, kBackwardThreads))) * dim * 4, 256);
 }
-// shared memory of the rows on their way: as many stages as `room` bytes hold
-size_t stages_of(BranchArgs* a, bool vec, int tensors, int pieces, size_t room) {
-  const Shape s = shape_of(a->dim);
-  const size_t each = (size_t)tensors * pieces * 16 * s.tpr * s.rows;
+// shared memory of the rows on their way: as many stages as a CTA's share of 200 KB holds
+size_t stages_of(BranchArgs* a, bool vec, int tensors, int pieces, int threads) {
+  const size_t each = (size_t)tensors * pieces * 16 * threads_of(a->dim), room = (200 << 10) / ctas_of_sm(a->dim, threads);
   a->stages = vec ? (int)std::max<size_t>(1, std::min<size_t>(kMaxStages, room / each)) : 0;
   return a->stages * each;
 }
@@ -862,41 +882,57 @@ cudaError_t launch_ring(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem
 
 template <typename TI, typename TR, bool kVec, int kMax>
 cudaError_t launch_forward_as(BranchArgs& a, bool layer, cudaStream_t st) {
-  const Shape s = shape_of(a.dim);
-  const Work k = work_of(a.rows, a.dim, kForwardCtas);
+  const Work k = work_of(a.rows, a.dim, kForwardThreads);
   a.run = k.run;
   a.workers = k.workers;
-  const size_t smem = stages_of(&a, kVec, 2, sizeof(TR) == 4 ? 2 : 1, (kMax == 256 ? 200 / kForwardCtas : 200) << 10);
-  const dim3 grid((unsigned)ceil_div(k.workers, s.rows)), block(s.tpr, s.rows);
+  const size_t smem = stages_of(&a, kVec, 2, sizeof(TR) == 4 ? 2 : 1, kForwardThreads);
+  const dim3 grid((unsigned)k.workers), block(threads_of(a.dim));
   return layer ? launch_ring(k_branch_forward<TI, TR, kVec, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_forward<TI, TR, kVec, false, kMax>, grid, block, smem, st, a);
 }
 template <typename TI, typename TR, bool kVec>
 cudaError_t launch_forward(BranchArgs& a, bool layer, cudaStream_t st) {
-  const int tpr = shape_of(a.dim).tpr;
+  const int tpr = threads_of(a.dim);
   if (tpr <= 256) return launch_forward_as<TI, TR, kVec, 256>(a, layer, st);
   return tpr <= 512 ? launch_forward_as<TI, TR, kVec, 512>(a, layer, st) : launch_forward_as<TI, TR, kVec, 1024>(a, layer, st);
 }
 
 template <typename TI, typename TR, bool kVec, int kMax>
 cudaError_t launch_backward_as(BranchArgs& a, bool layer, cudaStream_t st) {
-  const Shape s = shape_of(a.dim);
-  const Work k = work_of(a.rows, a.dim, kBackwardCtas);
+  const Work k = work_of(a.rows, a.dim, kBackwardThreads);
   a.run = k.run;
   a.workers = k.workers;
   const bool groups = a.gate && a.per < a.rows;
-  const size_t smem = stages_of(&a, kVec, 4, sizeof(TR) == 4 ? 2 : 1, (kMax == 256 ? 200 / kBackwardCtas : 200) << 10);
-  const dim3 grid((unsigned)ceil_div(k.workers, s.rows)), block(s.tpr, s.rows);
+  const size_t smem = stages_of(&a, kVec, 4, sizeof(TR) == 4 ? 2 : 1, kBackwardThreads);
+  const dim3 grid((unsigned)k.workers), block(threads_of(a.dim));
   cudaError_t e;
   if (layer) e = groups ? launch_ring(k_branch_backward<TI, TR, kVec, true, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_backward<TI, TR, kVec, true, false, kMax>, grid, block, smem, st, a);
   else e = groups ? launch_ring(k_branch_backward<TI, TR, kVec, false, true, kMax>, grid, block, smem, st, a) : launch_ring(k_branch_backward<TI, TR, kVec, false, false, kMax>, grid, block, smem, st, a);
   if (e != cudaSuccess || !a.part) return e;
-  const SumsArgs q = {a, layer, groups};
-  const int64_t shared = groups && a.dgate && a.per > 1 ? std::min<int64_t>(ceil_div(a.rows, a.per), 1024) : 0;
-  return launch_pdl(k_branch_sums, dim3((unsigned)ceil_div(a.dim, 32), (unsigned)(2 + shared)), dim3(32 * kSlices), 0, st, q);
+  SumsArgs q = {a, layer, groups, 1};
+  while (q.each < kSlices && q.each * 8 * a.run < a.per) q.each *= 2;      // (about eight workers a warp)
+  const int64_t shared = groups && a.dgate && a.per > 1 ? std::min<int64_t>(ceil_div(ceil_div(a.rows, a.per), kSumCtas * kSlices / q.each), 1024) : 0;
+  // CTAs of a cluster: as many as stay well within a wave (4096 x 2048, 293 workers: 29.0 us for the whole gradient with four, 32.7 with eight;
+  // 6304 x 768, 701 workers: 36.6 and 33.7)
+  const int64_t columns = ceil_div(a.dim, 32);
+  int ctas = kSumCtas;
+  while (ctas > 1 && columns * (2 + shared) * ctas > 800) ctas /= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)columns, (unsigned)(2 + shared), (unsigned)ctas);
+  cfg.blockDim = dim3(32 * kSlices);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = (unsigned)ctas;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, k_branch_sums, q);
 }
 template <typename TI, typename TR, bool kVec>
 cudaError_t launch_backward(BranchArgs& a, bool layer, cudaStream_t st) {
-  const int tpr = shape_of(a.dim).tpr;
+  const int tpr = threads_of(a.dim);
   if (tpr <= 256) return launch_backward_as<TI, TR, kVec, 256>(a, layer, st);
   return tpr <= 512 ? launch_backward_as<TI, TR, kVec, 512>(a, layer, st) : launch_backward_as<TI, TR, kVec, 1024>(a, layer, st);
 }
