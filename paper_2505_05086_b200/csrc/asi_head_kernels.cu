@@ -37,7 +37,7 @@ constexpr int kK = 64;                                    // k of a box: 64 bf16
 constexpr int kMaxStages = 3;
 constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's box
 constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
-constexpr int kSeg = 16;                                  // pairs of boxes that add up in TMEM where results are held to fp32
+constexpr int kSeg = 16, kWhole = 12;                                   // pairs of boxes that add up in TMEM at most where results are held to fp32, and that need no segments
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -942,7 +942,11 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   for (int q = 0; q < g.np; ++q) {
     HeadProb& p = g.p[q];
     parts = std::max(parts, (p.a_terms + p.b_terms) * p.sub);
-    p.seg = segmented ? std::max(1, kSeg / p.pairs) : 1 << 30;
+    p.seg = 1 << 30;
+    if (segmented && p.per * p.pairs > kWhole) {
+      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, kSeg));
+      p.seg = (int)ceil_div(p.per, n);
+    }
   }
   g.stage = parts * kHalf;
   g.nst = (192 << 10) / g.stage;
@@ -1038,7 +1042,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
     }
     // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, with segments 0.8e-6; 359 and 378 us)
-    e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kSeg, st);
+    e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
     if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
     RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c};
     e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
@@ -1076,7 +1080,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       const KeptArgs k = {g, reinterpret_cast<const float*>(ws + l.kept) + v0, static_cast<__nv_bfloat16*>(G), nt * kTile, l.cols, n};
       e = launch_pdl(k_head_kept, dim3((unsigned)ceil_div(n, 1024), (unsigned)T), dim3(256), 0, st, k);
     } else {
-      e = launch_gemm<kGrad>(g, fine, st);
+      e = launch_gemm<kGrad>(g, fine && logits.kc * logits.pairs > kWhole, st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
     // (the first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
@@ -1117,7 +1121,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     if (c.dw) g.p[g.np++] = pw;
     for (int q = 0; q < g.np; ++q) set_store(&g.p[q], g.p[q].M, D);
     // sums that leave TMEM on the way, where results are held to fp32 and long enough for it to show
-    const bool long_dw = c.dw && dw_kind == kF32 && pw.kc * pw.pairs > kSeg, long_dx = c.dx && fine && px.per * px.pairs > kSeg;
+    const bool long_dw = c.dw && dw_kind == kF32 && pw.kc * pw.pairs > kWhole, long_dx = c.dx && fine && px.per * px.pairs > kWhole;
     e = launch_gemm<kOut>(g, long_dw || long_dx, st);
     if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
   }
