@@ -474,7 +474,8 @@ asi_status_t asi_head_logprobs(const asi_head_desc_t* desc, const void* x, const
 /*   lse, entropy [in] as asi_head_logprobs wrote them (entropy may be null where dentropy is)
  *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
  *   dx [out] device in_dtype [rows][dim];  dw [in/out] device dw_dtype [vocab][dim], written over, or added to what is there (accumulate
- *      != 0).  One of them may be null */
+ *      != 0; subnormal sums may count as 0 there).  One of them may be null.  bf16 rows of a dim that is a multiple of 8 start on 16 bytes in x
+ *      and w */
 asi_status_t asi_head_grad(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy, void* dx, void* dw, int32_t accumulate,
                            void* ws, size_t ws_bytes, void* stream);

@@ -6,9 +6,12 @@
 //
 // Four matrix products, all by k_head_gemm: the logits' tiles leave nothing but a maximum and two sums a row (and the target's logit)
 // behind, k_head_rows joins these, and then for a piece of the vocabulary at a time the logits are computed again, this time
-// leaving G (in the workspace), from which one launch makes the piece's share of dx and its rows of dw.
+// leaving G (in the workspace), from which one launch makes the piece's share of dx and its rows of dw.  Few rows keep their logits (in
+// fp32, in the workspace) where these take no more than a piece of G would.
 //
-// What bounds it: the tensor cores, 2 T V D operations a product (for a few rows the bytes of w, read twice, and of dw).
+// What bounds it: the tensor cores, 2 T V D operations a product (for a few rows the bytes of w, read twice, and of dw).  4096 x 32000 x 2048
+// bf16 in bursts: logits and their sums 334 us (1608 TFLOP/s), G of 16128 columns 184 (1470), both products of G 373 (1450); in long loops the
+// power cap takes 15 % of that.
 //
 // Operands are bf16.  fp32 ones are split into three terms each (hi, mid, lo: 24 bits) by k_head_split, and a product takes the
 // six pairs of terms down to 2^-16 of the first (what is left out is 2^-24).  G is split likewise where its product goes to
@@ -37,7 +40,7 @@ constexpr int kK = 64;                                    // k of a box: 64 bf16
 constexpr int kMaxStages = 3;
 constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's box
 constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
-constexpr int kSeg = 16, kWhole = 12;                                   // pairs of boxes that add up in TMEM at most where results are held to fp32, and that need no segments
+constexpr int kSeg = 16, kWhole = 12;                     // pairs of boxes that add up in TMEM at most where results are held to fp32; as many need no segments
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -237,9 +240,9 @@ __device__ __forceinline__ void put_words(const float* s, int lane, TO* to, cons
 // A pair of CTAs owns a tile of 256 x 256: each brings half of either operand's chunk (128 rows) to its shared memory, products are
 // issued for both by the first one (tcgen05, cta_group 2: each tensor core reads its own half of A and both halves of B), and each
 // has the 128 x 256 accumulators of its rows in its TMEM, twice, so that the next tile's products run under this one's epilogue.
-// (A CTA by itself would read twice the bytes of B for the same products.)  Roles: a producer thread, an issuer thread,
-// eight epilogue warps (a thread a row and half of the columns).
-// kSegmented: results held to fp32.  The unit's own sums truncate, so they go to registers after every kSeg chunks.
+// (A CTA by itself would read twice the bytes of B for the same products.)  Roles: a producer warp, an issuer warp, eight epilogue warps (a
+// thread a row and half of the columns).
+// kSegmented: results held to fp32.  The unit's own sums truncate, so they go to registers on the way (HeadProb::seg).
 template <int kEpi, bool kSegmented>
 __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant__ HeadArgs g) {
   extern __shared__ __align__(1024) uint8_t head_smem[];
@@ -716,8 +719,8 @@ struct KeptArgs {
 __global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptArgs p) {
   pdl_wait();
   pdl_launch_dependents();
-  const int row = blockIdx.y;
-  const int64_t j0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const int row = blockIdx.x;
+  const int64_t j0 = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
   if (j0 >= p.n) return;
   const RowGrad r = row_grad(p.h, row);
   const float4 in = *reinterpret_cast<const float4*>(p.x + row * p.ld_x + j0);
@@ -738,7 +741,7 @@ struct SplitArgs {
   int64_t rows, D, ld;
   int terms;
 };
-// (eight neighbours a thread: 30011 x 771 fp32 @SPLIT@ us, a value a thread 94)
+// (eight neighbours a thread: 30011 x 771 fp32 41 us, a value a thread 94)
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_split(const __grid_constant__ SplitArgs p) {
   pdl_wait();
@@ -781,7 +784,7 @@ __global__ void __launch_bounds__(256) k_head_join(const __grid_constant__ JoinA
   pdl_launch_dependents();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.n; i += (int64_t)gridDim.x * 256) {
     float s = 0.f;
-#pragma unroll 4
+#pragma unroll 16
     for (int e = 0; e < p.splits; ++e) s += p.in[e * p.n + i];
     if (p.off) {
       const int64_t t = i / p.D, y = p.y[t];
@@ -824,7 +827,7 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   l.in_terms = d->in_dtype == ASI_F32 ? 3 : 1;
   l.g_terms = d->dw_dtype == ASI_F32 ? 3 : 1;            // (dx of fp32 operands comes with dw in fp32)
   l.split = d->in_dtype == ASI_F32 || d->dim % 8 != 0;
-  l.ld = (d->dim + 63) / 64 * 64;                        // (rows on 128 bytes: on 16 alone a row of a copy meets two lines, and 771 fp32 columns took @LD@)
+  l.ld = (d->dim + 63) / 64 * 64;                        // (rows on 128 bytes: on 16 alone a row of a copy meets two lines, and 1001 x 30011 x 771 fp32 took 794 us instead of 768)
   size_t at = 256;                                       // status word
   auto take = [&](size_t bytes) {
     const size_t a = at;
@@ -851,7 +854,8 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   }
   l.least = l.bytes = at;
   // Logits of few rows take no more than a piece of G may: where the workspace has room for them they stay, in fp32, and the third of the
-  // four products is spared (the same bits).  9 x 50257 x 768: @K1@; 1001 x 30011 x 771 fp32: @K2@
+  // four products is spared (the same bits).  9 x 50257 x 768 bf16: 136 us instead of 168; 1001 x 30011 x 771 fp32: 768
+  // instead of 939.
   if (grad && T && !d->vocab_chunk && all * T * 4 <= kPieceBytes) {
     l.kept = take((size_t)(all * T * 4));
     l.bytes = at;
@@ -936,8 +940,8 @@ void share_tiles(HeadArgs* g, int pairs) {
 template <int kEpi>
 cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   // Stages of what the larger chunk takes (64 KB for one term of either operand, 96 for three), as many as 192 KB hold, beside a place for
-  // each warp's results on their way out.  What bounds the issuer is not the bytes: a stage of 64 k took it 560 cycles for 512 of products
-  // (waiting 120, four products 270, commit 170), and five stages were no faster than three.
+  // each warp's results on their way out.  Chunks of 128 k and not 64 for the issuer's sake: one of 64 took it 560 cycles (waiting 120, four products
+  // 270, commit 170) for 512 of products.
   int parts = 0;
   for (int q = 0; q < g.np; ++q) {
     HeadProb& p = g.p[q];
@@ -1041,7 +1045,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       set_store(&g.p[0], T, nt * kTile);
       if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
     }
-    // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, with segments 0.8e-6; 359 and 378 us)
+    // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, in two segments 0.8e-6; 345 us either way)
     e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
     if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
     RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c};
@@ -1078,7 +1082,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     if (keep) {
       const int64_t n = ceil_div(nv, kTile) * kTile;
       const KeptArgs k = {g, reinterpret_cast<const float*>(ws + l.kept) + v0, static_cast<__nv_bfloat16*>(G), nt * kTile, l.cols, n};
-      e = launch_pdl(k_head_kept, dim3((unsigned)ceil_div(n, 1024), (unsigned)T), dim3(256), 0, st, k);
+      e = launch_pdl(k_head_kept, dim3((unsigned)T, (unsigned)ceil_div(n, 1024)), dim3(256), 0, st, k);
     } else {
       e = launch_gemm<kGrad>(g, fine && logits.kc * logits.pairs > kWhole, st);
     }

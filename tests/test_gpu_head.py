@@ -254,3 +254,25 @@ def test_an_ordinary_size_with_many_pieces():
     w.check(got)
     f = World(1000, 9000, 1032, bf16=False, bf16_dw=False, ent=True, vocab_chunk=4000)
     f.check(f.loss())
+
+
+def test_many_rows_of_few_columns():
+    """More rows than a grid's second dimension has places, their logits kept."""
+    w = World(70000, 3, 8, bf16_dw=False)
+    w.check(w.loss())
+    w.op.forward(w.x, w.w, w.y)
+    assert ((w.op.lse - head(w.x, w.w, w.y, 1.0, -100)["lse"]).abs() <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("bf16,bf16_dw", [(True, True), (True, False), (False, False)])
+def test_gradients_off_16_bytes(bf16, bf16_dw):
+    for chunk in (0, 512):
+        w = World(70, 1100, 72, bf16, bf16_dw, vocab_chunk=chunk)
+        start = torch.randn(1100, 72, device="cuda").mul_(1 / 70).to(DT[bf16_dw])
+        want = w.loss(accumulate=True, start=start)
+        gx = torch.zeros(70 * 72 + 1, device="cuda", dtype=DT[bf16])
+        gw = torch.zeros(1100 * 72 + 3, device="cuda", dtype=DT[bf16_dw])
+        gw[3:].view(1100, 72).copy_(start)
+        w.op.loss(w.x, w.w, w.y, w.dlogp, None, gx[1:].view(70, 72), gw[3:].view(1100, 72), accumulate=True)
+        assert torch.equal(gx[1:].view(70, 72), want["dx"]) and torch.equal(gw[3:].view(1100, 72), want["dw"])
+        assert gx[0] == 0 and (gw[:3] == 0).all()
