@@ -201,44 +201,45 @@ struct BranchArgs {
 // partial sums of a worker: over the first of its gate's rows, over the last one, over all
 enum Part { kHead1 = 0, kTail1 = 1, kNext1 = 2, kAfter1 = 3, kHead0 = 4, kTail0 = 5, kNext0 = 6, kAfter0 = 7, kParts = 8 };
 
-// Sums of a value or two over the threads of a CTA, for all of them (a multiple of 32, kMax at most)
+// Sums of up to three values over the threads of a CTA, for all of them (a multiple of 32, kMax at most)
 template <int kMax>
 struct RowSum {
-  static constexpr int kWarps = kMax / 32;
-  float* sh;               // [2][2 kWarps], 0 where no warp writes
+  static constexpr int kWarps = kMax / 32, kMost = 3;
+  float* sh;               // [2][kMost][kWarps], 0 where no warp writes
   uint32_t phase = 0;
   __device__ __forceinline__ RowSum(float* s) : sh(s) {
-    for (int i = threadIdx.x; i < 4 * kWarps; i += blockDim.x) s[i] = 0.f;
+    for (int i = threadIdx.x; i < 2 * kMost * kWarps; i += blockDim.x) s[i] = 0.f;
     __syncthreads();
   }
-  template <bool kTwo>
-  __device__ __forceinline__ float2 get(float a, float b) {
+  template <int kN>
+  __device__ __forceinline__ void get(float (&v)[kN]) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      a += __shfl_xor_sync(~0u, a, o);
-      if (kTwo) b += __shfl_xor_sync(~0u, b, o);
-    }
-    if (blockDim.x == 32) return make_float2(a, b);
+    for (int o = 16; o; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] += __shfl_xor_sync(~0u, v[i], o);
+    if (blockDim.x == 32) return;
     float* s = sh + phase;
-    phase ^= 2 * kWarps;
-    if ((threadIdx.x & 31) == 0) {
-      s[threadIdx.x >> 5] = a;
-      if (kTwo) s[kWarps + (threadIdx.x >> 5)] = b;
-    }
-    __syncthreads();
-    float x[2] = {0.f, 0.f}, y[2] = {0.f, 0.f};
+    phase ^= kMost * kWarps;
+    if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int i = 0; i < kWarps; i += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(s + i);
-      const float v0[2] = {v.x, v.y}, v1[2] = {v.z, v.w};
-      add2(x, x, v0), add2(x, x, v1);
-      if (kTwo) {
-        const float4 u = *reinterpret_cast<const float4*>(s + kWarps + i);
-        const float u0[2] = {u.x, u.y}, u1[2] = {u.z, u.w};
-        add2(y, y, u0), add2(y, y, u1);
+      for (int i = 0; i < kN; ++i) s[i * kWarps + (threadIdx.x >> 5)] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      float x[2] = {0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < kWarps; k += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(s + i * kWarps + k);
+        const float lo[2] = {q.x, q.y}, hi[2] = {q.z, q.w};
+        add2(x, x, lo), add2(x, x, hi);
       }
+      v[i] = x[0] + x[1];
     }
-    return make_float2(x[0] + x[1], y[0] + y[1]);
+  }
+  __device__ __forceinline__ float one(float a) {
+    float v[1] = {a};
+    get(v);
+    return v[0];
   }
 };
 
@@ -285,23 +286,30 @@ struct Columns {
       for (int i = 0; i < kEach; ++i) f[i] = there(i) ? __ldg(p + at(i)) : 0.f;
     }
   }
-  // f to drop(f) in row t
-  __device__ __forceinline__ void mask(const Drop& d, uint32_t step_no, int64_t t, float (&f)[kEach]) const {
+  // which of this thread's values of row t stay, a bit each
+  __device__ __forceinline__ uint32_t kept_bits(const Drop& d, uint32_t step_no, int64_t t) const {
     const uint64_t e = (uint64_t)t * dim + first;
+    uint32_t bits = 0;
     if constexpr (kVec) {
       const Words w = words_of(d, step_no, e >> 3);         // (dim is a multiple of eight)
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) f[i] = kept(d, w, i) ? f[i] * d.more : 0.f;
+      for (int i = 0; i < kEach; ++i) bits |= kept(d, w, i) ? 1u << i : 0u;
     } else {
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
-        if (at(i) < dim) f[i] = kept_alone(d, step_no, e + (uint64_t)i * step) ? f[i] * d.more : 0.f;
+        if (at(i) < dim) bits |= kept_alone(d, step_no, e + (uint64_t)i * step) ? 1u << i : 0u;
     }
+    return bits;
+  }
+  static __device__ __forceinline__ void drop(const Drop& d, uint32_t bits, Eight& f) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] = bits >> i & 1 ? f[i] * d.more : 0.f;
   }
 };
 
 // Rows on their way: a thread copies its eight values of the next rows to shared memory by itself and reads them there itself, so
-// that nobody waits for anybody (rows on 16 bytes alone).  A stage is a row: kTensors slots of kPieces times 16 bytes a thread.
+// that nobody waits for anybody (rows on 16 bytes alone).  A stage is a row: kTensors slots of kPieces times 16 bytes a thread, 0 where
+// nothing is fetched (columns beyond the row's end, tensors that a call has not).
 constexpr int kMaxStages = 4;
 template <int kTensors, int kPieces>
 struct Ring {
@@ -312,6 +320,10 @@ struct Ring {
     piece = blockDim.x * 16;
     stage_bytes = kTensors * kPieces * piece;
     stages = left = n;
+  }
+  __device__ __forceinline__ void clear() const {
+    for (int i = 0; i < stages * kTensors * kPieces; ++i)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(mine + i * piece), "r"(0) : "memory");
   }
   template <int kTensor, typename T>
   __device__ __forceinline__ void fetch(uint32_t to, const T* p) const {
@@ -358,7 +370,7 @@ template <bool kLayer, bool kVec, int kMax>
 __device__ __forceinline__ float2 normalise(Eight& f, const Columns<kVec>& c, const BranchArgs& p, RowSum<kMax>& sum) {
   float m = 0.f;
   if constexpr (kLayer) {
-    m = sum.template get<false>(sum8(f), 0.f).x * p.inv_dim;   // (0 where there is no column)
+    m = sum.one(sum8(f)) * p.inv_dim;   // (0 where there is no column)
     add8(f, f, -m);
     if (!kVec) {
 #pragma unroll
@@ -367,7 +379,7 @@ __device__ __forceinline__ float2 normalise(Eight& f, const Columns<kVec>& c, co
   }
   float q = dot8(f, f);
   if (kLayer && kVec) q = c.there(0) ? q : 0.f;
-  const float r = rsqrtf(fmaf(sum.template get<false>(q, 0.f).x, p.inv_dim, p.eps));   // (off by 2^-22 at most)
+  const float r = rsqrtf(fmaf(sum.one(q), p.inv_dim, p.eps));   // (off by 2^-22 at most)
   mul8(f, f, r);
   return make_float2(m, r);
 }
@@ -407,7 +419,7 @@ __device__ __forceinline__ void branch_factor(float (&w)[kEach], const float* a,
 template <typename TI, typename TR, bool kVec, bool kLayer, int kMax>
 __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const __grid_constant__ BranchArgs p) {
   extern __shared__ __align__(16) uint8_t ring_smem[];
-  __shared__ __align__(16) float sh[kMax / 8];
+  __shared__ __align__(16) float sh[6 * kMax / 32];
   constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
@@ -431,8 +443,10 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
     ahead += p.dim;
     ring.commit();
   };
-  if (kVec)
+  if (kVec) {
+    if (!mine || !res) ring.clear();
     for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
+  }
   int64_t next_group = groups ? t0 : INT64_MAX;            // row from which on another of the gate's rows holds
   const float* gate = p.gate;
   float w[kEach], b[kEach];
@@ -447,13 +461,9 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
     const int64_t t = t0 + k;
     float f[kEach], h[kEach], x[kEach];
     if constexpr (kVec) {
-      clear8(f);
-      clear8(h);
       ring.wait();
-      if (mine) {
-        ring.template take<0>(y, f);
-        if (res) ring.template take<1>(h_in, h);
-      }
+      ring.template take<0>(y, f);
+      ring.template take<1>(h_in, h);
       fetch(ring.at);
       ring.advance();
     } else {
@@ -476,7 +486,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
     }
     if (kLayer) fma8(f, f, w, b);
     else mul8(f, f, w);
-    if (p.drop.below) c.mask(p.drop, step, t, f);
+    if (p.drop.below) c.drop(p.drop, c.kept_bits(p.drop, step, t), f);
     fma8(f, h, p.rs, f);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -523,7 +533,7 @@ __device__ __forceinline__ void put_gate(const BranchArgs& p, const Columns<kVec
 template <typename TI, typename TR, bool kVec, bool kLayer, bool kGroups, int kMax>
 __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(const __grid_constant__ BranchArgs p) {
   extern __shared__ __align__(16) uint8_t ring_smem[];
-  __shared__ __align__(16) float sh[kMax / 8];
+  __shared__ __align__(16) float sh[6 * kMax / 32];
   constexpr bool kHeld = kMax <= 512;
   pdl_wait();
   pdl_launch_dependents();
@@ -551,19 +561,23 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
     ahead += p.dim;
     ring.commit();
   };
-  if (kVec)
+  if (kVec) {
+    if (!mine || !next || !more) ring.clear();
     for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
+  }
   float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {};
   bool again = false;                                      // (kGroups) the sums over all of the gate's rows have been begun
   const int64_t first = kGroups ? t0 / p.per : 0;
   int64_t group = first, next_group = kGroups ? (first + 1) * p.per : INT64_MAX;
   const float* gate = p.gate ? p.gate + (kGroups && t0 < p.rows ? group * p.dim : 0) : nullptr;
-  float w[kEach];                                          // gate w_a
-  if (kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
+  float w[kEach];                                          // b gate w_a
+  if (kHeld) branch_factor(w, p.aw, 1.f, p.bs, gate, c);
   const Param<kVec, kHeld> nw(p.nw, 1.f, c);
   auto part = [&](int which) { return p.part + ((int64_t)which * p.workers + worker) * p.dim; };
   // the sums over the worker's rows of one of the gate's
   auto flush = [&](bool whole) {
+    mul8(s1, s1, p.bs);
+    if (kLayer) mul8(s0, s0, p.bs);
     float g[kEach];
     c.param(gate, g, 1.f, on16(gate));
     if (p.dgate) {
@@ -597,74 +611,84 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
 #pragma unroll 1
   for (int k = 0; k < rows; ++k, at += p.dim) {
     const int64_t t = t0 + k;
-    float d[kEach], f[kEach], x[kEach];
+    float d[kEach], f[kEach];
     const float* s = p.stats + 4 * t;
     const float4 st = on16(s) ? *reinterpret_cast<const float4*>(s) : make_float4(s[0], s[1], s[2], s[3]);
+    const uint32_t bits = p.drop.below ? c.kept_bits(p.drop, step, t) : 0u;
+    float x[kEach], y_[kEach];
     if constexpr (kVec) {
       ring.wait();
-      clear8(d);
-      if (mine && more) ring.template take<2>(dh_out, d);
-    } else {
-      c.load(dh_out + at, d, more);
-    }
-    if (next) {
-      if constexpr (kVec) {
-        clear8(x);
-        clear8(f);
-        if (mine) {
-          ring.template take<0>(dx, x);
-          ring.template take<1>(h_out, f);
-        }
-      } else {
-        c.load(dx + at, x);
-        c.load(h_out + at, f);
-      }
-      float v[kEach];
-      nw.get(v, c);
-      if (kLayer) fma8(f, f, st.w, -st.z * st.w);
-      else mul8(f, f, st.w);
-      fma8(n1, x, f, n1);                                  // (x is 0 where there is no column, and so are its products)
-      if (kLayer) add8(n0, n0, x);
-      mul8(x, x, v);
-      const float2 m = sum.template get<kLayer>(dot8(x, f), kLayer ? sum8(x) : 0.f);
-      // d + s (x - m0 - f m1)
-      fma8(x, f, -m.x * p.inv_dim, x);
-      if (kLayer) add8(x, x, -m.y * p.inv_dim);
-      fma8(d, x, st.w, d);
-    }
-    if (p.dh) {
-      mul8(x, d, p.rs);
-      c.store(static_cast<TR*>(p.dh) + at, x);
-    }
-    mul8(d, d, p.bs);
-    if (p.drop.below) c.mask(p.drop, step, t, d);
-    if constexpr (kVec) {
-      clear8(f);
-      if (mine) ring.template take<3>(y, f);
+      ring.template take<0>(dx, x);
+      ring.template take<1>(h_out, f);
+      ring.template take<2>(dh_out, d);
+      ring.template take<3>(y, y_);
       fetch(ring.at);
       ring.advance();
     } else {
-      c.load(y + at, f);
+      c.load(dh_out + at, d, more);
+      c.load(dx + at, x, next);
+      c.load(h_out + at, f, next);
+      c.load(y + at, y_);
     }
     if (kGroups && t >= next_group) {
       flush(group != first || first * p.per >= t0);
       group = t / p.per;
       next_group = (group + 1) * p.per;
       gate = p.gate + group * p.dim;
-      if (kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
+      if (kHeld) branch_factor(w, p.aw, 1.f, p.bs, gate, c);
     }
-    if (!kHeld) branch_factor(w, p.aw, 1.f, 1.f, gate, c);
-    if (p.norm_after) {
-      if (kLayer) fma8(f, f, st.y, -st.x * st.y);
-      else mul8(f, f, st.y);
+    if (!kHeld) branch_factor(w, p.aw, 1.f, p.bs, gate, c);
+    float v[kEach];
+    nw.get(v, c);
+    if (p.norm_after) {                                    // y^
+      if (kLayer) fma8(y_, y_, st.y, -st.x * st.y);
+      else mul8(y_, y_, st.y);
     }
-    fma8(s1, d, f, s1);
+    // (x and w are 0 where there is no column, and so are their products)
+    if (kLayer) fma8(f, f, st.w, -st.z * st.w);            // h^
+    else mul8(f, f, st.w);
+    fma8(n1, x, f, n1);
+    if (kLayer) add8(n0, n0, x);
+    mul8(x, x, v);                                         // a
+    float m1 = 0.f;                                        // mean(v y^)
+    if constexpr (!kLayer) {
+      // All sums of a row at once: with e = d' + s_n a and q = b keep gate w_a y^ the second mean is that of q e - s_n mean(a h^) q h^, so that a
+      // row meets one barrier instead of two (4096 x 2048 bf16: 28.5 us instead of 29.2)
+      float sums[3] = {dot8(x, f), 0.f, 0.f};
+      fma8(d, x, st.w, d);                                 // e
+      if (p.norm_after) {
+        mul8(x, y_, w);
+        if (p.drop.below) c.drop(p.drop, bits, x);
+        sums[1] = dot8(x, d), sums[2] = dot8(x, f);
+      }
+      sum.get(sums);
+      const float m = -sums[0] * p.inv_dim * st.w;
+      fma8(d, f, m, d);
+      m1 = fmaf(m, sums[2], sums[1]) * p.inv_dim;
+    } else if (next) {
+      float sums[2] = {dot8(x, f), sum8(x)};
+      sum.get(sums);
+      // d' + s (a - m0 - h^ m1)
+      fma8(x, f, -sums[0] * p.inv_dim, x);
+      add8(x, x, -sums[1] * p.inv_dim);
+      fma8(d, x, st.w, d);
+    }
+    if (p.dh) {
+      mul8(x, d, p.rs);
+      c.store(static_cast<TR*>(p.dh) + at, x);
+    }
+    if (p.drop.below) c.drop(p.drop, bits, d);             // u / b
+    fma8(s1, d, y_, s1);
     if (kLayer) add8(s0, s0, d);
-    mul8(d, d, w);                                         // (w is 0 where there is no column)
+    mul8(d, d, w);                                         // v
     if (p.norm_after) {
-      const float2 m = sum.template get<kLayer>(dot8(d, f), kLayer ? sum8(d) : 0.f);
-      fma8(d, f, -m.x * p.inv_dim, d);
-      if (kLayer) add8(d, d, -m.y * p.inv_dim);
+      if constexpr (kLayer) {
+        float sums[2] = {dot8(d, y_), sum8(d)};
+        sum.get(sums);
+        m1 = sums[0] * p.inv_dim;
+        add8(d, d, -sums[1] * p.inv_dim);
+      }
+      fma8(d, y_, -m1, d);
       mul8(d, d, st.y);
     }
     c.store(static_cast<TI*>(p.dy) + at, d);
@@ -676,6 +700,10 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   }
   if (!p.part) return;
   auto keep = [&](int which, const float (&v)[kEach]) { c.store(part(which), v); };
+  if (!kGroups) {
+    mul8(s1, s1, p.bs);
+    if (kLayer) mul8(s0, s0, p.bs);
+  }
   if (!kGroups && (p.dgate || p.daw)) keep(kHead1, s1);
   if (!kGroups && kLayer && (p.dgate || p.dab)) keep(kHead0, s0);
   if (p.dnw) keep(kNext1, n1);
