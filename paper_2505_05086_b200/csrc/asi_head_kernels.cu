@@ -917,15 +917,21 @@ cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k_head_gemm<kEpi, kSegmented>, g);
 }
 
+// cycles of a tile's results on their way out, as measured.  (With few tokens a tile of dw is hardly anything else: 5 x 25417 x 366 bf16 took
+// 146 us when tiles were shared out by their products alone, 91 so.  128 columns a row at a time, by words that start at sectors, took 117.)
+constexpr double kCopiesOut = 6e3, kWordsOut = 24e3;
+// Cycles that a tile keeps its pair busy: its products, or its results' way out where that takes longer (it runs under the next one's products)
+double tile_cost(const HeadProb& p, bool words) { return std::max(512.0 * p.per * p.pairs, words ? kWordsOut : kCopiesOut); }
+
 // Shares out the tiles of the second product so that all pairs end at about the same time: `few` pairs have had one tile more of the
 // first (each worth `ratio` of the second's).
 void share_tiles(HeadArgs* g, int pairs) {
   const int tiles1 = g->tiles - g->tiles0, base = g->tiles0 / pairs;
   g->few = g->tiles0 - base * pairs;
   const int rest = pairs - g->few;
-  const double ratio = (double)g->p[0].per * g->p[0].pairs / ((double)g->p[1].per * g->p[1].pairs);
+  const double ratio = tile_cost(g->p[0], g->p[0].how == kWords) / tile_cost(g->p[1], g->p[1].how == kWords);
   // each_few x few + (each_few + ratio) x rest = tiles1
-  double share = (tiles1 - ratio * rest) / pairs;
+  const double share = (tiles1 - ratio * rest) / pairs;
   int to_few = share > 0 ? (int)std::lround(share * g->few) : 0;
   if (g->few == 0) to_few = 0;
   to_few = std::min(to_few, tiles1);
@@ -1105,9 +1111,10 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     pw.add = c.accumulate ? pw.out : nullptr;
     pw.add_kind = c.accumulate ? dw_kind : kNone;
     if (i == 0) {
-      // few tiles of dx: shares of k, about half of what a pair has to do in all
-      const int64_t tx = (int64_t)px.mt * px.nt, tw = c.dw ? (int64_t)pw.mt * pw.nt : 0;
-      const int64_t load = (tx * px.kc * px.pairs + tw * pw.kc * pw.pairs) / 74, share = std::max<int64_t>(load / 2 / px.pairs, 8);
+      // few tiles of dx: shares of k, about half of what a pair has to do in all (eight chunks at least)
+      const double each = 512.0 * px.pairs, tw = c.dw ? (double)pw.mt * pw.nt * tile_cost(pw, D * size_of(d->dw_dtype) % 16 != 0) : 0.0;
+      const double load = ((double)px.mt * px.nt * px.kc * each + tw) / 74;
+      const int64_t share = std::max<int64_t>((int64_t)(load / 2 / each), 8);
       splits = (int)std::max<int64_t>(1, std::min({ceil_div(px.kc, share), l.acc_rows / T, (int64_t)64}));
     }
     px.per = (int)ceil_div(px.kc, splits);
