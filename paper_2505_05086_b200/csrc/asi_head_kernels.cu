@@ -221,7 +221,8 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int st
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// Column `lane` of staged results (32 x 32, column i of row r at i ^ r), up to 32 rows, added to another's and stored.  What is added is on its way for all rows at once.
+// Column `lane` of staged results (32 x 32, column i of row r at i ^ r), up to 32 rows, added to another's and stored.  What is added is on its
+// way for sixteen rows at once.
 template <typename TO, typename TA>
 __device__ __forceinline__ void put_words(const float* s, int lane, TO* to, const TA* add, int64_t ld, int rows) {
 #pragma unroll 1
