@@ -271,18 +271,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   pdl_launch_dependents();
 
   struct Tile { int q, m, n, s, chunks, k0; };
-  // The tiles of a pair: every `pairs`-th of the first product; of the second one a stretch, whose length makes up for what the
-  // first left uneven (pairs below `few` had one tile more)
+  // The tiles of a pair: every `pairs`-th of the first product, and of the second one every so many of a stretch for pairs that had as many
+  // of the first (pairs below `few` had one more; the stretches' lengths make up for that).  Pairs side by side work on tiles side by side, which
+  // share a row of G (a stretch a pair read 1.19 GB instead of 0.43 for 4096 x 16128 x 2048, in 371 us instead of 340)
   const int mine0 = (g.tiles0 - pair + pairs - 1) / pairs;
   const bool late = pair >= g.few;
   const int q1 = late ? pair - g.few : pair, each1 = late ? g.each_rest : g.each_few, more1 = late ? g.more_rest : g.more_few;
-  const int from1 = (late ? g.few * g.each_few + g.more_few : 0) + q1 * each1 + (q1 < more1 ? q1 : more1);
+  const int from1 = (late ? g.few * g.each_few + g.more_few : 0) + q1, step1 = late ? pairs - g.few : g.few;
   const int mine = mine0 + (g.np > 1 ? each1 + (q1 < more1 ? 1 : 0) : 0);
   auto tile_of = [&](int i) {
     Tile x;
     x.q = i >= mine0 ? 1 : 0;
     const HeadProb& p = g.p[x.q];
-    int t = x.q ? from1 + i - mine0 : pair + i * pairs;
+    int t = x.q ? from1 + (i - mine0) * step1 : pair + i * pairs;
     const int each = p.mt * p.nt;
     x.s = t / each;
     t -= x.s * each;
