@@ -51,7 +51,8 @@ __device__ __forceinline__ bool kept_alone(const Drop& d, uint32_t step, uint64_
   return (j & 1 ? x >> 16 : x & 0xffffu) >= d.below;
 }
 
-// eight neighbouring values, 16-byte aligned
+// eight neighbouring values, aligned to as many bytes as they have.  (32 bytes of fp32 in one piece: two of 16 would each touch every sector of
+// the warp's kilobyte and write half of it)
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[kEach]) {
   const uint4 w = *reinterpret_cast<const uint4*>(p);
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -59,8 +60,10 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[kEach])
   for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(u[i] << 16), f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
 }
 __device__ __forceinline__ void load8(const float* p, float (&f)[kEach]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7])
+               : "l"(p)
+               : "memory");
 }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t r;
@@ -71,8 +74,9 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&f)[kEach]
   *reinterpret_cast<uint4*>(p) = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
 __device__ __forceinline__ void store8(float* p, const float (&f)[kEach]) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]),
+               "f"(f[6]), "f"(f[7])
+               : "memory");
 }
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -307,8 +311,9 @@ struct Columns {
   }
 };
 
-// Rows on their way: a thread copies its eight values of the next rows to shared memory by itself and reads them there itself, so
-// that nobody waits for anybody (rows on 16 bytes alone).  A stage is a row: kTensors slots of kPieces times 16 bytes a thread, 0 where
+// Rows on their way: a warp copies its values of the next rows to shared memory and reads them there itself, so that no warp waits for
+// another (rows on 16 bytes, of fp32 on 32, alone).  A thread brings 16 bytes at a time, neighbours side by side: of fp32 half of its own
+// eight values or another's (its own two halves would read every sector twice, past L1: 6304 x 768 34.1 us instead of 33.4).  A stage is a row: kTensors slots of kPieces times 16 bytes a thread, 0 where
 // nothing is fetched (columns beyond the row's end, tensors that a call has not).
 constexpr int kMaxStages = 4;
 template <int kTensors, int kPieces>
@@ -325,11 +330,20 @@ struct Ring {
     for (int i = 0; i < stages * kTensors * kPieces; ++i)
       asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(mine + i * piece), "r"(0) : "memory");
   }
+  // the warp's part of a row into stage `to`; first: this thread's first column
   template <int kTensor, typename T>
-  __device__ __forceinline__ void fetch(uint32_t to, const T* p) const {
+  __device__ __forceinline__ void fetch(uint32_t to, const T* row, int first, int dim) const {
+    if constexpr (sizeof(T) == 2) {
+      if (first < dim) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + kTensor * kPieces * piece), "l"(row + first) : "memory");
+    } else {
+      const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (kTensor * kPieces + i) * piece), "l"(p + i * (16 / (int)sizeof(T))) : "memory");
+      for (int i = 0; i < 2; ++i) {
+        const int c = i * 32 + lane, col = first - lane * kEach + c * 4;
+        const uint32_t at_ = to + (uint32_t)(((c >> 1) - lane) * 16) + (kTensor * kPieces + (c & 1)) * piece;
+        if (col < dim) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at_), "l"(row + col) : "memory");
+      }
+    }
   }
   __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
   __device__ __forceinline__ void wait() const {            // the oldest row is there
@@ -337,6 +351,7 @@ struct Ring {
     else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
   }
   template <int kTensor, typename T>
   __device__ __forceinline__ void take(const T*, Eight& f) const {
@@ -364,6 +379,7 @@ __device__ __forceinline__ void clear8(float (&f)[kEach]) {
 }
 
 __device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+__device__ __forceinline__ bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 
 // Mean (layer norm) and reciprocal deviation of a row; f is what the norm makes of it on return (rubbish in columns that are not there).
 template <bool kLayer, bool kVec, int kMax>
@@ -394,14 +410,14 @@ struct Param {
   float none;
   float v[kHeld ? kEach : 1];
   __device__ __forceinline__ Param(const float* q, float n, const Columns<kVec>& c) : p(q), none(n) {
-    if constexpr (kHeld) c.param(q, v, n, on16(q));
+    if constexpr (kHeld) c.param(q, v, n, on32(q));
   }
   __device__ __forceinline__ void get(float (&f)[kEach], const Columns<kVec>& c) const {
     if constexpr (kHeld) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) f[i] = v[i];
     } else {
-      c.param(p, f, none, on16(p));
+      c.param(p, f, none, on32(p));
     }
   }
 };
@@ -409,9 +425,9 @@ struct Param {
 // The branch's factor and offset: drop(f W + B) with W = b gate w_a, B = b gate b_a in a row of the gate
 template <bool kVec>
 __device__ __forceinline__ void branch_factor(float (&w)[kEach], const float* a, float none, float scale, const float* gate, const Columns<kVec>& c) {
-  c.param(a, w, none, on16(a));
+  c.param(a, w, none, on32(a));
   float g[kEach];
-  c.param(gate, g, 1.f, on16(gate));
+  c.param(gate, g, 1.f, on32(gate));
 #pragma unroll
   for (int i = 0; i < kEach; ++i) w[i] *= scale * g[i];
 }
@@ -433,18 +449,19 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
   const TI* y = static_cast<const TI*>(p.y);
   const TR* h_in = static_cast<const TR*>(p.h);
   const int rows = t1 > t0 ? (int)(t1 - t0) : 0;           // (of this worker)
-  int64_t ahead = t0 * p.dim + c.first;                    // first element of the row to be fetched next
+  int64_t ahead = t0 * p.dim;                              // the row to be fetched next
   int fetched = 0;
   auto fetch = [&](uint32_t to) {
-    if (fetched++ < rows && mine) {
-      ring.template fetch<0>(to, y + ahead);
-      if (res) ring.template fetch<1>(to, h_in + ahead);
+    if (fetched++ < rows) {
+      ring.template fetch<0>(to, y + ahead, c.first, p.dim);
+      if (res) ring.template fetch<1>(to, h_in + ahead, c.first, p.dim);
     }
     ahead += p.dim;
     ring.commit();
   };
   if (kVec) {
     if (!mine || !res) ring.clear();
+    __syncwarp();
     for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
   }
   int64_t next_group = groups ? t0 : INT64_MAX;            // row from which on another of the gate's rows holds
@@ -464,6 +481,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
       ring.wait();
       ring.template take<0>(y, f);
       ring.template take<1>(h_in, h);
+      __syncwarp();
       fetch(ring.at);
       ring.advance();
     } else {
@@ -518,8 +536,8 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 3)) k_branch_forward(const
 template <bool kVec>
 __device__ __forceinline__ void put_gate(const BranchArgs& p, const Columns<kVec>& c, int64_t s, const float (&s1)[kEach], const float (&s0)[kEach]) {
   float w[kEach], b[kEach];
-  c.param(p.aw, w, 1.f, on16(p.aw));
-  c.param(p.ab, b, 0.f, on16(p.ab));
+  c.param(p.aw, w, 1.f, on32(p.aw));
+  c.param(p.ab, b, 0.f, on32(p.ab));
 #pragma unroll
   for (int i = 0; i < kEach; ++i)
     if (c.there(i)) {
@@ -547,22 +565,23 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   const TI *dx = static_cast<const TI*>(p.dx), *y = static_cast<const TI*>(p.y);
   const TR *h_out = static_cast<const TR*>(p.h_out), *dh_out = static_cast<const TR*>(p.dh_out);
   const int rows = t1 > t0 ? (int)(t1 - t0) : 0;           // (of this worker)
-  int64_t ahead = t0 * p.dim + c.first;                    // first element of the row to be fetched next
+  int64_t ahead = t0 * p.dim;                              // the row to be fetched next
   int fetched = 0;
   auto fetch = [&](uint32_t to) {
-    if (fetched++ < rows && mine) {
+    if (fetched++ < rows) {
       if (next) {
-        ring.template fetch<0>(to, dx + ahead);
-        ring.template fetch<1>(to, h_out + ahead);
+        ring.template fetch<0>(to, dx + ahead, c.first, p.dim);
+        ring.template fetch<1>(to, h_out + ahead, c.first, p.dim);
       }
-      if (more) ring.template fetch<2>(to, dh_out + ahead);
-      ring.template fetch<3>(to, y + ahead);
+      if (more) ring.template fetch<2>(to, dh_out + ahead, c.first, p.dim);
+      ring.template fetch<3>(to, y + ahead, c.first, p.dim);
     }
     ahead += p.dim;
     ring.commit();
   };
   if (kVec) {
     if (!mine || !next || !more) ring.clear();
+    __syncwarp();
     for (int i = 0; i < p.stages; ++i) fetch(ring.mine + i * ring.stage_bytes);
   }
   float s1[kEach] = {}, s0[kEach] = {}, n1[kEach] = {}, n0[kEach] = {};
@@ -573,13 +592,18 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   float w[kEach];                                          // b gate w_a
   if (kHeld) branch_factor(w, p.aw, 1.f, p.bs, gate, c);
   const Param<kVec, kHeld> nw(p.nw, 1.f, c);
+  auto stats_of = [&](int64_t t) {
+    const float* q = p.stats + 4 * t;
+    return on16(q) ? *reinterpret_cast<const float4*>(q) : make_float4(q[0], q[1], q[2], q[3]);
+  };
+  float4 ahead_st = stats_of(t0);                          // (t0 < rows: there are no more workers than rows)
   auto part = [&](int which) { return p.part + ((int64_t)which * p.workers + worker) * p.dim; };
   // the sums over the worker's rows of one of the gate's
   auto flush = [&](bool whole) {
     mul8(s1, s1, p.bs);
     if (kLayer) mul8(s0, s0, p.bs);
     float g[kEach];
-    c.param(gate, g, 1.f, on16(gate));
+    c.param(gate, g, 1.f, on32(gate));
     if (p.dgate) {
       if (whole) {
         put_gate(p, c, group, s1, s0);
@@ -612,8 +636,8 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   for (int k = 0; k < rows; ++k, at += p.dim) {
     const int64_t t = t0 + k;
     float d[kEach], f[kEach];
-    const float* s = p.stats + 4 * t;
-    const float4 st = on16(s) ? *reinterpret_cast<const float4*>(s) : make_float4(s[0], s[1], s[2], s[3]);
+    const float4 st = ahead_st;
+    if (k + 1 < rows) ahead_st = stats_of(t + 1);          // (waited for here it cost a fifth of a row's time)
     const uint32_t bits = p.drop.below ? c.kept_bits(p.drop, step, t) : 0u;
     float x[kEach], y_[kEach];
     if constexpr (kVec) {
@@ -622,6 +646,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
       ring.template take<1>(h_out, f);
       ring.template take<2>(dh_out, d);
       ring.template take<3>(y, y_);
+      __syncwarp();
       fetch(ring.at);
       ring.advance();
     } else {
@@ -982,7 +1007,7 @@ asi_status_t asi_dropout(const asi_dropout_t* drop, int32_t dtype, int64_t n, co
   if (!fine({{x, bytes, e}, {residual == x ? nullptr : residual, bytes, e}, {drop->step_dev, 8, 8}}, {{out, bytes, e, residual && out == residual ? residual : x}}))
     return ASI_ERR_INVALID_ARG;
   a.x = x, a.res = residual, a.out = out, a.n = n;
-  const bool vec = aligned(x, 16) && aligned(out, 16) && (!residual || aligned(residual, 16));
+  const bool vec = aligned(x, 8 * e) && aligned(out, 8 * e) && (!residual || aligned(residual, 8 * e));
   const dim3 grid((unsigned)ceil_div(ceil_div(n, kEach), kDropThreads)), block(kDropThreads);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t r;
@@ -991,7 +1016,7 @@ asi_status_t asi_dropout(const asi_dropout_t* drop, int32_t dtype, int64_t n, co
   return cuda_status(r, "dropout");
 }
 
-asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_t* t, void* stream) {
+asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_t* t, void* stream) try {
   Drop drop = {};
   const asi_status_t s = check_desc(desc, &drop);
   if (s != ASI_OK) return s;
@@ -1007,7 +1032,7 @@ asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_
     return ASI_ERR_INVALID_ARG;
   BranchArgs a = args_of(desc, t, drop);
   a.h = t->h, a.h_out = t->h_out, a.x = t->x;
-  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 16) && aligned(a.h, 16) && aligned(a.h_out, 16) && aligned(a.x, 16);
+  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 8 * ei) && aligned(a.h, 8 * er) && aligned(a.h_out, 8 * er) && aligned(a.x, 8 * ei);
   const bool layer = desc->norm == ASI_NORM_LAYER;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   using B = __nv_bfloat16;
@@ -1016,6 +1041,8 @@ asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_
   else if (desc->res_dtype == ASI_F32) e = vec ? launch_forward<B, float, true>(a, layer, st) : launch_forward<B, float, false>(a, layer, st);
   else e = vec ? launch_forward<B, B, true>(a, layer, st) : launch_forward<B, B, false>(a, layer, st);
   return cuda_status(e, "branch and residual stream");
+} catch (...) {
+  return no_host_memory();
 }
 
 size_t asi_branch_backward_ws_bytes(const asi_branch_desc_t* desc) {
@@ -1023,7 +1050,7 @@ size_t asi_branch_backward_ws_bytes(const asi_branch_desc_t* desc) {
   return check_desc(desc, &drop) == ASI_OK ? part_bytes(desc->rows, desc->dim) : 0;
 }
 
-asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch_t* t, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch_t* t, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) try {
   Drop drop = {};
   const asi_status_t s = check_desc(desc, &drop);
   if (s != ASI_OK) return s;
@@ -1060,14 +1087,16 @@ asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch
   a.dgate = t->dgate, a.daw = t->dafter_weight, a.dab = t->dafter_bias, a.dnw = t->dnext_weight, a.dnb = t->dnext_bias;
   a.accumulate = accumulate != 0;
   a.part = sums ? static_cast<float*>(ws) : nullptr;
-  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 16) && aligned(t->dx ? a.h_out : nullptr, 16) && aligned(a.dx, 16) && aligned(a.dh_out, 16) &&
-                   aligned(a.dy, 16) && aligned(a.dh, 16);
+  const bool vec = desc->dim % kEach == 0 && aligned(a.y, 8 * ei) && aligned(t->dx ? a.h_out : nullptr, 8 * er) && aligned(a.dx, 8 * ei) && aligned(a.dh_out, 8 * er) &&
+                   aligned(a.dy, 8 * ei) && aligned(a.dh, 8 * er);
   using B = __nv_bfloat16;
   cudaError_t e;
   if (desc->in_dtype == ASI_F32) e = vec ? launch_backward<float, float, true>(a, layer, st) : launch_backward<float, float, false>(a, layer, st);
   else if (desc->res_dtype == ASI_F32) e = vec ? launch_backward<B, float, true>(a, layer, st) : launch_backward<B, float, false>(a, layer, st);
   else e = vec ? launch_backward<B, B, true>(a, layer, st) : launch_backward<B, B, false>(a, layer, st);
   return cuda_status(e, "gradient of branch and residual stream");
+} catch (...) {
+  return no_host_memory();
 }
 
 }  // extern "C"
