@@ -423,7 +423,7 @@ typedef struct {
   const void* h;                 /* [in] res_dtype; null: no residual (0) */
   const float* gate;             /* [in] [ceil(rows / rows_per_gate)][dim]; null where rows_per_gate is 0 */
   const float *after_weight, *after_bias;      /* [in] [dim], each may be null (1 and 0); both null without norm_after */
-  const float *next_weight, *next_bias;        /* [in] [dim], each may be null (1 and 0) */
+  const float *next_weight, *next_bias;        /* [in] [dim], each may be null (1 and 0).  Biases are ASI_NORM_LAYER's alone */
   void* h_out;                   /* [out] res_dtype; [in] of the gradient.  It may be h itself */
   void* x;                       /* [out] in_dtype; null: no norm follows */
   float* stats;                  /* [out] [rows][4]: mean and 1 / sqrt(..) of the norm after, of the next one (mean 0 of ASI_NORM_RMS; all

@@ -1022,7 +1022,7 @@ asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_
   if (s != ASI_OK) return s;
   if (!t) return ASI_ERR_INVALID_ARG;
   if (desc->rows == 0) return ASI_OK;
-  if (!t->y || !t->h_out || !t->stats || (desc->rows_per_gate && !t->gate) || (!desc->norm_after && (t->after_weight || t->after_bias))) return ASI_ERR_INVALID_ARG;
+  if (!t->y || !t->h_out || !t->stats || (desc->rows_per_gate && !t->gate) || (!desc->norm_after && (t->after_weight || t->after_bias)) || (desc->norm == ASI_NORM_RMS && (t->after_bias || t->next_bias))) return ASI_ERR_INVALID_ARG;
   const size_t ei = size_of(desc->in_dtype), er = size_of(desc->res_dtype), n = (size_t)desc->rows * desc->dim, w = (size_t)desc->dim * 4;
   const size_t gates = desc->rows_per_gate ? (size_t)ceil_div(desc->rows, desc->rows_per_gate) * w : 0;
   const float* gate = desc->rows_per_gate ? t->gate : nullptr;
@@ -1059,6 +1059,7 @@ asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch
   const size_t ei = size_of(desc->in_dtype), er = size_of(desc->res_dtype), n = (size_t)desc->rows * desc->dim, w = (size_t)desc->dim * 4;
   const bool layer = desc->norm == ASI_NORM_LAYER;
   if ((t->dgate && !desc->rows_per_gate) || (!desc->norm_after && (t->dafter_weight || t->dafter_bias || t->after_weight || t->after_bias))) return ASI_ERR_INVALID_ARG;
+  if (!layer && (t->after_bias || t->next_bias || t->dafter_bias || t->dnext_bias)) return ASI_ERR_INVALID_ARG;
   if (desc->rows == 0) {                                   // sums of nothing (a gate has no rows then)
     if (accumulate) return ASI_OK;
     for (float* p : {t->dafter_weight, t->dafter_bias, t->dnext_weight, t->dnext_bias}) {

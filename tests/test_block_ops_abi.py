@@ -15,6 +15,15 @@ def B():
     return binding
 
 
+@pytest.fixture()
+def no_gpu():
+    """For calls with addresses that are none, of which nothing is wrong but that: they go as far as a launch, which only a host without a GPU
+    answers with an error."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("needs a host without a GPU")
+
+
 def at(i):
     return (i + 1) << 40
 
@@ -54,7 +63,7 @@ ROWS, DIM = 6, 40
 
 
 def branch_desc(B, drop_=None, **kw):
-    d = dict(in_dtype=1, res_dtype=0, norm=0, norm_after=1, rows=ROWS, dim=DIM, rows_per_gate=2, eps=1e-5, res_scale=1.0, branch_scale=1.0,
+    d = dict(in_dtype=1, res_dtype=0, norm=1, norm_after=1, rows=ROWS, dim=DIM, rows_per_gate=2, eps=1e-5, res_scale=1.0, branch_scale=1.0,
              drop=drop_ or drop(B))
     d.update(kw)
     return B.BranchDesc(*[d[f] for f, _ in B.BranchDesc._fields_])
@@ -105,6 +114,15 @@ def test_branch_buffers(B):
         assert L.asi_branch_forward(d, branch(B, **{name: at(30) + shift}), None) == INVALID, name
     for name, shift in (("y", 1), ("h_out", 2), ("dx", 1), ("dh_out", 2), ("dy", 1), ("dh", 2), ("dgate", 2), ("dnext_bias", 1)):
         assert L.asi_branch_backward(d, branch(B, **{name: at(30) + shift}), 0, at(60), NEED, None) == INVALID, name
+
+
+def test_root_mean_square_norms_have_no_biases(B):
+    L, d = B.lib(), branch_desc(B, norm=0)
+    none = dict(after_bias=None, next_bias=None, dafter_bias=None, dnext_bias=None)
+    for name in ("after_bias", "next_bias"):
+        assert both(B, d, branch(B, **{**none, name: at(50)})) == (INVALID, INVALID)
+    for name in ("dafter_bias", "dnext_bias"):
+        assert L.asi_branch_backward(d, branch(B, **{**none, name: at(50)}), 0, at(60), NEED, None) == INVALID
 
 
 def sizes(forward):
@@ -171,15 +189,23 @@ def head_desc(B, **kw):
     return B.HeadDesc(*[d[f] for f, _ in B.HeadDesc._fields_])
 
 
-def calls(B, d, p, ws=at(60), n=NEED):
-    """Codes of the three entry points for buffers by name."""
-    L = B.lib()
+ARGS = (("x", "w", "y", "logp", "entropy", "lse"), ("x", "w", "y", "lse", "entropy", "dlogp", "dent", "dx", "dw"),
+        ("x", "w", "y", "dlogp", "dent", "logp", "entropy", "lse", "dx", "dw"))
+FORWARD, GRAD, LOSS = range(3)
 
-    def of(*names):
-        return [p.get(x) for x in names]
-    return (L.asi_head_logprobs(d, *of("x", "w", "y", "logp", "entropy", "lse"), ws, n, None),
-            L.asi_head_grad(d, *of("x", "w", "y", "lse", "entropy", "dlogp", "dent", "dx", "dw"), 0, ws, n, None),
-            L.asi_head_loss(d, *of("x", "w", "y", "dlogp", "dent", "logp", "entropy", "lse", "dx", "dw"), 0, ws, n, None))
+
+def call(B, k, d, p, ws=at(60), n=NEED):
+    """The code of entry point k for buffers by name."""
+    L = B.lib()
+    args = [p.get(x) for x in ARGS[k]]
+    if k == FORWARD:
+        return L.asi_head_logprobs(d, *args, ws, n, None)
+    return (L.asi_head_grad if k == GRAD else L.asi_head_loss)(d, *args, 0, ws, n, None)
+
+
+def refused(B, d, p, code=INVALID, which=(FORWARD, GRAD, LOSS), **kw):
+    """(No entry point is called that has nothing to refuse: it would go as far as a launch.)"""
+    return all(call(B, k, d, p, **kw) == code for k in which)
 
 
 NAMES = ("x", "w", "y", "dlogp", "dent", "logp", "entropy", "lse", "dx", "dw")
@@ -197,63 +223,60 @@ def buffers(**kw):
 ])
 def test_head_descriptors(B, bad, code):
     d = head_desc(B, **bad)
-    assert calls(B, d, buffers()) == (code,) * 3
+    assert refused(B, d, buffers(), code)
     assert B.lib().asi_head_ws_bytes(d, 0) == B.lib().asi_head_ws_bytes(d, 1) == 0
-    assert calls(B, None, buffers()) == (INVALID,) * 3
+    assert refused(B, None, buffers())
 
 
 def test_head_buffers(B):
     d = head_desc(B)
     for hole in ("x", "w", "y"):
-        assert calls(B, d, buffers(**{hole: None})) == (INVALID,) * 3
-    for hole in ("logp", "lse"):
-        f, g, both_ = calls(B, d, buffers(**{hole: None}))
-        assert f == both_ == INVALID and (hole == "logp" or g == INVALID)
-    for holes in (("dlogp",), ("dx", "dw"), ("entropy",)):              # (entropy missing where dentropy is there)
-        assert calls(B, d, buffers(**dict.fromkeys(holes)))[1:] == (INVALID,) * 2
-    for name, shift in (("x", 2), ("x", 8), ("w", 8), ("y", 4), ("logp", 2), ("lse", 1), ("entropy", 2)):   # x and w on 16 bytes (dim 24)
-        assert INVALID in calls(B, d, buffers(**{name: at(30) + shift})), name
-    for name, shift in (("dlogp", 2), ("dent", 2), ("dx", 1), ("dw", 2)):
-        assert calls(B, d, buffers(**{name: at(30) + shift}))[1:] == (INVALID,) * 2, name
-    assert calls(B, d, buffers(), ws=None) == (INVALID,) * 3
+        assert refused(B, d, buffers(**{hole: None}))
+    for hole, which in (("logp", (FORWARD, LOSS)), ("lse", (FORWARD, GRAD, LOSS)), ("dlogp", (GRAD, LOSS)), ("entropy", (GRAD, LOSS))):
+        assert refused(B, d, buffers(**{hole: None}), which=which), hole      # (entropy missing where dentropy is there)
+    assert refused(B, d, buffers(dx=None, dw=None), which=(GRAD, LOSS))
+    for name, shift in (("x", 2), ("x", 8), ("w", 8), ("y", 4), ("logp", 2), ("lse", 1), ("entropy", 2), ("dlogp", 2), ("dent", 2), ("dx", 1), ("dw", 2)):
+        which = [k for k in range(3) if name in ARGS[k]]                      # x and w on 16 bytes (dim 24)
+        assert refused(B, d, buffers(**{name: at(30) + shift}), which=which), name
+    assert refused(B, d, buffers(), ws=None)
 
 
 def test_head_outputs_that_meet_another_buffer(B):
     d = head_desc(B)
     size = dict(x=2 * T * D, w=2 * V * D, y=8 * T, dlogp=4 * T, dent=4 * T, logp=4 * T, entropy=4 * T, lse=4 * T, dx=2 * T * D, dw=4 * V * D)
     writes = (("logp", "entropy", "lse"), ("dx", "dw"), ("logp", "entropy", "lse", "dx", "dw"))
-    reads = (("x", "w", "y"), ("x", "w", "y", "lse", "entropy", "dlogp", "dent"), ("x", "w", "y", "dlogp", "dent"))
+    need = B.lib().asi_head_ws_bytes(d, 1)
     for k in range(3):
         for out in writes[k]:
-            for other in writes[k] + reads[k]:
+            for other in ARGS[k]:
                 for shift in (0, size[other] // 16 * 16 - 16, 16 - size[out] // 16 * 16):
                     p = buffers()
                     p[out] = p[other] + shift
                     if other != out and p[out] < p[other] + size[other] and p[other] < p[out] + size[out]:
-                        assert calls(B, d, p)[k] == INVALID, (k, out, other, shift)
-        for name in writes[k] + reads[k]:
-            assert calls(B, d, buffers(**{name: at(60) + 256}), n=B.lib().asi_head_ws_bytes(d, 1))[k] == INVALID, (k, name)
+                        assert refused(B, d, p, which=(k,)), (k, out, other, shift)
+        for name in ARGS[k]:
+            assert refused(B, d, buffers(**{name: at(60) + 256}), which=(k,), n=need), (k, name)
 
 
 def test_head_workspace(B):
     L, d = B.lib(), head_desc(B, vocab_chunk=256)                       # (no logits are kept: all of it is needed)
     assert L.asi_head_ws_bytes(d, 0) < L.asi_head_ws_bytes(d, 1)
-    for grad in (0, 1):
+    for grad, which in ((0, (FORWARD,)), (1, (GRAD, LOSS))):
         need = L.asi_head_ws_bytes(d, grad)
-        assert need % 256 == 0
-        for got in calls(B, d, buffers(), n=need - 1)[1 if grad else 0:None if grad else 1]:
-            assert got == WORKSPACE
-    assert calls(B, d, buffers(), ws=at(60) + 128) == (WORKSPACE,) * 3
+        assert need % 256 == 0 and refused(B, d, buffers(), WORKSPACE, which, n=need - 1)
+    assert refused(B, d, buffers(), WORKSPACE, ws=at(60) + 128)
     assert L.asi_head_ws_bytes(head_desc(B, vocab_chunk=256, vocab=100000, rows=4000), 1) < L.asi_head_ws_bytes(head_desc(B, vocab=100000, rows=4000), 1)
-    # room for kept logits is not insisted on
-    kept = head_desc(B)
+
+
+def test_room_for_kept_logits_is_not_insisted_on(B, no_gpu):
+    L, kept = B.lib(), head_desc(B)
     assert L.asi_head_ws_bytes(kept, 1) > L.asi_head_ws_bytes(head_desc(B, vocab_chunk=V), 1)
-    assert calls(B, kept, buffers(), n=L.asi_head_ws_bytes(head_desc(B, vocab_chunk=V), 1))[2] == CUDA
+    assert call(B, LOSS, kept, buffers(), n=L.asi_head_ws_bytes(head_desc(B, vocab_chunk=V), 1)) == CUDA
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(in_dtype=0), dict(dim=771), dict(vocab_chunk=1000), dict(in_dtype=1, dw_dtype=1)])
 @pytest.mark.parametrize("vocab", [1, 5000, 130000])
-def test_a_head_workspace_serves_fewer_rows(B, kw, vocab):
+def test_a_head_workspace_serves_fewer_rows(B, no_gpu, kw, vocab):
     """What fewer rows cannot do without fits (they may find room to keep their logits in as well, or not)."""
     L = B.lib()
     least = 0
@@ -267,7 +290,7 @@ def test_a_head_workspace_serves_fewer_rows(B, kw, vocab):
             p = dict(x=1 << 50, w=1 << 51, y=1 << 52, dlogp=1 << 53, logp=1 << 54, lse=1 << 55, dx=1 << 56, dw=1 << 57)
             while hi - lo > 256:
                 mid = (lo + hi) // 512 * 256
-                if calls(B, d, p, n=mid)[2] == WORKSPACE:
+                if call(B, LOSS, d, p, n=mid) == WORKSPACE:
                     lo = mid
                 else:
                     hi = mid
