@@ -198,6 +198,7 @@ struct BranchArgs {
   int64_t rows, per;       // rows of a gate's row
   int64_t run;             // rows of a worker
   int workers, dim, norm_after, accumulate;
+  int zero_sums;           // S0 is wanted (a bias behind the norm after: of dgate, or its own gradient)
   int stages;              // rows on their way at once
   float eps, rs, bs, inv_dim;
   Drop drop;
@@ -601,7 +602,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   // the sums over the worker's rows of one of the gate's
   auto flush = [&](bool whole) {
     mul8(s1, s1, p.bs);
-    if (kLayer) mul8(s0, s0, p.bs);
+    if (kLayer && p.zero_sums) mul8(s0, s0, p.bs);
     float g[kEach];
     c.param(gate, g, 1.f, on32(gate));
     if (p.dgate) {
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
         for (int i = 0; i < kEach; ++i)
           if (c.there(i)) {
             q1[c.at(i)] = s1[i];
-            if (kLayer) q0[c.at(i)] = s0[i];
+            if (kLayer && p.zero_sums) q0[c.at(i)] = s0[i];
           }
       }
     }
@@ -629,7 +630,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
     if (kLayer && p.dab) add(kAfter0, s0);
     again = true;
     clear8(s1);
-    clear8(s0);
+    if (kLayer) clear8(s0);
   };
   int64_t at = t0 * p.dim;
 #pragma unroll 1
@@ -704,7 +705,7 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
     }
     if (p.drop.below) c.drop(p.drop, bits, d);             // u / b
     fma8(s1, d, y_, s1);
-    if (kLayer) add8(s0, s0, d);
+    if (kLayer && p.zero_sums) add8(s0, s0, d);
     mul8(d, d, w);                                         // v
     if (p.norm_after) {
       if constexpr (kLayer) {
@@ -727,10 +728,10 @@ __global__ void __launch_bounds__(kMax, ctas_of(kMax, 2)) k_branch_backward(cons
   auto keep = [&](int which, const float (&v)[kEach]) { c.store(part(which), v); };
   if (!kGroups) {
     mul8(s1, s1, p.bs);
-    if (kLayer) mul8(s0, s0, p.bs);
+    if (kLayer && p.zero_sums) mul8(s0, s0, p.bs);
   }
   if (!kGroups && (p.dgate || p.daw)) keep(kHead1, s1);
-  if (!kGroups && kLayer && (p.dgate || p.dab)) keep(kHead0, s0);
+  if (!kGroups && kLayer && p.zero_sums) keep(kHead0, s0);
   if (p.dnw) keep(kNext1, n1);
   if (kLayer && p.dnb) keep(kNext0, n0);
 }
@@ -796,7 +797,7 @@ __global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_const
       return;
     }
     if (!p.dgate && !p.daw && !p.dab) return;
-    const bool one = p.dgate || p.daw, two = a.layer && (p.dgate || p.dab);
+    const bool one = p.dgate || p.daw, two = p.zero_sums != 0;
     float2 r = total(one ? kHead1 : kHead0, one && two ? kHead0 : -1);
     if (!one) r.y = r.x;
     if (rank || slice || col >= p.dim) return;
@@ -820,7 +821,7 @@ __global__ void __launch_bounds__(32 * kSlices) k_branch_sums(const __grid_const
           for (int64_t w = w0 + sub; w <= w1; w += a.each) {
             const bool tail = w == w0 && !head;
             x += p.part[((int64_t)(tail ? kTail1 : kHead1) * p.workers + w) * p.dim + col];
-            if (a.layer) y += p.part[((int64_t)(tail ? kTail0 : kHead0) * p.workers + w) * p.dim + col];
+            if (p.zero_sums) y += p.part[((int64_t)(tail ? kTail0 : kHead0) * p.workers + w) * p.dim + col];
           }
       }
       __syncthreads();
@@ -1087,6 +1088,7 @@ asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch
   a.dx = t->dx, a.dh_out = t->dh_out, a.dy = t->dy, a.dh = t->dh;
   a.dgate = t->dgate, a.daw = t->dafter_weight, a.dab = t->dafter_bias, a.dnw = t->dnext_weight, a.dnb = t->dnext_bias;
   a.accumulate = accumulate != 0;
+  a.zero_sums = a.dab || (a.dgate && a.ab);
   a.part = sums ? static_cast<float*>(ws) : nullptr;
   const bool vec = desc->dim % kEach == 0 && aligned(a.y, 8 * ei) && aligned(t->dx ? a.h_out : nullptr, 8 * er) && aligned(a.dx, 8 * ei) && aligned(a.dh_out, 8 * er) &&
                    aligned(a.dy, 8 * ei) && aligned(a.dh, 8 * er);
