@@ -10,7 +10,7 @@
 // fp32, in the workspace) where these take no more than a piece of G would.
 //
 // What bounds it: the tensor cores, 2 T V D operations a product (for a few rows the bytes of w, read twice, and of dw).  4096 x 32000 x 2048
-// bf16 in bursts: logits and their sums 334 us (1608 TFLOP/s), G of 16128 columns 184 (1470), both products of G 373 (1450); in long loops the
+// bf16 in bursts: logits and their sums 334 us (1608 TFLOP/s), G of 16128 columns 184 (1470), both products of G 340 (1590); in long loops the
 // power cap takes 15 % of that.
 //
 // Operands are bf16.  fp32 ones are split into three terms each (hi, mid, lo: 24 bits) by k_head_split, and a product takes the
@@ -40,7 +40,10 @@ constexpr int kK = 64;                                    // k of a box: 64 bf16
 constexpr int kMaxStages = 3;
 constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's box
 constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
-constexpr int kSeg = 16, kWhole = 12;                     // pairs of boxes that add up in TMEM at most where results are held to fp32; as many need no segments
+// Pairs of boxes that add up in TMEM at most where results are held to fp32 (kWhole need no segments).  What truncation takes from a logit is in
+// proportion to them: lse of 40 x 11324 x 761 fp32 5.4e-7 too small with 16, 2.9e-7 with 8 (entropy 1.0e-6 and 5.4e-7 too large).  8 of them cost operands
+// in three terms 0 to 4 % (1001 x 30011 x 771 760 us -> 794; scoring 1000 x 30000 x 2000 577 -> 566), single ones 6 % (4096 x 32000 x 2048 345 -> 367).
+constexpr int kSeg = 16, kSegTerms = 8, kWhole = 12;
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -956,7 +959,7 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
     parts = std::max(parts, (p.a_terms + p.b_terms) * p.sub);
     p.seg = 1 << 30;
     if (segmented && p.per * p.pairs > kWhole) {
-      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, kSeg));
+      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, p.pairs > 1 ? kSegTerms : kSeg));
       p.seg = (int)ceil_div(p.per, n);
     }
   }

@@ -545,7 +545,7 @@ class ResidualNormRunner(_Steps):
     """The end of a block for up to `rows` rows: norm after its branch, gate, dropout, residual sum and the next block's norm, and their
     gradient.  Holds the rows' statistics (`stats`, that backward() reads as the last forward() left them; another
     contiguous fp32 [>= rows, 4] buffer may be assigned) and the backward workspace: calls (and graphs captured from them) that may run
-    at the same time need a runner each."""
+    at the same time need a runner each.  Biases are for norm="layer" alone."""
 
     def __init__(self, rows, dim, bf16=False, bf16_residual=False, norm="rms", norm_after=False, rows_per_gate=0, eps=1e-5, res_scale=1.0,
                  branch_scale=1.0, dropout=0.0, seed=0, stream_id=0, device="cuda:0"):
