@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         }
         const int n = n0 + cc * 32;
         if (!live) continue;
-        if constexpr (kEpi == kOut && !kSegmented) {
+        if constexpr (kEpi == kOut) {
           // One entry of G's row is as large as all others together, and its rounding no less: it comes back as off[t] w[y]
           if (p.correct && off != 0.f) {
 #pragma unroll
