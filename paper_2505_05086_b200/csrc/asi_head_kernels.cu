@@ -730,7 +730,8 @@ __global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptA
   const RowGrad r = row_grad(p.h, row);
   const float4 in = *reinterpret_cast<const float4*>(p.x + row * p.ld_x + j0);
   float v[4] = {in.x, in.y, in.z, in.w};
-  to_gradient<4, true>(v, r, p.h, p.h.v0 + j0);
+  if (p.h.terms == 1) to_gradient<4, false>(v, r, p.h, p.h.v0 + j0);
+  else to_gradient<4, true>(v, r, p.h, p.h.v0 + j0);
   for (int e = 0; e < p.h.terms; ++e) {
     const uint2 w = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
     *reinterpret_cast<uint2*>(p.out + ((int64_t)e * p.h.T + row) * p.ld + j0) = w;
@@ -859,8 +860,8 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   }
   l.least = l.bytes = at;
   // Logits of few rows take no more than a piece of G may: where the workspace has room for them they stay, in fp32, and the third of the
-  // four products is spared (the same bits).  9 x 50257 x 768 bf16: 136 us instead of 168; 1001 x 30011 x 771 fp32: 768
-  // instead of 939.
+  // four products is spared (the same bits, but for G in bf16 where sums of more than 768 k are not segmented).  9 x 50257 x 768 bf16:
+  // 136 us instead of 168; 1001 x 30011 x 771 fp32: 768 instead of 939.
   if (grad && T && !d->vocab_chunk && all * T * 4 <= kPieceBytes) {
     l.kept = take((size_t)(all * T * 4));
     l.bytes = at;
@@ -1095,7 +1096,9 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       const KeptArgs k = {g, reinterpret_cast<const float*>(ws + l.kept) + v0, static_cast<__nv_bfloat16*>(G), nt * kTile, l.cols, n};
       e = launch_pdl(k_head_kept, dim3((unsigned)T, (unsigned)ceil_div(n, 1024)), dim3(256), 0, st, k);
     } else {
-      e = launch_gemm<kGrad>(g, fine && logits.kc * logits.pairs > kWhole, st);
+      // G in terms (24 bits) wants logits summed as those behind lse.  To G in bf16, whose step is 2^-9, what truncation takes from a logit
+      // (1.7e-6 at D = 2048) is nothing, and summing them in segments costs 4096 x 32000 x 2048 2 % (1451 us -> 1483)
+      e = launch_gemm<kGrad>(g, terms > 1 && logits.kc * logits.pairs > kWhole, st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
     // (the first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
