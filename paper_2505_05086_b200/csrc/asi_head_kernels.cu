@@ -174,8 +174,8 @@ __device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
   return r;
 }
 
-// kN logits of a row, the first in column j0 of the vocabulary, become their gradients (by a whole warp; kFine: G is stored in terms)
-template <int kN, bool kFine>
+// kN logits of a row, the first in column j0 of the vocabulary, become their gradients (by a whole warp)
+template <int kN>
 __device__ __forceinline__ void to_gradient(float (&v)[kN], const RowGrad& r, const HeadArgs& g, int64_t j0) {
   const float a = -g.scale * r.alpha;
   if (__any_sync(~0u, r.beta != 0.f)) {
@@ -185,13 +185,10 @@ __device__ __forceinline__ void to_gradient(float (&v)[kN], const RowGrad& r, co
       const float x = fmaf(v[i], g.c, -r.hi) - r.lo, p = ex2(x);
       v[i] = p * fmaf(-b, fmaf(fmaxf(x, -200.f), kLn2, r.h), a);
     }
-  } else if (kFine) {
+  } else {
+    // (hi and lo apart: their sum is off by 2^-24 of it, which logits of 10^4 and more would show in bf16 too)
 #pragma unroll
     for (int i = 0; i < kN; ++i) v[i] = ex2(fmaf(v[i], g.c, -r.hi) - r.lo) * a;
-  } else {
-    const float z = -(r.hi + r.lo);                        // (off by 2^-24 of it: less than bf16 shows)
-#pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = ex2(fmaf(v[i], g.c, z)) * a;
   }
   const int hot = r.y - (int)j0;                           // (V <= 2^24)
   if (hot >= 0 && hot < kN) {
@@ -545,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
           if (g.terms == 1) {
             // rows of 128 bytes (64 columns), 16-byte units swizzled by the row as the tensor copy expects them
             if ((cc & 1) == 0) out = next_place();
-            to_gradient<32, false>(v, rg, g, g.v0 + n);
+            to_gradient<32>(v, rg, g, g.v0 + n);
 #pragma unroll
             for (int u = 0; u < 4; ++u)
               *reinterpret_cast<uint4*>(out + lane * 128 + ((((cc & 1) * 4 + u) ^ (lane & 7)) * 16)) =
@@ -560,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             }
           } else {
             // a term after the other, rows of 64 bytes (32 columns)
-            to_gradient<32, true>(v, rg, g, g.v0 + n);
+            to_gradient<32>(v, rg, g, g.v0 + n);
 #pragma unroll 1
             for (int e = 0; e < 3; ++e) {
               out = next_place();
@@ -730,8 +727,7 @@ __global__ void __launch_bounds__(256) k_head_kept(const __grid_constant__ KeptA
   const RowGrad r = row_grad(p.h, row);
   const float4 in = *reinterpret_cast<const float4*>(p.x + row * p.ld_x + j0);
   float v[4] = {in.x, in.y, in.z, in.w};
-  if (p.h.terms == 1) to_gradient<4, false>(v, r, p.h, p.h.v0 + j0);
-  else to_gradient<4, true>(v, r, p.h, p.h.v0 + j0);
+  to_gradient<4>(v, r, p.h, p.h.v0 + j0);
   for (int e = 0; e < p.h.terms; ++e) {
     const uint2 w = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
     *reinterpret_cast<uint2*>(p.out + ((int64_t)e * p.h.T + row) * p.ld + j0) = w;

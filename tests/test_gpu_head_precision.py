@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from tests.test_gpu_head import World
+from tests.block_util import U16, U32, head
+from tests.test_gpu_head import DT, World
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,38 @@ def test_dx_gets_back_what_rounding_takes_from_g_at_the_target(T, V, D, bf16_dw)
     lost = off[:, None] * w.w[w.y.clamp(min=0)].double()
     share = float(((got["dx"].double() - r["dx"]) * lost).sum() / lost.square().sum())
     assert abs(share) <= 0.25
+
+
+def far_world(T, V, offset, bf16, bf16_dw, **kw):
+    """Logits around offset[0] * offset[1] whose products and sums are exact in fp32 (multiples of 1/8), and columns of x that are 1 in one row alone and
+    meet zeros of w, so that dw holds G as it is."""
+    w = World(T, V, 16 + T, bf16, bf16_dw, ignored=0.0, **kw)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x, t = torch.zeros(T, 16 + T, device="cuda"), torch.arange(T, device="cuda")
+    x[:, 1:16] = torch.randint(-4, 5, (T, 15), generator=g, device="cuda").float()
+    x[:, 0], x[t, 16 + t] = offset[0], 1.0
+    k = torch.zeros(V, 16 + T, device="cuda")
+    k[:, 1:16] = torch.randint(-2, 3, (V, 15), generator=g, device="cuda").float() / 8
+    k[:, 0] = offset[1]
+    w.x, w.w = x.to(DT[bf16]), k.to(DT[bf16])
+    w.dlogp.fill_(0.75)
+    return w
+
+
+def check_far(w, gw):
+    """G, as dw holds it, where lse is large: with |log p| <= 16 exponents are off by 2^-24 of |log p| and of the logit's distance from the maximum, twice at
+    most, each times ln 2, the factor in them by as much, the power and the sum by 2^-21 together, and G's own rounding comes on top."""
+    r = head(w.x, w.w, w.y, 1.0, -100, w.dlogp)
+    got, want = gw[:, 16:].T.double(), r["G"]
+    lp = r["p"].log()
+    bound = 0.75 * r["p"] * ((8 * lp.abs() + 32) * U32) + (2 * U16 if w.bf16_dw else 4 * U32) * want.abs()
+    assert (((got - want).abs() <= bound) | (lp < -16)).all()
+
+
+@pytest.mark.parametrize("bf16,bf16_dw,offset", [(False, False, (64, 16)), (True, False, (64, 16)), (True, False, (-64, 16)), (True, True, (512, 256)),
+                                                 (True, True, (-512, 256))])
+@pytest.mark.parametrize("T,V", [(20, 600), (300, 1100)])
+@pytest.mark.parametrize("chunk", [0, 512])
+def test_gradient_of_large_logits(T, V, bf16, bf16_dw, offset, chunk):
+    w = far_world(T, V, offset, bf16, bf16_dw, vocab_chunk=chunk)
+    check_far(w, w.loss()["dw"])
