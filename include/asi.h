@@ -471,7 +471,8 @@ size_t asi_head_ws_bytes(const asi_head_desc_t* desc, int32_t grad);
  *   logp, entropy, lse [out] device fp32 [rows];  entropy may be null */
 asi_status_t asi_head_logprobs(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, float* logp,
                                float* entropy, float* lse, void* ws, size_t ws_bytes, void* stream);
-/*   lse, entropy [in] as asi_head_logprobs wrote them (entropy may be null where dentropy is)
+/*   lse, entropy [in] as asi_head_logprobs wrote them (entropy may be null where dentropy is).  p = exp(X - lse) is off by 2^-24 |lse|;
+ *           where a row that is not ignored has |lse| >= 128 (dx or dw in fp32) or 4096 (both in bf16), one more product sums such rows again
  *   dlogp [in] device fp32 [rows];  dentropy [in] device fp32 [rows] or null
  *   dx [out] device in_dtype [rows][dim];  dw [in/out] device dw_dtype [vocab][dim], written over, or added to what is there (accumulate
  *      != 0; subnormal sums may count as 0 there).  One of them may be null.  bf16 rows of a dim that is a multiple of 8 start on 16 bytes in x

@@ -88,8 +88,9 @@ struct HeadArgs {
   int T;
   float c, scale;               // c = scale log2(e)
   float *pm, *ps, *pw, *xy;     // [2 nt][T]: maximum (base 2), sum, weighted sum; [T]: the target's logit
-  const float2* row;            // maximum (base 2) and log2 of the sum of each row, or
-  const float* lse;             // (null: row)
+  const float2* row;            // maximum (base 2) and log2 of the sum of each row
+  const float* lse;             // null, or what a row goes by where it is below `far`.  Then kStats sums the others alone (see kFarLse)
+  float far;
   const float *entropy, *dlogp, *dent;
   float* off;                   // [T]: what rounding took from G at the target (bf16 operands), or null; w and its row stride beside it
   const __nv_bfloat16* w;
@@ -144,6 +145,12 @@ struct RowStats {
   }
 };
 
+// What a gradient without its forward pass takes lse for: p = exp(x - lse) is off by 2^-24 |lse|, 2^-17 of it from 128 on where G goes out in terms, 2^-12 from
+// 4096 on beside the 2^-9 of a rounding to bf16.  Rows beyond that are summed again: the forward direction's kernels are launched in any case and have
+// nothing to do where their rows are near (9 x 32000 x 2048 bf16 133 us instead of 126).
+constexpr float kFarLseTerms = 128.f, kFarLse = 4096.f;
+__device__ __forceinline__ bool is_far(const float* lse, const int64_t* y, int64_t ignore, int64_t row, float far) { return fabsf(lse[row]) >= far && y[row] != ignore; }
+
 // what G of a row needs
 struct RowGrad {
   float hi, lo, alpha, beta, h;
@@ -162,11 +169,11 @@ __device__ __forceinline__ RowGrad row_grad(const HeadArgs& g, int row) {
   r.off = g.off ? g.off + row : nullptr;
   r.alpha = in ? g.dlogp[row] : NAN;
   if (g.dent) r.beta = g.dent[row], r.h = g.entropy[row];
-  if (g.row) {
+  const float l = g.lse ? g.lse[row] : 0.f;
+  if (!g.lse || fabsf(l) >= g.far) {
     const float2 q = g.row[row];
     r.hi = q.x, r.lo = q.y;
   } else {
-    const float l = g.lse[row];
     r.hi = l * kLog2e;
     r.lo = fmaf(l, kLog2e, -r.hi) + l * kLog2eLow;
   }
@@ -274,7 +281,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   // The tiles of a pair: every `pairs`-th of the first product, and of the second one every so many of a stretch for pairs that had as many
   // of the first (pairs below `few` had one more; the stretches' lengths make up for that).  Pairs side by side work on tiles side by side, which
   // share a row of G (a stretch a pair read 1.19 GB instead of 0.43 for 4096 x 16128 x 2048, in 371 us instead of 340)
-  const int mine0 = (g.tiles0 - pair + pairs - 1) / pairs;
+  int mine0 = (g.tiles0 - pair + pairs - 1) / pairs;
+  if constexpr (kEpi == kStats) {
+    if (g.lse) {                                         // (tiles of a column: a tile's rows come again after mt of them at most)
+      const int mt = g.p[0].mt, some = mine0 < mt ? mine0 : mt;
+      bool any = false;
+#pragma unroll 4
+      for (int i = 0; i < some; ++i) {
+        const int64_t row = (int64_t)((pair + (int64_t)i * pairs) % mt) * kTile + tid;
+        any |= tid < kTile && row < g.T && is_far(g.lse, g.y, g.ignore, row, g.far);
+      }
+      if (!__syncthreads_or(any)) mine0 = 0;
+    }
+  }
   const bool late = pair >= g.few;
   const int q1 = late ? pair - g.few : pair, each1 = late ? g.each_rest : g.each_few, more1 = late ? g.more_rest : g.more_few;
   const int from1 = (late ? g.few * g.each_few + g.more_few : 0) + q1, step1 = late ? pairs - g.few : g.few;
@@ -648,6 +667,8 @@ struct RowsArgs {
   float2* row;
   int T, parts;
   float c;
+  const float* given;          // null, or an earlier call's lse: rows below `far` are left out
+  float far;
 };
 constexpr int kAhead = 8;
 __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ RowsArgs p) {
@@ -655,7 +676,9 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  int row = blockIdx.x * 32 + slice;                     // (the row that this warp's first lane writes)
+  int row = blockIdx.x * 32 + lane;
+  if (p.given && !__syncthreads_or(row < p.T && is_far(p.given, p.y, p.ignore, row, p.far))) return;
+  row = blockIdx.x * 32 + slice;                         // (the row that this warp's first lane writes)
   const int64_t y = row < p.T ? p.y[row] : 0;
   const float xy = row < p.T && p.logp && y >= 0 && y < p.V ? p.xy[row] : 0.f;
   row = blockIdx.x * 32 + lane;
@@ -1043,30 +1066,31 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   if (!operand_map(&logits.a, x, D, T, ld, l.in_terms, T * ld, kK, 128) || !operand_map(&logits.b, w, D, V, ld, l.in_terms, V * ld, kK, 128))
     return cuda_status(cudaErrorNotSupported, "tensor map");
   const bool keep = c.forward && c.grad && l.kept && ws_bytes >= l.bytes;
-  if (c.forward) {
-    g.p[0] = logits;
-    g.np = 1;
-    if (keep) {
-      g.p[0].out = ws + l.kept;
-      g.p[0].out_kind = kF32;
-      g.p[0].ld = nt * kTile;
-      set_store(&g.p[0], T, nt * kTile);
-      if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
-    }
-    // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, in two segments 0.8e-6; 345 us either way)
-    e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
-    if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
-    RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c};
-    e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
-    if (e != cudaSuccess) return cuda_status(e, "rows of the output layer");
+  const int terms = c.dw && d->dw_dtype == ASI_F32 ? 3 : fine ? 3 : 1;   // of G (without dw in fp32, G of bf16 operands has one)
+  if (!c.forward) {
+    g.lse = c.lse_in;
+    g.far = terms > 1 ? kFarLseTerms : kFarLse;
   }
+  g.p[0] = logits;
+  g.np = 1;
+  if (keep) {
+    g.p[0].out = ws + l.kept;
+    g.p[0].out_kind = kF32;
+    g.p[0].ld = nt * kTile;
+    set_store(&g.p[0], T, nt * kTile);
+    if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
+  }
+  // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, in two segments 0.8e-6; 345 us either way)
+  e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
+  if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
+  const RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c, g.lse, g.far};
+  e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
+  if (e != cudaSuccess) return cuda_status(e, "rows of the output layer");
   if (!c.grad) return ASI_OK;
-  g.row = c.forward ? row : nullptr;
-  g.lse = c.lse_in;
+  g.row = row;
   g.entropy = c.entropy_in;
   g.dlogp = c.dlogp;
   g.dent = c.dent;
-  const int terms = c.dw && d->dw_dtype == ASI_F32 ? 3 : fine ? 3 : 1;   // (without dw in fp32, G of bf16 operands has one)
   g.terms = terms;
   g.off = !fine && c.dx ? reinterpret_cast<float*>(ws + l.off) : nullptr;
   g.w = static_cast<const __nv_bfloat16*>(w);

@@ -59,3 +59,31 @@ def check_far(w, gw):
 def test_gradient_of_large_logits(T, V, bf16, bf16_dw, offset, chunk):
     w = far_world(T, V, offset, bf16, bf16_dw, vocab_chunk=chunk)
     check_far(w, w.loss()["dw"])
+
+
+@pytest.mark.parametrize("bf16,bf16_dw,offset", [(False, False, (64, 16)), (True, False, (64, 16)), (True, False, (-64, 16)), (True, True, (512, 256))])
+@pytest.mark.parametrize("T,V", [(20, 600), (300, 1100)])
+def test_gradient_apart_from_its_forward_pass_where_lse_is_large(T, V, bf16, bf16_dw, offset):
+    """By an lse of 1024 that is rounded to fp32 p would be off by 2^-14 (half a step; 2^-7 at 131072), in all of a row alike."""
+    w = far_world(T, V, offset, bf16, bf16_dw)
+    gw = torch.empty(V, 16 + T, device="cuda", dtype=DT[bf16_dw])
+    w.op.forward(w.x, w.w, w.y)
+    lse = w.op.lse.clone()
+    w.op.backward(w.x, w.w, w.y, w.dlogp, None, None, gw)
+    check_far(w, gw)
+    assert torch.equal(w.op.lse, lse)
+
+
+def test_rows_near_and_far_in_one_call():
+    """A row with a large lse changes nothing in the rows beside it."""
+    near, far = far_world(40, 700, (4, 2), False, False), far_world(40, 700, (4, 2), False, False)
+    far.x[::3, 0] = 512
+    out = []
+    for w in (near, far):
+        gx, gw = torch.empty_like(w.x), torch.empty(700, 56, device="cuda")
+        w.op.forward(w.x, w.w, w.y)
+        w.op.backward(w.x, w.w, w.y, w.dlogp, None, gx, gw)
+        out.append((gx, gw))
+    keep = [t for t in range(40) if t % 3]
+    assert torch.equal(out[0][0][keep], out[1][0][keep])
+    assert torch.equal(out[0][1][:, [16 + t for t in keep]], out[1][1][:, [16 + t for t in keep]])
