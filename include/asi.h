@@ -484,7 +484,8 @@ asi_status_t asi_head_grad(const asi_head_desc_t* desc, const void* x, const voi
 asi_status_t asi_head_loss(const asi_head_desc_t* desc, const void* x, const void* w, const int64_t* targets, const float* dlogp,
                            const float* dentropy, float* logp, float* entropy, float* lse, void* dx, void* dw, int32_t accumulate,
                            void* ws, size_t ws_bytes, void* stream);
-/* The device status that the last call on `ws` left (ASI_OK or ASI_ERR_TIMEOUT).  Synchronises `stream`. */
+/* The device status that the last call on `ws` left (ASI_OK or ASI_ERR_TIMEOUT; whatever the memory held before the first one).  Synchronises
+ * `stream`.  A call without rows may do without a workspace, and leaves ASI_OK in one that is given. */
 asi_status_t asi_head_status(const void* ws, void* stream, asi_status_t* device_status);
 
 /* Number of kernel launches the last call of each kind enqueues for this plan. */

@@ -1216,8 +1216,12 @@ asi_status_t call(const asi_head_desc_t* d, const Call& c, void* ws, size_t ws_b
   if (s != ASI_OK) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (d->rows == 0) {
+    if (c.grad && c.dw && !c.accumulate && off_element(c.dw, size_of(d->dw_dtype))) return ASI_ERR_INVALID_ARG;
+    if (ws && ws_bytes >= 4 && aligned(ws, 4)) {           // (a workspace may be missing here)
+      const cudaError_t e = cudaMemsetAsync(ws, 0, 4, st);
+      if (e != cudaSuccess) return cuda_status(e, "output layer's status");
+    }
     if (!c.grad || !c.dw || c.accumulate) return ASI_OK;   // no rows: their gradient of w is 0
-    if (off_element(c.dw, size_of(d->dw_dtype))) return ASI_ERR_INVALID_ARG;
     return cuda_status(cudaMemsetAsync(c.dw, 0, (size_t)d->vocab * d->dim * size_of(d->dw_dtype), st), "gradient of no rows");
   }
   s = check_call(d, c, ws, ws_bytes);

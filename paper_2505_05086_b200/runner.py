@@ -644,6 +644,7 @@ class HeadRunner(_RowResults):
         self._descriptor = _Descriptor(HeadDesc(_DTYPES[self.in_dtype], _DTYPES[self.dw_dtype], self.rows, self.vocab, self.dim,
                                                 int(vocab_chunk), int(ignore_index), float(scale), int(flags)))
         self.ws = torch.empty(binding.head_ws_bytes(self.desc, self.grad), dtype=torch.uint8, device=self.device)
+        self.ws[:256].zero_()              # (the status word, before the first call)
         self._bind(self._new())
         self._made(self.device)
 
