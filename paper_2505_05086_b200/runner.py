@@ -660,13 +660,19 @@ class HeadRunner(_RowResults):
                       _take("weight", weight, (self.vocab, self.dim), self.in_dtype, self.device),
                       _take("targets", targets, targets.shape, torch.int64, self.device))
 
-    def _gradients(self, n, x, dlogp, dentropy, dx, dw):
+    def _gradients(self, n, x, dlogp, dentropy, dx, dw, stream):
+        """Addresses of weights and gradients, and the weights, to be held until the call is queued."""
         if not self.grad:
             raise ValueError("the runner was made without gradients")
-        return ((_take("dlogp", dlogp.reshape(-1), (n,), torch.float32, self.device),
-                 _take("dentropy", dentropy.reshape(-1), (n,), torch.float32, self.device) if dentropy is not None else 0),
+        weights = [w if w is None or w.is_contiguous() else self._copy(w, stream) for w in (dlogp, dentropy)]
+        return (tuple(0 if w is None else _take(name, w.view(-1), (n,), torch.float32, self.device) for name, w in zip(("dlogp", "dentropy"), weights)),
                 (_take("dx", dx, x.shape, self.in_dtype, self.device) if dx is not None else 0,
-                 _take("dw", dw, (self.vocab, self.dim), self.dw_dtype, self.device) if dw is not None else 0))
+                 _take("dw", dw, (self.vocab, self.dim), self.dw_dtype, self.device) if dw is not None else 0), weights)
+
+    @staticmethod
+    def _copy(x, stream):
+        with torch.cuda.stream(stream):        # (the call's own, in whose order it is read and its memory used again)
+            return x.contiguous()
 
     def forward(self, x, weight, targets, stream=None):
         desc, n, inputs = self._inputs(x, weight, targets)
@@ -677,7 +683,7 @@ class HeadRunner(_RowResults):
         """The gradient of sum(dlogp * logp + dentropy * entropy) into dx and dw (either may be None; dw is increased with accumulate),
         from the lse and entropy that forward() left, or from those given."""
         desc, n, inputs = self._inputs(x, weight, targets)
-        weights, grads = self._gradients(n, x, dlogp, dentropy, dx, dw)
+        weights, grads, _held = self._gradients(n, x, dlogp, dentropy, dx, dw, stream)
         if lse is None and entropy is None:
             self._outputs(n, stats=True)
             _, h, z = self._stats
@@ -691,7 +697,7 @@ class HeadRunner(_RowResults):
     def loss(self, x, weight, targets, dlogp, dentropy, dx, dw, accumulate=False, stream=None):
         """forward() and backward() in one, for weights that do not depend on the result."""
         desc, n, inputs = self._inputs(x, weight, targets)
-        weights, grads = self._gradients(n, x, dlogp, dentropy, dx, dw)
+        weights, grads, _held = self._gradients(n, x, dlogp, dentropy, dx, dw, stream)
         self._outputs(n)
         self._call(stream, binding.head_loss, desc, *inputs, *weights, *self._stats, *grads, accumulate, self.ws.data_ptr(),
                    self.ws.numel())
