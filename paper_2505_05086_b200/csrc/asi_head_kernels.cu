@@ -40,10 +40,12 @@ constexpr int kK = 64;                                    // k of a box: 64 bf16
 constexpr int kMaxStages = 3;
 constexpr uint32_t kHalf = 128 * kK * 2;                  // a CTA's half of an operand's box
 constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged results: 32 rows of 128 bytes
-// Pairs of boxes that add up in TMEM at most where results are held to fp32 (kWhole need no segments).  What truncation takes from a logit is in
-// proportion to them: lse of 40 x 11324 x 761 fp32 5.4e-7 too small with 16, 2.9e-7 with 8 (entropy 1.0e-6 and 5.4e-7 too large).  8 of them cost operands
-// in three terms 0 to 4 % (1001 x 30011 x 771 760 us -> 794; scoring 1000 x 30000 x 2000 577 -> 566), single ones 6 % (4096 x 32000 x 2048 345 -> 367).
-constexpr int kSeg = 16, kSegTerms = 8, kWhole = 12;
+// Pairs of boxes that a product's segments in TMEM aim at where results are held to fp32 (kWhole need no segments), before they are rounded up to
+// whole chunks: 8 with one term of either operand (512 k), 12 with six pairs of terms a chunk (128 k of the operands), 9 with three (192).  What truncation
+// takes from a logit is in proportion to them: lse of 40 x 11324 x 761 fp32 5.4e-7 too small with 18, 2.9e-7 with 12 (entropy 1.0e-6 and 5.4e-7 too
+// large); of 4096 x 32000 x 2048 bf16 5.9e-6 with 16, 2.9e-6 with 8 (lse around 13; entropy 5.5e-6 and 2.3e-6).  Aiming at 16 instead would spare operands in
+// three terms 0 to 4 % (1001 x 30011 x 771 794 us -> 760), single terms 4 % (scoring 4096 x 32000 x 2048 373 us -> 357).
+constexpr int kSeg = 8, kWhole = 12;
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -979,7 +981,7 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
     parts = std::max(parts, (p.a_terms + p.b_terms) * p.sub);
     p.seg = 1 << 30;
     if (segmented && p.per * p.pairs > kWhole) {
-      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, p.pairs > 1 ? kSegTerms : kSeg));
+      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, kSeg));
       p.seg = (int)ceil_div(p.per, n);
     }
   }
@@ -1080,7 +1082,6 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     set_store(&g.p[0], T, nt * kTile);
     if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
   }
-  // (sums that the unit truncates over all of K = 2048 leave entropies 1.7e-6 off, in two segments 0.8e-6; 345 us either way)
   e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
   if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
   const RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c, g.lse, g.far};
@@ -1117,7 +1118,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
       e = launch_pdl(k_head_kept, dim3((unsigned)T, (unsigned)ceil_div(n, 1024)), dim3(256), 0, st, k);
     } else {
       // G in terms (24 bits) wants logits summed as those behind lse.  To G in bf16, whose step is 2^-9, what truncation takes from a logit
-      // (1.7e-6 at D = 2048) is nothing, and summing them in segments costs 4096 x 32000 x 2048 2 % (1451 us -> 1483)
+      // (about 1e-5 at D = 2048) is nothing, and summing them in segments costs 4096 x 32000 x 2048 2 % (1451 us -> 1483)
       e = launch_gemm<kGrad>(g, terms > 1 && logits.kc * logits.pairs > kWhole, st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
