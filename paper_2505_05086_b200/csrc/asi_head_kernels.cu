@@ -46,6 +46,9 @@ constexpr uint32_t kStaged = 32 * 128;                    // a warp's staged res
 // large); of 4096 x 32000 x 2048 bf16 5.9e-6 with 16, 2.9e-6 with 8 (lse around 13; entropy 5.5e-6 and 2.3e-6).  Aiming at 16 instead would spare operands in
 // three terms 0 to 4 % (1001 x 30011 x 771 794 us -> 760), single terms 4 % (scoring 4096 x 32000 x 2048 373 us -> 357).
 constexpr int kSeg = 8, kWhole = 12;
+// The same where results are rounded to bf16 (by 2^-8 of them at most): truncation takes 1.6e-3 of a sum of 4096 pairs (dw of 262144 rows), always towards zero, so
+// that sums of more than 512 (2e-4) go in segments of about 64.
+constexpr int kSegB16 = 64, kWholeB16 = 512;
 constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = 1.925963033500e-8f, kLn2 = 0.69314718055994531f;
 
 enum Epi { kStats = 0, kGrad = 1, kOut = 2 };
@@ -63,6 +66,7 @@ struct HeadProb {
   int sub, a_terms, b_terms;
   int pairs;                    // pairs of parts (64 k of a term) that are multiplied
   uint32_t a_part, b_part;      // of each pair, two bits
+  int seg_pairs, whole;         // pairs of boxes that its segments aim at, and that need none (kSeg, kWhole)
   int seg;                      // chunks that add up in TMEM (kSegmented), or all
   int n_first;                  // tiles of a row follow one another (else tiles of a column)
   const void* add;              // added to the result, laid out like it; null: nothing
@@ -252,7 +256,7 @@ __device__ __forceinline__ void put_words(const float* s, int lane, TO* to, cons
 // has the 128 x 256 accumulators of its rows in its TMEM, twice, so that the next tile's products run under this one's epilogue.
 // (A CTA by itself would read twice the bytes of B for the same products.)  Roles: a producer warp, an issuer warp, eight epilogue warps (a
 // thread a row and half of the columns).
-// kSegmented: results held to fp32.  The unit's own sums truncate, so they go to registers on the way (HeadProb::seg).
+// kSegmented: long sums.  The unit's own sums truncate, so they go to registers on the way (HeadProb::seg).
 template <int kEpi, bool kSegmented>
 __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant__ HeadArgs g) {
   extern __shared__ __align__(1024) uint8_t head_smem[];
@@ -920,7 +924,9 @@ void set_chunks(HeadProb* p, int64_t K, int a_terms, int b_terms) {
   p->kc = (int)ceil_div(K, kK * p->sub);
   p->per = p->kc;
   p->splits = 1;
+  p->seg_pairs = kSeg, p->whole = kWhole;
 }
+bool too_long(const HeadProb& p) { return p.per * p.pairs > p.whole; }
 
 template <int kEpi, bool kSegmented>
 cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
@@ -980,8 +986,8 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
     HeadProb& p = g.p[q];
     parts = std::max(parts, (p.a_terms + p.b_terms) * p.sub);
     p.seg = 1 << 30;
-    if (segmented && p.per * p.pairs > kWhole) {
-      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, kSeg));
+    if (segmented && too_long(p)) {
+      const int n = std::max(2, (int)ceil_div(p.per * p.pairs, p.seg_pairs));
       p.seg = (int)ceil_div(p.per, n);
     }
   }
@@ -1082,7 +1088,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     set_store(&g.p[0], T, nt * kTile);
     if (g.p[0].how != kCopy) return cuda_status(cudaErrorNotSupported, "tensor map");
   }
-  e = launch_gemm<kStats>(g, logits.kc * logits.pairs > kWhole, st);
+  e = launch_gemm<kStats>(g, too_long(logits), st);
   if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
   const RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c, g.lse, g.far};
   e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
@@ -1119,15 +1125,17 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     } else {
       // G in terms (24 bits) wants logits summed as those behind lse.  To G in bf16, whose step is 2^-9, what truncation takes from a logit
       // (about 1e-5 at D = 2048) is nothing, and summing them in segments costs 4096 x 32000 x 2048 2 % (1451 us -> 1483)
-      e = launch_gemm<kGrad>(g, terms > 1 && logits.kc * logits.pairs > kWhole, st);
+      e = launch_gemm<kGrad>(g, terms > 1 && too_long(logits), st);
     }
     if (e != cudaSuccess) return cuda_status(e, "gradient of the logits");
     // (the first operand lies with k together for dx, with its rows together for dw; x and w with their rows together)
     size_product(&px, T, D);
     set_chunks(&px, nv, fine ? 3 : 1, fine ? 3 : 1);
+    if (!fine) px.seg_pairs = kSegB16, px.whole = kWholeB16;
     px.a_mn = 0, px.b_mn = 1, px.b_k = (int)v0, px.n_first = 1;
     size_product(&pw, nv, D);
     set_chunks(&pw, T, dw_kind == kF32 ? 3 : 1, l.in_terms);
+    if (dw_kind == kB16) pw.seg_pairs = kSegB16, pw.whole = kWholeB16;
     pw.a_mn = 1, pw.b_mn = 1, pw.n_first = 1;
     if (i == 0) {
       bool maps = operand_map(&px.a, G, l.cols, T, l.cols, terms, T * l.cols, kK, 128) && operand_map(&px.b, w, D, V, ld, l.in_terms, V * ld, 64, kK * px.sub);
@@ -1160,9 +1168,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     if (c.dx) g.p[g.np++] = px;
     if (c.dw) g.p[g.np++] = pw;
     for (int q = 0; q < g.np; ++q) set_store(&g.p[q], g.p[q].M, D);
-    // sums that leave TMEM on the way, where results are held to fp32 and long enough for it to show
-    const bool long_dw = c.dw && dw_kind == kF32 && pw.kc * pw.pairs > kWhole, long_dx = c.dx && fine && px.per * px.pairs > kWhole;
-    e = launch_gemm<kOut>(g, long_dw || long_dx, st);
+    // (sums that leave TMEM on the way)
+    e = launch_gemm<kOut>(g, (c.dw && too_long(pw)) || (c.dx && too_long(px)), st);
     if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
   }
   if (c.dx && splits > 1) {
