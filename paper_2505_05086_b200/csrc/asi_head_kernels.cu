@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
             // a term after the other, rows of 64 bytes (32 columns)
             to_gradient<32>(v, rg, g, g.v0 + n);
 #pragma unroll 1
-            for (int e = 0; e < 3; ++e) {
+            for (int e = 0; e < g.terms; ++e) {
               out = next_place();
 #pragma unroll
               for (int u = 0; u < 4; ++u) {
@@ -842,12 +842,16 @@ asi_status_t check_desc(const asi_head_desc_t* d) {
 
 constexpr int64_t kPieceBytes = 128 << 20;               // of G in the workspace, where 1024 columns take no more
 constexpr int64_t kJoinRows = 4096;                      // rows of shares of dx beyond dx itself
+// Rows (one tile) up to which G goes into a bf16 dw as two terms (17 bits) instead of one.  The roundings of few rows do not average out (9 x 50257 x 768: dw
+// 0.0026 off with one, 0.0017 with two, which is its own rounding), and the second product mostly hides behind dw's way out (9 x 50257 x 768 97 us with both;
+// 256 x 32000 x 2048 162 -> 169, 256 x 60000 x 1000 185 -> 194; 384 rows 216 -> 240).
+constexpr int64_t kFewRows = 256;
 
 struct Layout {
   size_t part, xy, row, off, xs, ws, g, acc, kept, least, bytes;   // least: without logits that are kept (kept 0: never)
   int64_t ld;                                            // of split operands
   int64_t cols;                                          // of a piece
-  int in_terms, g_terms;
+  int in_terms;
   bool split;                                            // operands go through k_head_split
   int64_t acc_rows;
 };
@@ -856,7 +860,6 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
   Layout l = {};
   const int64_t T = d->rows, V = d->vocab, nt = ceil_div(V, kTile), all = nt * kTile;
   l.in_terms = d->in_dtype == ASI_F32 ? 3 : 1;
-  l.g_terms = d->dw_dtype == ASI_F32 ? 3 : 1;            // (dx of fp32 operands comes with dw in fp32)
   l.split = d->in_dtype == ASI_F32 || d->dim % 8 != 0;
   l.ld = (d->dim + 63) / 64 * 64;                        // (rows on 128 bytes: on 16 alone a row of a copy meets two lines, and 1001 x 30011 x 771 fp32 took 794 us instead of 768)
   size_t at = 256;                                       // status word
@@ -874,7 +877,8 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
     l.ws = take((size_t)l.in_terms * V * l.ld * 2);
   }
   if (grad && T) {
-    const int64_t col = (int64_t)l.g_terms * 2 * T;      // bytes of a column of G
+    // bytes of a column of G (dx of fp32 operands comes with dw in fp32; never less than fewer rows take)
+    const int64_t col = d->dw_dtype == ASI_F32 ? 6 * T : std::max(2 * T, 4 * std::min(T, kFewRows));
     int64_t most = d->vocab_chunk ? ceil_div(std::min(d->vocab_chunk, V), kTile) * kTile * col : std::max(kPieceBytes, 1024 * col);
     most = std::min(most, all * col);
     l.cols = most / col / kTile * kTile;
@@ -992,7 +996,7 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
     }
   }
   g.stage = parts * kHalf;
-  g.nst = (192 << 10) / g.stage;
+  g.nst = std::min<int>(kMaxStages, (192 << 10) / g.stage);   // (two terms by one, alone: 48 KB)
   g.place = kEpi == kGrad && g.terms > 1 ? kStaged / 2 : 0;
   g.tiles0 = g.p[0].mt * g.p[0].nt * g.p[0].splits;
   g.tiles = g.tiles0 + (g.np > 1 ? g.p[1].mt * g.p[1].nt * g.p[1].splits : 0);
@@ -1074,7 +1078,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   if (!operand_map(&logits.a, x, D, T, ld, l.in_terms, T * ld, kK, 128) || !operand_map(&logits.b, w, D, V, ld, l.in_terms, V * ld, kK, 128))
     return cuda_status(cudaErrorNotSupported, "tensor map");
   const bool keep = c.forward && c.grad && l.kept && ws_bytes >= l.bytes;
-  const int terms = c.dw && d->dw_dtype == ASI_F32 ? 3 : fine ? 3 : 1;   // of G (without dw in fp32, G of bf16 operands has one)
+  // of G (bf16 operands: what dw wants)
+  const int terms = fine || (c.dw && d->dw_dtype == ASI_F32) ? 3 : c.dw && T <= kFewRows ? 2 : 1;
   if (!c.forward) {
     g.lse = c.lse_in;
     g.far = terms > 1 ? kFarLseTerms : kFarLse;
@@ -1134,7 +1139,7 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     if (!fine) px.seg_pairs = kSegB16, px.whole = kWholeB16;
     px.a_mn = 0, px.b_mn = 1, px.b_k = (int)v0, px.n_first = 1;
     size_product(&pw, nv, D);
-    set_chunks(&pw, T, dw_kind == kF32 ? 3 : 1, l.in_terms);
+    set_chunks(&pw, T, terms, l.in_terms);
     if (dw_kind == kB16) pw.seg_pairs = kSegB16, pw.whole = kWholeB16;
     pw.a_mn = 1, pw.b_mn = 1, pw.n_first = 1;
     if (i == 0) {

@@ -109,3 +109,20 @@ def test_a_bf16_dw_of_very_many_rows_is_not_biased():
         want += head(w.x[s], w.w, w.y[s], 1.0, -100, w.dlogp[s])["dw"]
     off = ((gw.double() - want) / want)[1:]
     assert abs(float(off.mean())) <= 5.4e-5
+
+
+@pytest.mark.parametrize("T,V,D", [(1, 700, 64), (9, 9000, 264), (40, 1100, 75), (256, 2000, 136), (256, 600, 1032)])
+@pytest.mark.parametrize("add", [False, True])
+def test_a_bf16_dw_of_few_rows_is_rounded_once(T, V, D, add):
+    """World.check's bounds of dw, but for G's rounding: two terms of bf16 leave 2^-17 of each entry (2^-8 twice, and what is left has the sign and half of the
+    last step), and dw itself half a step."""
+    w = World(T, V, D, bf16=True, bf16_dw=True, ignored=0.0 if T < 9 else 0.15)
+    start = (torch.randn(V, D, device="cuda") / (4 * T)).bfloat16() if add else None
+    got, r = w.loss(accumulate=add, start=start, dx=add), w.reference()      # (dw alone, too)
+    w.check(got, start)
+    want = r["dw"] + (start.double() if add else 0)
+    logit = (D / 16 + 2) * 2 * U32 * r["S"]
+    p_off = 2 * (logit + 16 * U32 * (1 + r["lse"].abs() + r["S"])) + 8 * U32 * (1 + r["lse"].abs())
+    size = r["size"].T
+    cost = (p_off * size + size * (2.0 ** -16 + (T / 16 + 64) * 2 * U32)) @ w.x.double().abs() + 2.0 ** -123 * w.x.double().abs().sum(0)
+    assert ((got["dw"].double() - want).abs() <= cost + U16 * want.abs()).all()
