@@ -115,15 +115,6 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ uint32_t rank_in_pair() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void pair_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // maximum, sum and weighted sum (of e_j = 2^a_j: sum e_j, sum e_j a_j) of what a thread has seen of its row
 struct RowStats {
   float top = -INFINITY, m = 0.f, s = 0.f, w = 0.f;      // top: largest logit; m = c top, what exponents are relative to
@@ -264,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done[2], acc_free[2], drained[1];
   __shared__ uint32_t tmem_slot[1];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)rank_in_pair(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int rank = (int)cluster_rank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   if (tid == 0) {
     for (int i = 0; i < kMaxStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
     for (int i = 0; i < 2; ++i) mbar_init(done + i, 1), mbar_init(acc_free + i, 2 * kWorkers);
@@ -277,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  pair_sync();
+  cluster_sync_all();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
@@ -660,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  pair_sync();                                          // the other CTA's products read this one's memory
+  cluster_sync_all();                                          // the other CTA's products read this one's memory
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
