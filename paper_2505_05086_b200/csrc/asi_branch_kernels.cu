@@ -1025,7 +1025,7 @@ asi_status_t asi_branch_forward(const asi_branch_desc_t* desc, const asi_branch_
   if (desc->rows == 0) return ASI_OK;
   if (!t->y || !t->h_out || !t->stats || (desc->rows_per_gate && !t->gate) || (!desc->norm_after && (t->after_weight || t->after_bias)) || (desc->norm == ASI_NORM_RMS && (t->after_bias || t->next_bias))) return ASI_ERR_INVALID_ARG;
   const size_t ei = size_of(desc->in_dtype), er = size_of(desc->res_dtype), n = (size_t)desc->rows * desc->dim, w = (size_t)desc->dim * 4;
-  const size_t gates = desc->rows_per_gate ? (size_t)ceil_div(desc->rows, desc->rows_per_gate) * w : 0;
+  const size_t gates = desc->rows_per_gate ? (size_t)((desc->rows - 1) / desc->rows_per_gate + 1) * w : 0;   // (rows > 0, any int64 of them a gate)
   const float* gate = desc->rows_per_gate ? t->gate : nullptr;
   if (!fine({{t->y, n * ei, ei}, {t->h, n * er, er}, {gate, gates, 4}, {t->after_weight, w, 4}, {t->after_bias, w, 4}, {t->next_weight, w, 4},
              {t->next_bias, w, 4}, {desc->drop.step_dev, 8, 8}},
@@ -1072,7 +1072,7 @@ asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch
   }
   if (!t->y || !t->stats || !t->dy || (!t->dx && !t->dh_out) || (t->dx && !t->h_out) || (desc->rows_per_gate && !t->gate)) return ASI_ERR_INVALID_ARG;
   if (!t->dx && (t->dnext_weight || t->dnext_bias)) return ASI_ERR_INVALID_ARG;
-  const size_t gates = desc->rows_per_gate ? (size_t)ceil_div(desc->rows, desc->rows_per_gate) * w : 0;
+  const size_t gates = desc->rows_per_gate ? (size_t)((desc->rows - 1) / desc->rows_per_gate + 1) * w : 0;   // (rows > 0, any int64 of them a gate)
   const float* gate = desc->rows_per_gate ? t->gate : nullptr;
   const size_t need = part_bytes(desc->rows, desc->dim);
   const bool sums = t->dgate || t->dafter_weight || t->dafter_bias || t->dnext_weight || t->dnext_bias;
