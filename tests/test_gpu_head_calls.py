@@ -51,3 +51,54 @@ def test_the_status_before_any_call():
     old = torch.full((32 << 20,), 0x5A, dtype=torch.uint8, device="cuda")
     del old
     assert World(40, 600, 72).op.device_status() == 0
+
+
+def test_gradients_apart_captured_and_beside_another():
+    """backward() in a graph whose inputs change between replays, rows with a large lse among them, while another runner's runs on its own stream."""
+    a, b = World(300, 1500, 136, bf16=False, bf16_dw=False, ent=True, seed=1), World(300, 1500, 136, ent=True, seed=2)
+
+    def grads(w):
+        gx, gw = torch.empty_like(w.x), torch.empty(1500, 136, device="cuda", dtype=torch.bfloat16 if w.bf16_dw else torch.float32)
+        w.op.backward(w.x, w.w, w.y, w.dlogp, w.dent, gx, gw)
+        return gx, gw
+    a.op.forward(a.x, a.w, a.y), b.op.forward(b.x, b.w, b.y)
+    other = grads(b)
+    gx, gw = torch.empty_like(a.x), torch.empty(1500, 136, device="cuda")
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        a.op.forward(a.x, a.w, a.y)
+        a.op.backward(a.x, a.w, a.y, a.dlogp, a.dent, gx, gw)
+    side.wait_stream(torch.cuda.current_stream())
+    for scale in (1.0, 60.0, 1.0):                                    # (at 60 |lse| is beyond 128 in most rows)
+        a.x.mul_(scale)
+        graph.replay()
+        with torch.cuda.stream(side):
+            beside = grads(b)
+        torch.cuda.synchronize()
+        assert (a.op.lse.abs().max() > 128) == (scale > 1)
+        want = grads(a)
+        assert torch.equal(gx, want[0]) and torch.equal(gw, want[1])
+        assert torch.equal(beside[0], other[0]) and torch.equal(beside[1], other[1])
+        a.check(dict(logp=a.op.logp, entropy=a.op.entropy, lse=a.op.lse, dx=gx, dw=gw))
+        a.x.div_(scale)
+
+
+@pytest.mark.parametrize("bf16,bf16_dw", [(True, True), (True, False), (False, False)])
+def test_waits_of_a_gradient_apart_that_run_out_are_reported(bf16, bf16_dw):
+    """The test hook again (barriers are armed and no copy is issued, waits end after a millisecond)."""
+    from paper_2505_05086_b200.binding import ASI_ERR_TIMEOUT, ASI_FLAG_TEST_EXPIRE_WAIT
+    w = World(300, 2000, 136, bf16, bf16_dw)
+    w.op.forward(w.x, w.w, w.y)
+
+    def grads():
+        gx, gw = torch.empty_like(w.x), torch.empty(2000, 136, device="cuda", dtype=torch.bfloat16 if bf16_dw else torch.float32)
+        w.op.backward(w.x, w.w, w.y, w.dlogp, None, gx, gw)
+        return gx, gw
+    want = grads()
+    assert w.op.device_status() == 0
+    w.op.desc.flags = ASI_FLAG_TEST_EXPIRE_WAIT
+    grads()
+    assert w.op.device_status() == ASI_ERR_TIMEOUT
+    w.op.desc.flags = 0
+    got = grads()
+    assert w.op.device_status() == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
