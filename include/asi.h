@@ -449,8 +449,8 @@ asi_status_t asi_branch_backward(const asi_branch_desc_t* desc, const asi_branch
  *   lse, logp, entropy as of asi_token_logprobs;  G = dlogits of asi_token_logprobs_grad;  dx = G w;  dw = G^T x.
  * Products of bf16 values are exact, sums fp32 on the tensor cores.  fp32 operands are taken as three bf16 terms each (24 bits, the six
  * products that matter; values from 3.39e38 on and infinities give NaN), and so is G where its product is stored in fp32.  For products
- * stored in bf16 G is rounded to bf16; what that takes from the target's entry comes back in dx, and up to 256 rows have G for dw in two
- * terms (17 bits).  Logits are computed twice, for the sums and for the gradient: G exists for `vocab_chunk` columns at a time, in the
+ * stored in bf16 G is rounded to bf16; what that takes from the target's entry comes back in dx, and in dw from two rows of a target that four
+ * at most share.  Up to 256 rows have G for dw in two terms (17 bits) instead.  Logits are computed twice, for the sums and for the gradient: G exists for `vocab_chunk` columns at a time, in the
  * workspace.  There, too, lie the terms of fp32 operands, 6 bytes for each value of x and w (1.5 times their own, rows padded to 64
  * values), and copies of bf16 rows whose dim is no multiple of 8; each call writes them again.
  * Rows as there: ignored ones have logp 0 and G 0, targets outside [0, vocab) and logits of NaN or +inf give NaN (in dw as well, whose

@@ -16,6 +16,8 @@
 // Operands are bf16.  fp32 ones are split into three terms each (hi, mid, lo: 24 bits) by k_head_split, and a product takes the
 // six pairs of terms down to 2^-16 of the first (what is left out is 2^-24).  G is split likewise where its product goes to
 // fp32.  Rows of bf16 off 16 bytes, which tensor copies cannot fetch, go through the same kernel as one term.
+// G for results in bf16 is rounded to bf16.  One entry of its row, the target's, is as large as all others together, and its rounding no less: that comes
+// back as rank-one terms, off[t] w[y] in dx, off[t] x[t] in row y of dw (struct Back); few rows have two terms of G for dw instead (kFewRows).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -75,8 +77,10 @@ struct HeadProb {
   int64_t ld, split_stride;     // elements
   CUtensorMap o;                // the result in boxes of 32 rows of 128 bytes
   int how;                      // Store: how results leave
-  int correct;                  // what rounding took from G at the targets is added (dx of bf16 operands)
+  int correct;                  // Correct: where what rounding took from G at the targets is added
 };
+// not at all, to rows of x's gradient (off[t] w[y]), or to those of w's (off[t] x[t] for the rows t of that target)
+enum Correct { kNowhere = 0, kToDx = 1, kToDw = 2 };
 // by coalesced words (any alignment, `add` of any kind), by tensor copies, or added to fp32 by tensor copies (add is out)
 enum Store { kWords = 0, kCopy = 1, kAdd = 2 };
 struct HeadArgs {
@@ -99,12 +103,20 @@ struct HeadArgs {
   float far;
   const float *entropy, *dlogp, *dent;
   float* off;                   // [T]: what rounding took from G at the target (bf16 operands), or null; w and its row stride beside it
-  const __nv_bfloat16* w;
+  const __nv_bfloat16 *w, *x;   // (x has it too)
   int64_t ld_w;
+  const int *first, *next;      // [V], [T]: rows of a target, one after another in any order; each is its number + 1, 0 ends them
   CUtensorMap g;                // G: boxes of 32 rows of 64 columns (one term) or 32
   int terms;                    // of G
 };
 
+__device__ __forceinline__ void add_scaled(float* v, float a, const uint4& x) {   // v += a x, eight values, two an instruction
+  const uint32_t h[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%0, %1};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "+f"(v[2 * i]), "+f"(v[2 * i + 1]) : "f"(__uint_as_float(h[i] << 16)), "f"(__uint_as_float(h[i] & 0xffff0000u)), "f"(a));
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -115,6 +127,64 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// The rows of a target, for what rounding took from G there.  Of up to kWalk rows the first kBack in order have theirs given back, from more none: a thread walks the
+// list of its row of dw and reads rows of x for it, which many would hold up.  A tile's epilogue waits for its own instructions, so that warps without
+// such rows skip all of it (300 x 32000 x 2048 bf16 220 us instead of 234; 208 without the lists, 251 with four rows given back).
+constexpr int kBack = 2, kWalk = 4, kNoRow = 1 << 30;
+struct Back {
+  bool some = false, more = false;   // any lane of the warp has one, or two
+  int row[kBack];
+  float off[kBack];
+  uint4 x[kBack][4];               // 32 columns of theirs
+  // t: the first of this lane's list
+  __device__ __forceinline__ void find(const HeadArgs& g, int t) {
+    some = __any_sync(~0u, t != 0);
+    if (!some) return;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kBack; ++i) row[i] = kNoRow;
+#pragma unroll 1
+    for (; t && n <= kWalk; t = g.next[t - 1], ++n) {
+      int r = t - 1;
+#pragma unroll
+      for (int i = 0; i < kBack; ++i) {
+        const int low = min(row[i], r);
+        r = max(row[i], r);
+        row[i] = low;
+      }
+    }
+    if (n > kWalk) row[0] = row[1] = kNoRow;
+#pragma unroll
+    for (int i = 0; i < kBack; ++i) off[i] = row[i] != kNoRow ? g.off[row[i]] : 0.f;
+    more = __any_sync(~0u, row[1] != kNoRow);
+  }
+  // columns from n of N on (rows of x, or of its terms, go on to a multiple of 8)
+  __device__ __forceinline__ void bring(const HeadArgs& g, int n, int N) {
+    if (!some) return;
+    bring_of(g, 0, n, N);
+    if (more) bring_of(g, 1, n, N);
+  }
+  __device__ __forceinline__ void give(float (&v)[32], int n, int N) const {
+    if (!some) return;
+    give_of(0, v, n, N);
+    if (more) give_of(1, v, n, N);
+  }
+  __device__ __forceinline__ void bring_of(const HeadArgs& g, int i, int n, int N) {
+    if (row[i] == kNoRow) return;
+    const uint4* at = reinterpret_cast<const uint4*>(g.x + row[i] * g.ld_w + n);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (n + 8 * u < N) x[i][u] = __ldg(at + u);
+  }
+  __device__ __forceinline__ void give_of(int i, float (&v)[32], int n, int N) const {
+    if (row[i] == kNoRow) return;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (n + 8 * u < N) add_scaled(v + 8 * u, off[i], x[i][u]);
+  }
+};
+static_assert(kBack == 2, "some and more stand for the two");
+
 // maximum, sum and weighted sum (of e_j = 2^a_j: sum e_j, sum e_j a_j) of what a thread has seen of its row
 struct RowStats {
   float top = -INFINITY, m = 0.f, s = 0.f, w = 0.f;      // top: largest logit; m = c top, what exponents are relative to
@@ -248,7 +318,8 @@ __device__ __forceinline__ void put_words(const float* s, int lane, TO* to, cons
 // (A CTA by itself would read twice the bytes of B for the same products.)  Roles: a producer warp, an issuer warp, eight epilogue warps (a
 // thread a row and half of the columns).
 // kSegmented: long sums.  The unit's own sums truncate, so they go to registers on the way (HeadProb::seg).
-template <int kEpi, bool kSegmented>
+// kLists: rows of dw get back what rounding took from G (Correct).
+template <int kEpi, bool kSegmented, bool kLists>
 __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant__ HeadArgs g) {
   extern __shared__ __align__(1024) uint8_t head_smem[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(head_smem) + 1023) & ~(uintptr_t)1023);
@@ -431,12 +502,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
       return staged + flip * place;
     };
     uint8_t* out = staged;
+    // the first in the list of a row of dw
+    auto first_of = [&](const HeadProb& p, int row) { return p.correct == kToDw && row < p.M ? g.first[g.v0 + row] : 0; };
+    constexpr bool kAheadOf = kLists && !kSegmented;     // (segments' sums leave no registers: there lists are walked for every 32 columns)
+    int first = 0;                                       // in the next tile
+    auto next_first = [&](int t) {
+      if (t >= mine) return;
+      const Tile x = tile_of(t);
+      first = first_of(g.p[x.q], x.m * kTile + rank * 128 + quad * 32 + lane);
+    };
+    if (kAheadOf) next_first(0);
 #pragma unroll 1
     for (int t = 0; t < mine && ok; ++t) {
       const Tile x = tile_of(t);
       const HeadProb& p = g.p[x.q];
       const int row0 = x.m * kTile + rank * 128 + quad * 32, row = row0 + lane;
       const int n0 = x.n * kTile + col0;
+      Back back;
+      if constexpr (kAheadOf) {
+        back.find(g, first);
+        back.bring(g, n0, p.N);
+        next_first(t + 1);
+      }
       float acc[kSegmented ? 128 : 1];
       if constexpr (kSegmented) {
 #pragma unroll
@@ -498,8 +585,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
       RowStats stats;
       RowGrad rg;
       if constexpr (kEpi == kGrad) rg = row_grad(g, row);
-      const int64_t y = (kEpi == kStats || (kEpi == kOut && p.correct)) && row < g.T ? g.y[row] : -1;
-      const bool corrected = kEpi == kOut && p.correct && y >= 0 && y < g.V && y != g.ignore;
+      const int64_t y = (kEpi == kStats || (kEpi == kOut && p.correct == kToDx)) && row < g.T ? g.y[row] : -1;
+      const bool corrected = kEpi == kOut && p.correct == kToDx && y >= 0 && y < g.V && y != g.ignore;
       const float off = corrected ? g.off[row] : 0.f;
       const __nv_bfloat16* hot_row = g.w + (corrected ? y * g.ld_w : 0);
 #pragma unroll
@@ -524,19 +611,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_head_gemm(const __grid_constant
         const int n = n0 + cc * 32;
         if (!live) continue;
         if constexpr (kEpi == kOut) {
-          // One entry of G's row is as large as all others together, and its rounding no less: it comes back as off[t] w[y]
-          if (p.correct && off != 0.f) {
+          if (p.correct == kToDx && off != 0.f) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              if (n + 8 * u >= p.N) break;
-              const uint4 q = __ldg(reinterpret_cast<const uint4*>(hot_row + n + 8 * u));   // (rows of w, or of its terms, go on to a multiple of 8)
-              const uint32_t h[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                v[8 * u + 2 * i] = fmaf(off, __uint_as_float(h[i] << 16), v[8 * u + 2 * i]);
-                v[8 * u + 2 * i + 1] = fmaf(off, __uint_as_float(h[i] & 0xffff0000u), v[8 * u + 2 * i + 1]);
-              }
-            }
+            for (int u = 0; u < 4; ++u)                    // (rows of w, or of its terms, go on to a multiple of 8)
+              if (n + 8 * u < p.N) add_scaled(v + 8 * u, off, __ldg(reinterpret_cast<const uint4*>(hot_row + n + 8 * u)));
+          }
+          if constexpr (kLists) {
+            if (kSegmented) back.find(g, first_of(p, row)), back.bring(g, n, p.N);
+            back.give(v, n, p.N);
+            if (kAheadOf && cc < 3) back.bring(g, n + 32, p.N);
           }
         }
         if constexpr (kEpi == kStats) {
@@ -666,6 +749,7 @@ struct RowsArgs {
   float c;
   const float* given;          // null, or an earlier call's lse: rows below `far` are left out
   float far;
+  int *first, *next;           // as in HeadArgs, to be made (from 0s), or null
 };
 constexpr int kAhead = 8;
 __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ RowsArgs p) {
@@ -674,6 +758,10 @@ __global__ void __launch_bounds__(1024) k_head_rows(const __grid_constant__ Rows
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
   int row = blockIdx.x * 32 + lane;
+  if (p.first && slice == 0 && row < p.T) {
+    const int64_t y = p.y[row];
+    if (y >= 0 && y < p.V && y != p.ignore) p.next[row] = atomicExch(p.first + y, row + 1);
+  }
   if (p.given && !__syncthreads_or(row < p.T && is_far(p.given, p.y, p.ignore, row, p.far))) return;
   row = blockIdx.x * 32 + slice;                         // (the row that this warp's first lane writes)
   const int64_t y = row < p.T ? p.y[row] : 0;
@@ -839,10 +927,11 @@ constexpr int64_t kJoinRows = 4096;                      // rows of shares of dx
 constexpr int64_t kFewRows = 256;
 
 struct Layout {
-  size_t part, xy, row, off, xs, ws, g, acc, kept, least, bytes;   // least: without logits that are kept (kept 0: never)
+  size_t first, next, part, xy, row, off, xs, ws, g, acc, kept, least, bytes;   // least: without logits that are kept (kept 0: never)
   int64_t ld;                                            // of split operands
   int64_t cols;                                          // of a piece
   int in_terms;
+  bool lists;                                            // of each target's rows
   bool split;                                            // operands go through k_head_split
   int64_t acc_rows;
 };
@@ -859,6 +948,11 @@ Layout layout_of(const asi_head_desc_t* d, bool grad) {
     at = align_up(at + bytes, 256);
     return a;
   };
+  l.lists = grad && T > kFewRows && d->dw_dtype == ASI_BF16;
+  if (l.lists) {
+    l.first = take((size_t)V * 4);                       // (right behind the status word: cleared with it)
+    l.next = take((size_t)T * 4);
+  }
   l.part = take((size_t)2 * nt * T * 12);
   l.xy = take((size_t)T * 4);
   l.row = take((size_t)T * 8);
@@ -923,10 +1017,10 @@ void set_chunks(HeadProb* p, int64_t K, int a_terms, int b_terms) {
 }
 bool too_long(const HeadProb& p) { return p.per * p.pairs > p.whole; }
 
-template <int kEpi, bool kSegmented>
+template <int kEpi, bool kSegmented, bool kLists>
 cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
   const size_t smem = 1024 + (size_t)g.nst * g.stage + kWorkers * (kStaged + (kEpi == kGrad && g.terms > 1 ? 0 : g.place));
-  const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented>), smem);
+  const cudaError_t e = opt_in_smem(reinterpret_cast<const void*>(k_head_gemm<kEpi, kSegmented, kLists>), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * std::min(g.tiles, 74)));    // a pair on each pair of SMs
@@ -942,7 +1036,7 @@ cudaError_t launch_gemm_as(HeadArgs& g, cudaStream_t st) {
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_head_gemm<kEpi, kSegmented>, g);
+  return cudaLaunchKernelEx(&cfg, k_head_gemm<kEpi, kSegmented, kLists>, g);
 }
 
 // cycles of a tile's results on their way out, as measured.  (With few tokens a tile of dw is hardly anything else: 5 x 25417 x 366 bf16 took
@@ -971,7 +1065,7 @@ void share_tiles(HeadArgs* g, int pairs) {
   g->more_rest = rest ? to_rest - g->each_rest * rest : 0;
 }
 
-template <int kEpi>
+template <int kEpi, bool kLists = false>
 cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   // Stages of what the larger chunk takes (64 KB for one term of either operand, 96 for three), as many as 192 KB hold, beside a place for
   // each warp's results on their way out.  Chunks of 128 k and not 64 for the issuer's sake: one of 64 took it 560 cycles (waiting 120, four products
@@ -994,7 +1088,7 @@ cudaError_t launch_gemm(HeadArgs& g, bool segmented, cudaStream_t st) {
   g.few = 0;
   g.each_few = g.more_few = g.each_rest = g.more_rest = 0;
   if (g.np > 1) share_tiles(&g, std::min(g.tiles, 74));
-  return segmented ? launch_gemm_as<kEpi, true>(g, st) : launch_gemm_as<kEpi, false>(g, st);
+  return segmented ? launch_gemm_as<kEpi, true, kLists>(g, st) : launch_gemm_as<kEpi, false, kLists>(g, st);
 }
 
 cudaError_t launch_split(const asi_head_desc_t* d, const Layout& l, const void* in, int64_t rows, void* out, cudaStream_t st) {
@@ -1037,7 +1131,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   const int64_t T = d->rows, V = d->vocab, D = d->dim;
   const bool fine = d->in_dtype == ASI_F32;              // logits and dx are held to fp32
   int* status = reinterpret_cast<int*>(ws);
-  cudaError_t e = cudaMemsetAsync(status, 0, 4, st);
+  const bool lists = l.lists && c.dw;
+  cudaError_t e = cudaMemsetAsync(status, 0, lists ? l.first + (size_t)V * 4 : 4, st);
   if (e != cudaSuccess) return cuda_status(e, "output layer's status");
   const void *x = c.x, *w = c.w;
   int64_t ld = D;
@@ -1086,7 +1181,8 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   }
   e = launch_gemm<kStats>(g, too_long(logits), st);
   if (e != cudaSuccess) return cuda_status(e, "logits of the output layer");
-  const RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c, g.lse, g.far};
+  const RowsArgs r = {g.pm, g.ps, g.pw, g.xy, c.y, d->ignore_index, V, c.logp, c.entropy, c.lse, row, (int)T, (int)(2 * nt), g.c, g.lse, g.far,
+                      lists ? reinterpret_cast<int*>(ws + l.first) : nullptr, reinterpret_cast<int*>(ws + l.next)};
   e = launch_pdl(k_head_rows, dim3((unsigned)ceil_div(T, 32)), dim3(1024), 0, st, r);
   if (e != cudaSuccess) return cuda_status(e, "rows of the output layer");
   if (!c.grad) return ASI_OK;
@@ -1095,8 +1191,11 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
   g.dlogp = c.dlogp;
   g.dent = c.dent;
   g.terms = terms;
-  g.off = !fine && c.dx ? reinterpret_cast<float*>(ws + l.off) : nullptr;
+  g.off = (!fine && c.dx) || lists ? reinterpret_cast<float*>(ws + l.off) : nullptr;
+  g.first = reinterpret_cast<const int*>(ws + l.first);
+  g.next = reinterpret_cast<const int*>(ws + l.next);
   g.w = static_cast<const __nv_bfloat16*>(w);
+  g.x = static_cast<const __nv_bfloat16*>(x);
   g.ld_w = ld;
   void* G = ws + l.g;
   HeadProb px = {}, pw = {};
@@ -1159,17 +1258,19 @@ asi_status_t run(const asi_head_desc_t* d, const Call& c, char* ws, size_t ws_by
     px.add_kind = i ? kF32 : kNone;
     px.out = last ? c.dx : static_cast<void*>(acc);
     px.out_kind = last ? dx_kind : kF32;
-    px.correct = last && g.off;
+    px.correct = last && !fine ? kToDx : kNowhere;
+    pw.correct = lists ? kToDw : kNowhere;
     g.np = 0;
     if (c.dx) g.p[g.np++] = px;
     if (c.dw) g.p[g.np++] = pw;
     for (int q = 0; q < g.np; ++q) set_store(&g.p[q], g.p[q].M, D);
     // (sums that leave TMEM on the way)
-    e = launch_gemm<kOut>(g, (c.dw && too_long(pw)) || (c.dx && too_long(px)), st);
+    const bool segmented = (c.dw && too_long(pw)) || (c.dx && too_long(px));
+    e = lists ? launch_gemm<kOut, true>(g, segmented, st) : launch_gemm<kOut>(g, segmented, st);
     if (e != cudaSuccess) return cuda_status(e, "gradients of the output layer");
   }
   if (c.dx && splits > 1) {
-    JoinArgs j = {acc, c.dx, T * D, D, splits, dx_kind, g.off, c.y, d->ignore_index, V, ld, g.w};
+    const JoinArgs j = {acc, c.dx, T * D, D, splits, dx_kind, fine ? nullptr : g.off, c.y, d->ignore_index, V, ld, g.w};
     e = launch_pdl(k_head_join, dim3((unsigned)std::min<int64_t>(ceil_div(T * D, 256), 148 * 8)), dim3(256), 0, st, j);
     if (e != cudaSuccess) return cuda_status(e, "shares of dx");
   }

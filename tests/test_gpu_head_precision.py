@@ -126,3 +126,58 @@ def test_a_bf16_dw_of_few_rows_is_rounded_once(T, V, D, add):
     size = r["size"].T
     cost = (p_off * size + size * (2.0 ** -16 + (T / 16 + 64) * 2 * U32)) @ w.x.double().abs() + 2.0 ** -123 * w.x.double().abs().sum(0)
     assert ((got["dw"].double() - want).abs() <= cost + U16 * want.abs()).all()
+
+
+def hot_rounding(w):
+    """What rounding to bf16 takes from G at each row's target."""
+    r = w.reference()
+    hot = r["G"][torch.arange(w.T, device="cuda"), w.y.clamp(min=0)]
+    return r, torch.where(w.y != -100, hot - hot.float().bfloat16().double(), 0.0)
+
+
+@pytest.mark.parametrize("add,dx", [(False, True), (True, False)])
+@pytest.mark.parametrize("T,V,D,chunk", [(257, 3000, 136, 0), (300, 4000, 136, 1024), (1500, 4000, 128, 0), (2100, 3000, 75, 0), (700, 300, 264, 0), (40000, 30000, 24, 0)])
+def test_dw_gets_back_what_rounding_takes_from_g_at_the_target(T, V, D, chunk, add, dx):
+    """As for dx, for rows of dw with one or two tokens: their remainders come back, sum over t of off_t x_t.  (Of more some or all are left;
+    the last size has sums that leave the accumulators on the way.)"""
+    w = World(T, V, D, bf16=True, bf16_dw=True, scale=0.7, vocab_chunk=chunk)
+    if T > 10000:
+        w.y[torch.rand(T, device="cuda") < 0.9] = -100
+    start = (torch.randn(V, D, device="cuda") / (4 * T)).bfloat16() if add else None
+    got = w.loss(accumulate=add, start=start, dx=dx)
+    r, off = hot_rounding(w)
+    many = torch.bincount(w.y.clamp(min=0)[w.y != -100], minlength=V) > 2
+    lost = torch.zeros(V, D, device="cuda", dtype=torch.float64).index_add_(0, w.y.clamp(min=0), off[:, None] * w.x.double())
+    lost[many] = 0
+    want = r["dw"] + (start.double() if add else 0)
+    share = float(((got["dw"].double() - want) * lost).sum() / lost.square().sum())
+    assert abs(share) <= 0.25
+
+
+def test_targets_of_many_rows():
+    """More tokens of a target than are given back one by one, in whatever order their rows were met: the same bits each time, and within the bounds."""
+    for targets in (1, 40, 150):
+        w = World(900, 500, 72, bf16=True, bf16_dw=True)
+        w.y = torch.where(w.y >= 0, w.y % targets, w.y)
+        first = w.loss()
+        w.check(first)
+        for _ in range(5):
+            again = w.loss()
+            assert torch.equal(again["dw"], first["dw"]) and torch.equal(again["dx"], first["dx"])
+        # the gradient apart
+        w.op.forward(w.x, w.w, w.y)
+        gw = torch.empty_like(first["dw"])
+        w.op.backward(w.x, w.w, w.y, w.dlogp, None, None, gw)
+        w.check(dict(first, dx=None, dw=gw))
+
+
+def test_ignored_rows_are_in_no_target_s_list():
+    """An ignored index inside the vocabulary, and targets outside it: nothing of such rows reaches dw but NaN from the latter."""
+    w = World(300, 700, 72, bf16=True, bf16_dw=True, ignored=0.0, ignore_index=7)
+    w.y[::3], w.y[1] = 7, 8
+    got, r = w.loss(), head(w.x, w.w, w.y, 1.0, 7, w.dlogp)
+    assert (got["dx"][::3] == 0).all()
+    assert float((got["dw"].double() - r["dw"]).norm() / r["dw"].norm()) <= U16      # (each value is rounded by half a step at most, G's rest by less)
+    w.y[4], w.y[5] = 700, -1
+    got = w.loss()
+    assert got["dw"].isnan().all() and got["dx"][4:6].isnan().all() and got["dx"][7:].isfinite().all()
