@@ -10,7 +10,7 @@
 // fp32, in the workspace) where these take no more than a piece of G would.
 //
 // What bounds it: the tensor cores, 2 T V D operations a product (for a few rows the bytes of w, read twice, and of dw).  4096 x 32000 x 2048
-// bf16 in bursts: logits and their sums 334 us (1608 TFLOP/s), G of 16128 columns 184 (1470), both products of G 340 (1590); in long loops the
+// bf16 in bursts: logits and their sums 356 us (1508 TFLOP/s), G of 16128 columns 182 (1487), both products of G 336 (1611); in long loops the
 // power cap takes 15 % of that.
 //
 // Operands are bf16.  fp32 ones are split into three terms each (hi, mid, lo: 24 bits) by k_head_split, and a product takes the
